@@ -71,7 +71,7 @@ const char* ds_last_error(void);
 /* Library version: major * 10000 + minor * 100 + patch (a library utility: no counterpart in the paper). */
 int ds_version(void);
 
-/* sizeof of the ABI structs as compiled into the library (0: ds_weights, 1: ds_layer), so that
+/* sizeof of the ABI structs as compiled into the library (0: ds_weights, 1: ds_layer, 2: ds_f8_matrix), so that
  * bindings can check their layout; 0 for any other argument (a library utility: no counterpart in the paper). */
 size_t ds_abi_struct_size(int which);
 
@@ -516,6 +516,156 @@ ds_status ds_conv2d_shift_specialized(const ds_specialized* h, const int32_t* x,
                                       const int32_t* residual, int32_t* y, int N, int H, int W, uint32_t flags,
                                       uint32_t* amax_io, void* stream);
 void ds_specialized_destroy(ds_specialized* h);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit floating point: matrices with a scale per block of 128, their product,
+ * and the operators around it in a feed-forward block.
+ *
+ * The paper keeps activations in fixed point and names 8 bits as the next step
+ * (Sec. 5.2.1); on this GPU the 8-bit path with twice the bf16 rate is floating
+ * point.  A shift weight s * 2^p, p in [-15, 0], is exact in e4m3 with the
+ * scale 2^-8, so a shift layer runs on it with its own weights; float layers
+ * run on it with weights rounded to blocks.
+ *
+ * A ds_f8_matrix describes device memory (the library keeps no pointer to it
+ * after a call): 8-bit values q, row r at q + r * ld, and float32 scales; the
+ * value of an element is q[r][c] * scale.  `blocks` says which scale:
+ *   DS_F8_ROWS   scale[r * ld_scale + c / 128]: one per row and 128 columns
+ *   DS_F8_TILES  scale[(r / 128) * ld_scale + c / 128]: one per 128 x 128
+ * q is 16-byte aligned and ld a multiple of 16 (cols need not be; bytes beyond
+ * cols are neither read into results nor written).  The last block of a row or
+ * column may be short.
+ *
+ * Writing a block: with amax the largest finite magnitude in it and MAX the
+ * largest value of the format (448, 57344),
+ *   scale = max(amax / MAX, 2^-126), rounded up to a power of two with
+ *   DS_F8_POW2;  q = value * (1 / scale) rounded to nearest, ties to even.
+ * Infinities and NaN become the 8-bit NaN.  With DS_F8_POW2 q * scale needs no
+ * rounding in float32, and changing the blocks of such a matrix later changes
+ * only values that fall below the format's range.
+ *
+ * Rows: 0 is accepted everywhere (an expert or a step without tokens): nothing
+ * is launched for the outputs that then have no elements, and sums over rows
+ * are written as zeros.  Types of the other tensors are DS_TYPE_*; their base
+ * pointers need only their type's alignment (16 bytes take the vector path),
+ * except `weight`, 16 bytes.  Arithmetic is float32; a value is rounded once,
+ * where it is stored.  Limits: rows and cols below 2^31 - 256, rows * ld at
+ * most 2^48.  Outputs must not overlap inputs except where a call says so.
+ * ------------------------------------------------------------------------- */
+#define DS_TYPE_F32 0
+#define DS_TYPE_BF16 1
+#define DS_TYPE_F16 2
+
+#define DS_F8_E4M3 0
+#define DS_F8_E5M2 1
+
+#define DS_F8_ROWS 0
+#define DS_F8_TILES 1
+
+#define DS_F8_POW2 1u /* scales are powers of two */
+
+typedef struct ds_f8_matrix {
+  void* q;          /* device, 8-bit values */
+  float* scale;     /* device, 4-byte aligned */
+  int64_t rows, cols;
+  int64_t ld;       /* bytes between rows */
+  int64_t ld_scale; /* floats between rows of scales */
+  int32_t format;   /* DS_F8_E4M3, DS_F8_E5M2 */
+  int32_t blocks;   /* DS_F8_ROWS, DS_F8_TILES */
+} ds_f8_matrix;
+
+/*
+ * Rounds x (device, [rows][cols] of `type`, row stride ldx elements) to 8 bits:
+ *   out    [rows][cols], DS_F8_ROWS or DS_F8_TILES, or NULL
+ *   out_t  the transposed matrix [cols][rows] (its DS_F8_ROWS blocks run down
+ *          the columns of x: the operand of a product that sums over rows), or
+ *          NULL; with DS_F8_TILES it is the exact transpose of a DS_F8_TILES out
+ * At least one is given; both cost one pass over x.  flags: DS_F8_POW2 or 0.
+ */
+ds_status ds_quantize_f8(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const ds_f8_matrix* out,
+                         const ds_f8_matrix* out_t, uint32_t flags, void* stream);
+
+/* The same from the values of another 8-bit matrix: other blocks, another format, or the transpose. */
+ds_status ds_requantize_f8(const ds_f8_matrix* x, const ds_f8_matrix* out, const ds_f8_matrix* out_t, uint32_t flags,
+                           void* stream);
+
+/* The weights s * 2^p of packed codes (Eq. 3) as an e4m3 matrix in tiles: q = s * 2^(p + 8), every scale 2^-8; exact.
+ * out is [n_out][k_red], DS_F8_E4M3, DS_F8_TILES.  Stream-ordered. */
+ds_status ds_expand_shift_weights_f8(const ds_weights* w, const ds_f8_matrix* out, void* stream);
+
+/*
+ * y[m][n] = bias[n] + add[m][n] + sum_k x[m][k] * w[n][k] over 8-bit matrices
+ * x [M][K] and w [N][K], on the tensor cores (tcgen05).  Each operand has its
+ * own format and blocks.  Products within a block of 128 k are summed by the
+ * tensor core; a block's sum is multiplied by its two scales and added in
+ * float32.  So y = x w^T for a layer's forward pass, dy (w_t)^T for its input
+ * gradient, and dy_t (x_t)^T for its weight gradient.
+ *   bias  device float32 [N] or NULL
+ *   add   device float32 [M][N], row stride ld_add, or NULL; may be y itself
+ *         (DS_TYPE_F32, ldy == ld_add): gradients accumulate in place
+ *   y     device, `type`, row stride ldy elements
+ * K = 0 gives bias + add.  Results do not depend on timing; their rounding
+ * depends on M (the reduction of small calls is split).
+ */
+ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* bias, const float* add,
+                       int64_t ld_add, void* y, int type, int64_t ldy, void* stream);
+
+/* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8. */
+int ds_f8_fault_flag(void);
+void ds_f8_set_wait_limit(long long cycles);
+
+/*
+ * Root-mean-square norm of a residual stream with an 8-bit output:
+ *   h = x + residual;  rstd = (mean_c h^2 + eps)^(-1/2);  out = h * rstd * weight, in 8 bits (DS_F8_ROWS)
+ *   x, residual  device [rows][cols] of `type`; residual may be NULL (h = x)
+ *   weight       device float32 [cols]
+ *   h            device, `type`, row stride ldh, or NULL; may be x or residual
+ *                itself (same row stride).  The norm is that of the unrounded h.
+ *   rstd         device float32 [rows] or NULL
+ * flags: DS_F8_POW2 or 0.
+ *
+ * Backward (the rounding to 8 bits passes gradients unchanged, as the paper's
+ * straight-through estimate does for its own, Eq. 8): with dy the gradient of
+ * out, h and rstd from the forward call and dh the gradient of h from the
+ * stream that continues (or NULL),
+ *   dx = dh + rstd * (dy weight - h rstd mean_c(dy weight h rstd))   (of x and of residual alike)
+ *   dw[c] = sum_r dy[r][c] h[r][c] rstd[r]                           (float32 [cols], overwritten)
+ * dx may be dy, h or dh itself (same row stride).  ws: device, 16-byte aligned,
+ * of ds_rmsnorm_f8_backward_workspace_bytes(rows, cols) bytes.  The sum over
+ * rows has a fixed order.
+ */
+ds_status ds_rmsnorm_f8(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight, int type,
+                        int64_t rows, int64_t cols, float eps, const ds_f8_matrix* out, void* h, int64_t ldh,
+                        float* rstd, uint32_t flags, void* stream);
+size_t ds_rmsnorm_f8_backward_workspace_bytes(int64_t rows, int64_t cols);
+ds_status ds_rmsnorm_f8_backward(const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* rstd,
+                                 const float* weight, const void* dh, int64_t lddh, int type, int64_t rows,
+                                 int64_t cols, void* dx, int64_t lddx, float* dw, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/*
+ * SiLU-gated activation a = silu(g) * u with an 8-bit output, and a checkpoint
+ * of g and u in 8 bits for its backward pass.
+ *   gu    device [rows][up + features] of `type`, row stride ld: g in columns
+ *         [0, features), u in [up, up + features), up = features rounded up to
+ *         a multiple of 128 (no block holds both; columns between are ignored)
+ *   out   a, [rows][features], DS_F8_ROWS
+ *   ckpt  g and u as [rows][up + features], DS_F8_ROWS (zeros between), or NULL
+ *
+ * Backward: with g and u the values of ckpt and da [rows][features] of `type`
+ * (row stride ld) the gradient of a,
+ *   du = da silu(g),  dg = da u sig(g) (1 + g (1 - sig(g)))
+ *   dgu    [rows][up + features], DS_F8_ROWS (zeros between), or NULL
+ *   dgu_t  its transpose [up + features][rows], DS_F8_ROWS, or NULL
+ *   a_t    a again, from ckpt, transposed: [features][rows], DS_F8_ROWS, or NULL
+ * At least one is given; each is rounded from float32, not from another.
+ * flags: DS_F8_POW2 or 0.
+ */
+ds_status ds_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_t features, const ds_f8_matrix* out,
+                      const ds_f8_matrix* ckpt, uint32_t flags, void* stream);
+ds_status ds_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int type, int64_t ld, int64_t features,
+                               const ds_f8_matrix* dgu, const ds_f8_matrix* dgu_t, const ds_f8_matrix* a_t,
+                               uint32_t flags, void* stream);
 
 #ifdef __cplusplus
 }

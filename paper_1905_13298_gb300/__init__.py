@@ -40,6 +40,16 @@ DS_OP_FC = 2
 DS_OP_MAXPOOL = 3
 DS_OP_AVGPOOL = 4
 
+DS_TYPE_F32 = 0
+DS_TYPE_BF16 = 1
+DS_TYPE_F16 = 2
+
+DS_F8_E4M3 = 0
+DS_F8_E5M2 = 1
+DS_F8_ROWS = 0
+DS_F8_TILES = 1
+DS_F8_POW2 = 1
+
 DS_WEIGHTS_MAGIC = 0x31575344
 DS_FORMAT_PLANES6 = 1
 DS_FORMAT_CODES5 = 2
@@ -67,7 +77,14 @@ class ds_layer(ctypes.Structure):
                 ("flags", ctypes.c_uint32), ("w", ctypes.POINTER(ds_weights)), ("bias", ctypes.c_void_p)]
 
 
+class ds_f8_matrix(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_scale", ctypes.c_int64),
+                ("format", ctypes.c_int32), ("blocks", ctypes.c_int32)]
+
+
 _lib = None
+_F8 = ctypes.POINTER(ds_f8_matrix)
 
 _SIGNATURES = {
     "ds_last_error": (ctypes.c_char_p, []),
@@ -123,6 +140,28 @@ _SIGNATURES = {
                                                   ctypes.c_void_p]),
     "ds_conv2d_shift_backward_x": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p] +
                                    [ctypes.c_int] * 11 + [ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p]),
+    "ds_quantize_f8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int] + [ctypes.c_int64] * 3 +
+                       [_F8, _F8, ctypes.c_uint32, ctypes.c_void_p]),
+    "ds_requantize_f8": (ctypes.c_int, [_F8, _F8, _F8, ctypes.c_uint32, ctypes.c_void_p]),
+    "ds_expand_shift_weights_f8": (ctypes.c_int, [ctypes.POINTER(ds_weights), _F8, ctypes.c_void_p]),
+    "ds_linear_f8": (ctypes.c_int, [_F8, _F8, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                    ctypes.c_int, ctypes.c_int64, ctypes.c_void_p]),
+    "ds_f8_fault_flag": (ctypes.c_int, []),
+    "ds_f8_set_wait_limit": (None, [ctypes.c_longlong]),
+    "ds_rmsnorm_f8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                     ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_float,
+                                     _F8, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_uint32,
+                                     ctypes.c_void_p]),
+    "ds_rmsnorm_f8_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
+    "ds_rmsnorm_f8_backward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                              ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                              ctypes.c_void_p]),
+    "ds_gated_f8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int] + [ctypes.c_int64] * 3 +
+                    [_F8, _F8, ctypes.c_uint32, ctypes.c_void_p]),
+    "ds_gated_f8_backward": (ctypes.c_int, [_F8, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                            _F8, _F8, _F8, ctypes.c_uint32, ctypes.c_void_p]),
 }
 
 
@@ -137,7 +176,7 @@ def lib() -> ctypes.CDLL:
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
-        for which, st in ((0, ds_weights), (1, ds_layer)):
+        for which, st in ((0, ds_weights), (1, ds_layer), (2, ds_f8_matrix)):
             if L.ds_abi_struct_size(which) != ctypes.sizeof(st):
                 raise ImportError(f"{st.__name__} layout differs between the binding and {LIB_PATH}")
         _lib = L
@@ -351,6 +390,57 @@ def ds_quantize_q16(x, n: int, q, stream=None) -> None:
     _check(lib().ds_quantize_q16(_ptr(x), n, _ptr(q), _stream(stream)))
 
 
+# An 8-bit matrix argument is a ds_f8_matrix or None.
+
+def ds_quantize_f8(x, type_: int, rows: int, cols: int, ldx: int, out, out_t, flags: int = 0, stream=None) -> None:
+    _check(lib().ds_quantize_f8(_ptr(x), type_, rows, cols, ldx, out, out_t, flags, _stream(stream)))
+
+
+def ds_requantize_f8(x, out, out_t, flags: int = 0, stream=None) -> None:
+    _check(lib().ds_requantize_f8(x, out, out_t, flags, _stream(stream)))
+
+
+def ds_expand_shift_weights_f8(w: ds_weights, out, stream=None) -> None:
+    _check(lib().ds_expand_shift_weights_f8(ctypes.byref(w), out, _stream(stream)))
+
+
+def ds_linear_f8(x, w, bias, add, ld_add: int, y, type_: int, ldy: int, stream=None) -> None:
+    _check(lib().ds_linear_f8(x, w, _ptr(bias), _ptr(add), ld_add, _ptr(y), type_, ldy, _stream(stream)))
+
+
+def ds_f8_fault_flag() -> int:
+    return int(lib().ds_f8_fault_flag())
+
+
+def ds_f8_set_wait_limit(cycles: int) -> None:
+    lib().ds_f8_set_wait_limit(cycles)
+
+
+def ds_rmsnorm_f8(x, ldx: int, residual, ldr: int, weight, type_: int, rows: int, cols: int, eps: float, out, h,
+                  ldh: int, rstd, flags: int = 0, stream=None) -> None:
+    _check(lib().ds_rmsnorm_f8(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), type_, rows, cols, eps, out, _ptr(h),
+                               ldh, _ptr(rstd), flags, _stream(stream)))
+
+
+def ds_rmsnorm_f8_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().ds_rmsnorm_f8_backward_workspace_bytes(rows, cols))
+
+
+def ds_rmsnorm_f8_backward(dy, lddy: int, h, ldh: int, rstd, weight, dh, lddh: int, type_: int, rows: int, cols: int,
+                           dx, lddx: int, dw, ws, ws_bytes: int, stream=None) -> None:
+    _check(lib().ds_rmsnorm_f8_backward(_ptr(dy), lddy, _ptr(h), ldh, _ptr(rstd), _ptr(weight), _ptr(dh), lddh, type_,
+                                        rows, cols, _ptr(dx), lddx, _ptr(dw), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def ds_gated_f8(gu, type_: int, ld: int, rows: int, features: int, out, ckpt, flags: int = 0, stream=None) -> None:
+    _check(lib().ds_gated_f8(_ptr(gu), type_, ld, rows, features, out, ckpt, flags, _stream(stream)))
+
+
+def ds_gated_f8_backward(ckpt, da, type_: int, ld: int, features: int, dgu, dgu_t, a_t, flags: int = 0,
+                         stream=None) -> None:
+    _check(lib().ds_gated_f8_backward(ckpt, _ptr(da), type_, ld, features, dgu, dgu_t, a_t, flags, _stream(stream)))
+
+
 # ---------------------------------------------------------------------------
 # Tensor-level helpers (allocate outputs with torch, then call the ABI)
 # ---------------------------------------------------------------------------
@@ -562,3 +652,7 @@ def conv2d_shift(x, w: PackedShiftWeights, kernel_size, bias=None, stride=(1, 1)
     ds_conv2d_shift(x, w.desc, bias, residual, y, N, C, H, W, K, R, S, stride[0], stride[1], padding[0],
                     padding[1], f, amax_io, stream)
     return y
+
+
+from .float8 import (F8Matrix, expand_shift_weights_f8, gated_f8, gated_f8_backward, linear_f8,  # noqa: E402,F401
+                     quantize_f8, rmsnorm_f8, rmsnorm_f8_backward)

@@ -242,7 +242,10 @@ const char* ds_last_error(void) { return g_last_error; }
 int ds_version(void) { return 100; }
 
 size_t ds_abi_struct_size(int which) {
-  return which == 0 ? sizeof(ds_weights) : (which == 1 ? sizeof(ds_layer) : 0);
+  return which == 0   ? sizeof(ds_weights)
+         : which == 1 ? sizeof(ds_layer)
+         : which == 2 ? sizeof(ds_f8_matrix)
+                      : 0;
 }
 
 size_t ds_packed_weight_bytes(int64_t n_out, int64_t k_red) {

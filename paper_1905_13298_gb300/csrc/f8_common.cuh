@@ -1,0 +1,271 @@
+// Shared device code of the 8-bit floating-point operators: loads of eight
+// consecutive values of any supported type, the block scale and the rounding
+// to 8 bits.
+//
+// A block of 128 values (one row, or 128 x 128 for a tile) is held as
+//     q = round8(v * (1 / s)),   s = max(amax / MAX, 2^-126),
+// amax its largest finite magnitude and MAX the format's largest value (448
+// for e4m3, 57344 for e5m2); with DS_F8_POW2 s is rounded up to a power of
+// two, so that q * s is exact in the source's type range and a later change of
+// blocks rounds nothing but values that leave the format's range.  A
+// non-finite value becomes the 8-bit NaN, and does not enter the scale.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ds_common.cuh"
+
+namespace ds {
+
+constexpr int kF8Block = 128;
+
+template <int TYPE>
+struct TypeOf;
+template <>
+struct TypeOf<DS_TYPE_F32> {
+  using T = float;
+};
+template <>
+struct TypeOf<DS_TYPE_BF16> {
+  using T = __nv_bfloat16;
+};
+template <>
+struct TypeOf<DS_TYPE_F16> {
+  using T = __half;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ void from_float(float v, float& o) { o = v; }
+__device__ __forceinline__ void from_float(float v, __nv_bfloat16& o) { o = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void from_float(float v, __half& o) { o = __float2half_rn(v); }
+
+__device__ __forceinline__ void unpack2(uint32_t u, float& a, float& b, const __nv_bfloat16*) {
+  a = __uint_as_float(u << 16);
+  b = __uint_as_float(u & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack2(uint32_t u, float& a, float& b, const __half*) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+  a = f.x;
+  b = f.y;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, const __nv_bfloat16*) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, const __half*) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Eight consecutive values as they lie in memory; `vec` says that p is 16-byte aligned.  The `n` first exist, the
+// others read as zero.
+template <typename T>
+struct Raw8 {
+  uint4 u;
+  __device__ __forceinline__ void load(const T* p, int n, bool vec) {
+    if (vec && n >= 8) {
+      u = *reinterpret_cast<const uint4*>(p);
+    } else {
+      const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = (2 * i < n ? s[2 * i] : 0u) | ((2 * i + 1 < n ? (uint32_t)s[2 * i + 1] : 0u) << 16);
+      u = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  __device__ __forceinline__ void get(float v[8]) const {
+    unpack2(u.x, v[0], v[1], (const T*)nullptr);
+    unpack2(u.y, v[2], v[3], (const T*)nullptr);
+    unpack2(u.z, v[4], v[5], (const T*)nullptr);
+    unpack2(u.w, v[6], v[7], (const T*)nullptr);
+  }
+};
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, int n, bool vec) {
+    if (vec && n >= 8) {
+      a = reinterpret_cast<const float4*>(p)[0];
+      b = reinterpret_cast<const float4*>(p)[1];
+    } else {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+      a = make_float4(v[0], v[1], v[2], v[3]);
+      b = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  }
+  __device__ __forceinline__ void get(float v[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, bool vec, const float v[8]) {
+  if (vec && n >= 8) {
+    *reinterpret_cast<uint4*>(p) =
+        make_uint4(pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr),
+                   pack2(v[4], v[5], (const T*)nullptr), pack2(v[6], v[7], (const T*)nullptr));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) from_float(v[i], p[i]);
+  }
+}
+template <>
+__device__ __forceinline__ void store8<float>(float* p, int n, bool vec, const float v[8]) {
+  if (vec && n >= 8) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = v[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// 8-bit formats
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t f8x2(float lo, float hi, bool e5m2) {
+  uint16_t r;
+  if (e5m2)
+    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 f8x2_value(uint16_t q, bool e5m2) {
+  uint32_t h;
+  if (e5m2)
+    asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"(q));
+  else
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(q));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+__device__ __forceinline__ void f8x8_value(uint2 q, bool e5m2, float v[8]) {
+  const uint32_t w[2] = {q.x, q.y};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float2 a = f8x2_value((uint16_t)(w[i] & 0xFFFFu), e5m2);
+    const float2 b = f8x2_value((uint16_t)(w[i] >> 16), e5m2);
+    v[4 * i] = a.x, v[4 * i + 1] = a.y, v[4 * i + 2] = b.x, v[4 * i + 3] = b.y;
+  }
+}
+
+struct F8Scale {
+  float s, inv;
+};
+// max and the scale's rounding are those of the matrix that is written
+__device__ __forceinline__ F8Scale f8_scale(float amax, bool e5m2, bool pow2) {
+  float s = fmaxf(__fdiv_rn(amax, e5m2 ? 57344.f : 448.f), 1.17549435e-38f);
+  if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
+  return F8Scale{s, __frcp_rn(s)};
+}
+// v * 0 is NaN for a non-finite v and 0 otherwise: infinities do not saturate silently
+__device__ __forceinline__ float f8_unit(float v, float inv) { return fmaf(v, 0.f, v * inv); }
+__device__ __forceinline__ uint2 f8x8(const float v[8], float inv, bool e5m2) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = f8x2(f8_unit(v[4 * i], inv), f8_unit(v[4 * i + 1], inv), e5m2) |
+           (f8x2(f8_unit(v[4 * i + 2], inv), f8_unit(v[4 * i + 3], inv), e5m2) << 16);
+  return make_uint2(w[0], w[1]);
+}
+// The address is 8-byte aligned: rows start 16 bytes apart or a multiple of it.
+__device__ __forceinline__ void store_q8(uint8_t* p, int n, uint2 q) {
+  if (n >= 8) {
+    *reinterpret_cast<uint2*>(p) = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint8_t)((i < 4 ? q.x >> (8 * i) : q.y >> (8 * (i - 4))) & 0xFFu);
+  }
+}
+
+__device__ __forceinline__ float finite_abs(float v) {
+  const float a = fabsf(v);
+  return a < __int_as_float(0x7F800000) ? a : 0.f;  // false for NaN as well
+}
+__device__ __forceinline__ float amax8(const float v[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[i]));
+  return m;
+}
+// The largest over the 16 lanes that hold one block of 128 columns.
+__device__ __forceinline__ float max16(float m) {
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  return m;
+}
+
+// ---------------------------------------------------------------------------
+// Launch parameters
+// ---------------------------------------------------------------------------
+struct F8Out {  // an 8-bit matrix that a kernel writes (q == NULL: none)
+  uint8_t* q;
+  float* s;
+  int64_t ld, lds;
+  int e5m2, tiles;
+};
+inline F8Out f8_out(const ds_f8_matrix* m) {
+  if (m == nullptr) return F8Out{nullptr, nullptr, 0, 0, 0, 0};
+  return F8Out{static_cast<uint8_t*>(m->q), m->scale, m->ld, m->ld_scale, m->format == DS_F8_E5M2,
+               m->blocks == DS_F8_TILES};
+}
+
+struct RmsnormParams {
+  const void *x, *residual;
+  int64_t ldx, ldr;
+  const float* weight;
+  int64_t rows, cols;
+  float eps;
+  F8Out out;
+  void* h;
+  int64_t ldh;
+  float* rstd;
+  int pow2;
+};
+struct RmsnormBackwardParams {
+  const void *dy, *h, *dh;
+  int64_t lddy, ldh, lddh;
+  const float *rstd, *weight;
+  int64_t rows, cols;
+  void* dx;
+  int64_t lddx;
+  float *dw, *partial;
+};
+struct LinearF8Params {
+  const ds_f8_matrix *x, *w;
+  const float *bias, *add;
+  int64_t ld_add;
+  void* y;
+  int type;
+  int64_t ldy;
+};
+
+constexpr int64_t kF8NormPartials = 608;  // rows of partial weight gradients: 4 CTAs on each of 152 SMs
+
+cudaError_t launch_quantize_f8(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const F8Out& out,
+                               const F8Out& out_t, bool pow2, cudaStream_t st);
+cudaError_t launch_requantize_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool pow2,
+                                 cudaStream_t st);
+cudaError_t launch_expand_f8(const uint8_t* blob, int64_t n_out, int64_t k_red, const F8Out& out, cudaStream_t st);
+cudaError_t launch_rmsnorm_f8(const RmsnormParams& p, int type, cudaStream_t st);
+cudaError_t launch_rmsnorm_f8_backward(const RmsnormBackwardParams& p, int type, cudaStream_t st);
+cudaError_t launch_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_t features, const F8Out& out,
+                            const F8Out& ckpt, bool pow2, cudaStream_t st);
+cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int type, int64_t ld, int64_t features,
+                                     const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool pow2,
+                                     cudaStream_t st);
+cudaError_t launch_linear_f8(const LinearF8Params& p, cudaStream_t st);
+int read_f8_fault_flag();
+void set_f8_wait_cycles(long long cycles);
+
+}  // namespace ds

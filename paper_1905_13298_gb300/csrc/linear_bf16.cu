@@ -25,12 +25,9 @@
 // MMAs of the CTA finished, waited for before TMEM is freed).  Every wait is
 // bounded by a clock deadline; on expiry the kernel records a fault flag,
 // stops issuing work, waits (bounded) for issued work and frees its TMEM.
-#include <cuda.h>
-
 #include <atomic>
-#include <cudaTypedefs.h>
 
-#include "ds_common.cuh"
+#include "tensor_core.cuh"
 
 namespace ds {
 
@@ -46,7 +43,6 @@ constexpr int ACC_BUFS = 2;
 constexpr int TMEM_COLS = ACC_BUFS * BN;  // 512: the whole tensor memory of an SM
 constexpr int kThreads = 192;
 constexpr int kEpiWarps = 4;
-constexpr long long kTimeoutCycles = 4000000000LL;  // about 2 s at 2 GHz
 // the wait limit of the next launches (a diagnostic can shorten it to make the waits run out)
 std::atomic<long long> g_wait_cycles{kTimeoutCycles};
 
@@ -68,73 +64,6 @@ struct __align__(8) Barriers {
   int abort;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-__device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait for the phase with the given parity; false when the CTA
-// aborted or the deadline passed (then the fault flag and abort are set).
-__device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort, long long limit) {
-  const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
-    if (*abort) return false;
-    if (clock64() - t0 > limit) {
-      *abort = 1;
-      atomicExch(&g_bf16_fault, 1);
-      return false;
-    }
-  }
-  return true;
-}
-// Bounded wait that ignores the abort flag (draining work already issued);
-// always the full limit, so that issued copies and MMAs land before the CTA
-// frees its tensor memory or exits.
-__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
-  const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kTimeoutCycles) {
-  }
-}
-
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::
-          "r"(smem_u32(dst)),
-      "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y)
-      : "memory");
-}
-
-// Shared-memory matrix descriptor of a K-major tile with 128-byte swizzle:
-// rows of 128 bytes, 8-row groups 1024 bytes apart (tile base 1024-aligned).
-__device__ __forceinline__ uint64_t sw128_desc(uint32_t addr) {
-  uint64_t d = (uint64_t)((addr >> 4) & 0x3FFFu);  // start address
-  d |= (uint64_t)1 << 16;                          // leading byte offset (unused for swizzled K-major)
-  d |= (uint64_t)(1024 >> 4) << 32;                // stride byte offset
-  d |= (uint64_t)1 << 46;                          // descriptor version of this architecture
-  d |= (uint64_t)2 << 61;                          // 128-byte swizzle
-  return d;
-}
-
 // Instruction descriptor: kind::f16 with bf16 A and B (K-major), fp32 D, M = 128, N = 256.
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) |
                             ((uint32_t)(BM >> 4) << 24);
@@ -147,11 +76,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t adesc, uint6
       "l"(adesc), "l"(bdesc), "r"(kIdesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-               : "memory");
-}
-
 // Tile t of the grouped order: rows [m0, m0 + BM), columns [n0, n0 + BN).
 __device__ __forceinline__ void tile_of(int64_t t, int64_t tiles_m, int64_t tiles_n, int64_t G, int& m0, int& n0) {
   const int64_t per_group = G * tiles_n;
@@ -215,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int kt = 0; kt < nk; ++kt, ++it) {
           const int s = (int)(it % STAGES);
           const uint32_t ph = (uint32_t)(it / STAGES) & 1u;
-          if (it >= STAGES && !mbar_wait(&bars->empty[s], ph ^ 1u, abort, P.wait_cycles)) {
+          if (it >= STAGES && !mbar_wait(&bars->empty[s], ph ^ 1u, abort, P.wait_cycles, &g_bf16_fault)) {
             ok = false;
             break;
           }
@@ -238,13 +162,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int64_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x, ++i) {
         const int b = (int)(i & 1);
         // accumulator b is free once the epilogue has read tile i - 2 out of it
-        if (i >= ACC_BUFS && !mbar_wait(&bars->tempty[b], (uint32_t)((i / ACC_BUFS) - 1) & 1u, abort, P.wait_cycles)) break;
+        if (i >= ACC_BUFS && !mbar_wait(&bars->tempty[b], (uint32_t)((i / ACC_BUFS) - 1) & 1u, abort, P.wait_cycles, &g_bf16_fault)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t tmem_d = tmem_base + (uint32_t)(b * BN);
         for (int kt = 0; kt < nk; ++kt, ++it) {
           const int s = (int)(it % STAGES);
           const uint32_t ph = (uint32_t)(it / STAGES) & 1u;
-          if (!mbar_wait(&bars->full[s], ph, abort, P.wait_cycles)) {
+          if (!mbar_wait(&bars->full[s], ph, abort, P.wait_cycles, &g_bf16_fault)) {
             ok = false;
             break;
           }
@@ -270,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     int64_t i = 0;
     for (int64_t t = blockIdx.x; t < ntiles; t += gridDim.x, ++i) {
       const int b = (int)(i & 1);
-      if (!mbar_wait(&bars->tfull[b], (uint32_t)(i / ACC_BUFS) & 1u, abort, P.wait_cycles)) break;
+      if (!mbar_wait(&bars->tfull[b], (uint32_t)(i / ACC_BUFS) & 1u, abort, P.wait_cycles, &g_bf16_fault)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       int tm0, tn0;
       tile_of(t, tiles_m, tiles_n, G, tm0, tn0);
@@ -365,31 +289,9 @@ __global__ void expand_bf16_kernel(const uint8_t* __restrict__ blob, int64_t n_o
   }
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
-  // once per process, thread-safe (function-local static)
-  static const PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    return static_cast<PFN_cuTensorMapEncodeTiled_v12000>(nullptr);
-  }();
-  return fn;
-}
-
 bool make_map(CUtensorMap* map, const void* ptr, int64_t inner, int64_t outer, int64_t row_stride_elems,
               uint32_t box_outer) {
-  PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode();
-  if (enc == nullptr) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  cuuint64_t strides[1] = {(cuuint64_t)row_stride_elems * 2};
-  cuuint32_t box[2] = {(cuuint32_t)BK, box_outer};
-  cuuint32_t estr[2] = {1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return make_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ptr, inner, outer, row_stride_elems * 2, BK, box_outer);
 }
 
 }  // namespace

@@ -1,0 +1,289 @@
+"""Tensor-level helpers of the 8-bit floating-point operators (see the header's section on them).
+
+An ``F8Matrix`` holds 8-bit values and their scales, one per block of 128.  The helpers check what the C ABI cannot
+see (dtype, shape, strides, device), allocate outputs with torch, and make one call each.
+
+A training step of a gated feed-forward block reads::
+
+    n, h, rstd = rmsnorm_f8(x, norm_w, residual=stream)        # 8-bit rows of the norm, the new residual stream
+    gu = linear_f8(n, w_gu)                                    # w_gu: quantize_f8(weight, "tiles", "tiles")[0]
+    a, kept = gated_f8(gu, features)                           # only `kept` is needed again
+    y = linear_f8(a, w_down)
+    ...
+    d, d_t = quantize_f8(dy, "rows", "rows")                   # the gradient by rows and by columns
+    da = linear_f8(d, w_down_t)
+    dgu, dgu_t, a_t = gated_f8_backward(kept, da)
+    grad_down = linear_f8(d_t, a_t, add=grad_down, out=grad_down, dtype=torch.float32)
+    n_t = quantize_f8(n, None, "rows")[1]
+    grad_gu = linear_f8(dgu_t, n_t, add=grad_gu, out=grad_gu, dtype=torch.float32)
+    dx, grad_norm = rmsnorm_f8_backward(linear_f8(dgu, w_gu_t), h, rstd, norm_w, dh=dy)
+"""
+from __future__ import annotations
+
+import torch
+
+from . import (DS_F8_E4M3, DS_F8_E5M2, DS_F8_POW2, DS_F8_ROWS, DS_F8_TILES, DS_TYPE_BF16, DS_TYPE_F16, DS_TYPE_F32,
+               _on_one_gpu, ds_expand_shift_weights_f8, ds_f8_matrix, ds_gated_f8, ds_gated_f8_backward, ds_linear_f8,
+               ds_quantize_f8, ds_requantize_f8, ds_rmsnorm_f8, ds_rmsnorm_f8_backward,
+               ds_rmsnorm_f8_backward_workspace_bytes)
+
+_TYPES = {torch.float32: DS_TYPE_F32, torch.bfloat16: DS_TYPE_BF16, torch.float16: DS_TYPE_F16}
+_FORMATS = {torch.float8_e4m3fn: DS_F8_E4M3, torch.float8_e5m2: DS_F8_E5M2}
+_BLOCKS = {"rows": DS_F8_ROWS, "tiles": DS_F8_TILES}
+BLOCK = 128
+
+
+class F8Matrix:
+    """8-bit values ``q`` [rows, cols] (``torch.float8_e4m3fn`` or ``float8_e5m2``, rows a multiple of 16 bytes apart)
+    and float32 scales: ``scale`` [rows, ceil(cols / 128)], or with ``tiles`` [ceil(rows / 128), ceil(cols / 128)]."""
+
+    __slots__ = ("q", "scale", "desc")
+
+    def __init__(self, q, scale, tiles: bool = False):
+        fmt = _FORMATS.get(q.dtype)
+        if fmt is None:
+            raise ValueError(f"q must be torch.float8_e4m3fn or torch.float8_e5m2, got {q.dtype}")
+        if scale.dtype != torch.float32:
+            raise ValueError(f"scale must be torch.float32, got {scale.dtype}")
+        if q.dim() != 2:
+            raise ValueError("q must be [rows, cols]")
+        rows, cols = q.shape
+        ld = _row_stride(q, "q")
+        if ld % 16:
+            raise ValueError(f"rows of q must start a multiple of 16 bytes apart, got {ld} (pad the columns)")
+        want = (-(-rows // BLOCK) if tiles else rows, -(-cols // BLOCK))
+        if scale.shape != want:
+            raise ValueError(f"scale has shape {tuple(scale.shape)}, expected {want}")
+        if q.device != scale.device or q.device.type != "cuda":
+            raise ValueError("q and scale must be CUDA tensors of one device")
+        self.q, self.scale = q, scale
+        self.desc = ds_f8_matrix(q.data_ptr(), scale.data_ptr(), rows, cols, ld, _row_stride(scale, "scale"), fmt,
+                                 DS_F8_TILES if tiles else DS_F8_ROWS)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device, dtype=torch.float8_e4m3fn, tiles: bool = False) -> "F8Matrix":
+        """Uninitialised memory for a matrix, rows padded to a multiple of 16 bytes."""
+        fmt = _FORMATS.get(dtype)
+        if fmt is None:
+            raise ValueError(f"dtype must be torch.float8_e4m3fn or torch.float8_e5m2, got {dtype}")
+        m = cls.__new__(cls)
+        ld, nb = (cols + 15) // 16 * 16, (cols + BLOCK - 1) // BLOCK
+        m.q = torch.empty((rows, ld), dtype=dtype, device=device)
+        if ld != cols:
+            m.q = m.q[:, :cols]
+        m.scale = torch.empty(((rows + BLOCK - 1) // BLOCK if tiles else rows, nb), dtype=torch.float32, device=device)
+        m.desc = ds_f8_matrix(m.q.data_ptr(), m.scale.data_ptr(), rows, cols, ld, nb, fmt,
+                              DS_F8_TILES if tiles else DS_F8_ROWS)
+        return m
+
+    @property
+    def rows(self) -> int:
+        return self.desc.rows
+
+    @property
+    def cols(self) -> int:
+        return self.desc.cols
+
+    @property
+    def tiles(self) -> bool:
+        return self.desc.blocks == DS_F8_TILES
+
+    def dequantize(self):
+        """The float32 values [rows, cols]."""
+        s = self.scale.repeat_interleave(BLOCK, 1)[:, : self.cols]
+        if self.tiles:
+            s = s.repeat_interleave(BLOCK, 0)[: self.rows]
+        return self.q.float() * s
+
+
+def _row_stride(t, name: str) -> int:
+    """Elements between the rows of a matrix whose columns are next to each other (a row alone has any stride)."""
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have consecutive columns")
+    ld = t.stride(0)
+    if rows <= 1 or cols == 0:  # the stride is not used; torch may have set it to anything
+        ld = max(ld, cols)
+        if t.element_size() == 1:
+            ld = (ld + 15) // 16 * 16
+    elif ld < cols:
+        raise ValueError(f"rows of {name} overlap")
+    return ld
+
+
+def _matrix(t, name: str, shape=None, dtype=None):
+    """Checks a [rows, cols] tensor; returns its row stride (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype not in _TYPES if dtype is None else t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype or 'float32, bfloat16 or float16'}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return _row_stride(t, name)
+
+
+def _vector(t, name: str, n: int) -> None:
+    if t is None:
+        return
+    if t.dtype != torch.float32:
+        raise ValueError(f"{name} must be torch.float32, got {t.dtype}")
+    if tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n} values, got shape {tuple(t.shape)}")
+
+
+def _f8(m, name: str):
+    if not isinstance(m, F8Matrix):
+        raise ValueError(f"{name} must be an F8Matrix")
+    return m.desc
+
+
+def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, pow2: bool = False,
+                dtype=torch.float8_e4m3fn, stream=None):
+    """Rounds x [rows, cols] (a tensor, or an F8Matrix whose blocks change) to 8 bits with a scale per block of 128.
+
+    ``blocks`` is the kind of blocks of the result ("rows", "tiles", or None for no result) and ``transposed`` that of
+    its transpose [cols, rows]; returns (result, transpose), made in one pass over x.  ``pow2`` rounds scales up to
+    powers of two.
+    """
+    for b in (blocks, transposed):
+        if b is not None and b not in _BLOCKS:
+            raise ValueError(f"blocks are 'rows', 'tiles' or None, got {b!r}")
+    if dtype not in _FORMATS:
+        raise ValueError(f"dtype must be torch.float8_e4m3fn or torch.float8_e5m2, got {dtype}")
+    if blocks is None and transposed is None:
+        raise ValueError("neither the matrix nor its transpose is asked for")
+    is_f8 = isinstance(x, F8Matrix)
+    if is_f8:
+        rows, cols, device = x.rows, x.cols, x.q.device
+    else:
+        ld = _matrix(x, "x")
+        _on_one_gpu(x=x)
+        rows, cols, device = x.shape[0], x.shape[1], x.device
+    out = F8Matrix.empty(rows, cols, device, dtype, blocks == "tiles") if blocks else None
+    out_t = F8Matrix.empty(cols, rows, device, dtype, transposed == "tiles") if transposed else None
+    d, d_t = out.desc if out else None, out_t.desc if out_t else None
+    flags = DS_F8_POW2 if pow2 else 0
+    if is_f8:
+        ds_requantize_f8(x.desc, d, d_t, flags, stream)
+    else:
+        ds_quantize_f8(x, _TYPES[x.dtype], rows, cols, ld, d, d_t, flags, stream)
+    return out, out_t
+
+
+def expand_shift_weights_f8(w, stream=None) -> F8Matrix:
+    """The weights s * 2^p of a PackedShiftWeights as an e4m3 matrix in tiles (exact: q = s * 2^(p + 8), scales 2^-8)."""
+    m = F8Matrix.empty(w.n_out, w.k_red, w.blob.device, tiles=True)
+    ds_expand_shift_weights_f8(w.desc, m.desc, stream)
+    return m
+
+
+def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=torch.bfloat16, stream=None):
+    """y = x @ w^T + bias + add for 8-bit x [M, K] and w [N, K]: a tensor [M, N] of ``dtype`` (or ``out``'s).
+
+    ``bias`` is float32 [N], ``add`` float32 [M, N]; ``out`` may be ``add`` itself, which then accumulates."""
+    dx, dw = _f8(x, "x"), _f8(w, "w")
+    M, N = dx.rows, dw.rows
+    _vector(bias, "bias", N)
+    ld_add = _matrix(add, "add", (M, N), torch.float32)
+    y = out
+    if y is None:
+        if dtype not in _TYPES:
+            raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+        y = torch.empty((M, N), dtype=dtype, device=x.q.device)
+        ldy = N
+    else:
+        ldy = _matrix(y, "out", (M, N))
+    _on_one_gpu(x=x.q, w=w.q, bias=bias, add=add, out=out)
+    ds_linear_f8(dx, dw, bias, add, ld_add, y, _TYPES[y.dtype], ldy, stream)
+    return y
+
+
+def rmsnorm_f8(x, weight, residual=None, eps: float = 1e-5, pow2: bool = False, dtype=torch.float8_e4m3fn, h=None,
+               stream=None):
+    """Root-mean-square norm of h = x + residual, in 8 bits with a scale per row and 128 columns.
+
+    Returns (n, h, rstd): the F8Matrix of h * rstd * weight, h in x's dtype (x itself without a residual, ``h`` where
+    given; it may be x or residual), and the float32 reciprocal root mean squares that the backward pass reads."""
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    _vector(weight, "weight", cols)
+    ldr = _matrix(residual, "residual", (rows, cols), x.dtype)
+    ldh = _matrix(h, "h", (rows, cols), x.dtype)
+    _on_one_gpu(x=x, weight=weight, residual=residual, h=h)
+    store = h
+    if h is None:
+        if residual is None:
+            h = x
+        else:
+            store = h = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+            ldh = cols
+    n = F8Matrix.empty(rows, cols, x.device, dtype)
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    ds_rmsnorm_f8(x, ldx, residual, ldr, weight, _TYPES[x.dtype], rows, cols, eps, n.desc, store, ldh, rstd,
+                  DS_F8_POW2 if pow2 else 0, stream)
+    return n, h, rstd
+
+
+def rmsnorm_f8_backward(dy, h, rstd, weight, dh=None, out=None, stream=None):
+    """Backward pass of rmsnorm_f8: (dx, dweight) from the gradient dy of the norm (the rounding to 8 bits passes it
+    unchanged), what the forward pass returned, and the gradient dh that the stream h brings (or None).  dx is the
+    gradient of x and of residual alike; ``out`` may be dy, h or dh."""
+    lddy = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    ldh = _matrix(h, "h", (rows, cols), dy.dtype)
+    lddh = _matrix(dh, "dh", (rows, cols), dy.dtype)
+    _vector(rstd, "rstd", rows)
+    _vector(weight, "weight", cols)
+    dx = out
+    lddx = _matrix(out, "out", (rows, cols), dy.dtype)
+    if dx is None:
+        dx, lddx = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device), cols
+    _on_one_gpu(dy=dy, h=h, rstd=rstd, weight=weight, dh=dh, out=out)
+    dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    nbytes = ds_rmsnorm_f8_backward_workspace_bytes(rows, cols)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device)
+    ds_rmsnorm_f8_backward(dy, lddy, h, ldh, rstd, weight, dh, lddh, _TYPES[dy.dtype], rows, cols, dx, lddx, dw, ws,
+                           nbytes, stream)
+    return dx, dw
+
+
+def _gate_width(features: int) -> int:
+    """Columns of a gate's input: the up half starts at the next multiple of 128."""
+    return (features + BLOCK - 1) // BLOCK * BLOCK + features
+
+
+def gated_f8(gu, features: int, checkpoint: bool = True, pow2: bool = False, dtype=torch.float8_e4m3fn, stream=None):
+    """a = silu(g) * u in 8 bits, for gu [rows, up + features] with g in columns [0, features) and u from column
+    up = features rounded up to a multiple of 128.  Returns (a, kept): kept is the 8-bit checkpoint of gu that
+    gated_f8_backward reads (None without ``checkpoint``)."""
+    ld = _matrix(gu, "gu")
+    rows, width = gu.shape
+    if features <= 0 or width != _gate_width(features):
+        raise ValueError(f"gu has {width} columns, expected {_gate_width(features)} for {features} features")
+    _on_one_gpu(gu=gu)
+    a = F8Matrix.empty(rows, features, gu.device, dtype)
+    kept = F8Matrix.empty(rows, width, gu.device, dtype) if checkpoint else None
+    ds_gated_f8(gu, _TYPES[gu.dtype], ld, rows, features, a.desc, kept.desc if kept else None,
+                DS_F8_POW2 if pow2 else 0, stream)
+    return a, kept
+
+
+def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8_e4m3fn, transposed: bool = True,
+                      stream=None):
+    """Backward pass of gated_f8 from its checkpoint and the gradient da [rows, features] of a.  Returns
+    (dgu, dgu_t, a_t) in 8 bits: the gradient of gu, its transpose, and the transpose of a made again from the
+    checkpoint (the operands of the two weight gradients; None without ``transposed``)."""
+    dk = _f8(kept, "kept")
+    ld = _matrix(da, "da")
+    rows, features = da.shape
+    if features == 0 or dk.rows != rows or dk.cols != _gate_width(features):
+        raise ValueError(f"kept is {dk.rows} x {dk.cols}, expected {rows} x {_gate_width(features)}")
+    _on_one_gpu(da=da, kept=kept.q)
+    dgu = F8Matrix.empty(rows, dk.cols, da.device, dtype)
+    dgu_t = F8Matrix.empty(dk.cols, rows, da.device, dtype) if transposed else None
+    a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None
+    ds_gated_f8_backward(dk, da, _TYPES[da.dtype], ld, features, dgu.desc, dgu_t.desc if dgu_t else None,
+                         a_t.desc if a_t else None, DS_F8_POW2 if pow2 else 0, stream)
+    return dgu, dgu_t, a_t
