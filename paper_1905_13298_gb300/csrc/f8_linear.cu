@@ -42,7 +42,9 @@ struct Params {
   int nk;         // blocks of the reduction
   uint32_t idesc;  // formats of the operands, without the tile's shape
   int type;       // of y
+  int scale4;     // rows of scales are aligned for loads of four
   int vec;        // y's rows are aligned for stores of four values, add's for loads of four
+  int sectors;    // y's rows are aligned for stores of 32 bytes, add's for loads of four
   long long wait_cycles;
 };
 
@@ -72,6 +74,11 @@ __device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
   return r;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  lo = __uint_as_float((uint32_t)v);
+  hi = __uint_as_float((uint32_t)(v >> 32));
 }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   uint64_t r;
@@ -149,38 +156,131 @@ __device__ __forceinline__ void finish4(const Params& P, int64_t m, int64_t n, f
   }
 }
 
+// 32 bytes of one row: a whole sector of the second-level cache.
+__device__ __forceinline__ void store_sector(void* p, const uint32_t v[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+// COLS consecutive sums of row m from column n, by one thread: bias and `add` added, rounded once, stored by sectors.
+// All columns exist and the rows of y (and add) are aligned to 32 bytes.
+template <int COLS>
+__device__ __forceinline__ void store_row(const Params& P, int64_t m, int64_t n, float v[COLS]) {
+  if (P.bias) {
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) v[j] += P.bias[n + j];
+  }
+  if (P.add) {
+    const float4* a = reinterpret_cast<const float4*>(P.add + m * P.ld_add + n);
+#pragma unroll
+    for (int j = 0; j < COLS; j += 4) {
+      const float4 f = a[j / 4];
+      v[j] += f.x, v[j + 1] += f.y, v[j + 2] += f.z, v[j + 3] += f.w;
+    }
+  }
+  uint32_t w[8];
+  if (P.type == DS_TYPE_F32) {
+    float* y = static_cast<float*>(P.y) + m * P.ldy + n;
+#pragma unroll
+    for (int j = 0; j < COLS; j += 8) {
+#pragma unroll
+      for (int l = 0; l < 8; ++l) w[l] = __float_as_uint(v[j + l]);
+      store_sector(y + j, w);
+    }
+  } else if (P.type == DS_TYPE_BF16) {
+    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(P.y) + m * P.ldy + n;
+#pragma unroll
+    for (int j = 0; j < COLS; j += 16) {
+#pragma unroll
+      for (int l = 0; l < 8; ++l) w[l] = pack2(v[j + 2 * l], v[j + 2 * l + 1], (const __nv_bfloat16*)nullptr);
+      store_sector(y + j, w);
+    }
+  } else {
+    __half* y = static_cast<__half*>(P.y) + m * P.ldy + n;
+#pragma unroll
+    for (int j = 0; j < COLS; j += 16) {
+#pragma unroll
+      for (int l = 0; l < 8; ++l) w[l] = pack2(v[j + 2 * l], v[j + 2 * l + 1], (const __half*)nullptr);
+      store_sector(y + j, w);
+    }
+  }
+}
+
 constexpr int BK = 128;    // bytes of a row per stage: one block of the reduction
 constexpr int ROWS = 128;  // rows of w per tile: the lanes of tensor memory
-constexpr int kThreads = 192;
-constexpr int kEpiWarps = 4;
+// A position in a ring of N barriers: the slot and the parity of its phase.
+template <int N>
+struct Ring {
+  uint32_t slot = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++slot == N) {
+      slot = 0;
+      parity ^= 1u;
+    }
+  }
+};
 
+// The scales of PER rows on their way to shared memory, GROUP blocks of the reduction at a time.
+template <int PER, int GROUP>
+struct ScaleFeed {
+  const float* src[PER];  // at a row's first block; NULL: no such row, and zeros in its products
+  float next[PER][GROUP];
+  __device__ __forceinline__ void load(int i0, int nk, bool vec) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+#pragma unroll
+      for (int b = 0; b < GROUP; ++b) next[i][b] = 0.f;
+      if (src[i] == nullptr) continue;
+      if (vec && nk - i0 >= GROUP) {
+        if constexpr (GROUP == 4) {
+          const float4 f = *reinterpret_cast<const float4*>(src[i] + i0);
+          next[i][0] = f.x, next[i][1] = f.y, next[i][2] = f.z, next[i][3] = f.w;
+        } else {
+          const float2 f = *reinterpret_cast<const float2*>(src[i] + i0);
+          next[i][0] = f.x, next[i][1] = f.y;
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < GROUP; ++b)
+          if (i0 + b < nk) next[i][b] = src[i][i0 + b];
+      }
+    }
+  }
+};
+
+constexpr int kThreads = 256;
+constexpr int kEpiWarps = 4;
+// After a wait gave up, a stage's barrier may miss the arrivals of warps that left; its copies land within
+// microseconds, and this many cycles (8 ms) are waited for them.
+constexpr long long kLandedCycles = 1 << 24;
+
+// STAGES of the data ring, ACC accumulators in tensor memory, CTAs that share an SM.
 template <int BN>
 struct Cfg;
-// STAGES: two CTAs per SM up to BN = 64; ACC: accumulators in tensor memory
 template <>
 struct Cfg<16> {
-  static constexpr int STAGES = 6, ACC = 4;
+  static constexpr int STAGES = 5, ACC = 4, CTAS = 2;
 };
 template <>
 struct Cfg<32> {
-  static constexpr int STAGES = 5, ACC = 4;
+  static constexpr int STAGES = 5, ACC = 4, CTAS = 2;
 };
 template <>
 struct Cfg<64> {
-  static constexpr int STAGES = 4, ACC = 4;
+  static constexpr int STAGES = 4, ACC = 4, CTAS = 2;
 };
 template <>
 struct Cfg<128> {
-  static constexpr int STAGES = 6, ACC = 4;
+  static constexpr int STAGES = 5, ACC = 4, CTAS = 1;
 };
 
 template <int BN>
 struct __align__(16) Shared {
-  float col_scale[kEpiWarps][2][BN];
-  uint64_t full[Cfg<BN>::STAGES];
-  uint64_t empty[Cfg<BN>::STAGES];
-  uint64_t tfull[Cfg<BN>::ACC];
-  uint64_t tempty[Cfg<BN>::ACC];
+  static constexpr int SLOTS = Cfg<BN>::STAGES + Cfg<BN>::ACC + 1;  // of scales: see kScaleSlots
+  float scale[SLOTS][ROWS + BN];                                    // rows of w, then rows of x
+  uint64_t full[Cfg<BN>::STAGES];   // a stage's copies and scales have come
+  uint64_t mult[Cfg<BN>::STAGES];   // its products are done
+  uint64_t tempty[Cfg<BN>::ACC];    // an accumulator has been read
   uint64_t done;
   uint32_t tmem_base;
   int abort;
@@ -192,9 +292,10 @@ constexpr size_t smem_bytes() {
 }
 
 // One tile: 128 rows of w (n0 ..), BN rows of x (m0 ..).  blockIdx.x = tile * split + rank in the cluster; the rank takes
-// the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2-5 scale.
+// the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2 and 3
+// bring scales (as in the large kernel below), warps 4-7 add.
 template <int BN>
-__global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_constant__ CUtensorMap tmap_w,
+__global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(const __grid_constant__ CUtensorMap tmap_w,
                                                              const __grid_constant__ CUtensorMap tmap_x,
                                                              const Params P, const int split) {
   constexpr int STAGES = Cfg<BN>::STAGES, ACC = Cfg<BN>::ACC;
@@ -207,24 +308,21 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   Shared<BN>* sh = reinterpret_cast<Shared<BN>*>(ring + STAGES * STAGE_BYTES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t tiles_n = (P.N + ROWS - 1) / ROWS;
-  const int64_t tile = blockIdx.x / split;
+  const uint32_t tiles_n = (uint32_t)((P.N + ROWS - 1) / ROWS);
+  const uint32_t tile = blockIdx.x / split;
   const int rank = (int)(blockIdx.x - tile * split);
-  const int64_t tm = tile / tiles_n;
-  const int64_t n0 = (tile - tm * tiles_n) * ROWS, m0 = tm * BN;
+  const uint32_t tm = tile / tiles_n;
+  const int n0 = (int)(tile - tm * tiles_n) * ROWS, m0 = (int)tm * BN;
   const int kb0 = (int)((int64_t)P.nk * rank / split);
   const int nk = (int)((int64_t)P.nk * (rank + 1) / split) - kb0;
   volatile int* abort = &sh->abort;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&sh->full[s], 1);
-      mbar_init(&sh->empty[s], 1);
+      mbar_init(&sh->full[s], 3);  // the copies, and two warps with scales
+      mbar_init(&sh->mult[s], 1);
     }
-    for (int b = 0; b < ACC; ++b) {
-      mbar_init(&sh->tfull[b], 1);
-      mbar_init(&sh->tempty[b], kEpiWarps);
-    }
+    for (int b = 0; b < ACC; ++b) mbar_init(&sh->tempty[b], kEpiWarps);
     mbar_init(&sh->done, 1);
     sh->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -246,74 +344,95 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
 
   if (warp == 0) {
     if (lane == 0) {
+      Ring<STAGES> st;
       int i = 0;
-      for (; i < nk; ++i) {
-        const int s = i % STAGES;
-        if (i >= STAGES &&
-            !mbar_wait(&sh->empty[s], (uint32_t)((i / STAGES) & 1) ^ 1u, abort, P.wait_cycles, &g_f8_fault))
-          break;
-        unsigned char* a = ring + s * STAGE_BYTES;
-        mbar_expect_tx(&sh->full[s], STAGE_BYTES);
-        tma_load_2d(a, &tmap_w, &sh->full[s], (kb0 + i) * BK, (int)n0);
-        tma_load_2d(a + A_BYTES, &tmap_x, &sh->full[s], (kb0 + i) * BK, (int)m0);
+      for (; i < nk; ++i, st.next()) {
+        if (!mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault)) break;
+        unsigned char* a = ring + st.slot * STAGE_BYTES;
+        mbar_expect_tx(&sh->full[st.slot], STAGE_BYTES);
+        tma_load_2d(a, &tmap_w, &sh->full[st.slot], (kb0 + i) * BK, n0);
+        tma_load_2d(a + A_BYTES, &tmap_x, &sh->full[st.slot], (kb0 + i) * BK, m0);
       }
-      for (int j = (i > STAGES ? i - STAGES : 0); j < i; ++j)
-        mbar_drain(&sh->full[j % STAGES], (uint32_t)(j / STAGES) & 1u);
+      // the last copies issued land before the CTA leaves
+      for (int j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        mbar_drain(&sh->full[j % STAGES], (uint32_t)(j / STAGES) & 1u, *abort ? kLandedCycles : kTimeoutCycles);
     }
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t idesc = P.idesc | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
-      for (int i = 0; i < nk; ++i) {
-        const int s = i % STAGES, b = i % ACC;
-        if (i >= ACC &&
-            !mbar_wait(&sh->tempty[b], (uint32_t)((i / ACC) - 1) & 1u, abort, P.wait_cycles, &g_f8_fault))
+      const uint64_t adesc = sw128_desc(smem_u32(ring)), bdesc = sw128_desc(smem_u32(ring) + A_BYTES);
+      Ring<STAGES> st;
+      Ring<ACC> ac;
+      for (int i = 0; i < nk; ++i, st.next(), ac.next()) {
+        if (!mbar_wait(&sh->full[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault) ||
+            !mbar_wait(&sh->tempty[ac.slot], ac.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault))
           break;
-        if (!mbar_wait(&sh->full[s], (uint32_t)(i / STAGES) & 1u, abort, P.wait_cycles, &g_f8_fault)) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t a = smem_u32(ring + s * STAGE_BYTES), x = a + A_BYTES;
+        const uint64_t at = (uint64_t)(st.slot * (STAGE_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < BK / 32; ++k)
-          umma_f8(tmem_base + (uint32_t)(b * BN), sw128_desc(a + 32 * k), sw128_desc(x + 32 * k), idesc, k > 0);
-        umma_commit(&sh->empty[s]);
-        umma_commit(&sh->tfull[b]);
+          umma_f8(tmem_base + ac.slot * BN, adesc + at + 2 * k, bdesc + at + 2 * k, idesc, k > 0);
+        umma_commit(&sh->mult[st.slot]);
       }
       // every MMA issued by this CTA has completed before its memory is used again
       umma_commit(&sh->done);
       mbar_drain(&sh->done, 0u);
     }
-  } else {
-    const int q = warp & 3, e = warp - 2;
-    constexpr int PER = (BN + 31) / 32;
-    const int64_t n = n0 + 32 * q + lane;
-    const float* sw = P.w.s + (n >> P.w.shift) * P.w.ld + kb0;
-    const float* sx[PER];
-    bool has[PER];
+  } else if (warp < 4) {
+    constexpr int XROWS = (BN + 63) / 64, PER = 2 + XROWS, GROUP = 4;
+    const int j = threadIdx.x - 64;
+    ScaleFeed<PER, GROUP> feed;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int64_t m = m0 + 32 * j + lane;
-      has[j] = 32 * j + lane < BN && m < P.M;
-      sx[j] = P.x.s + (m >> P.x.shift) * P.x.ld + kb0;
+    for (int i = 0; i < PER; ++i) {
+      const int64_t n = n0 + j + 64 * i, m = m0 + j + 64 * (i - 2);
+      feed.src[i] = nullptr;
+      if (i < 2) {
+        if (n < P.N) feed.src[i] = P.w.s + (n >> P.w.shift) * P.w.ld + kb0;
+      } else if (j + 64 * (i - 2) < BN && m < P.M) {
+        feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld + kb0;
+      }
     }
-    float rs = 0.f, cs[PER];
-    auto fetch = [&](int i) {  // scales of block i (a row that does not exist has no scale, and zeros in its products)
-      rs = n < P.N ? sw[i] : 0.f;
+    const bool vec = P.scale4 && kb0 % 4 == 0;
+    feed.load(0, nk, vec);
+    Ring<STAGES> st;
+    Ring<Shared<BN>::SLOTS> sc;
+    bool ok = true;
+    for (int i0 = 0; i0 < nk && ok; i0 += GROUP) {
+      float v[PER][GROUP];
 #pragma unroll
-      for (int j = 0; j < PER; ++j) cs[j] = has[j] ? sx[j][i] : 0.f;
-    };
-    if (nk > 0) fetch(0);
-    for (int i = 0; i < nk; ++i) {
-      const int b = i % ACC;
-      float* col = sh->col_scale[e][i & 1];
+      for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int j = 0; j < PER; ++j)
-        if (32 * j + lane < BN) col[32 * j + lane] = cs[j];
-      const uint64_t row2 = pair(__float_as_uint(rs), __float_as_uint(rs));
-      __syncwarp();
-      if (i + 1 < nk) fetch(i + 1);
-      const bool ok = mbar_wait(&sh->tfull[b], (uint32_t)(i / ACC) & 1u, abort, P.wait_cycles, &g_f8_fault);
+        for (int b = 0; b < GROUP; ++b) v[i][b] = feed.next[i][b];
+      if (i0 + GROUP < nk) feed.load(i0 + GROUP, nk, vec);
+#pragma unroll
+      for (int b = 0; b < GROUP; ++b) {
+        if (i0 + b >= nk) break;
+        ok = __all_sync(0xFFFFFFFFu,
+                        mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault));
+        if (!ok) break;
+        float* to = sh->scale[sc.slot] + j;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i < 2 || j + 64 * (i - 2) < BN) to[64 * i] = v[i][b];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->full[st.slot]);
+        st.next();
+        sc.next();
+      }
+    }
+  } else {
+    const int q = warp & 3;
+    Ring<STAGES> st;
+    Ring<ACC> ac;
+    Ring<Shared<BN>::SLOTS> sc;
+    for (int i = 0; i < nk; ++i, st.next(), ac.next(), sc.next()) {
+      const bool ok = mbar_wait(&sh->mult[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault);
       if (!__all_sync(0xFFFFFFFFu, ok)) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)(b * BN);
+      const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + ac.slot * BN;
+      const float* scale = sh->scale[sc.slot];
+      const float rs = scale[32 * q + lane];
+      const uint64_t row2 = pair(rs, rs);
 #pragma unroll
       for (int c = 0; c < BN; c += 16) {
         uint32_t r[16];
@@ -321,14 +440,14 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
         tmem_wait_ld();
 #pragma unroll
         for (int j = 0; j < 16; j += 4) {
-          const ulonglong2 s2 = *reinterpret_cast<const ulonglong2*>(&col[c + j]);
+          const ulonglong2 s2 = *reinterpret_cast<const ulonglong2*>(&scale[ROWS + c + j]);
           acc[(c + j) / 2] = fma2(mul2(pair(r[j], r[j + 1]), row2), s2.x, acc[(c + j) / 2]);
           acc[(c + j) / 2 + 1] = fma2(mul2(pair(r[j + 2], r[j + 3]), row2), s2.y, acc[(c + j) / 2 + 1]);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh->tempty[b]);
+      if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -340,7 +459,7 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
   }
   // the ring is free: the CTA's sums, [x row][w row]
   float* part = reinterpret_cast<float*>(ring);
-  if (warp >= 2) {
+  if (warp >= 4) {
     const int at = 32 * (warp & 3) + lane;
 #pragma unroll
     for (int j = 0; j < BN / 2; ++j) {
@@ -348,6 +467,7 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
       part[(2 * j + 1) * ROWS + at] = __uint_as_float((uint32_t)(acc[j] >> 32));
     }
   }
+  __syncwarp();
   if (split > 1)
     cluster_sync();
   else
@@ -369,21 +489,332 @@ __global__ void __launch_bounds__(kThreads) linear_f8_kernel(const __grid_consta
   if (split > 1) cluster_sync();  // a CTA's sums are read by the others until here
 }
 
+// ---------------------------------------------------------------------------
+// Large products: one persistent CTA per SM walks tiles of 128 rows of x (the
+// lanes) by 256 rows of w (the columns).  Warp 0 loads, warp 1 multiplies block
+// after block into two accumulators of 256 columns in turn, and eight warps
+// read each block back and add it, scaled, to the tile's sums: 128 float32 per
+// thread.  Warps 2 and 3 write a block's scales to shared memory as part of
+// its stage (the stage's barrier counts them with the copies), so the warps
+// that add wait for one barrier per block.
+//
+// A block's products take 512 cycles; what the adding warps do for it has to
+// fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
+// shared memory 40: a second barrier per block for the scales made it 1100.
+// ---------------------------------------------------------------------------
+constexpr int BIG_N = 256, BIG_STAGES = 4, BIG_ACC = 2;
+constexpr int kBigEpiWarps = 8;
+constexpr int kBigCols = BIG_N / (kBigEpiWarps / 4);  // columns of a tile that a warp adds up
+constexpr int kBigThreads = 32 * (4 + kBigEpiWarps);
+// Slots of the scales' ring.  A slot of the data ring is free when the products of the block 4 before are done, which
+// needed the accumulator of the block 6 before, whose readers were done with the block 7 before: so a slot of the
+// scales' ring may be written again 8 blocks later without a wait of its own.
+constexpr int kScaleSlots = 8;
+static_assert(kScaleSlots > BIG_STAGES + BIG_ACC, "scales in use");
+constexpr int kScaleRows = ROWS + BIG_N;
+constexpr int kStagePitch = 20;  // floats between the rows of a warp's 16 x 16 output patch: conflict-free 16-byte accesses
+
+struct __align__(16) BigShared {
+  float out[kBigEpiWarps][16 * kStagePitch];
+  float scale[kScaleSlots][kScaleRows];  // rows of x, then rows of w
+  uint64_t full[BIG_STAGES];   // a stage's copies and scales have come
+  uint64_t mult[BIG_STAGES];   // its products are done: the sums may be read, the stage written again
+  uint64_t tempty[BIG_ACC];    // an accumulator has been read
+  uint64_t done;
+  uint32_t tmem_base;
+  int abort;
+};
+constexpr int kBigStageBytes = (ROWS + BIG_N) * BK;
+constexpr size_t kBigSmem = (size_t)BIG_STAGES * kBigStageBytes + sizeof(BigShared) + 1024;
+static_assert(kBigSmem <= 232448, "shared memory of a CTA");
+
+// Tile t in grouped order: G row tiles, columns slowest inside a group, so that the tiles in flight share rows of both
+// operands in L2.
+struct TileOrder {
+  uint32_t tiles_m, tiles_n, G;
+  __device__ __forceinline__ uint32_t count() const { return tiles_m * tiles_n; }
+  __device__ __forceinline__ void at(uint32_t t, int& m0, int& n0) const {
+    const uint32_t per_group = G * tiles_n, g = t / per_group, first = g * G;
+    const uint32_t size = tiles_m - first < G ? tiles_m - first : G;
+    const uint32_t r = t - g * per_group;
+    m0 = (int)((first + r % size) * ROWS);
+    n0 = (int)((r / size) * BIG_N);
+  }
+};
+
+// COLS: w has a scale per row, so the columns of a tile differ; otherwise a warp's 128 columns share one.
+template <bool COLS>
+__global__ void __launch_bounds__(kBigThreads, 1)
+    linear_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
+                         const Params P, const TileOrder tiles) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  BigShared* sh = reinterpret_cast<BigShared*>(ring + BIG_STAGES * kBigStageBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t ntiles = tiles.count();
+  const int nk = P.nk;
+  volatile int* abort = &sh->abort;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < BIG_STAGES; ++s) {
+      mbar_init(&sh->full[s], 3);  // the copies, and two warps with scales
+      mbar_init(&sh->mult[s], 1);
+    }
+    for (int b = 0; b < BIG_ACC; ++b) mbar_init(&sh->tempty[b], kBigEpiWarps);
+    mbar_init(&sh->done, 1);
+    sh->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                 "r"(BIG_ACC * BIG_N)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = sh->tmem_base;
+
+  // 384 threads are launched with 168 registers each; 4 warps keep 72 and 8 warps take 216: 4 * 72 + 8 * 216 = 12 * 168
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 0 && lane == 0) {
+      // A slot's first use waits for the phase before the first one, which a fresh barrier reports as complete.
+      Ring<BIG_STAGES> st;
+      uint32_t issued = 0;
+      bool ok = true;
+      for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        int m0, n0;
+        tiles.at(t, m0, n0);
+        for (int i = 0; i < nk; ++i, ++issued, st.next()) {
+          ok = mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault);
+          if (!ok) break;
+          unsigned char* a = ring + st.slot * kBigStageBytes;
+          mbar_expect_tx(&sh->full[st.slot], kBigStageBytes);
+          tma_load_2d(a, &tmap_x, &sh->full[st.slot], i * BK, m0);
+          tma_load_2d(a + ROWS * BK, &tmap_w, &sh->full[st.slot], i * BK, n0);
+        }
+      }
+      // the last copies issued land before the CTA leaves
+      for (uint32_t j = issued > BIG_STAGES ? issued - BIG_STAGES : 0; j < issued; ++j)
+        mbar_drain(&sh->full[j % BIG_STAGES], (j / BIG_STAGES) & 1u, *abort ? kLandedCycles : kTimeoutCycles);
+    } else if (warp == 1 && lane == 0) {
+      const uint32_t idesc = P.idesc | ((uint32_t)(BIG_N >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
+      const uint64_t adesc = sw128_desc(smem_u32(ring)), bdesc = sw128_desc(smem_u32(ring) + ROWS * BK);
+      const uint32_t mine = blockIdx.x < ntiles ? (ntiles - blockIdx.x - 1) / gridDim.x + 1 : 0;
+      const int64_t total = (int64_t)mine * nk;
+      Ring<BIG_STAGES> st;
+      Ring<BIG_ACC> ac;
+      // The waits for the next block stand between this block's products, which keep the tensor core busy meanwhile.
+      bool ok = total > 0 && mbar_wait(&sh->full[0], 0u, abort, P.wait_cycles, &g_f8_fault);
+      for (int64_t n = 0; n < total && ok; ++n) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t at = (uint64_t)(st.slot * (kBigStageBytes >> 4));
+        const uint32_t d = tmem_base + ac.slot * BIG_N;
+        uint64_t* const mult = &sh->mult[st.slot];
+        umma_f8(d, adesc + at, bdesc + at, idesc, 0u);
+        umma_f8(d, adesc + at + 2, bdesc + at + 2, idesc, 1u);
+        st.next();
+        ac.next();
+        if (n + 1 < total) ok = mbar_wait(&sh->full[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault);
+        umma_f8(d, adesc + at + 4, bdesc + at + 4, idesc, 1u);
+        umma_f8(d, adesc + at + 6, bdesc + at + 6, idesc, 1u);
+        umma_commit(mult);
+        if (n + 1 < total)
+          ok = ok && mbar_wait(&sh->tempty[ac.slot], ac.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault);
+      }
+      umma_commit(&sh->done);
+      mbar_drain(&sh->done, 0u);
+    } else if (warp >= 2) {
+      // Scales: thread j holds rows j, j + 64 of x and j, .. j + 192 of w (one of each 128 where they share), of GROUP
+      // blocks at a time; the next group is on its way while this one is written.
+      constexpr int PER = COLS ? 6 : 3, GROUP = COLS ? 2 : 4;
+      const int j = threadIdx.x - 64;
+      ScaleFeed<PER, GROUP> feed;
+      auto point = [&](uint32_t t) {  // at the scales of a tile's rows
+        int m0, n0;
+        tiles.at(t, m0, n0);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          feed.src[i] = nullptr;
+          if (i < 2) {
+            const int64_t m = m0 + j + 64 * i;
+            if (m < P.M) feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld;
+          } else if (COLS) {
+            const int64_t n = n0 + j + 64 * (i - 2);
+            if (n < P.N) feed.src[i] = P.w.s + n * P.w.ld;
+          } else {
+            const int64_t n = n0 + 128 * j;
+            if (j < 2 && n < P.N) feed.src[i] = P.w.s + (n >> 7) * P.w.ld;
+          }
+        }
+      };
+      Ring<BIG_STAGES> st;
+      uint32_t it = 0;
+      bool ok = true;
+      point(blockIdx.x);
+      feed.load(0, nk, P.scale4);
+      for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        for (int i0 = 0; i0 < nk && ok; i0 += GROUP) {
+          float v[PER][GROUP];
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int b = 0; b < GROUP; ++b) v[i][b] = feed.next[i][b];
+          if (i0 + GROUP < nk) {
+            feed.load(i0 + GROUP, nk, P.scale4);
+          } else if (t + gridDim.x < ntiles) {
+            point(t + gridDim.x);
+            feed.load(0, nk, P.scale4);
+          }
+#pragma unroll
+          for (int b = 0; b < GROUP; ++b) {
+            if (i0 + b >= nk) break;
+            ok = __all_sync(0xFFFFFFFFu,
+                            mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault));
+            if (!ok) break;
+            float* to = sh->scale[it % kScaleSlots] + j;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+              if (i < 2 || COLS || j < 2) to[64 * i] = v[i][b];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->full[st.slot]);
+            st.next();
+            ++it;
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int q = warp & 3, e = warp - 4, col0 = (e >> 2) * kBigCols;
+    const uint32_t tmem = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)col0;
+    Ring<BIG_STAGES> st;
+    Ring<BIG_ACC> ac;
+    uint32_t it = 0;
+    bool ok = true;
+    for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+      float acc[kBigCols];
+#pragma unroll
+      for (int j = 0; j < kBigCols; ++j) acc[j] = 0.f;
+      for (int i = 0; i < nk; ++i, ++it) {
+        ok = __all_sync(0xFFFFFFFFu,
+                        mbar_wait(&sh->mult[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault));
+        if (!ok) break;
+        st.next();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t taddr = tmem + ac.slot * BIG_N;
+        const float* scale = sh->scale[it % kScaleSlots];
+        const float* col = scale + ROWS + col0;
+        auto release = [&] {  // the block is in registers: the accumulator may be written again
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
+          ac.next();
+        };
+        if constexpr (COLS) {
+          const float s = scale[32 * q + lane];
+          const uint64_t row2 = pair(__float_as_uint(s), __float_as_uint(s));
+#pragma unroll
+          for (int c = 0; c < kBigCols / 16; ++c) {
+            uint32_t v[16];
+            tmem_ld16(taddr + 16 * c, v);
+            tmem_wait_ld();
+            if (c == kBigCols / 16 - 1) release();
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(&col[16 * c + j]);
+              float* o = &acc[16 * c + j];
+              unpair(fma2(mul2(pair(v[j], v[j + 1]), row2), f.x, pair(o[0], o[1])), o[0], o[1]);
+              unpair(fma2(mul2(pair(v[j + 2], v[j + 3]), row2), f.y, pair(o[2], o[3])), o[2], o[3]);
+            }
+          }
+        } else {
+          const float s = scale[32 * q + lane] * scale[ROWS + col0 / 128];
+          uint32_t r[2][16];
+          tmem_ld16(taddr, r[0]);
+#pragma unroll
+          for (int c = 0; c < kBigCols / 16; ++c) {
+            tmem_wait_ld();
+            if (c < kBigCols / 16 - 1)
+              tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
+            else
+              release();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(r[c & 1][j]), s, acc[16 * c + j]);
+          }
+        }
+      }
+      int m0, n0;
+      tiles.at(t, m0, n0);
+      if (P.sectors && n0 + col0 + kBigCols <= P.N) {
+        if (m0 + 32 * q + lane < P.M) store_row<kBigCols>(P, m0 + 32 * q + lane, n0 + col0, acc);
+        continue;
+      }
+      // Rows that are not aligned, and the last columns: 16 rows x 16 columns at a time through shared memory, so that
+      // neighbouring threads write neighbouring columns.
+      float* out = sh->out[e];
+#pragma unroll
+      for (int c = 0; c < kBigCols / 16; ++c) {
+        const int64_t n = n0 + col0 + 16 * c + 4 * (lane & 3);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          __syncwarp();
+          if ((lane >> 4) == h) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              *reinterpret_cast<float4*>(&out[(lane & 15) * kStagePitch + 4 * j]) = make_float4(
+                  acc[16 * c + 4 * j], acc[16 * c + 4 * j + 1], acc[16 * c + 4 * j + 2], acc[16 * c + 4 * j + 3]);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 8 * i + (lane >> 2);
+            const int64_t m = m0 + 32 * q + 16 * h + row;
+            const float4 v = *reinterpret_cast<const float4*>(&out[row * kStagePitch + 4 * (lane & 3)]);
+            if (m < P.M && n < P.N) finish4(P, m, n, v);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(BIG_ACC * BIG_N)
+                 : "memory");
+  }
+}
+
+template <bool COLS>
+cudaError_t launch_big(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, cudaStream_t st) {
+  static const cudaError_t attr =
+      cudaFuncSetAttribute(linear_f8_big_kernel<COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem);
+  if (attr != cudaSuccess) return attr;
+  TileOrder t{(uint32_t)((p.M + ROWS - 1) / ROWS), (uint32_t)((p.N + BIG_N - 1) / BIG_N), 1};
+  const uint32_t sms = sm_count() > 0 ? sm_count() : 1, grid = t.tiles_m * t.tiles_n < sms ? t.tiles_m * t.tiles_n : sms;
+  t.G = (grid + t.tiles_n - 1) / t.tiles_n;  // about one wave of tiles per group
+  if (t.G > t.tiles_m) t.G = t.tiles_m;
+  linear_f8_big_kernel<COLS><<<grid, kBigThreads, kBigSmem, st>>>(mx, mw, p, t);
+  return cudaGetLastError();
+}
+
 bool make_map(CUtensorMap* map, const ds_f8_matrix* m, uint32_t box_rows) {
   return make_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, m->q, m->cols, m->rows, m->ld, BK, box_rows);
 }
 
 template <int BN>
-cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p, int split, cudaStream_t st) {
   constexpr size_t smem = smem_bytes<BN>();
+  static_assert(Cfg<BN>::CTAS * (smem + 1024) <= 233472, "CTAs of an SM");
   // once per process, thread-safe (function-local static)
   static const cudaError_t attr =
       cudaFuncSetAttribute(linear_f8_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (attr != cudaSuccess) return attr;
   const int64_t tiles = (p.M + BN - 1) / BN * ((p.N + ROWS - 1) / ROWS);
-  // Split the reduction while that fills SMs that would idle and leaves each CTA a block.
-  int split = 1;
-  while (split < 8 && tiles * split * 2 <= 2 * (int64_t)sm_count() && split * 2 <= p.nk) split *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * split));
   cfg.blockDim = dim3(kThreads);
@@ -399,8 +830,41 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
   return cudaLaunchKernelEx(&cfg, linear_f8_kernel<BN>, mw, mx, p, split);
 }
 
+// Which kernel: a product's time is about its waves of CTAs times what one CTA takes.  Measured on one GB300 (bf16
+// results; N 512 .. 8192, K 512 .. 8192, M 1 .. 4096), in microseconds: a CTA of the small kernel takes 3 + 0.30, 0.32,
+// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.95 with a scale per row
+// of w).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for
+// 27 / 32 of the CTAs that would fit one by one, 24 / 32 where an SM holds one CTA.
+struct Plan {
+  int bn, split;  // bn = 0: the large kernel
+};
+Plan plan_of(const Params& p) {
+  const int bn = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : (p.M <= 64 ? 64 : 128));
+  const double per_block = bn == 16 ? 0.30 : (bn == 32 ? 0.32 : (bn == 64 ? 0.38 : 0.63));
+  const int64_t sms = sm_count() > 0 ? sm_count() : 1;
+  const int64_t tiles = (p.M + bn - 1) / bn * ((p.N + ROWS - 1) / ROWS);
+  Plan best{bn, 1};
+  double time = 1e30;
+  for (int split = 1; split <= 8 && (split == 1 || split <= p.nk); split *= 2) {
+    const int64_t room = sms * (bn <= 64 ? 2 : 1) * (split < 8 ? 32 : (bn <= 64 ? 27 : 24)) / 32;
+    const double t = (double)((tiles * split + room - 1) / room) * (3.0 + per_block * ((p.nk + split - 1) / split));
+    if (t < 0.98 * time) {
+      time = t;
+      best.split = split;
+    }
+  }
+  const int64_t big = (p.M + ROWS - 1) / ROWS * ((p.N + BIG_N - 1) / BIG_N);
+  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.95) * p.nk < time) best.bn = 0;
+  return best;
+}
+
 Scales scales_of(const ds_f8_matrix* m) {
   return Scales{m->scale, m->ld_scale, m->blocks == DS_F8_TILES ? 7 : 0};
+}
+
+// kind::f8f6f4: float32 D, the formats of A (along the lanes) and B, both K-major; the tile's shape is added later.
+uint32_t idesc_of(const ds_f8_matrix* a, const ds_f8_matrix* b) {
+  return (1u << 4) | ((uint32_t)a->format << 7) | ((uint32_t)b->format << 10);
 }
 
 }  // namespace
@@ -417,25 +881,27 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   p.ld_add = l.ld_add;
   p.ldy = l.ldy;
   p.nk = (int)((l.x->cols + BK - 1) / BK);
-  // kind::f8f6f4: float32 D, formats of A (w) and B (x), both K-major
-  p.idesc = (1u << 4) | ((uint32_t)l.w->format << 7) | ((uint32_t)l.x->format << 10);
+  p.idesc = idesc_of(l.w, l.x);
   p.type = l.type;
   const size_t size = l.type == DS_TYPE_F32 ? 4 : 2;
   p.vec = reinterpret_cast<uintptr_t>(l.y) % (4 * size) == 0 && l.ldy % 4 == 0 &&
           (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 16 == 0 && l.ld_add % 4 == 0));
+  p.sectors = p.vec && reinterpret_cast<uintptr_t>(l.y) % 32 == 0 && l.ldy * (int64_t)size % 32 == 0;
+  p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
+             reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;
   p.wait_cycles = g_wait_cycles.load(std::memory_order_relaxed);
-  const int bn = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : (p.M <= 64 ? 64 : 128));
-  CUtensorMap mw, mx;
-  if (p.nk > 0) {
-    if (!make_map(&mw, l.w, ROWS) || !make_map(&mx, l.x, (uint32_t)bn)) return cudaErrorInvalidValue;
-  } else {  // an empty reduction loads nothing
-    mw = mx = CUtensorMap{};
-  }
-  switch (bn) {
-    case 16: return launch<16>(mw, mx, p, st);
-    case 32: return launch<32>(mw, mx, p, st);
-    case 64: return launch<64>(mw, mx, p, st);
-    default: return launch<128>(mw, mx, p, st);
+  const Plan plan = plan_of(p);
+  CUtensorMap mw = {}, mx = {};  // an empty reduction loads nothing
+  if (p.nk > 0 && (!make_map(&mw, l.w, plan.bn ? ROWS : BIG_N) || !make_map(&mx, l.x, plan.bn ? plan.bn : ROWS)))
+    return cudaErrorInvalidValue;
+  switch (plan.bn) {
+    case 0:
+      p.idesc = idesc_of(l.x, l.w);  // x along the lanes
+      return p.w.shift ? launch_big<false>(mx, mw, p, st) : launch_big<true>(mx, mw, p, st);
+    case 16: return launch<16>(mw, mx, p, plan.split, st);
+    case 32: return launch<32>(mw, mx, p, plan.split, st);
+    case 64: return launch<64>(mw, mx, p, plan.split, st);
+    default: return launch<128>(mw, mx, p, plan.split, st);
   }
 }
 

@@ -36,27 +36,41 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// The same, suspended for up to `ns` nanoseconds: a waiting warp that polls
+// takes shared-memory and issue slots from those that work.
+__device__ __forceinline__ bool mbar_try_wait_for(uint64_t* bar, uint32_t parity, uint32_t ns) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(ns)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait for the phase with the given parity; false when the CTA
 // aborted or the deadline passed (then `fault` and abort are set).
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort, long long limit,
                                           int* fault) {
+  if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
+  do {
     if (*abort) return false;
     if (clock64() - t0 > limit) {
       *abort = 1;
       atomicExch(fault, 1);
       return false;
     }
-  }
+  } while (!mbar_try_wait_for(bar, parity, 20000));
   return true;
 }
-// Bounded wait that ignores the abort flag (draining work already issued);
-// always the full limit, so that issued copies and MMAs land before the CTA
-// frees its tensor memory or exits.
-__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
+// Bounded wait that ignores the abort flag (draining work already issued), so
+// that issued copies and MMAs land before the CTA frees its tensor memory or
+// exits.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity, long long limit = kTimeoutCycles) {
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kTimeoutCycles) {
+  while (!mbar_try_wait(bar, parity) && clock64() - t0 < limit) {
   }
 }
 

@@ -23,9 +23,7 @@ from __future__ import annotations
 import torch
 
 from . import (DS_F8_E4M3, DS_F8_E5M2, DS_F8_POW2, DS_F8_ROWS, DS_F8_TILES, DS_TYPE_BF16, DS_TYPE_F16, DS_TYPE_F32,
-               _on_one_gpu, ds_expand_shift_weights_f8, ds_f8_matrix, ds_gated_f8, ds_gated_f8_backward, ds_linear_f8,
-               ds_quantize_f8, ds_requantize_f8, ds_rmsnorm_f8, ds_rmsnorm_f8_backward,
-               ds_rmsnorm_f8_backward_workspace_bytes)
+               _check, _stream, ds_expand_shift_weights_f8, ds_f8_matrix, lib)
 
 _TYPES = {torch.float32: DS_TYPE_F32, torch.bfloat16: DS_TYPE_BF16, torch.float16: DS_TYPE_F16}
 _FORMATS = {torch.float8_e4m3fn: DS_F8_E4M3, torch.float8_e5m2: DS_F8_E5M2}
@@ -45,19 +43,19 @@ class F8Matrix:
             raise ValueError(f"q must be torch.float8_e4m3fn or torch.float8_e5m2, got {q.dtype}")
         if scale.dtype != torch.float32:
             raise ValueError(f"scale must be torch.float32, got {scale.dtype}")
-        if q.dim() != 2:
-            raise ValueError("q must be [rows, cols]")
+        if q.dim() != 2 or scale.dim() != 2:
+            raise ValueError("q and scale must have two dimensions")
         rows, cols = q.shape
-        ld = _row_stride(q, "q")
+        ld, ld_scale = _row_stride(q, "q"), _row_stride(scale, "scale")
         if ld % 16:
             raise ValueError(f"rows of q must start a multiple of 16 bytes apart, got {ld} (pad the columns)")
         want = (-(-rows // BLOCK) if tiles else rows, -(-cols // BLOCK))
         if scale.shape != want:
             raise ValueError(f"scale has shape {tuple(scale.shape)}, expected {want}")
-        if q.device != scale.device or q.device.type != "cuda":
+        if q.get_device() < 0 or q.get_device() != scale.get_device():
             raise ValueError("q and scale must be CUDA tensors of one device")
         self.q, self.scale = q, scale
-        self.desc = ds_f8_matrix(q.data_ptr(), scale.data_ptr(), rows, cols, ld, _row_stride(scale, "scale"), fmt,
+        self.desc = ds_f8_matrix(q.data_ptr(), scale.data_ptr(), rows, cols, ld, ld_scale, fmt,
                                  DS_F8_TILES if tiles else DS_F8_ROWS)
 
     @classmethod
@@ -99,9 +97,9 @@ class F8Matrix:
 def _row_stride(t, name: str) -> int:
     """Elements between the rows of a matrix whose columns are next to each other (a row alone has any stride)."""
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name} must have consecutive columns")
-    ld = t.stride(0)
     if rows <= 1 or cols == 0:  # the stride is not used; torch may have set it to anything
         ld = max(ld, cols)
         if t.element_size() == 1:
@@ -111,26 +109,57 @@ def _row_stride(t, name: str) -> int:
     return ld
 
 
-def _matrix(t, name: str, shape=None, dtype=None):
-    """Checks a [rows, cols] tensor; returns its row stride (0 for None)."""
-    if t is None:
-        return 0
-    if t.dtype not in _TYPES if dtype is None else t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype or 'float32, bfloat16 or float16'}, got {t.dtype}")
+def _on_gpu(t, name: str, device: int = -1) -> int:
+    """The tensor's device index: a GPU, and `device` where given."""
+    d = t.get_device()
+    if d < 0:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if device >= 0 and d != device:
+        raise ValueError(f"{name} is on cuda:{d}, the input on cuda:{device}")
+    return d
+
+
+def _matrix(t, name: str) -> int:
+    """Checks a [rows, cols] tensor of a supported type; returns its row stride."""
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return _row_stride(t, name)
 
 
-def _vector(t, name: str, n: int) -> None:
+def _like(t, name: str, rows: int, cols: int, dtype, device: int) -> tuple:
+    """Checks a [rows, cols] tensor of one type; returns (address, row stride), (None, 0) for None."""
     if t is None:
-        return
+        return None, 0
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    _on_gpu(t, name, device)
+    return t.data_ptr(), _row_stride(t, name)
+
+
+def _vector(t, name: str, n: int, device: int):
+    """Checks a contiguous float32 vector of n values; returns its address (None for None)."""
+    if t is None:
+        return None
     if t.dtype != torch.float32:
         raise ValueError(f"{name} must be torch.float32, got {t.dtype}")
-    if tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous vector of {n} values, got shape {tuple(t.shape)}")
+    _on_gpu(t, name, device)
+    return t.data_ptr()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _on_stream(stream, device: int):
+    """The caller's stream, or the current one of the tensors' device (by torch's short way where it has one)."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def _f8(m, name: str):
@@ -156,19 +185,21 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
         raise ValueError("neither the matrix nor its transpose is asked for")
     is_f8 = isinstance(x, F8Matrix)
     if is_f8:
-        rows, cols, device = x.rows, x.cols, x.q.device
+        rows, cols, device = x.desc.rows, x.desc.cols, x.q.device
     else:
         ld = _matrix(x, "x")
-        _on_one_gpu(x=x)
-        rows, cols, device = x.shape[0], x.shape[1], x.device
+        _on_gpu(x, "x")
+        rows, cols = x.shape
+        device = x.device
     out = F8Matrix.empty(rows, cols, device, dtype, blocks == "tiles") if blocks else None
     out_t = F8Matrix.empty(cols, rows, device, dtype, transposed == "tiles") if transposed else None
     d, d_t = out.desc if out else None, out_t.desc if out_t else None
     flags = DS_F8_POW2 if pow2 else 0
+    stream = _on_stream(stream, device.index)
     if is_f8:
-        ds_requantize_f8(x.desc, d, d_t, flags, stream)
+        _check(lib().ds_requantize_f8(x.desc, d, d_t, flags, stream))
     else:
-        ds_quantize_f8(x, _TYPES[x.dtype], rows, cols, ld, d, d_t, flags, stream)
+        _check(lib().ds_quantize_f8(x.data_ptr(), _TYPES[x.dtype], rows, cols, ld, d, d_t, flags, stream))
     return out, out_t
 
 
@@ -185,18 +216,21 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
     ``bias`` is float32 [N], ``add`` float32 [M, N]; ``out`` may be ``add`` itself, which then accumulates."""
     dx, dw = _f8(x, "x"), _f8(w, "w")
     M, N = dx.rows, dw.rows
-    _vector(bias, "bias", N)
-    ld_add = _matrix(add, "add", (M, N), torch.float32)
+    device = x.q.get_device()
+    _on_gpu(w.q, "w", device)
     y = out
     if y is None:
         if dtype not in _TYPES:
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
         y = torch.empty((M, N), dtype=dtype, device=x.q.device)
-        ldy = N
+        py, ldy = y.data_ptr(), N
     else:
-        ldy = _matrix(y, "out", (M, N))
-    _on_one_gpu(x=x.q, w=w.q, bias=bias, add=add, out=out)
-    ds_linear_f8(dx, dw, bias, add, ld_add, y, _TYPES[y.dtype], ldy, stream)
+        if y.dtype not in _TYPES:
+            raise ValueError(f"out must be float32, bfloat16 or float16, got {y.dtype}")
+        py, ldy = _like(y, "out", M, N, y.dtype, device)
+    pa, ld_add = _like(add, "add", M, N, torch.float32, device)
+    _check(lib().ds_linear_f8(dx, dw, _vector(bias, "bias", N, device), pa, ld_add, py, _TYPES[y.dtype], ldy,
+                              _on_stream(stream, device)))
     return y
 
 
@@ -208,21 +242,20 @@ def rmsnorm_f8(x, weight, residual=None, eps: float = 1e-5, pow2: bool = False, 
     given; it may be x or residual), and the float32 reciprocal root mean squares that the backward pass reads."""
     ldx = _matrix(x, "x")
     rows, cols = x.shape
-    _vector(weight, "weight", cols)
-    ldr = _matrix(residual, "residual", (rows, cols), x.dtype)
-    ldh = _matrix(h, "h", (rows, cols), x.dtype)
-    _on_one_gpu(x=x, weight=weight, residual=residual, h=h)
-    store = h
+    device, kind = _on_gpu(x, "x"), x.dtype
+    pw = _vector(weight, "weight", cols, device)
+    pr, ldr = _like(residual, "residual", rows, cols, kind, device)
+    ph, ldh = _like(h, "h", rows, cols, kind, device)
     if h is None:
         if residual is None:
             h = x
         else:
-            store = h = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-            ldh = cols
+            h = torch.empty((rows, cols), dtype=kind, device=x.device)
+            ph, ldh = h.data_ptr(), cols
     n = F8Matrix.empty(rows, cols, x.device, dtype)
     rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    ds_rmsnorm_f8(x, ldx, residual, ldr, weight, _TYPES[x.dtype], rows, cols, eps, n.desc, store, ldh, rstd,
-                  DS_F8_POW2 if pow2 else 0, stream)
+    _check(lib().ds_rmsnorm_f8(x.data_ptr(), ldx, pr, ldr, pw, _TYPES[kind], rows, cols, eps, n.desc, ph, ldh,
+                               rstd.data_ptr(), DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
     return n, h, rstd
 
 
@@ -232,20 +265,20 @@ def rmsnorm_f8_backward(dy, h, rstd, weight, dh=None, out=None, stream=None):
     gradient of x and of residual alike; ``out`` may be dy, h or dh."""
     lddy = _matrix(dy, "dy")
     rows, cols = dy.shape
-    ldh = _matrix(h, "h", (rows, cols), dy.dtype)
-    lddh = _matrix(dh, "dh", (rows, cols), dy.dtype)
-    _vector(rstd, "rstd", rows)
-    _vector(weight, "weight", cols)
+    device, kind = _on_gpu(dy, "dy"), dy.dtype
+    ph, ldh = _like(h, "h", rows, cols, kind, device)
+    pdh, lddh = _like(dh, "dh", rows, cols, kind, device)
+    pr, pw = _vector(rstd, "rstd", rows, device), _vector(weight, "weight", cols, device)
+    pdx, lddx = _like(out, "out", rows, cols, kind, device)
     dx = out
-    lddx = _matrix(out, "out", (rows, cols), dy.dtype)
     if dx is None:
-        dx, lddx = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device), cols
-    _on_one_gpu(dy=dy, h=h, rstd=rstd, weight=weight, dh=dh, out=out)
+        dx = torch.empty((rows, cols), dtype=kind, device=dy.device)
+        pdx, lddx = dx.data_ptr(), cols
     dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
-    nbytes = ds_rmsnorm_f8_backward_workspace_bytes(rows, cols)
+    nbytes = lib().ds_rmsnorm_f8_backward_workspace_bytes(rows, cols)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device)
-    ds_rmsnorm_f8_backward(dy, lddy, h, ldh, rstd, weight, dh, lddh, _TYPES[dy.dtype], rows, cols, dx, lddx, dw, ws,
-                           nbytes, stream)
+    _check(lib().ds_rmsnorm_f8_backward(dy.data_ptr(), lddy, ph, ldh, pr, pw, pdh, lddh, _TYPES[kind], rows, cols, pdx,
+                                        lddx, dw.data_ptr(), ws.data_ptr(), nbytes, _on_stream(stream, device)))
     return dx, dw
 
 
@@ -262,11 +295,11 @@ def gated_f8(gu, features: int, checkpoint: bool = True, pow2: bool = False, dty
     rows, width = gu.shape
     if features <= 0 or width != _gate_width(features):
         raise ValueError(f"gu has {width} columns, expected {_gate_width(features)} for {features} features")
-    _on_one_gpu(gu=gu)
+    device = _on_gpu(gu, "gu")
     a = F8Matrix.empty(rows, features, gu.device, dtype)
     kept = F8Matrix.empty(rows, width, gu.device, dtype) if checkpoint else None
-    ds_gated_f8(gu, _TYPES[gu.dtype], ld, rows, features, a.desc, kept.desc if kept else None,
-                DS_F8_POW2 if pow2 else 0, stream)
+    _check(lib().ds_gated_f8(gu.data_ptr(), _TYPES[gu.dtype], ld, rows, features, a.desc,
+                             kept.desc if kept else None, DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
     return a, kept
 
 
@@ -280,10 +313,11 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     rows, features = da.shape
     if features == 0 or dk.rows != rows or dk.cols != _gate_width(features):
         raise ValueError(f"kept is {dk.rows} x {dk.cols}, expected {rows} x {_gate_width(features)}")
-    _on_one_gpu(da=da, kept=kept.q)
+    device = _on_gpu(da, "da", kept.q.get_device())
     dgu = F8Matrix.empty(rows, dk.cols, da.device, dtype)
     dgu_t = F8Matrix.empty(dk.cols, rows, da.device, dtype) if transposed else None
     a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None
-    ds_gated_f8_backward(dk, da, _TYPES[da.dtype], ld, features, dgu.desc, dgu_t.desc if dgu_t else None,
-                         a_t.desc if a_t else None, DS_F8_POW2 if pow2 else 0, stream)
+    _check(lib().ds_gated_f8_backward(dk, da.data_ptr(), _TYPES[da.dtype], ld, features, dgu.desc,
+                                      dgu_t.desc if dgu_t else None, a_t.desc if a_t else None,
+                                      DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
     return dgu, dgu_t, a_t
