@@ -167,15 +167,20 @@ __device__ __forceinline__ F8Scale f8_scale(float amax, bool e5m2, bool pow2) {
   if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
   return F8Scale{s, __frcp_rn(s)};
 }
-// v * 0 is NaN for a non-finite v and 0 otherwise: infinities do not saturate silently
-__device__ __forceinline__ float f8_unit(float v, float inv) { return fmaf(v, 0.f, v * inv); }
+// Values by 1 / s.  CHECK: the values may hold infinities, which have to become NaN and not the largest value (v * 0 is
+// NaN for them and 0 otherwise); NaN stays NaN by itself.
+template <bool CHECK>
+__device__ __forceinline__ float f8_unit(float v, float inv) {
+  return CHECK ? fmaf(v, 0.f, v * inv) : v * inv;
+}
+template <bool CHECK>
+__device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d, float inv, bool e5m2) {
+  return f8x2(f8_unit<CHECK>(a, inv), f8_unit<CHECK>(b, inv), e5m2) |
+         (f8x2(f8_unit<CHECK>(c, inv), f8_unit<CHECK>(d, inv), e5m2) << 16);
+}
+template <bool CHECK>
 __device__ __forceinline__ uint2 f8x8(const float v[8], float inv, bool e5m2) {
-  uint32_t w[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    w[i] = f8x2(f8_unit(v[4 * i], inv), f8_unit(v[4 * i + 1], inv), e5m2) |
-           (f8x2(f8_unit(v[4 * i + 2], inv), f8_unit(v[4 * i + 3], inv), e5m2) << 16);
-  return make_uint2(w[0], w[1]);
+  return make_uint2(f8x4<CHECK>(v[0], v[1], v[2], v[3], inv, e5m2), f8x4<CHECK>(v[4], v[5], v[6], v[7], inv, e5m2));
 }
 // The address is 8-byte aligned: rows start 16 bytes apart or a multiple of it.
 __device__ __forceinline__ void store_q8(uint8_t* p, int n, uint2 q) {
@@ -188,11 +193,20 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int n, uint2 q) {
   }
 }
 
+constexpr float kInf = __builtin_huge_valf();
+
 __device__ __forceinline__ float finite_abs(float v) {
   const float a = fabsf(v);
-  return a < __int_as_float(0x7F800000) ? a : 0.f;  // false for NaN as well
+  return a < kInf ? a : 0.f;  // false for NaN as well
 }
+// The largest magnitude; NaN is passed over (fmaxf), an infinity is the result.
 __device__ __forceinline__ float amax8(const float v[8]) {
+  float m = fabsf(v[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
+  return fmaxf(m, 0.f);
+}
+__device__ __forceinline__ float amax8_finite(const float v[8]) {
   float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[i]));
@@ -203,6 +217,16 @@ __device__ __forceinline__ float max16(float m) {
 #pragma unroll
   for (int d = 8; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
   return m;
+}
+// The scale and the 8-bit values of a block that 16 lanes hold; all 32 lanes of the warp call it.  Infinities are
+// rare: they are looked for by the largest magnitude, and the block is then gone over again.
+__device__ __forceinline__ F8Scale f8_block(const float v[8], bool e5m2, bool pow2, uint2& q) {
+  float m = max16(amax8(v));
+  const bool inf = __any_sync(0xFFFFFFFFu, !(m < kInf));
+  if (inf) m = max16(amax8_finite(v));
+  const F8Scale s = f8_scale(m, e5m2, pow2);
+  q = inf ? f8x8<true>(v, s.inv, e5m2) : f8x8<false>(v, s.inv, e5m2);
+  return s;
 }
 
 // ---------------------------------------------------------------------------

@@ -56,17 +56,19 @@ __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t
     ru.get(u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) a[j] = g[j] * sigmoid(g[j]) * u[j];
-    const F8Scale sa = f8_scale(max16(amax8(a)), out.e5m2, pow2);
-    if (n > 0) store_q8(out.q + r * out.ld + c, n, f8x8(a, sa.inv, out.e5m2));
+    uint2 qa;
+    const F8Scale sa = f8_block(a, out.e5m2, pow2, qa);
+    if (n > 0) store_q8(out.q + r * out.ld + c, n, qa);
     if (in && sub == 0) out.s[r * out.lds + b] = sa.s;
     if (ckpt.q) {
-      const F8Scale sg = f8_scale(max16(amax8(g)), ckpt.e5m2, pow2);
-      const F8Scale su = f8_scale(max16(amax8(u)), ckpt.e5m2, pow2);
+      uint2 qg, qu;
+      const F8Scale sg = f8_block(g, ckpt.e5m2, pow2, qg);
+      const F8Scale su = f8_block(u, ckpt.e5m2, pow2, qu);
       if (in) {
         uint8_t* q = ckpt.q + r * ckpt.ld + c;
         const int pad = left8(up, c);  // the columns between the halves are zeros (0 / s)
-        store_q8(q, pad, f8x8(g, sg.inv, ckpt.e5m2));
-        if (n > 0) store_q8(q + up, n, f8x8(u, su.inv, ckpt.e5m2));
+        store_q8(q, pad, qg);
+        if (n > 0) store_q8(q + up, n, qu);
         if (sub == 0) {
           ckpt.s[r * ckpt.lds + b] = sg.s;
           ckpt.s[r * ckpt.lds + nb + b] = su.s;
@@ -76,66 +78,86 @@ __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t
   }
 }
 
+// Each result has its turned tile and column maxima, so that one pass of barriers serves all three.
 struct TileSmem {
-  uint8_t turned[128 * 128];
-  float col_max[kTileWarps][128];
-  float col_inv[128];
+  uint8_t turned[3][128 * 128];
+  float col_max[3][kTileWarps][128];
+  float col_inv[3][128];
 };
 
-// One 128 x 128 tile of a result: its rows to `rows_out` at column c0, its columns to `cols_out` at row c0.  v is the
-// thread's 4 x 8 patch (zero beyond the matrix), m rows and n columns of it exist, n_rows columns of the row form are
-// written (the zeros between the halves are part of it).
-__device__ __forceinline__ void write_tile(TileSmem& sm, const float v[4][8], const F8Out& rows_out,
-                                           const F8Out& cols_out, int64_t rows, int64_t r0, int64_t tile_r,
-                                           int64_t c0, int64_t c_tile, int m, int n_rows, int n_cols, bool pow2) {
-  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
-  if (rows_out.q) {
+// A 4 x 8 patch of a result, its largest magnitudes by columns (the warp's 8 rows together) to shared memory.
+__device__ __forceinline__ void column_maxima(float (*col_max)[128], const float v[4][8], bool check) {
+  const int tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
+  float cm[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const F8Scale s = f8_scale(max16(amax8(v[i])), rows_out.e5m2, pow2);
-      if (i < m) {
-        if (n_rows > 0) store_q8(rows_out.q + (r0 + i) * rows_out.ld + c0, n_rows, f8x8(v[i], s.inv, rows_out.e5m2));
-        if (tc == 0) rows_out.s[(r0 + i) * rows_out.lds + c_tile / kF8Block] = s.s;
-      }
+  for (int j = 0; j < 8; ++j) {
+    if (check) {
+      cm[j] = fmaxf(fmaxf(finite_abs(v[0][j]), finite_abs(v[1][j])), fmaxf(finite_abs(v[2][j]), finite_abs(v[3][j])));
+    } else {
+      cm[j] = fmaxf(fmaxf(fabsf(v[0][j]), fabsf(v[1][j])), fmaxf(fabsf(v[2][j]), fabsf(v[3][j])));
     }
   }
-  if (cols_out.q) {
+  const bool up = threadIdx.x & 16;
+  float c[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float m4 = 0.f;
+  for (int j = 0; j < 4; ++j)
+    c[j] = fmaxf(up ? cm[j + 4] : cm[j], __shfl_xor_sync(0xFFFFFFFFu, up ? cm[j] : cm[j + 4], 16));
+  *reinterpret_cast<float4*>(&col_max[warp][tc * 8 + (up ? 4 : 0)]) = make_float4(c[0], c[1], c[2], c[3]);
+}
+
+// The row form of a patch: m of its rows, n of its columns.
+__device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out, int64_t r0, int64_t c0, int64_t block,
+                                           int m, int n, bool check, bool pow2) {
+  const int tc = threadIdx.x & 15;
+  float rm[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m4 = fmaxf(m4, finite_abs(v[i][j]));
-      m4 = fmaxf(m4, __shfl_xor_sync(0xFFFFFFFFu, m4, 16));
-      if ((threadIdx.x & 16) == 0) sm.col_max[warp][tc * 8 + j] = m4;
-    }
-    __syncthreads();
-    if (threadIdx.x < 128) {
-      float mx = 0.f;
+  for (int i = 0; i < 4; ++i) rm[i] = check ? amax8_finite(v[i]) : amax8(v[i]);
+  // lane l of the 16 gets row l & 3: each exchange halves the rows a lane answers for
+  float a[2];
 #pragma unroll
-      for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[w][threadIdx.x]);
-      const F8Scale s = f8_scale(mx, cols_out.e5m2, pow2);
-      sm.col_inv[threadIdx.x] = s.inv;
-      if ((int64_t)threadIdx.x < n_cols) cols_out.s[(c_tile + threadIdx.x) * cols_out.lds + tile_r] = s.s;
-    }
-    __syncthreads();
+  for (int i = 0; i < 2; ++i) {
+    const bool up = tc & 2;
+    a[i] = fmaxf(up ? rm[i + 2] : rm[i], __shfl_xor_sync(0xFFFFFFFFu, up ? rm[i] : rm[i + 2], 2));
+  }
+  const bool up = tc & 1;
+  float b = fmaxf(up ? a[1] : a[0], __shfl_xor_sync(0xFFFFFFFFu, up ? a[0] : a[1], 1));
+  b = fmaxf(b, __shfl_xor_sync(0xFFFFFFFFu, b, 4));
+  b = fmaxf(b, __shfl_xor_sync(0xFFFFFFFFu, b, 8));
+  const F8Scale s = f8_scale(b, out.e5m2, pow2);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float inv = sm.col_inv[tc * 8 + j];
-      const uint32_t q = f8x2(f8_unit(v[0][j], inv), f8_unit(v[1][j], inv), cols_out.e5m2) |
-                         (f8x2(f8_unit(v[2][j], inv), f8_unit(v[3][j], inv), cols_out.e5m2) << 16);
-      *reinterpret_cast<uint32_t*>(&sm.turned[(tc * 8 + j) * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]) = q;
-    }
-    __syncthreads();
-    const int64_t rr = tile_r * kF8Block + tc * 8;
-    const int nr = left8(rows, rr);
+  for (int i = 0; i < 4; ++i) {
+    const float inv = __shfl_sync(0xFFFFFFFFu, s.inv, i, 16);
+    const uint2 q = check ? f8x8<true>(v[i], inv, out.e5m2) : f8x8<false>(v[i], inv, out.e5m2);
+    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, q);
+  }
+  if (tc < m && tc < 4) out.s[(r0 + tc) * out.lds + block] = s.s;
+}
+
+// The patch by columns, as bytes, to the turned tile.
+__device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv, const float v[4][8], bool e5m2,
+                                           bool check) {
+  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int col = tr + 32 * k;
-      if (col < n_cols && nr > 0)
-        store_q8(cols_out.q + (c_tile + col) * cols_out.ld + rr, nr,
-                 *reinterpret_cast<const uint2*>(&sm.turned[col * 128 + ((tc ^ (col >> 3)) << 3)]));
-    }
-    __syncthreads();  // the next tile writes col_max and turned again
+  for (int j = 0; j < 8; ++j) {
+    const float inv = col_inv[tc * 8 + j];
+    const uint32_t q = check ? f8x4<true>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2)
+                             : f8x4<false>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2);
+    *reinterpret_cast<uint32_t*>(&turned[(tc * 8 + j) * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]) = q;
+  }
+}
+
+// The turned tile to the transposed matrix: columns c_tile .., n of them, rows of block tile_r.
+__device__ __forceinline__ void write_turned(const uint8_t* turned, const F8Out& out, int64_t rows, int64_t tile_r,
+                                             int64_t c_tile, int n) {
+  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
+  const int64_t rr = tile_r * kF8Block + tc * 8;
+  const int nr = left8(rows, rr);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int col = tr + 32 * k;
+    if (col < n && nr > 0)
+      store_q8(out.q + (c_tile + col) * out.ld + rr, nr,
+               *reinterpret_cast<const uint2*>(&turned[col * 128 + ((tc ^ (col >> 3)) << 3)]));
   }
 }
 
@@ -160,11 +182,12 @@ __device__ __forceinline__ uint2 load_q8(const uint8_t* p, int n) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kTileThreads) gated_f8_backward_kernel(const GatedIn in, const T* da, int64_t ld,
-                                                                         bool vec, int64_t rows, int64_t features,
-                                                                         const F8Out dgu, const F8Out dgu_t,
-                                                                         const F8Out a_t, bool pow2) {
-  __shared__ __align__(16) TileSmem sm;
+__global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(const GatedIn in, const T* da, int64_t ld,
+                                                                            bool vec, int64_t rows, int64_t features,
+                                                                            const F8Out dgu, const F8Out dgu_t,
+                                                                            const F8Out a_t, bool pow2) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  TileSmem& sm = *reinterpret_cast<TileSmem*>(smem_raw);
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
   const int64_t nb = (features + kF8Block - 1) / kF8Block, up = nb * kF8Block;
   const int64_t tile_r = blockIdx.x / nb, tile_c = blockIdx.x - tile_r * nb;
@@ -174,6 +197,7 @@ __global__ void __launch_bounds__(kTileThreads) gated_f8_backward_kernel(const G
   const int64_t cc = n > 0 ? c0 : 0;
 
   float dg[4][8], du[4][8], a[4][8];
+  bool bad = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t r = i < m ? r0 + i : 0;
@@ -194,12 +218,49 @@ __global__ void __launch_bounds__(kTileThreads) gated_f8_backward_kernel(const G
       du[i][j] = d[j] * act;
       dg[i][j] = d[j] * uj * (sig * (1.f + gj * (1.f - sig)));
     }
+    // an infinity in any of the three shows in the sum of their magnitudes
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      bad = bad || !(fmaxf(fmaxf(fabsf(a[i][j]), fabsf(du[i][j])), fabsf(dg[i][j])) < kInf);
   }
+  const bool check = __syncthreads_or(bad);
   const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);
-  // the gate half's rows go on to the up half with zeros, and so do its columns in the transposed matrix
-  write_tile(sm, dg, dgu, dgu_t, rows, r0, tile_r, c0, c_tile, m, 8, kF8Block, pow2);
-  write_tile(sm, du, dgu, dgu_t, rows, r0, tile_r, up + c0, up + c_tile, m, n, cols, pow2);
-  write_tile(sm, a, F8Out{}, a_t, rows, r0, tile_r, c0, c_tile, m, 0, cols, pow2);
+  if (dgu_t.q) {
+    column_maxima(sm.col_max[0], dg, check);
+    column_maxima(sm.col_max[1], du, check);
+  }
+  if (a_t.q) column_maxima(sm.col_max[2], a, check);
+  if (dgu.q) {
+    // the gate half's rows go on to the up half with zeros
+    write_rows(dg, dgu, r0, c0, tile_c, m, 8, check, pow2);
+    write_rows(du, dgu, r0, up + c0, nb + tile_c, m, n, check, pow2);
+  }
+  __syncthreads();
+  if (threadIdx.x < 384) {  // a column's scale each: of dg, du and a
+    const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
+    const F8Out& out = which < 2 ? dgu_t : a_t;
+    if (out.q) {
+      float mx = 0.f;
+#pragma unroll
+      for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[which][w][c]);
+      const F8Scale s = f8_scale(mx, out.e5m2, pow2);
+      sm.col_inv[which][c] = s.inv;
+      // the gate half's columns go on to the up half with zeros
+      if (which == 0 || c < cols) out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
+    }
+  }
+  __syncthreads();
+  if (dgu_t.q) {
+    turn_patch(sm.turned[0], sm.col_inv[0], dg, dgu_t.e5m2, check);
+    turn_patch(sm.turned[1], sm.col_inv[1], du, dgu_t.e5m2, check);
+  }
+  if (a_t.q) turn_patch(sm.turned[2], sm.col_inv[2], a, a_t.e5m2, check);
+  __syncthreads();
+  if (dgu_t.q) {
+    write_turned(sm.turned[0], dgu_t, rows, tile_r, c_tile, kF8Block);
+    write_turned(sm.turned[1], dgu_t, rows, tile_r, up + c_tile, cols);
+  }
+  if (a_t.q) write_turned(sm.turned[2], a_t, rows, tile_r, c_tile, cols);
 }
 
 template <typename T>
@@ -221,8 +282,12 @@ cudaError_t backward(const ds_f8_matrix* ckpt, const void* da, int64_t ld, int64
                    ckpt->format == DS_F8_E5M2};
   const int64_t tiles = (ckpt->rows + kF8Block - 1) / kF8Block * ((features + kF8Block - 1) / kF8Block);
   const bool vec = (reinterpret_cast<uintptr_t>(da) & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  gated_f8_backward_kernel<T><<<(unsigned)tiles, kTileThreads, 0, st>>>(in, static_cast<const T*>(da), ld, vec,
-                                                                        ckpt->rows, features, dgu, dgu_t, a_t, pow2);
+  // once per process, thread-safe (function-local static)
+  static const cudaError_t attr = cudaFuncSetAttribute(
+      gated_f8_backward_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(TileSmem));
+  if (attr != cudaSuccess) return attr;
+  gated_f8_backward_kernel<T><<<(unsigned)tiles, kTileThreads, sizeof(TileSmem), st>>>(
+      in, static_cast<const T*>(da), ld, vec, ckpt->rows, features, dgu, dgu_t, a_t, pow2);
   return cudaGetLastError();
 }
 

@@ -67,9 +67,10 @@ __device__ __forceinline__ void emit(const RmsnormParams& P, const Aligned& al, 
   rw.get(w);
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = v[i] * rstd * w[i];
-  const F8Scale s = f8_scale(max16(amax8(y)), P.out.e5m2, P.pow2);
+  uint2 q;
+  const F8Scale s = f8_block(y, P.out.e5m2, P.pow2, q);
   if (n > 0) {
-    store_q8(P.out.q + r * P.out.ld + c, n, f8x8(y, s.inv, P.out.e5m2));
+    store_q8(P.out.q + r * P.out.ld + c, n, q);
     if ((threadIdx.x & 15) == 0) P.out.s[r * P.out.lds + c / kF8Block] = s.s;
     if (P.h) store8(static_cast<T*>(P.h) + r * P.ldh + c, n, al.c, v);
   }

@@ -3,9 +3,12 @@
 // Two kernels.  Rows alone (one scale per row and 128 columns): 16 lanes hold
 // a block, 8 values each, and find its amax with four shuffles.  Tiles, and
 // everything that is written transposed: a CTA holds a 128 x 128 tile in
-// registers (an 8 x 8 patch per thread), takes row maxima by shuffles and
-// column maxima through shared memory, and turns the tile around as bytes in
-// shared memory, so that the source is read once whatever is written from it.
+// registers (an 8 x 8 patch per thread, 16-bit sources as they came), takes row
+// maxima by shuffles and column maxima through shared memory, and turns the
+// tile around as bytes in shared memory, so that the source is read once
+// whatever is written from it.  Both are bound by HBM where their instructions
+// fit beside it: a tile's are about 10 per value and direction, and infinities
+// (the only values that need more) send the tile down a second path.
 #include "f8_common.cuh"
 
 namespace ds {
@@ -13,24 +16,27 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Sources: eight values (r, c .. c + 7) of which n exist.
+// Sources: eight values (r, c .. c + 7), of which n exist, as a Raw that gives them in float32 and their largest
+// magnitudes.
 template <typename T>
 struct SourceFloat {
+  using Raw = Raw8<T>;
+  static constexpr bool PACKED = sizeof(T) == 2;  // 16-bit values: maxima of their bits, two at a time
   const T* p;
   int64_t ld;
   bool vec;
-  __device__ __forceinline__ void load(int64_t r, int64_t c, int n, float v[8]) const {
-    Raw8<T> raw;
+  __device__ __forceinline__ void load(int64_t r, int64_t c, int n, Raw& raw) const {
     raw.load(p + r * ld + c, n, vec);
-    raw.get(v);
   }
 };
 struct SourceF8 {
+  using Raw = Raw8<float>;
+  static constexpr bool PACKED = false;
   const uint8_t* q;
   const float* s;
   int64_t ld, lds;
   bool e5m2, tiles;
-  __device__ __forceinline__ void load(int64_t r, int64_t c, int n, float v[8]) const {
+  __device__ __forceinline__ void load(int64_t r, int64_t c, int n, Raw& raw) const {
     const uint8_t* p = q + r * ld + c;
     uint2 u = make_uint2(0u, 0u);
     if (n >= 8) {
@@ -44,10 +50,13 @@ struct SourceF8 {
           u.y |= b << (8 * (i - 4));
       }
     }
-    f8x8_value(u, e5m2, v);
     const float sc = n > 0 ? s[(tiles ? r / kF8Block : r) * lds + c / kF8Block] : 0.f;
+    float v[8];
+    f8x8_value(u, e5m2, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] * sc : 0.f;
+    raw.a = make_float4(v[0], v[1], v[2], v[3]);
+    raw.b = make_float4(v[4], v[5], v[6], v[7]);
   }
 };
 
@@ -71,10 +80,13 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const Source sr
     const int64_t r = in ? i / nb : 0, b = in ? i - r * nb : 0;
     const int64_t c = b * kF8Block + sub * 8;
     const int n = in ? left8(cols, c) : 0;
+    typename Source::Raw raw;
+    src.load(r, n > 0 ? c : 0, n, raw);
     float v[8];
-    src.load(r, n > 0 ? c : 0, n, v);
-    const F8Scale s = f8_scale(max16(amax8(v)), out.e5m2, pow2);
-    if (n > 0) store_q8(out.q + r * out.ld + c, n, f8x8(v, s.inv, out.e5m2));
+    raw.get(v);
+    uint2 q;
+    const F8Scale s = f8_block(v, out.e5m2, pow2, q);
+    if (n > 0) store_q8(out.q + r * out.ld + c, n, q);
     if (in && sub == 0) out.s[r * out.lds + b] = s.s;
   }
 }
@@ -82,80 +94,208 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const Source sr
 struct TileSmem {
   uint8_t turned[128 * 128];  // [column][row], 8-byte chunks XOR-swizzled
   float col_max[kThreads / 32][128];
+  float col_inv[128];
+  float warp_max[kThreads / 32];
 };
 
+// Largest magnitudes of the patch's rows and columns; where a value is not finite its row's is not either.
 template <typename Source>
-__global__ void __launch_bounds__(kThreads) quantize_tile_kernel(const Source src, int64_t rows, int64_t cols,
-                                                                 const F8Out out, const F8Out out_t, bool pow2) {
-  __shared__ __align__(16) TileSmem sm;
-  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
-  const int64_t tiles_c = (cols + kF8Block - 1) / kF8Block;
-  const int64_t tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x - tile_r * tiles_c;
-  const int64_t r0 = tile_r * kF8Block + tr * 8, c0 = tile_c * kF8Block + tc * 8;
-  const int n = left8(cols, c0), m = left8(rows, r0);
-  float v[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) src.load(i < m ? r0 + i : 0, n > 0 ? c0 : 0, i < m ? n : 0, v[i]);
-
-  float cm[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    cm[j] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cm[j] = fmaxf(cm[j], finite_abs(v[i][j]));
-    cm[j] = fmaxf(cm[j], __shfl_xor_sync(0xFFFFFFFFu, cm[j], 16));
-  }
-  if ((threadIdx.x & 16) == 0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sm.col_max[warp][tc * 8 + j] = cm[j];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    cm[j] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) cm[j] = fmaxf(cm[j], sm.col_max[w][tc * 8 + j]);
-  }
-  float tile_max = 0.f;
-  if (out.tiles || out_t.tiles) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) tile_max = fmaxf(tile_max, cm[j]);
-    tile_max = max16(tile_max);
-  }
-
-  if (out.q) {
-    const F8Scale t = f8_scale(tile_max, out.e5m2, pow2);
+__device__ __forceinline__ void patch_maxima(const typename Source::Raw (&raw)[8], float rm[8], float cm[8]) {
+  if constexpr (Source::PACKED) {
+    uint32_t col[4] = {0u, 0u, 0u, 0u};
+    typename Source::Raw out;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const F8Scale s = out.tiles ? t : f8_scale(max16(amax8(v[i])), out.e5m2, pow2);
-      if (i < m) {
-        if (n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, f8x8(v[i], s.inv, out.e5m2));
-        if (!out.tiles && tc == 0) out.s[(r0 + i) * out.lds + tile_c] = s.s;
-      }
+      const uint32_t w[4] = {raw[i].u.x & 0x7FFF7FFFu, raw[i].u.y & 0x7FFF7FFFu, raw[i].u.z & 0x7FFF7FFFu,
+                             raw[i].u.w & 0x7FFF7FFFu};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) col[k] = __vmaxu2(col[k], w[k]);
+      const uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+      out.u = make_uint4(m, 0u, 0u, 0u);
+      float v[8];
+      out.get(v);
+      // comparisons that keep a NaN: the bits of NaN are the largest
+      rm[i] = (m & 0xFFFFu) > (m >> 16) ? v[0] : v[1];
     }
-    if (out.tiles && threadIdx.x == 0) out.s[tile_r * out.lds + tile_c] = t.s;
+    out.u = make_uint4(col[0], col[1], col[2], col[3]);
+    out.get(cm);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cm[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      raw[i].get(v);
+      rm[i] = amax8(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cm[j] = fmaxf(cm[j], fabsf(v[j]));
+    }
   }
-  if (out_t.q) {
-    const F8Scale t = f8_scale(tile_max, out_t.e5m2, pow2);
+}
+
+// The maxima of a patch's 8 rows over the 16 lanes that share them; lane l of the 16 gets row l & 7.  Each exchange
+// halves the rows a lane answers for: 8 shuffles instead of 32.
+__device__ __forceinline__ float row_of_lane(const float rm[8]) {
+  float a[4], b[2];
+  const int lane = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool up = lane & 4;
+    a[i] = fmaxf(up ? rm[i + 4] : rm[i], __shfl_xor_sync(0xFFFFFFFFu, up ? rm[i] : rm[i + 4], 4));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const bool up = lane & 2;
+    b[i] = fmaxf(up ? a[i + 2] : a[i], __shfl_xor_sync(0xFFFFFFFFu, up ? a[i] : a[i + 2], 2));
+  }
+  const bool up = lane & 1;
+  const float c = fmaxf(up ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, up ? b[0] : b[1], 1));
+  return fmaxf(c, __shfl_xor_sync(0xFFFFFFFFu, c, 8));
+}
+
+struct TileAt {
+  int64_t rows, cols, r0, c0, tile_r, tile_c;
+  int m, n;  // rows and columns of the patch that exist
+};
+
+template <typename Raw, bool CHECK>
+__device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, const F8Out& out, const TileAt& t,
+                                           float tile_max, bool pow2) {
+  const int lane = threadIdx.x & 31, tc = lane & 15;
+  const F8Scale s = f8_scale(out.tiles ? tile_max : row_max, out.e5m2, pow2);  // lane i of 16: row i's
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float inv = __shfl_sync(0xFFFFFFFFu, s.inv, i, 16);
+    float v[8];
+    raw[i].get(v);
+    if (i < t.m && t.n > 0)
+      store_q8(out.q + (t.r0 + i) * out.ld + t.c0, t.n, f8x8<CHECK>(v, inv, out.e5m2));
+  }
+  if (!out.tiles) {
+    if (tc < t.m && tc < 8) out.s[(t.r0 + tc) * out.lds + t.tile_c] = s.s;
+  } else if (threadIdx.x == 0) {
+    out.s[t.tile_r * out.lds + t.tile_c] = s.s;
+  }
+}
+
+template <typename Raw, bool CHECK>
+__device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm, const F8Out& out_t) {
+  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
+  float inv[8];
+#pragma unroll
+  for (int j = 0; j < 8; j += 4) {
+    const float4 f = *reinterpret_cast<const float4*>(&sm.col_inv[tc * 8 + j]);
+    inv[j] = f.x, inv[j + 1] = f.y, inv[j + 2] = f.z, inv[j + 3] = f.w;
+  }
+  uint2 q[8];  // column j: rows 0 .. 7 of the patch
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    float a[8], b[8];
+    raw[i].get(a);
+    raw[i + 1].get(b);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const F8Scale s = out_t.tiles ? t : f8_scale(cm[j], out_t.e5m2, pow2);
-      float u[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = v[i][j];
-      const uint2 q = f8x8(u, s.inv, out_t.e5m2);
-      *reinterpret_cast<uint2*>(&sm.turned[(tc * 8 + j) * 128 + ((tr ^ tc) << 3)]) = q;
-      if (!out_t.tiles && tr == 0 && j < n) out_t.s[(c0 + j) * out_t.lds + tile_r] = s.s;
+      const uint32_t two = f8x2(f8_unit<CHECK>(a[j], inv[j]), f8_unit<CHECK>(b[j], inv[j]), out_t.e5m2);
+      uint32_t& w = i < 4 ? q[j].x : q[j].y;
+      w = (i & 2) ? w | (two << 16) : two;
     }
-    if (out_t.tiles && threadIdx.x == 0) out_t.s[tile_c * out_t.lds + tile_r] = t.s;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<uint2*>(&sm.turned[(tc * 8 + j) * 128 + ((tr ^ tc) << 3)]) = q[j];
+}
+
+template <typename Source>
+__global__ void __launch_bounds__(kThreads, Source::PACKED ? 3 : 2)
+    quantize_tile_kernel(const Source src, int64_t rows, int64_t cols, const F8Out out, const F8Out out_t, bool pow2) {
+  __shared__ __align__(16) TileSmem sm;
+  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
+  TileAt t;
+  const int64_t tiles_c = (cols + kF8Block - 1) / kF8Block;
+  t.rows = rows;
+  t.cols = cols;
+  t.tile_r = blockIdx.x / tiles_c;
+  t.tile_c = blockIdx.x - t.tile_r * tiles_c;
+  t.r0 = t.tile_r * kF8Block + tr * 8;
+  t.c0 = t.tile_c * kF8Block + tc * 8;
+  t.m = left8(rows, t.r0);
+  t.n = left8(cols, t.c0);
+  typename Source::Raw raw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) src.load(i < t.m ? t.r0 + i : 0, t.n > 0 ? t.c0 : 0, i < t.m ? t.n : 0, raw[i]);
+
+  float rm[8], cm[8];
+  patch_maxima<Source>(raw, rm, cm);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bad = bad || !(rm[i] < kInf);
+  const bool check = __syncthreads_or(bad);
+  if (check) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cm[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      raw[i].get(v);
+      rm[i] = amax8_finite(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) cm[j] = fmaxf(cm[j], finite_abs(v[j]));
+    }
+  }
+  {
+    float c[4];  // of the warp's 16 rows: its lower lanes columns 0 .. 3 of their 8, its upper lanes 4 .. 7
+    const bool up = threadIdx.x & 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c[j] = fmaxf(up ? cm[j + 4] : cm[j], __shfl_xor_sync(0xFFFFFFFFu, up ? cm[j] : cm[j + 4], 16));
+    *reinterpret_cast<float4*>(&sm.col_max[warp][tc * 8 + (up ? 4 : 0)]) = make_float4(c[0], c[1], c[2], c[3]);
+  }
+  const float row_max = row_of_lane(rm);
+  float tile_max = 0.f;
+  if (out.tiles || out_t.tiles) {
+    float m = row_max;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+    if ((threadIdx.x & 31) == 0) sm.warp_max[warp] = m;
+  }
+  __syncthreads();
+  if (out.tiles || out_t.tiles) {
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) tile_max = fmaxf(tile_max, sm.warp_max[w]);
+  }
+  if (out_t.q && threadIdx.x < 128) {
+    float m = 0.f;
+#pragma unroll
+    for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, sm.col_max[w][threadIdx.x]);
+    const F8Scale s = f8_scale(out_t.tiles ? tile_max : m, out_t.e5m2, pow2);
+    sm.col_inv[threadIdx.x] = s.inv;
+    const int64_t c = t.tile_c * kF8Block + threadIdx.x;
+    if (!out_t.tiles) {
+      if (c < cols) out_t.s[c * out_t.lds + t.tile_r] = s.s;
+    } else if (threadIdx.x == 0) {
+      out_t.s[t.tile_c * out_t.lds + t.tile_r] = s.s;
+    }
+  }
+  if (out.q) {
+    if (check)
+      write_rows<typename Source::Raw, true>(raw, row_max, out, t, tile_max, pow2);
+    else
+      write_rows<typename Source::Raw, false>(raw, row_max, out, t, tile_max, pow2);
+  }
+  if (out_t.q) {
+    __syncthreads();
+    if (check)
+      turn_columns<typename Source::Raw, true>(raw, sm, out_t);
+    else
+      turn_columns<typename Source::Raw, false>(raw, sm, out_t);
     __syncthreads();
     // 16 lanes write one 128-byte row of the transposed matrix
-    const int64_t rr = tile_r * kF8Block + tc * 8;
+    const int64_t rr = t.tile_r * kF8Block + tc * 8;
     const int nr = left8(rows, rr);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const int col = tr + 16 * k;
-      const int64_t c = tile_c * kF8Block + col;
+      const int64_t c = t.tile_c * kF8Block + col;
       if (c < cols && nr > 0)
         store_q8(out_t.q + c * out_t.ld + rr, nr,
                  *reinterpret_cast<const uint2*>(&sm.turned[col * 128 + ((tc ^ (col >> 3)) << 3)]));
