@@ -193,6 +193,20 @@ __device__ __forceinline__ void store_q8(uint8_t* p, int n, uint2 q) {
   }
 }
 
+// Eight 8-bit values of which n exist (the others read as zero); 8-byte aligned.
+__device__ __forceinline__ uint2 load_q8(const uint8_t* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const uint2*>(p);
+  uint2 u = make_uint2(0u, 0u);
+  for (int i = 0; i < n; ++i) {
+    const uint32_t b = p[i];
+    if (i < 4)
+      u.x |= b << (8 * i);
+    else
+      u.y |= b << (8 * (i - 4));
+  }
+  return u;
+}
+
 constexpr float kInf = __builtin_huge_valf();
 
 __device__ __forceinline__ float finite_abs(float v) {
@@ -218,6 +232,27 @@ __device__ __forceinline__ float max16(float m) {
   for (int d = 8; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
   return m;
 }
+// R maxima over the same 16 lanes at once: lane l gets that of value l & (R - 1).  Each exchange halves the values that
+// a lane answers for (8 shuffles for 8 values instead of 32), and a lane then makes one scale, not R.
+template <int R>
+__device__ __forceinline__ float lanes_max(const float (&m)[R]) {
+  float a[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) a[i] = m[i];
+#pragma unroll
+  for (int h = R / 2; h >= 1; h >>= 1) {
+    const bool up = threadIdx.x & h;
+#pragma unroll
+    for (int i = 0; i < h; ++i)
+      a[i] = fmaxf(up ? a[i + h] : a[i], __shfl_xor_sync(0xFFFFFFFFu, up ? a[i] : a[i + h], h));
+  }
+  float v = a[0];
+#pragma unroll
+  for (int d = R; d < 16; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+  return v;
+}
+__device__ __forceinline__ float of_lane(float v, int l) { return __shfl_sync(0xFFFFFFFFu, v, l, 16); }
+
 // The scale and the 8-bit values of a block that 16 lanes hold; all 32 lanes of the warp call it.  Infinities are
 // rare: they are looked for by the largest magnitude, and the block is then gone over again.
 __device__ __forceinline__ F8Scale f8_block(const float v[8], bool e5m2, bool pow2, uint2& q) {
@@ -227,6 +262,31 @@ __device__ __forceinline__ F8Scale f8_block(const float v[8], bool e5m2, bool po
   const F8Scale s = f8_scale(m, e5m2, pow2);
   q = inf ? f8x8<true>(v, s.inv, e5m2) : f8x8<false>(v, s.inv, e5m2);
   return s;
+}
+
+// Steps of a half-warp through the (row, block) units of a matrix in row order, without a division per step.
+struct Units {
+  int64_t r;
+  int64_t b, nb, step_r, step_b;
+  __device__ __forceinline__ Units(int64_t first, int64_t step, int64_t blocks) : nb(blocks) {
+    r = first / blocks;
+    b = first - r * blocks;
+    step_r = step / blocks;
+    step_b = step - step_r * blocks;
+  }
+  __device__ __forceinline__ void next() {
+    r += step_r;
+    b += step_b;
+    if (b >= nb) {
+      b -= nb;
+      ++r;
+    }
+  }
+};
+
+__device__ __forceinline__ int left8(int64_t cols, int64_t c) {
+  const int64_t n = cols - c;
+  return n >= 8 ? 8 : (n < 0 ? 0 : (int)n);
 }
 
 // ---------------------------------------------------------------------------

@@ -14,6 +14,8 @@
 // backward pass holds a 128 x 128 tile per CTA, 4 rows x 8 columns of it per
 // thread, and writes its five 8-bit outputs from registers, so the checkpoint
 // and da are read once.
+#include <type_traits>
+
 #include "f8_common.cuh"
 
 namespace ds {
@@ -23,56 +25,82 @@ constexpr int kThreads = 256;
 constexpr int kTileThreads = 512;
 constexpr int kTileWarps = kTileThreads / 32;
 
-__device__ __forceinline__ int left8(int64_t cols, int64_t c) {
-  const int64_t n = cols - c;
-  return n >= 8 ? 8 : (n < 0 ? 0 : (int)n);
+// sig(g) = 1 / (1 + 2^(-g log2 e)) by the special-function unit (each within 2 steps of 2^-23, and the rounding of the
+// exponent adds |g| 2^-24): 2^x is inf or 0 far out, and the quotient then 0 or 1, as it should be.
+__device__ __forceinline__ float sigmoid(float g) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
 }
 
-// sig(g) = 1 / (1 + exp(-g)): exp(-g) overflows to inf below -88.7 and the quotient is then 0, as it should be.
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+// Two rows of a unit (a block of 128 features) at a time: with the checkpoint six blocks, whose scales six lanes make.
+constexpr int R = 2;
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t ld, bool vec, int64_t rows,
                                                             int64_t features, const F8Out out, const F8Out ckpt,
                                                             bool pow2) {
-  const int64_t nb = (features + kF8Block - 1) / kF8Block;
-  const int64_t up = nb * kF8Block;
-  const int64_t total = rows * nb;
+  const int64_t nb = (features + kF8Block - 1) / kF8Block, up = nb * kF8Block, groups = (rows + R - 1) / R;
   const int sub = threadIdx.x & 15;
-  const int64_t first = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 4;
-  const int64_t step = (int64_t)gridDim.x * (kThreads / 16);
-  for (int64_t base = first & ~(int64_t)1; base < total; base += step) {
-    const int64_t i = base + (first & 1);
-    const bool in = i < total;
-    const int64_t r = in ? i / nb : 0, b = in ? i - r * nb : 0;
-    const int64_t c = b * kF8Block + sub * 8;
+  Units at(((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 4, (int64_t)gridDim.x * (kThreads / 16), nb);
+  for (; __any_sync(0xFFFFFFFFu, at.r < groups); at.next()) {
+    const int64_t r0 = at.r * R, c = at.b * kF8Block + sub * 8;
+    const bool in = at.r < groups;
     const int n = in ? left8(features, c) : 0;
-    const int64_t cc = n > 0 ? c : 0;
-    Raw8<T> rg, ru;
-    rg.load(gu + r * ld + cc, n, vec);
-    ru.load(gu + r * ld + up + cc, n, vec);
-    float g[8], u[8], a[8];
-    rg.get(g);
-    ru.get(u);
+    const int m = in ? (rows - r0 < R ? (int)(rows - r0) : R) : 0;
+    Raw8<T> rg[R], ru[R];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) a[j] = g[j] * sigmoid(g[j]) * u[j];
-    uint2 qa;
-    const F8Scale sa = f8_block(a, out.e5m2, pow2, qa);
-    if (n > 0) store_q8(out.q + r * out.ld + c, n, qa);
-    if (in && sub == 0) out.s[r * out.lds + b] = sa.s;
-    if (ckpt.q) {
-      uint2 qg, qu;
-      const F8Scale sg = f8_block(g, ckpt.e5m2, pow2, qg);
-      const F8Scale su = f8_block(u, ckpt.e5m2, pow2, qu);
-      if (in) {
-        uint8_t* q = ckpt.q + r * ckpt.ld + c;
-        const int pad = left8(up, c);  // the columns between the halves are zeros (0 / s)
-        store_q8(q, pad, qg);
-        if (n > 0) store_q8(q + up, n, qu);
-        if (sub == 0) {
-          ckpt.s[r * ckpt.lds + b] = sg.s;
-          ckpt.s[r * ckpt.lds + nb + b] = su.s;
-        }
+    for (int i = 0; i < R; ++i) {
+      const T* p = gu + (i < m ? r0 + i : 0) * ld + (n > 0 ? c : 0);
+      rg[i].load(p, i < m ? n : 0, vec);
+      ru[i].load(p + up, i < m ? n : 0, vec);
+    }
+    float a[R][8], mx[8];  // maxima of a, g and u of each row
+    mx[6] = mx[7] = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float g[8], u[8];
+      rg[i].get(g);
+      ru[i].get(u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a[i][j] = g[j] * sigmoid(g[j]) * u[j];
+      mx[i] = amax8(a[i]);
+      mx[2 + i] = ckpt.q ? amax8(g) : 0.f;
+      mx[4 + i] = ckpt.q ? amax8(u) : 0.f;
+    }
+    float mine = lanes_max<8>(mx);
+    const bool check = __any_sync(0xFFFFFFFFu, !(mine < kInf));
+    if (check) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        float g[8], u[8];
+        rg[i].get(g);
+        ru[i].get(u);
+        mx[i] = amax8_finite(a[i]);
+        mx[2 + i] = amax8_finite(g);
+        mx[4 + i] = amax8_finite(u);
+      }
+      mine = lanes_max<8>(mx);
+    }
+    const int which = sub & 7;  // the block whose scale this lane makes
+    const F8Out& to = which < 2 ? out : ckpt;
+    const F8Scale s = f8_scale(mine, to.e5m2, pow2);
+    if (sub < (ckpt.q ? 6 : 2) && (which & 1) < m)
+      to.s[(r0 + (which & 1)) * to.lds + at.b + (which >= 4 ? nb : 0)] = s.s;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float inv = of_lane(s.inv, i), inv_g = of_lane(s.inv, 2 + i), inv_u = of_lane(s.inv, 4 + i);
+      const uint2 q = check ? f8x8<true>(a[i], inv, out.e5m2) : f8x8<false>(a[i], inv, out.e5m2);
+      if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c, n, q);
+      if (ckpt.q && i < m) {
+        float g[8], u[8];
+        rg[i].get(g);
+        ru[i].get(u);
+        uint8_t* o = ckpt.q + (r0 + i) * ckpt.ld + c;
+        // the columns between the halves are zeros
+        *reinterpret_cast<uint2*>(o) = check ? f8x8<true>(g, inv_g, ckpt.e5m2) : f8x8<false>(g, inv_g, ckpt.e5m2);
+        if (n > 0) store_q8(o + up, n, check ? f8x8<true>(u, inv_u, ckpt.e5m2) : f8x8<false>(u, inv_u, ckpt.e5m2));
       }
     }
   }
@@ -86,12 +114,13 @@ struct TileSmem {
 };
 
 // A 4 x 8 patch of a result, its largest magnitudes by columns (the warp's 8 rows together) to shared memory.
-__device__ __forceinline__ void column_maxima(float (*col_max)[128], const float v[4][8], bool check) {
+template <bool CHECK>
+__device__ __forceinline__ void column_maxima(float (*col_max)[128], const float v[4][8]) {
   const int tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
   float cm[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (check) {
+    if (CHECK) {
       cm[j] = fmaxf(fmaxf(finite_abs(v[0][j]), finite_abs(v[1][j])), fmaxf(finite_abs(v[2][j]), finite_abs(v[3][j])));
     } else {
       cm[j] = fmaxf(fmaxf(fabsf(v[0][j]), fabsf(v[1][j])), fmaxf(fabsf(v[2][j]), fabsf(v[3][j])));
@@ -106,42 +135,31 @@ __device__ __forceinline__ void column_maxima(float (*col_max)[128], const float
 }
 
 // The row form of a patch: m of its rows, n of its columns.
+template <bool CHECK>
 __device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out, int64_t r0, int64_t c0, int64_t block,
-                                           int m, int n, bool check, bool pow2) {
+                                           int m, int n, bool pow2) {
   const int tc = threadIdx.x & 15;
   float rm[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) rm[i] = check ? amax8_finite(v[i]) : amax8(v[i]);
-  // lane l of the 16 gets row l & 3: each exchange halves the rows a lane answers for
-  float a[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const bool up = tc & 2;
-    a[i] = fmaxf(up ? rm[i + 2] : rm[i], __shfl_xor_sync(0xFFFFFFFFu, up ? rm[i] : rm[i + 2], 2));
-  }
-  const bool up = tc & 1;
-  float b = fmaxf(up ? a[1] : a[0], __shfl_xor_sync(0xFFFFFFFFu, up ? a[0] : a[1], 1));
-  b = fmaxf(b, __shfl_xor_sync(0xFFFFFFFFu, b, 4));
-  b = fmaxf(b, __shfl_xor_sync(0xFFFFFFFFu, b, 8));
+  for (int i = 0; i < 4; ++i) rm[i] = CHECK ? amax8_finite(v[i]) : amax8(v[i]);
+  const float b = lanes_max<4>(rm);  // lane l of 16: row l & 3
   const F8Scale s = f8_scale(b, out.e5m2, pow2);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float inv = __shfl_sync(0xFFFFFFFFu, s.inv, i, 16);
-    const uint2 q = check ? f8x8<true>(v[i], inv, out.e5m2) : f8x8<false>(v[i], inv, out.e5m2);
-    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, q);
+    const float inv = of_lane(s.inv, i);
+    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, f8x8<CHECK>(v[i], inv, out.e5m2));
   }
   if (tc < m && tc < 4) out.s[(r0 + tc) * out.lds + block] = s.s;
 }
 
 // The patch by columns, as bytes, to the turned tile.
-__device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv, const float v[4][8], bool e5m2,
-                                           bool check) {
+template <bool CHECK>
+__device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv, const float v[4][8], bool e5m2) {
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const float inv = col_inv[tc * 8 + j];
-    const uint32_t q = check ? f8x4<true>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2)
-                             : f8x4<false>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2);
+    const uint32_t q = f8x4<CHECK>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2);
     *reinterpret_cast<uint32_t*>(&turned[(tc * 8 + j) * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]) = q;
   }
 }
@@ -168,19 +186,6 @@ struct GatedIn {
   bool e5m2;
 };
 
-__device__ __forceinline__ uint2 load_q8(const uint8_t* p, int n) {
-  if (n >= 8) return *reinterpret_cast<const uint2*>(p);
-  uint2 u = make_uint2(0u, 0u);
-  for (int i = 0; i < n; ++i) {
-    const uint32_t b = p[i];
-    if (i < 4)
-      u.x |= b << (8 * i);
-    else
-      u.y |= b << (8 * (i - 4));
-  }
-  return u;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(const GatedIn in, const T* da, int64_t ld,
                                                                             bool vec, int64_t rows, int64_t features,
@@ -196,65 +201,80 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
   const int m = rows - r0 >= 4 ? 4 : (rows - r0 < 0 ? 0 : (int)(rows - r0));
   const int64_t cc = n > 0 ? c0 : 0;
 
-  float dg[4][8], du[4][8], a[4][8];
-  bool bad = false;
+  Raw8<T> rd[4];
+  uint2 qg[4], qu[4];
+  float sg[4], su[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t r = i < m ? r0 + i : 0;
     const int ni = i < m ? n : 0;
-    Raw8<T> rd;
-    rd.load(da + r * ld + cc, ni, vec);
-    const uint2 qg = load_q8(in.q + r * in.ld + cc, ni), qu = load_q8(in.q + r * in.ld + up + cc, ni);
-    const float sg = ni > 0 ? in.s[r * in.lds + tile_c] : 0.f, su = ni > 0 ? in.s[r * in.lds + nb + tile_c] : 0.f;
+    rd[i].load(da + r * ld + cc, ni, vec);
+    qg[i] = load_q8(in.q + r * in.ld + cc, ni);
+    qu[i] = load_q8(in.q + r * in.ld + up + cc, ni);
+    sg[i] = ni > 0 ? in.s[r * in.lds + tile_c] : 0.f;
+    su[i] = ni > 0 ? in.s[r * in.lds + nb + tile_c] : 0.f;
+  }
+  float dg[4][8], du[4][8], a[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     float d[8], g[8], u[8];
-    rd.get(d);
-    f8x8_value(qg, in.e5m2, g);
-    f8x8_value(qu, in.e5m2, u);
+    rd[i].get(d);
+    f8x8_value(qg[i], in.e5m2, g);
+    f8x8_value(qu[i], in.e5m2, u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float gj = g[j] * sg, uj = u[j] * su;
+      const float gj = g[j] * sg[i], uj = u[j] * su[i];
       const float sig = sigmoid(gj), act = gj * sig;
       a[i][j] = act * uj;
       du[i][j] = d[j] * act;
-      dg[i][j] = d[j] * uj * (sig * (1.f + gj * (1.f - sig)));
+      dg[i][j] = d[j] * uj * fmaf(act, 1.f - sig, sig);  // sig (1 + g (1 - sig))
     }
-    // an infinity in any of the three shows in the sum of their magnitudes
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      bad = bad || !(fmaxf(fmaxf(fabsf(a[i][j]), fabsf(du[i][j])), fabsf(dg[i][j])) < kInf);
   }
-  const bool check = __syncthreads_or(bad);
   const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);
-  if (dgu_t.q) {
-    column_maxima(sm.col_max[0], dg, check);
-    column_maxima(sm.col_max[1], du, check);
-  }
-  if (a_t.q) column_maxima(sm.col_max[2], a, check);
-  if (dgu.q) {
-    // the gate half's rows go on to the up half with zeros
-    write_rows(dg, dgu, r0, c0, tile_c, m, 8, check, pow2);
-    write_rows(du, dgu, r0, up + c0, nb + tile_c, m, n, check, pow2);
-  }
-  __syncthreads();
-  if (threadIdx.x < 384) {  // a column's scale each: of dg, du and a
-    const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
-    const F8Out& out = which < 2 ? dgu_t : a_t;
-    if (out.q) {
-      float mx = 0.f;
+  // a column's scale each: of dg, du and a; the gate half's columns go on to the up half with zeros
+  const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
+  const F8Out& out = which < 2 ? dgu_t : a_t;
+  auto column_scales = [&] {
+    float mx = 0.f;
+    if (which < 3) {
 #pragma unroll
       for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[which][w][c]);
       const F8Scale s = f8_scale(mx, out.e5m2, pow2);
       sm.col_inv[which][c] = s.inv;
-      // the gate half's columns go on to the up half with zeros
-      if (which == 0 || c < cols) out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
+      if (out.q && mx < kInf && (which == 0 || c < cols))
+        out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
     }
-  }
+    return mx;
+  };
+  auto maxima = [&](auto finite) {
+    column_maxima<decltype(finite)::value>(sm.col_max[0], dg);
+    column_maxima<decltype(finite)::value>(sm.col_max[1], du);
+    column_maxima<decltype(finite)::value>(sm.col_max[2], a);
+  };
+  auto emit = [&](auto finite) {
+    constexpr bool CHECK = decltype(finite)::value;
+    if (dgu.q) {
+      write_rows<CHECK>(dg, dgu, r0, c0, tile_c, m, 8, pow2);
+      write_rows<CHECK>(du, dgu, r0, up + c0, nb + tile_c, m, n, pow2);
+    }
+    if (dgu_t.q) {
+      turn_patch<CHECK>(sm.turned[0], sm.col_inv[0], dg, dgu_t.e5m2);
+      turn_patch<CHECK>(sm.turned[1], sm.col_inv[1], du, dgu_t.e5m2);
+    }
+    if (a_t.q) turn_patch<CHECK>(sm.turned[2], sm.col_inv[2], a, a_t.e5m2);
+  };
+  maxima(std::false_type());
   __syncthreads();
-  if (dgu_t.q) {
-    turn_patch(sm.turned[0], sm.col_inv[0], dg, dgu_t.e5m2, check);
-    turn_patch(sm.turned[1], sm.col_inv[1], du, dgu_t.e5m2, check);
+  // an infinity anywhere is some column's largest magnitude
+  if (__syncthreads_or(!(column_scales() < kInf))) {
+    maxima(std::true_type());
+    __syncthreads();
+    column_scales();
+    __syncthreads();
+    emit(std::true_type());
+  } else {
+    emit(std::false_type());
   }
-  if (a_t.q) turn_patch(sm.turned[2], sm.col_inv[2], a, a_t.e5m2, check);
   __syncthreads();
   if (dgu_t.q) {
     write_turned(sm.turned[0], dgu_t, rows, tile_r, c_tile, kF8Block);
@@ -267,7 +287,7 @@ template <typename T>
 cudaError_t forward(const void* gu, int64_t ld, int64_t rows, int64_t features, const F8Out& out, const F8Out& ckpt,
                     bool pow2, cudaStream_t st) {
   const int64_t nb = (features + kF8Block - 1) / kF8Block;
-  const int64_t want = (rows * nb + kThreads / 16 - 1) / (kThreads / 16);
+  const int64_t want = ((rows + R - 1) / R * nb + kThreads / 16 - 1) / (kThreads / 16);
   const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * 32;
   const bool vec = (reinterpret_cast<uintptr_t>(gu) & 15) == 0 && ld * sizeof(T) % 16 == 0;
   gated_f8_kernel<T><<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(static_cast<const T*>(gu), ld, vec,

@@ -32,11 +32,6 @@ __device__ __forceinline__ float cta_sum(float v, float* scratch) {
   return s;
 }
 
-__device__ __forceinline__ int left8(int64_t cols, int64_t c) {
-  const int64_t n = cols - c;
-  return n >= 8 ? 8 : (n < 0 ? 0 : (int)n);
-}
-
 struct Aligned {  // whether each array's rows start on 16-byte boundaries
   bool a, b, c, d;
 };
@@ -121,96 +116,141 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParam
   }
 }
 
+// One row of the backward pass, as it lies in memory: dy, h and dh.
 template <typename T, int NV>
-__global__ void __launch_bounds__(kThreads) rmsnorm_f8_backward_kernel(const RmsnormBackwardParams P,
-                                                                       const Aligned al) {
+struct RowIn {
+  Raw8<T> dy[NV], h[NV], dh[NV];
+  float rstd;
+  __device__ __forceinline__ void load(const RmsnormBackwardParams& P, const Aligned& al, int64_t r) {
+    rstd = P.rstd[r];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
+      const int n = left8(P.cols, c);
+      c = n > 0 ? c : 0;
+      dy[k].load(static_cast<const T*>(P.dy) + r * P.lddy + c, n, al.a);
+      h[k].load(static_cast<const T*>(P.h) + r * P.ldh + c, n, al.b);
+      if (P.dh) dh[k].load(static_cast<const T*>(P.dh) + r * P.lddh + c, n, al.c);
+    }
+  }
+};
+
+// A CTA walks rows with its share of the weights and of dw in registers; the next row is on its way while this one is
+// worked on, so that the reads never stop for the row's sum (two CTAs of an SM keep 48 KB in flight at 4096 bf16
+// columns).
+template <typename T, int NV>
+__global__ void __launch_bounds__(kThreads, NV == 1 ? (sizeof(T) == 2 ? 3 : 2) : (NV == 2 && sizeof(T) == 2 ? 2 : 1))
+    rmsnorm_f8_backward_kernel(const RmsnormBackwardParams P, const Aligned al) {
   __shared__ float scratch[2][kWarps];
-  constexpr int kHeld = NV > 0 ? NV : 1;
-  float* partial = P.partial + (int64_t)blockIdx.x * P.cols;
-  float dw[kHeld][8] = {};
+  // the next row, unless it would not fit in registers
+  constexpr bool AHEAD = NV * sizeof(Raw8<T>) <= 64;
+  float w[NV][8], dw[NV][8];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
+    const int n = left8(P.cols, c);
+    Raw8<float> rw;
+    rw.load(P.weight + (n > 0 ? c : 0), n, true);
+    rw.get(w[k]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
+  }
+  RowIn<T, NV> in, next;
   int turn = 0;
+  if (AHEAD) next.load(P, al, blockIdx.x);
   for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x, turn ^= 1) {
-    const float rstd = P.rstd[r];
-    float g[kHeld][8], x[kHeld][8];  // dy w and h rstd
+    if (AHEAD) {
+      in = next;
+      if (r + gridDim.x < P.rows) next.load(P, al, r + gridDim.x);
+    } else {
+      in.load(P, al, r);
+    }
     float dot = 0.f;
-    const T* dy_row = static_cast<const T*>(P.dy) + r * P.lddy;
-    const T* h_row = static_cast<const T*>(P.h) + r * P.ldh;
-    const T* dh_row = static_cast<const T*>(P.dh) + r * P.lddh;
-    T* dx_row = static_cast<T*>(P.dx) + r * P.lddx;
-    auto read = [&](int64_t c, int n, float gk[8], float xk[8], float dyk[8]) {
-      Raw8<T> a, b;
-      Raw8<float> w;
-      a.load(dy_row + c, n, al.a);
-      b.load(h_row + c, n, al.b);
-      w.load(P.weight + c, n, true);
-      a.get(dyk);
-      b.get(xk);
-      w.get(gk);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float dy[8], x[8];
+      in.dy[k].get(dy);
+      in.h[k].get(x);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        xk[i] *= rstd;
-        gk[i] *= dyk[i];
-      }
-    };
-    auto write = [&](int64_t c, int n, const float gk[8], const float xk[8], float mean) {
-      float d[8] = {};
-      if (P.dh) {
-        Raw8<T> a;
-        a.load(dh_row + c, n, al.c);
-        a.get(d);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, gk[i] - xk[i] * mean, d[i]);
-      store8(dx_row + c, n, al.d, d);
-    };
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
-        const int n = left8(P.cols, c);
-        float dyk[8];
-        read(n > 0 ? c : 0, n, g[k], x[k], dyk);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dot = fmaf(g[k][i], x[k][i], dot);
-          dw[k][i] = fmaf(dyk[i], x[k][i], dw[k][i]);
-        }
-      }
-    } else {
-      for (int64_t c = threadIdx.x * 8; c < P.cols; c += kThreads * 8) {
-        const int n = left8(P.cols, c);
-        float dyk[8];
-        read(c, n, g[0], x[0], dyk);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dot = fmaf(g[0][i], x[0][i], dot);
-          if (i < n) partial[c + i] = fmaf(dyk[i], x[0][i], r == blockIdx.x ? 0.f : partial[c + i]);
-        }
+        x[i] *= in.rstd;
+        const float t = dy[i] * x[i];
+        dot = fmaf(t, w[k][i], dot);
+        dw[k][i] += t;
       }
     }
     const float mean = cta_sum(dot, scratch[turn]) / (float)P.cols;
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
-        const int n = left8(P.cols, c);
-        if (n > 0) write(c, n, g[k], x[k], mean);
-      }
-    } else {
-      for (int64_t c = threadIdx.x * 8; c < P.cols; c += kThreads * 8) {
-        const int n = left8(P.cols, c);
-        float dyk[8];
-        read(c, n, g[0], x[0], dyk);
-        write(c, n, g[0], x[0], mean);
-      }
-    }
-  }
-  if constexpr (NV > 0) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
       const int n = left8(P.cols, c);
-      if (n > 0) store8(partial + c, n, P.cols % 4 == 0, dw[k]);
+      float dy[8], x[8], d[8] = {};
+      in.dy[k].get(dy);
+      in.h[k].get(x);
+      if (P.dh) in.dh[k].get(d);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = fmaf(in.rstd, dy[i] * w[k][i] - x[i] * in.rstd * mean, d[i]);
+      if (n > 0) store8(static_cast<T*>(P.dx) + r * P.lddx + c, n, al.d, d);
+    }
+  }
+  float* partial = P.partial + (int64_t)blockIdx.x * P.cols;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
+    const int n = left8(P.cols, c);
+    if (n > 0) store8(partial + c, n, P.cols % 4 == 0, dw[k]);
+  }
+}
+
+// Rows too long for registers: read twice, dw summed in the CTA's partial row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rmsnorm_f8_backward_long_kernel(const RmsnormBackwardParams P,
+                                                                            const Aligned al) {
+  __shared__ float scratch[2][kWarps];
+  float* partial = P.partial + (int64_t)blockIdx.x * P.cols;
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x, turn ^= 1) {
+    const float rstd = P.rstd[r];
+    auto read = [&](int64_t c, int n, float g[8], float x[8], float dy[8]) {
+      Raw8<T> a, b;
+      Raw8<float> w;
+      a.load(static_cast<const T*>(P.dy) + r * P.lddy + c, n, al.a);
+      b.load(static_cast<const T*>(P.h) + r * P.ldh + c, n, al.b);
+      w.load(P.weight + c, n, true);
+      a.get(dy);
+      b.get(x);
+      w.get(g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] *= rstd;
+        g[i] *= dy[i];
+      }
+    };
+    float dot = 0.f;
+    for (int64_t c = threadIdx.x * 8; c < P.cols; c += kThreads * 8) {
+      const int n = left8(P.cols, c);
+      float g[8], x[8], dy[8];
+      read(c, n, g, x, dy);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        dot = fmaf(g[i], x[i], dot);
+        if (i < n) partial[c + i] = fmaf(dy[i], x[i], r == blockIdx.x ? 0.f : partial[c + i]);
+      }
+    }
+    const float mean = cta_sum(dot, scratch[turn]) / (float)P.cols;
+    // dx may be one of the inputs: a thread reads its columns again before it writes them
+    for (int64_t c = threadIdx.x * 8; c < P.cols; c += kThreads * 8) {
+      const int n = left8(P.cols, c);
+      float g[8], x[8], dy[8], d[8] = {};
+      read(c, n, g, x, dy);
+      if (P.dh) {
+        Raw8<T> a;
+        a.load(static_cast<const T*>(P.dh) + r * P.lddh + c, n, al.c);
+        a.get(d);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = fmaf(rstd, g[i] - x[i] * mean, d[i]);
+      store8(static_cast<T*>(P.dx) + r * P.lddx + c, n, al.d, d);
     }
   }
 }
@@ -221,8 +261,10 @@ __global__ void __launch_bounds__(512) rmsnorm_dw_kernel(const float* partial, i
   const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < cols)
+  if (c < cols) {
+#pragma unroll 8
     for (int64_t i = group; i < n; i += 16) s += partial[i * cols + c];
+  }
   part[group][lane] = s;
   __syncthreads();
   if (group == 0 && c < cols) {
@@ -257,17 +299,20 @@ template <typename T>
 cudaError_t backward(const RmsnormBackwardParams& p, cudaStream_t st) {
   const Aligned al{rows16(p.dy, p.lddy, sizeof(T)), rows16(p.h, p.ldh, sizeof(T)), rows16(p.dh, p.lddh, sizeof(T)),
                    rows16(p.dx, p.lddx, sizeof(T))};
-  const int64_t n = p.rows < kF8NormPartials ? p.rows : kF8NormPartials;
+  const int nv = p.cols <= kThreads * 8 ? 1 : (p.cols <= 2 * kThreads * 8 ? 2 : (p.cols <= 4 * kThreads * 8 ? 4 : 0));
+  // the CTAs that fit at once (of the 152 SMs; fewer SMs take them in turn), each with a partial row of dw
+  const int64_t fit = kF8NormPartials / 4 * (nv == 0 ? 4 : (nv == 1 ? (sizeof(T) == 2 ? 3 : 2) : (nv == 2 && sizeof(T) == 2 ? 2 : 1)));
+  const int64_t n = p.rows < fit ? p.rows : fit;
   if (n > 0) {
     const unsigned grid = (unsigned)n;
-    if (p.cols <= kThreads * 8)
+    if (nv == 1)
       rmsnorm_f8_backward_kernel<T, 1><<<grid, kThreads, 0, st>>>(p, al);
-    else if (p.cols <= 2 * kThreads * 8)
+    else if (nv == 2)
       rmsnorm_f8_backward_kernel<T, 2><<<grid, kThreads, 0, st>>>(p, al);
-    else if (p.cols <= 4 * kThreads * 8)
+    else if (nv == 4)
       rmsnorm_f8_backward_kernel<T, 4><<<grid, kThreads, 0, st>>>(p, al);
     else
-      rmsnorm_f8_backward_kernel<T, 0><<<grid, kThreads, 0, st>>>(p, al);
+      rmsnorm_f8_backward_long_kernel<T><<<grid, kThreads, 0, st>>>(p, al);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }

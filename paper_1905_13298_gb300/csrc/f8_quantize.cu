@@ -29,65 +29,75 @@ struct SourceFloat {
     raw.load(p + r * ld + c, n, vec);
   }
 };
+// Eight 8-bit values and their scale, decoded where they are used: an eighth of the registers of the values.
+struct RawF8 {
+  uint2 u;
+  float s;
+  bool e5m2;
+  __device__ __forceinline__ void get(float v[8]) const {
+    f8x8_value(u, e5m2, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s;
+  }
+};
 struct SourceF8 {
-  using Raw = Raw8<float>;
+  using Raw = RawF8;
   static constexpr bool PACKED = false;
   const uint8_t* q;
   const float* s;
   int64_t ld, lds;
   bool e5m2, tiles;
   __device__ __forceinline__ void load(int64_t r, int64_t c, int n, Raw& raw) const {
-    const uint8_t* p = q + r * ld + c;
-    uint2 u = make_uint2(0u, 0u);
-    if (n >= 8) {
-      u = *reinterpret_cast<const uint2*>(p);
-    } else {
-      for (int i = 0; i < n; ++i) {
-        const uint32_t b = p[i];
-        if (i < 4)
-          u.x |= b << (8 * i);
-        else
-          u.y |= b << (8 * (i - 4));
-      }
-    }
-    const float sc = n > 0 ? s[(tiles ? r / kF8Block : r) * lds + c / kF8Block] : 0.f;
-    float v[8];
-    f8x8_value(u, e5m2, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] * sc : 0.f;
-    raw.a = make_float4(v[0], v[1], v[2], v[3]);
-    raw.b = make_float4(v[4], v[5], v[6], v[7]);
+    raw.u = load_q8(q + r * ld + c, n);
+    raw.s = n > 0 ? s[(tiles ? r / kF8Block : r) * lds + c / kF8Block] : 0.f;
+    raw.e5m2 = e5m2;
   }
 };
 
-__device__ __forceinline__ int left8(int64_t cols, int64_t c) {
-  const int64_t n = cols - c;
-  return n >= 8 ? 8 : (n < 0 ? 0 : (int)n);
-}
-
+// Rows alone: 16 lanes hold one block of each of R rows.
+constexpr int R = 4;
 template <typename Source>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const Source src, int64_t rows, int64_t cols,
                                                                  const F8Out out, bool pow2) {
-  const int64_t nb = (cols + kF8Block - 1) / kF8Block;
-  const int64_t total = rows * nb;
+  const int64_t nb = (cols + kF8Block - 1) / kF8Block, groups = (rows + R - 1) / R;
   const int sub = threadIdx.x & 15;
-  const int64_t first = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 4;
-  const int64_t step = (int64_t)gridDim.x * (kThreads / 16);
-  // both halves of a warp take the same number of rounds: the shuffles are full
-  for (int64_t base = first & ~(int64_t)1; base < total; base += step) {
-    const int64_t i = base + (first & 1);
-    const bool in = i < total;
-    const int64_t r = in ? i / nb : 0, b = in ? i - r * nb : 0;
-    const int64_t c = b * kF8Block + sub * 8;
-    const int n = in ? left8(cols, c) : 0;
-    typename Source::Raw raw;
-    src.load(r, n > 0 ? c : 0, n, raw);
-    float v[8];
-    raw.get(v);
-    uint2 q;
-    const F8Scale s = f8_block(v, out.e5m2, pow2, q);
-    if (n > 0) store_q8(out.q + r * out.ld + c, n, q);
-    if (in && sub == 0) out.s[r * out.lds + b] = s.s;
+  // both halves of a warp go on until the later one is done: the shuffles are full
+  Units at(((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 4, (int64_t)gridDim.x * (kThreads / 16), nb);
+  for (; __any_sync(0xFFFFFFFFu, at.r < groups); at.next()) {
+    const int64_t r0 = at.r * R, c = at.b * kF8Block + sub * 8;
+    const int n = at.r < groups ? left8(cols, c) : 0;
+    const int m = at.r < groups ? (rows - r0 < R ? (int)(rows - r0) : R) : 0;
+    typename Source::Raw raw[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) src.load(i < m ? r0 + i : 0, n > 0 ? c : 0, i < m ? n : 0, raw[i]);
+    float rm[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float v[8];
+      raw[i].get(v);
+      rm[i] = amax8(v);
+    }
+    float mx = lanes_max<R>(rm);
+    const bool check = __any_sync(0xFFFFFFFFu, !(mx < kInf));
+    if (check) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        float v[8];
+        raw[i].get(v);
+        rm[i] = amax8_finite(v);
+      }
+      mx = lanes_max<R>(rm);
+    }
+    const F8Scale s = f8_scale(mx, out.e5m2, pow2);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float inv = of_lane(s.inv, i);
+      float v[8];
+      raw[i].get(v);
+      const uint2 q = check ? f8x8<true>(v, inv, out.e5m2) : f8x8<false>(v, inv, out.e5m2);
+      if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c, n, q);
+    }
+    if (sub < m) out.s[(r0 + sub) * out.lds + at.b] = s.s;
   }
 }
 
@@ -133,26 +143,6 @@ __device__ __forceinline__ void patch_maxima(const typename Source::Raw (&raw)[8
   }
 }
 
-// The maxima of a patch's 8 rows over the 16 lanes that share them; lane l of the 16 gets row l & 7.  Each exchange
-// halves the rows a lane answers for: 8 shuffles instead of 32.
-__device__ __forceinline__ float row_of_lane(const float rm[8]) {
-  float a[4], b[2];
-  const int lane = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool up = lane & 4;
-    a[i] = fmaxf(up ? rm[i + 4] : rm[i], __shfl_xor_sync(0xFFFFFFFFu, up ? rm[i] : rm[i + 4], 4));
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const bool up = lane & 2;
-    b[i] = fmaxf(up ? a[i + 2] : a[i], __shfl_xor_sync(0xFFFFFFFFu, up ? a[i] : a[i + 2], 2));
-  }
-  const bool up = lane & 1;
-  const float c = fmaxf(up ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, up ? b[0] : b[1], 1));
-  return fmaxf(c, __shfl_xor_sync(0xFFFFFFFFu, c, 8));
-}
-
 struct TileAt {
   int64_t rows, cols, r0, c0, tile_r, tile_c;
   int m, n;  // rows and columns of the patch that exist
@@ -165,7 +155,7 @@ __device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, c
   const F8Scale s = f8_scale(out.tiles ? tile_max : row_max, out.e5m2, pow2);  // lane i of 16: row i's
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float inv = __shfl_sync(0xFFFFFFFFu, s.inv, i, 16);
+    const float inv = of_lane(s.inv, i);
     float v[8];
     raw[i].get(v);
     if (i < t.m && t.n > 0)
@@ -206,7 +196,7 @@ __device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm, 
 }
 
 template <typename Source>
-__global__ void __launch_bounds__(kThreads, Source::PACKED ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ? 3 : 2)
     quantize_tile_kernel(const Source src, int64_t rows, int64_t cols, const F8Out out, const F8Out out_t, bool pow2) {
   __shared__ __align__(16) TileSmem sm;
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
@@ -250,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, Source::PACKED ? 3 : 2)
       c[j] = fmaxf(up ? cm[j + 4] : cm[j], __shfl_xor_sync(0xFFFFFFFFu, up ? cm[j] : cm[j + 4], 16));
     *reinterpret_cast<float4*>(&sm.col_max[warp][tc * 8 + (up ? 4 : 0)]) = make_float4(c[0], c[1], c[2], c[3]);
   }
-  const float row_max = row_of_lane(rm);
+  const float row_max = lanes_max<8>(rm);  // lane l of 16: row l & 7
   float tile_max = 0.f;
   if (out.tiles || out_t.tiles) {
     float m = row_max;
@@ -308,7 +298,7 @@ cudaError_t run(const Source& src, int64_t rows, int64_t cols, const F8Out& out,
                 cudaStream_t st) {
   const int64_t nb = (cols + kF8Block - 1) / kF8Block;
   if (out_t.q == nullptr && !out.tiles) {
-    const int64_t want = (rows * nb + kThreads / 16 - 1) / (kThreads / 16);
+    const int64_t want = ((rows + R - 1) / R * nb + kThreads / 16 - 1) / (kThreads / 16);
     const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * 32;
     quantize_rows_kernel<<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(src, rows, cols, out, pow2);
   } else {
