@@ -550,7 +550,8 @@ void ds_specialized_destroy(ds_specialized* h);
  * pointers need only their type's alignment (16 bytes take the vector path),
  * except `weight`, 16 bytes.  Arithmetic is float32; a value is rounded once,
  * where it is stored.  Limits: rows and cols below 2^31 - 256, rows * ld at
- * most 2^48.  Outputs must not overlap inputs except where a call says so.
+ * most 2^48.  Outputs must not overlap inputs except where a call says so, and
+ * the 8-bit outputs of one call have one format.
  * ------------------------------------------------------------------------- */
 #define DS_TYPE_F32 0
 #define DS_TYPE_BF16 1

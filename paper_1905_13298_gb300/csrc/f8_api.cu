@@ -1,6 +1,8 @@
 // C ABI entry points of the 8-bit floating-point operators: argument
 // validation, then stream-ordered launches.  Nothing is launched and no
 // output is written when validation fails.
+#include <initializer_list>
+
 #include "f8_common.cuh"
 
 namespace ds {
@@ -104,14 +106,24 @@ ds_status check_tensor(const char* name, const void* p, int64_t rows, int64_t co
   return DS_OK;
 }
 
+// The 8-bit matrices that a call writes have one format.
+ds_status check_formats(const ds_f8_matrix* a, const ds_f8_matrix* b, const ds_f8_matrix* c, bool* e5m2) {
+  const ds_f8_matrix* first = a ? a : (b ? b : c);
+  for (const ds_f8_matrix* m : {a, b, c})
+    if (m && m->format != first->format) return fail(DS_ERR_INVALID_ARG, "the outputs have different 8-bit formats");
+  *e5m2 = first->format == DS_F8_E5M2;
+  return DS_OK;
+}
+
 // The outputs of a quantiser: shapes, at least one, no overlap with each other or the source.
 ds_status check_quantize(const Span (&src)[2], int64_t rows, int64_t cols, const ds_f8_matrix* out,
-                         const ds_f8_matrix* out_t, uint32_t flags) {
+                         const ds_f8_matrix* out_t, uint32_t flags, bool* e5m2) {
   if (!out && !out_t) return fail(DS_ERR_INVALID_ARG, "neither out nor out_t is given");
   ds_status r = check_flags(flags);
   if (r != DS_OK) return r;
   if ((r = check_f8_out("out", out, rows, cols, false)) != DS_OK) return r;
   if ((r = check_f8_out("out_t", out_t, cols, rows, false)) != DS_OK) return r;
+  if ((r = check_formats(out, out_t, nullptr, e5m2)) != DS_OK) return r;
   const Span outs[] = {values_of("out", out), scales_of("out's scales", out), values_of("out_t", out_t),
                        scales_of("out_t's scales", out_t)};
   if ((r = check_apart(outs, src)) != DS_OK) return r;
@@ -139,10 +151,11 @@ ds_status ds_quantize_f8(const void* x, int type, int64_t rows, int64_t cols, in
   if (!x && rows > 0 && cols > 0) return fail(DS_ERR_INVALID_ARG, "NULL x");
   if ((r = check_tensor("x", x, rows, cols, ldx, type_size(type))) != DS_OK) return r;
   const Span src[] = {span("x", x, strided(rows, cols, ldx, type_size(type))), span("x", nullptr, 0)};
-  if ((r = check_quantize(src, rows, cols, out, out_t, flags)) != DS_OK) return r;
+  bool e5m2 = false;
+  if ((r = check_quantize(src, rows, cols, out, out_t, flags, &e5m2)) != DS_OK) return r;
   if (rows == 0 || cols == 0) return DS_OK;
-  return cuda_check(launch_quantize_f8(x, type, rows, cols, ldx, f8_out(out), f8_out(out_t), flags & DS_F8_POW2,
-                                       static_cast<cudaStream_t>(stream)),
+  return cuda_check(launch_quantize_f8(x, type, rows, cols, ldx, f8_out(out), f8_out(out_t), e5m2,
+                                       (flags & DS_F8_POW2) != 0, static_cast<cudaStream_t>(stream)),
                     "quantize_f8 launch");
 }
 
@@ -154,9 +167,10 @@ ds_status ds_requantize_f8(const ds_f8_matrix* x, const ds_f8_matrix* out, const
   ds_status r = check_f8("x", x);
   if (r != DS_OK) return r;
   const Span src[] = {values_of("x", x), scales_of("x's scales", x)};
-  if ((r = check_quantize(src, x->rows, x->cols, out, out_t, flags)) != DS_OK) return r;
+  bool e5m2 = false;
+  if ((r = check_quantize(src, x->rows, x->cols, out, out_t, flags, &e5m2)) != DS_OK) return r;
   if (x->rows == 0 || x->cols == 0) return DS_OK;
-  return cuda_check(launch_requantize_f8(x, f8_out(out), f8_out(out_t), flags & DS_F8_POW2,
+  return cuda_check(launch_requantize_f8(x, f8_out(out), f8_out(out_t), e5m2, (flags & DS_F8_POW2) != 0,
                                          static_cast<cudaStream_t>(stream)),
                     "requantize_f8 launch");
 }
@@ -237,7 +251,7 @@ ds_status ds_rmsnorm_f8(const void* x, int64_t ldx, const void* residual, int64_
   if ((r = check_apart(outs, ins)) != DS_OK) return r;
   if (rows == 0) return DS_OK;
   const RmsnormParams p{x,  residual, ldx, ldr, weight, rows, cols, eps, f8_out(out),
-                        h,  ldh,      rstd, (flags & DS_F8_POW2) != 0};
+                        h,  ldh,      rstd, out->format == DS_F8_E5M2, (flags & DS_F8_POW2) != 0};
   return cuda_check(launch_rmsnorm_f8(p, type, static_cast<cudaStream_t>(stream)), "rmsnorm_f8 launch");
 }
 
@@ -297,12 +311,14 @@ ds_status ds_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_
   if ((r = check_tensor("gu", gu, rows, width, ld, size)) != DS_OK) return r;
   if ((r = check_f8_out("out", out, rows, features, true)) != DS_OK) return r;
   if ((r = check_f8_out("ckpt", ckpt, rows, width, true)) != DS_OK) return r;
+  bool e5m2 = false;
+  if ((r = check_formats(out, ckpt, nullptr, &e5m2)) != DS_OK) return r;
   const Span outs[] = {values_of("out", out), scales_of("out's scales", out), values_of("ckpt", ckpt),
                        scales_of("ckpt's scales", ckpt)};
   const Span ins[] = {span("gu", gu, strided(rows, width, ld, size))};
   if ((r = check_apart(outs, ins)) != DS_OK) return r;
   if (rows == 0) return DS_OK;
-  return cuda_check(launch_gated_f8(gu, type, ld, rows, features, f8_out(out), f8_out(ckpt),
+  return cuda_check(launch_gated_f8(gu, type, ld, rows, features, f8_out(out), f8_out(ckpt), e5m2,
                                     (flags & DS_F8_POW2) != 0, static_cast<cudaStream_t>(stream)),
                     "gated_f8 launch");
 }
@@ -326,6 +342,8 @@ ds_status ds_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int typ
   if ((r = check_f8_out("dgu", dgu, rows, width, true)) != DS_OK) return r;
   if ((r = check_f8_out("dgu_t", dgu_t, width, rows, true)) != DS_OK) return r;
   if ((r = check_f8_out("a_t", a_t, features, rows, true)) != DS_OK) return r;
+  bool e5m2 = false;
+  if ((r = check_formats(dgu, dgu_t, a_t, &e5m2)) != DS_OK) return r;
   const Span outs[] = {values_of("dgu", dgu),     scales_of("dgu's scales", dgu),
                        values_of("dgu_t", dgu_t), scales_of("dgu_t's scales", dgu_t),
                        values_of("a_t", a_t),     scales_of("a_t's scales", a_t)};
@@ -335,7 +353,7 @@ ds_status ds_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int typ
   if (rows == 0) return DS_OK;
   if (blocks_of(rows) * blocks_of(features) > ((int64_t)1 << 31) - 1)
     return fail(DS_ERR_UNSUPPORTED, "matrix too large");
-  return cuda_check(launch_gated_f8_backward(ckpt, da, type, ld, features, f8_out(dgu), f8_out(dgu_t), f8_out(a_t),
+  return cuda_check(launch_gated_f8_backward(ckpt, da, type, ld, features, f8_out(dgu), f8_out(dgu_t), f8_out(a_t), e5m2,
                                              (flags & DS_F8_POW2) != 0, static_cast<cudaStream_t>(stream)),
                     "gated_f8_backward launch");
 }

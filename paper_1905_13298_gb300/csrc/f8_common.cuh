@@ -132,28 +132,32 @@ __device__ __forceinline__ void store8<float>(float* p, int n, bool vec, const f
 // ---------------------------------------------------------------------------
 // 8-bit formats
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t f8x2(float lo, float hi, bool e5m2) {
+// The format is a template argument throughout: as a value it would cost both conversions and a selection.
+template <bool E5M2>
+__device__ __forceinline__ uint32_t f8x2(float lo, float hi) {
   uint16_t r;
-  if (e5m2)
+  if (E5M2)
     asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   else
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ float2 f8x2_value(uint16_t q, bool e5m2) {
+template <bool E5M2>
+__device__ __forceinline__ float2 f8x2_value(uint16_t q) {
   uint32_t h;
-  if (e5m2)
+  if (E5M2)
     asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"(q));
   else
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(q));
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
-__device__ __forceinline__ void f8x8_value(uint2 q, bool e5m2, float v[8]) {
+template <bool E5M2>
+__device__ __forceinline__ void f8x8_value(uint2 q, float v[8]) {
   const uint32_t w[2] = {q.x, q.y};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float2 a = f8x2_value((uint16_t)(w[i] & 0xFFFFu), e5m2);
-    const float2 b = f8x2_value((uint16_t)(w[i] >> 16), e5m2);
+    const float2 a = f8x2_value<E5M2>((uint16_t)(w[i] & 0xFFFFu));
+    const float2 b = f8x2_value<E5M2>((uint16_t)(w[i] >> 16));
     v[4 * i] = a.x, v[4 * i + 1] = a.y, v[4 * i + 2] = b.x, v[4 * i + 3] = b.y;
   }
 }
@@ -161,9 +165,9 @@ __device__ __forceinline__ void f8x8_value(uint2 q, bool e5m2, float v[8]) {
 struct F8Scale {
   float s, inv;
 };
-// max and the scale's rounding are those of the matrix that is written
-__device__ __forceinline__ F8Scale f8_scale(float amax, bool e5m2, bool pow2) {
-  float s = fmaxf(__fdiv_rn(amax, e5m2 ? 57344.f : 448.f), 1.17549435e-38f);
+template <bool E5M2>
+__device__ __forceinline__ F8Scale f8_scale(float amax, bool pow2) {
+  float s = fmaxf(__fdiv_rn(amax, E5M2 ? 57344.f : 448.f), 1.17549435e-38f);
   if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
   return F8Scale{s, __frcp_rn(s)};
 }
@@ -173,14 +177,14 @@ template <bool CHECK>
 __device__ __forceinline__ float f8_unit(float v, float inv) {
   return CHECK ? fmaf(v, 0.f, v * inv) : v * inv;
 }
-template <bool CHECK>
-__device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d, float inv, bool e5m2) {
-  return f8x2(f8_unit<CHECK>(a, inv), f8_unit<CHECK>(b, inv), e5m2) |
-         (f8x2(f8_unit<CHECK>(c, inv), f8_unit<CHECK>(d, inv), e5m2) << 16);
+template <bool E5M2, bool CHECK>
+__device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d, float inv) {
+  return f8x2<E5M2>(f8_unit<CHECK>(a, inv), f8_unit<CHECK>(b, inv)) |
+         (f8x2<E5M2>(f8_unit<CHECK>(c, inv), f8_unit<CHECK>(d, inv)) << 16);
 }
-template <bool CHECK>
-__device__ __forceinline__ uint2 f8x8(const float v[8], float inv, bool e5m2) {
-  return make_uint2(f8x4<CHECK>(v[0], v[1], v[2], v[3], inv, e5m2), f8x4<CHECK>(v[4], v[5], v[6], v[7], inv, e5m2));
+template <bool E5M2, bool CHECK>
+__device__ __forceinline__ uint2 f8x8(const float v[8], float inv) {
+  return make_uint2(f8x4<E5M2, CHECK>(v[0], v[1], v[2], v[3], inv), f8x4<E5M2, CHECK>(v[4], v[5], v[6], v[7], inv));
 }
 // The address is 8-byte aligned: rows start 16 bytes apart or a multiple of it.
 __device__ __forceinline__ void store_q8(uint8_t* p, int n, uint2 q) {
@@ -255,12 +259,13 @@ __device__ __forceinline__ float of_lane(float v, int l) { return __shfl_sync(0x
 
 // The scale and the 8-bit values of a block that 16 lanes hold; all 32 lanes of the warp call it.  Infinities are
 // rare: they are looked for by the largest magnitude, and the block is then gone over again.
-__device__ __forceinline__ F8Scale f8_block(const float v[8], bool e5m2, bool pow2, uint2& q) {
+template <bool E5M2>
+__device__ __forceinline__ F8Scale f8_block(const float v[8], bool pow2, uint2& q) {
   float m = max16(amax8(v));
   const bool inf = __any_sync(0xFFFFFFFFu, !(m < kInf));
   if (inf) m = max16(amax8_finite(v));
-  const F8Scale s = f8_scale(m, e5m2, pow2);
-  q = inf ? f8x8<true>(v, s.inv, e5m2) : f8x8<false>(v, s.inv, e5m2);
+  const F8Scale s = f8_scale<E5M2>(m, pow2);
+  q = inf ? f8x8<E5M2, true>(v, s.inv) : f8x8<E5M2, false>(v, s.inv);
   return s;
 }
 
@@ -284,6 +289,34 @@ struct Units {
   }
 };
 
+// 16 bytes of a turned tile: two 8-byte chunks of column `col` from chunk 2 k on (the chunks of a column are XORed with
+// the number of its group of 8).
+__device__ __forceinline__ uint4 turned16(const uint8_t* turned, int col, int k) {
+  const int sw = (col >> 3) & 15;
+  const uint4 v = *reinterpret_cast<const uint4*>(&turned[col * 128 + (((2 * k) ^ (sw & 14)) << 3)]);
+  return (sw & 1) ? make_uint4(v.z, v.w, v.x, v.y) : v;
+}
+// ... written where they exist; the address is 16-byte aligned.
+__device__ __forceinline__ void store_q16(uint8_t* p, int n, uint4 q) {
+  if (n >= 16) {
+    *reinterpret_cast<uint4*>(p) = q;
+  } else {
+    store_q8(p, n, make_uint2(q.x, q.y));
+    if (n > 8) store_q8(p + 8, n - 8, make_uint2(q.z, q.w));
+  }
+}
+// Column c's turned bytes to the transposed matrix: rows r0 + 16 k .. of `rows`, k = the thread's place among 8.
+__device__ __forceinline__ void write_turned(const uint8_t* turned, uint8_t* to, int64_t ld, int64_t r0, int64_t rows,
+                                             int cols, int threads) {
+  const int k = threadIdx.x & 7;
+  const int64_t left = rows - r0 - 16 * k;
+  const int n = left >= 16 ? 16 : (int)left;
+  if (left <= 0) return;
+  uint8_t* p = to + r0 + 16 * k + (int64_t)(threadIdx.x >> 3) * ld;
+  for (int col = threadIdx.x >> 3; col < cols; col += threads >> 3, p += (threads >> 3) * ld)
+    store_q16(p, n, turned16(turned, col, k));
+}
+
 __device__ __forceinline__ int left8(int64_t cols, int64_t c) {
   const int64_t n = cols - c;
   return n >= 8 ? 8 : (n < 0 ? 0 : (int)n);
@@ -292,16 +325,15 @@ __device__ __forceinline__ int left8(int64_t cols, int64_t c) {
 // ---------------------------------------------------------------------------
 // Launch parameters
 // ---------------------------------------------------------------------------
-struct F8Out {  // an 8-bit matrix that a kernel writes (q == NULL: none)
+struct F8Out {  // an 8-bit matrix that a kernel writes (q == NULL: none); its format goes with the launch
   uint8_t* q;
   float* s;
   int64_t ld, lds;
-  int e5m2, tiles;
+  int tiles;
 };
 inline F8Out f8_out(const ds_f8_matrix* m) {
-  if (m == nullptr) return F8Out{nullptr, nullptr, 0, 0, 0, 0};
-  return F8Out{static_cast<uint8_t*>(m->q), m->scale, m->ld, m->ld_scale, m->format == DS_F8_E5M2,
-               m->blocks == DS_F8_TILES};
+  if (m == nullptr) return F8Out{nullptr, nullptr, 0, 0, 0};
+  return F8Out{static_cast<uint8_t*>(m->q), m->scale, m->ld, m->ld_scale, m->blocks == DS_F8_TILES};
 }
 
 struct RmsnormParams {
@@ -314,7 +346,7 @@ struct RmsnormParams {
   void* h;
   int64_t ldh;
   float* rstd;
-  int pow2;
+  int e5m2, pow2;
 };
 struct RmsnormBackwardParams {
   const void *dy, *h, *dh;
@@ -336,17 +368,18 @@ struct LinearF8Params {
 
 constexpr int64_t kF8NormPartials = 608;  // rows of partial weight gradients: 4 CTAs on each of 152 SMs
 
+// e5m2: the format of every matrix that the call writes.
 cudaError_t launch_quantize_f8(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const F8Out& out,
-                               const F8Out& out_t, bool pow2, cudaStream_t st);
-cudaError_t launch_requantize_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool pow2,
+                               const F8Out& out_t, bool e5m2, bool pow2, cudaStream_t st);
+cudaError_t launch_requantize_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool e5m2, bool pow2,
                                  cudaStream_t st);
 cudaError_t launch_expand_f8(const uint8_t* blob, int64_t n_out, int64_t k_red, const F8Out& out, cudaStream_t st);
 cudaError_t launch_rmsnorm_f8(const RmsnormParams& p, int type, cudaStream_t st);
 cudaError_t launch_rmsnorm_f8_backward(const RmsnormBackwardParams& p, int type, cudaStream_t st);
 cudaError_t launch_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_t features, const F8Out& out,
-                            const F8Out& ckpt, bool pow2, cudaStream_t st);
+                            const F8Out& ckpt, bool e5m2, bool pow2, cudaStream_t st);
 cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int type, int64_t ld, int64_t features,
-                                     const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool pow2,
+                                     const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool e5m2, bool pow2,
                                      cudaStream_t st);
 cudaError_t launch_linear_f8(const LinearF8Params& p, cudaStream_t st);
 int read_f8_fault_flag();

@@ -37,7 +37,7 @@ __device__ __forceinline__ float sigmoid(float g) {
 // Two rows of a unit (a block of 128 features) at a time: with the checkpoint six blocks, whose scales six lanes make.
 constexpr int R = 2;
 
-template <typename T>
+template <typename T, bool E5M2>
 __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t ld, bool vec, int64_t rows,
                                                             int64_t features, const F8Out out, const F8Out ckpt,
                                                             bool pow2) {
@@ -85,13 +85,13 @@ __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t
     }
     const int which = sub & 7;  // the block whose scale this lane makes
     const F8Out& to = which < 2 ? out : ckpt;
-    const F8Scale s = f8_scale(mine, to.e5m2, pow2);
+    const F8Scale s = f8_scale<E5M2>(mine, pow2);
     if (sub < (ckpt.q ? 6 : 2) && (which & 1) < m)
       to.s[(r0 + (which & 1)) * to.lds + at.b + (which >= 4 ? nb : 0)] = s.s;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const float inv = of_lane(s.inv, i), inv_g = of_lane(s.inv, 2 + i), inv_u = of_lane(s.inv, 4 + i);
-      const uint2 q = check ? f8x8<true>(a[i], inv, out.e5m2) : f8x8<false>(a[i], inv, out.e5m2);
+      const uint2 q = check ? f8x8<E5M2, true>(a[i], inv) : f8x8<E5M2, false>(a[i], inv);
       if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c, n, q);
       if (ckpt.q && i < m) {
         float g[8], u[8];
@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t
         ru[i].get(u);
         uint8_t* o = ckpt.q + (r0 + i) * ckpt.ld + c;
         // the columns between the halves are zeros
-        *reinterpret_cast<uint2*>(o) = check ? f8x8<true>(g, inv_g, ckpt.e5m2) : f8x8<false>(g, inv_g, ckpt.e5m2);
-        if (n > 0) store_q8(o + up, n, check ? f8x8<true>(u, inv_u, ckpt.e5m2) : f8x8<false>(u, inv_u, ckpt.e5m2));
+        *reinterpret_cast<uint2*>(o) = check ? f8x8<E5M2, true>(g, inv_g) : f8x8<E5M2, false>(g, inv_g);
+        if (n > 0) store_q8(o + up, n, check ? f8x8<E5M2, true>(u, inv_u) : f8x8<E5M2, false>(u, inv_u));
       }
     }
   }
@@ -135,7 +135,7 @@ __device__ __forceinline__ void column_maxima(float (*col_max)[128], const float
 }
 
 // The row form of a patch: m of its rows, n of its columns.
-template <bool CHECK>
+template <bool E5M2, bool CHECK>
 __device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out, int64_t r0, int64_t c0, int64_t block,
                                            int m, int n, bool pow2) {
   const int tc = threadIdx.x & 15;
@@ -143,50 +143,35 @@ __device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out
 #pragma unroll
   for (int i = 0; i < 4; ++i) rm[i] = CHECK ? amax8_finite(v[i]) : amax8(v[i]);
   const float b = lanes_max<4>(rm);  // lane l of 16: row l & 3
-  const F8Scale s = f8_scale(b, out.e5m2, pow2);
+  const F8Scale s = f8_scale<E5M2>(b, pow2);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float inv = of_lane(s.inv, i);
-    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, f8x8<CHECK>(v[i], inv, out.e5m2));
+    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, f8x8<E5M2, CHECK>(v[i], inv));
   }
   if (tc < m && tc < 4) out.s[(r0 + tc) * out.lds + block] = s.s;
 }
 
 // The patch by columns, as bytes, to the turned tile.
-template <bool CHECK>
-__device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv, const float v[4][8], bool e5m2) {
+template <bool E5M2, bool CHECK>
+__device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv, const float v[4][8]) {
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
+  const float4 lo = *reinterpret_cast<const float4*>(&col_inv[tc * 8]);
+  const float4 hi = *reinterpret_cast<const float4*>(&col_inv[tc * 8 + 4]);
+  const float inv[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  uint32_t* to = reinterpret_cast<uint32_t*>(&turned[tc * 8 * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float inv = col_inv[tc * 8 + j];
-    const uint32_t q = f8x4<CHECK>(v[0][j], v[1][j], v[2][j], v[3][j], inv, e5m2);
-    *reinterpret_cast<uint32_t*>(&turned[(tc * 8 + j) * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]) = q;
-  }
-}
-
-// The turned tile to the transposed matrix: columns c_tile .., n of them, rows of block tile_r.
-__device__ __forceinline__ void write_turned(const uint8_t* turned, const F8Out& out, int64_t rows, int64_t tile_r,
-                                             int64_t c_tile, int n) {
-  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
-  const int64_t rr = tile_r * kF8Block + tc * 8;
-  const int nr = left8(rows, rr);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int col = tr + 32 * k;
-    if (col < n && nr > 0)
-      store_q8(out.q + (c_tile + col) * out.ld + rr, nr,
-               *reinterpret_cast<const uint2*>(&turned[col * 128 + ((tc ^ (col >> 3)) << 3)]));
-  }
+  for (int j = 0; j < 8; ++j) to[j * 32] = f8x4<E5M2, CHECK>(v[0][j], v[1][j], v[2][j], v[3][j], inv[j]);
 }
 
 struct GatedIn {
   const uint8_t* q;
   const float* s;
   int64_t ld, lds;
-  bool e5m2;
 };
 
-template <typename T>
+// IN5, E5M2: the formats of the checkpoint and of what is written.
+template <typename T, bool IN5, bool E5M2>
 __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(const GatedIn in, const T* da, int64_t ld,
                                                                             bool vec, int64_t rows, int64_t features,
                                                                             const F8Out dgu, const F8Out dgu_t,
@@ -219,8 +204,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
   for (int i = 0; i < 4; ++i) {
     float d[8], g[8], u[8];
     rd[i].get(d);
-    f8x8_value(qg[i], in.e5m2, g);
-    f8x8_value(qu[i], in.e5m2, u);
+    f8x8_value<IN5>(qg[i], g);
+    f8x8_value<IN5>(qu[i], u);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float gj = g[j] * sg[i], uj = u[j] * su[i];
@@ -239,7 +224,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
     if (which < 3) {
 #pragma unroll
       for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[which][w][c]);
-      const F8Scale s = f8_scale(mx, out.e5m2, pow2);
+      const F8Scale s = f8_scale<E5M2>(mx, pow2);
       sm.col_inv[which][c] = s.inv;
       if (out.q && mx < kInf && (which == 0 || c < cols))
         out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
@@ -254,14 +239,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
   auto emit = [&](auto finite) {
     constexpr bool CHECK = decltype(finite)::value;
     if (dgu.q) {
-      write_rows<CHECK>(dg, dgu, r0, c0, tile_c, m, 8, pow2);
-      write_rows<CHECK>(du, dgu, r0, up + c0, nb + tile_c, m, n, pow2);
+      write_rows<E5M2, CHECK>(dg, dgu, r0, c0, tile_c, m, 8, pow2);
+      write_rows<E5M2, CHECK>(du, dgu, r0, up + c0, nb + tile_c, m, n, pow2);
     }
     if (dgu_t.q) {
-      turn_patch<CHECK>(sm.turned[0], sm.col_inv[0], dg, dgu_t.e5m2);
-      turn_patch<CHECK>(sm.turned[1], sm.col_inv[1], du, dgu_t.e5m2);
+      turn_patch<E5M2, CHECK>(sm.turned[0], sm.col_inv[0], dg);
+      turn_patch<E5M2, CHECK>(sm.turned[1], sm.col_inv[1], du);
     }
-    if (a_t.q) turn_patch<CHECK>(sm.turned[2], sm.col_inv[2], a, a_t.e5m2);
+    if (a_t.q) turn_patch<E5M2, CHECK>(sm.turned[2], sm.col_inv[2], a);
   };
   maxima(std::false_type());
   __syncthreads();
@@ -276,56 +261,66 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
     emit(std::false_type());
   }
   __syncthreads();
+  const int64_t first = tile_r * kF8Block;
   if (dgu_t.q) {
-    write_turned(sm.turned[0], dgu_t, rows, tile_r, c_tile, kF8Block);
-    write_turned(sm.turned[1], dgu_t, rows, tile_r, up + c_tile, cols);
+    write_turned(sm.turned[0], dgu_t.q + c_tile * dgu_t.ld, dgu_t.ld, first, rows, kF8Block, kTileThreads);
+    write_turned(sm.turned[1], dgu_t.q + (up + c_tile) * dgu_t.ld, dgu_t.ld, first, rows, cols, kTileThreads);
   }
-  if (a_t.q) write_turned(sm.turned[2], a_t, rows, tile_r, c_tile, cols);
+  if (a_t.q) write_turned(sm.turned[2], a_t.q + c_tile * a_t.ld, a_t.ld, first, rows, cols, kTileThreads);
 }
 
 template <typename T>
 cudaError_t forward(const void* gu, int64_t ld, int64_t rows, int64_t features, const F8Out& out, const F8Out& ckpt,
-                    bool pow2, cudaStream_t st) {
+                    bool e5m2, bool pow2, cudaStream_t st) {
   const int64_t nb = (features + kF8Block - 1) / kF8Block;
   const int64_t want = ((rows + R - 1) / R * nb + kThreads / 16 - 1) / (kThreads / 16);
   const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * 32;
   const bool vec = (reinterpret_cast<uintptr_t>(gu) & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  gated_f8_kernel<T><<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(static_cast<const T*>(gu), ld, vec,
-                                                                               rows, features, out, ckpt, pow2);
+  auto* kernel = e5m2 ? gated_f8_kernel<T, true> : gated_f8_kernel<T, false>;
+  kernel<<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(static_cast<const T*>(gu), ld, vec, rows, features,
+                                                                   out, ckpt, pow2);
+  return cudaGetLastError();
+}
+
+template <typename T, bool IN5, bool E5M2>
+cudaError_t backward_as(const ds_f8_matrix* ckpt, const void* da, int64_t ld, int64_t features, const F8Out& dgu,
+                        const F8Out& dgu_t, const F8Out& a_t, bool pow2, cudaStream_t st) {
+  const GatedIn in{static_cast<const uint8_t*>(ckpt->q), ckpt->scale, ckpt->ld, ckpt->ld_scale};
+  const int64_t tiles = (ckpt->rows + kF8Block - 1) / kF8Block * ((features + kF8Block - 1) / kF8Block);
+  const bool vec = (reinterpret_cast<uintptr_t>(da) & 15) == 0 && ld * sizeof(T) % 16 == 0;
+  // once per process, thread-safe (function-local static)
+  static const cudaError_t attr =
+      cudaFuncSetAttribute(gated_f8_backward_kernel<T, IN5, E5M2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)sizeof(TileSmem));
+  if (attr != cudaSuccess) return attr;
+  gated_f8_backward_kernel<T, IN5, E5M2><<<(unsigned)tiles, kTileThreads, sizeof(TileSmem), st>>>(
+      in, static_cast<const T*>(da), ld, vec, ckpt->rows, features, dgu, dgu_t, a_t, pow2);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t backward(const ds_f8_matrix* ckpt, const void* da, int64_t ld, int64_t features, const F8Out& dgu,
-                     const F8Out& dgu_t, const F8Out& a_t, bool pow2, cudaStream_t st) {
-  const GatedIn in{static_cast<const uint8_t*>(ckpt->q), ckpt->scale, ckpt->ld, ckpt->ld_scale,
-                   ckpt->format == DS_F8_E5M2};
-  const int64_t tiles = (ckpt->rows + kF8Block - 1) / kF8Block * ((features + kF8Block - 1) / kF8Block);
-  const bool vec = (reinterpret_cast<uintptr_t>(da) & 15) == 0 && ld * sizeof(T) % 16 == 0;
-  // once per process, thread-safe (function-local static)
-  static const cudaError_t attr = cudaFuncSetAttribute(
-      gated_f8_backward_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(TileSmem));
-  if (attr != cudaSuccess) return attr;
-  gated_f8_backward_kernel<T><<<(unsigned)tiles, kTileThreads, sizeof(TileSmem), st>>>(
-      in, static_cast<const T*>(da), ld, vec, ckpt->rows, features, dgu, dgu_t, a_t, pow2);
-  return cudaGetLastError();
+                     const F8Out& dgu_t, const F8Out& a_t, bool e5m2, bool pow2, cudaStream_t st) {
+  auto* run = ckpt->format == DS_F8_E5M2 ? (e5m2 ? backward_as<T, true, true> : backward_as<T, true, false>)
+                                         : (e5m2 ? backward_as<T, false, true> : backward_as<T, false, false>);
+  return run(ckpt, da, ld, features, dgu, dgu_t, a_t, pow2, st);
 }
 
 }  // namespace
 
 cudaError_t launch_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_t features, const F8Out& out,
-                            const F8Out& ckpt, bool pow2, cudaStream_t st) {
-  if (type == DS_TYPE_F32) return forward<float>(gu, ld, rows, features, out, ckpt, pow2, st);
-  if (type == DS_TYPE_BF16) return forward<__nv_bfloat16>(gu, ld, rows, features, out, ckpt, pow2, st);
-  return forward<__half>(gu, ld, rows, features, out, ckpt, pow2, st);
+                            const F8Out& ckpt, bool e5m2, bool pow2, cudaStream_t st) {
+  if (type == DS_TYPE_F32) return forward<float>(gu, ld, rows, features, out, ckpt, e5m2, pow2, st);
+  if (type == DS_TYPE_BF16) return forward<__nv_bfloat16>(gu, ld, rows, features, out, ckpt, e5m2, pow2, st);
+  return forward<__half>(gu, ld, rows, features, out, ckpt, e5m2, pow2, st);
 }
 
 cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int type, int64_t ld, int64_t features,
-                                     const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool pow2,
+                                     const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool e5m2, bool pow2,
                                      cudaStream_t st) {
-  if (type == DS_TYPE_F32) return backward<float>(ckpt, da, ld, features, dgu, dgu_t, a_t, pow2, st);
-  if (type == DS_TYPE_BF16) return backward<__nv_bfloat16>(ckpt, da, ld, features, dgu, dgu_t, a_t, pow2, st);
-  return backward<__half>(ckpt, da, ld, features, dgu, dgu_t, a_t, pow2, st);
+  if (type == DS_TYPE_F32) return backward<float>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
+  if (type == DS_TYPE_BF16) return backward<__nv_bfloat16>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
+  return backward<__half>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
 }
 
 }  // namespace ds

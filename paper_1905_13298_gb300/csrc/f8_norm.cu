@@ -53,7 +53,7 @@ __device__ __forceinline__ void load_sum(const RmsnormParams& P, const Aligned& 
 }
 
 // Scales, rounds and stores eight columns; all 32 lanes call it.
-template <typename T>
+template <typename T, bool E5M2>
 __device__ __forceinline__ void emit(const RmsnormParams& P, const Aligned& al, int64_t r, int64_t c, int n,
                                      const float v[8], float rstd) {
   float w[8], y[8];
@@ -63,7 +63,7 @@ __device__ __forceinline__ void emit(const RmsnormParams& P, const Aligned& al, 
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = v[i] * rstd * w[i];
   uint2 q;
-  const F8Scale s = f8_block(y, P.out.e5m2, P.pow2, q);
+  const F8Scale s = f8_block<E5M2>(y, P.pow2, q);
   if (n > 0) {
     store_q8(P.out.q + r * P.out.ld + c, n, q);
     if ((threadIdx.x & 15) == 0) P.out.s[r * P.out.lds + c / kF8Block] = s.s;
@@ -71,7 +71,7 @@ __device__ __forceinline__ void emit(const RmsnormParams& P, const Aligned& al, 
   }
 }
 
-template <typename T, int NV>
+template <typename T, int NV, bool E5M2>
 __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParams P, const Aligned al) {
   __shared__ float scratch[kWarps];
   const int64_t r = blockIdx.x;
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParam
     for (int k = 0; k < NV; ++k) {
       const int64_t c = ((int64_t)k * kThreads + threadIdx.x) * 8;
       const int n = left8(P.cols, c);
-      emit<T>(P, al, r, n > 0 ? c : 0, n, v[k], rstd);
+      emit<T, E5M2>(P, al, r, n > 0 ? c : 0, n, v[k], rstd);
     }
   } else {
     // h may be stored over an input: a thread reads its columns again before it writes them
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParam
       const int64_t c = base + threadIdx.x * 8;
       const int n = left8(P.cols, c);
       load_sum<T>(P, al, r, n > 0 ? c : 0, n, v[0]);
-      emit<T>(P, al, r, n > 0 ? c : 0, n, v[0], rstd);
+      emit<T, E5M2>(P, al, r, n > 0 ? c : 0, n, v[0], rstd);
     }
   }
 }
@@ -279,20 +279,25 @@ bool rows16(const void* p, int64_t ld, size_t size) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (int64_t)size % 16 == 0;
 }
 
-template <typename T>
-cudaError_t forward(const RmsnormParams& p, cudaStream_t st) {
+template <typename T, bool E5M2>
+cudaError_t forward_as(const RmsnormParams& p, cudaStream_t st) {
   const Aligned al{rows16(p.x, p.ldx, sizeof(T)), rows16(p.residual, p.ldr, sizeof(T)), rows16(p.h, p.ldh, sizeof(T)),
                    rows16(p.weight, 0, 4)};
   const unsigned grid = (unsigned)p.rows;
   if (p.cols <= kThreads * 8)
-    rmsnorm_f8_kernel<T, 1><<<grid, kThreads, 0, st>>>(p, al);
+    rmsnorm_f8_kernel<T, 1, E5M2><<<grid, kThreads, 0, st>>>(p, al);
   else if (p.cols <= 2 * kThreads * 8)
-    rmsnorm_f8_kernel<T, 2><<<grid, kThreads, 0, st>>>(p, al);
+    rmsnorm_f8_kernel<T, 2, E5M2><<<grid, kThreads, 0, st>>>(p, al);
   else if (p.cols <= 4 * kThreads * 8)
-    rmsnorm_f8_kernel<T, 4><<<grid, kThreads, 0, st>>>(p, al);
+    rmsnorm_f8_kernel<T, 4, E5M2><<<grid, kThreads, 0, st>>>(p, al);
   else
-    rmsnorm_f8_kernel<T, 0><<<grid, kThreads, 0, st>>>(p, al);
+    rmsnorm_f8_kernel<T, 0, E5M2><<<grid, kThreads, 0, st>>>(p, al);
   return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t forward(const RmsnormParams& p, cudaStream_t st) {
+  return p.e5m2 ? forward_as<T, true>(p, st) : forward_as<T, false>(p, st);
 }
 
 template <typename T>

@@ -30,33 +30,33 @@ struct SourceFloat {
   }
 };
 // Eight 8-bit values and their scale, decoded where they are used: an eighth of the registers of the values.
+template <bool E5M2>
 struct RawF8 {
   uint2 u;
   float s;
-  bool e5m2;
   __device__ __forceinline__ void get(float v[8]) const {
-    f8x8_value(u, e5m2, v);
+    f8x8_value<E5M2>(u, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= s;
   }
 };
+template <bool E5M2>
 struct SourceF8 {
-  using Raw = RawF8;
+  using Raw = RawF8<E5M2>;
   static constexpr bool PACKED = false;
   const uint8_t* q;
   const float* s;
   int64_t ld, lds;
-  bool e5m2, tiles;
+  bool tiles;
   __device__ __forceinline__ void load(int64_t r, int64_t c, int n, Raw& raw) const {
     raw.u = load_q8(q + r * ld + c, n);
     raw.s = n > 0 ? s[(tiles ? r / kF8Block : r) * lds + c / kF8Block] : 0.f;
-    raw.e5m2 = e5m2;
   }
 };
 
 // Rows alone: 16 lanes hold one block of each of R rows.
 constexpr int R = 4;
-template <typename Source>
+template <typename Source, bool E5M2>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const Source src, int64_t rows, int64_t cols,
                                                                  const F8Out out, bool pow2) {
   const int64_t nb = (cols + kF8Block - 1) / kF8Block, groups = (rows + R - 1) / R;
@@ -88,13 +88,13 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const Source sr
       }
       mx = lanes_max<R>(rm);
     }
-    const F8Scale s = f8_scale(mx, out.e5m2, pow2);
+    const F8Scale s = f8_scale<E5M2>(mx, pow2);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const float inv = of_lane(s.inv, i);
       float v[8];
       raw[i].get(v);
-      const uint2 q = check ? f8x8<true>(v, inv, out.e5m2) : f8x8<false>(v, inv, out.e5m2);
+      const uint2 q = check ? f8x8<E5M2, true>(v, inv) : f8x8<E5M2, false>(v, inv);
       if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c, n, q);
     }
     if (sub < m) out.s[(r0 + sub) * out.lds + at.b] = s.s;
@@ -148,18 +148,18 @@ struct TileAt {
   int m, n;  // rows and columns of the patch that exist
 };
 
-template <typename Raw, bool CHECK>
+template <typename Raw, bool E5M2, bool CHECK>
 __device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, const F8Out& out, const TileAt& t,
                                            float tile_max, bool pow2) {
   const int lane = threadIdx.x & 31, tc = lane & 15;
-  const F8Scale s = f8_scale(out.tiles ? tile_max : row_max, out.e5m2, pow2);  // lane i of 16: row i's
+  const F8Scale s = f8_scale<E5M2>(out.tiles ? tile_max : row_max, pow2);  // lane i of 16: row i's
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float inv = of_lane(s.inv, i);
     float v[8];
     raw[i].get(v);
     if (i < t.m && t.n > 0)
-      store_q8(out.q + (t.r0 + i) * out.ld + t.c0, t.n, f8x8<CHECK>(v, inv, out.e5m2));
+      store_q8(out.q + (t.r0 + i) * out.ld + t.c0, t.n, f8x8<E5M2, CHECK>(v, inv));
   }
   if (!out.tiles) {
     if (tc < t.m && tc < 8) out.s[(t.r0 + tc) * out.lds + t.tile_c] = s.s;
@@ -168,8 +168,8 @@ __device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, c
   }
 }
 
-template <typename Raw, bool CHECK>
-__device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm, const F8Out& out_t) {
+template <typename Raw, bool E5M2, bool CHECK>
+__device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm) {
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
   float inv[8];
 #pragma unroll
@@ -185,7 +185,7 @@ __device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm, 
     raw[i + 1].get(b);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint32_t two = f8x2(f8_unit<CHECK>(a[j], inv[j]), f8_unit<CHECK>(b[j], inv[j]), out_t.e5m2);
+      const uint32_t two = f8x2<E5M2>(f8_unit<CHECK>(a[j], inv[j]), f8_unit<CHECK>(b[j], inv[j]));
       uint32_t& w = i < 4 ? q[j].x : q[j].y;
       w = (i & 2) ? w | (two << 16) : two;
     }
@@ -195,7 +195,7 @@ __device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm, 
     *reinterpret_cast<uint2*>(&sm.turned[(tc * 8 + j) * 128 + ((tr ^ tc) << 3)]) = q[j];
 }
 
-template <typename Source>
+template <typename Source, bool E5M2>
 __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ? 3 : 2)
     quantize_tile_kernel(const Source src, int64_t rows, int64_t cols, const F8Out out, const F8Out out_t, bool pow2) {
   __shared__ __align__(16) TileSmem sm;
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ?
     float m = 0.f;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) m = fmaxf(m, sm.col_max[w][threadIdx.x]);
-    const F8Scale s = f8_scale(out_t.tiles ? tile_max : m, out_t.e5m2, pow2);
+    const F8Scale s = f8_scale<E5M2>(out_t.tiles ? tile_max : m, pow2);
     sm.col_inv[threadIdx.x] = s.inv;
     const int64_t c = t.tile_c * kF8Block + threadIdx.x;
     if (!out_t.tiles) {
@@ -268,51 +268,60 @@ __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ?
   }
   if (out.q) {
     if (check)
-      write_rows<typename Source::Raw, true>(raw, row_max, out, t, tile_max, pow2);
+      write_rows<typename Source::Raw, E5M2, true>(raw, row_max, out, t, tile_max, pow2);
     else
-      write_rows<typename Source::Raw, false>(raw, row_max, out, t, tile_max, pow2);
+      write_rows<typename Source::Raw, E5M2, false>(raw, row_max, out, t, tile_max, pow2);
   }
   if (out_t.q) {
     __syncthreads();
     if (check)
-      turn_columns<typename Source::Raw, true>(raw, sm, out_t);
+      turn_columns<typename Source::Raw, E5M2, true>(raw, sm);
     else
-      turn_columns<typename Source::Raw, false>(raw, sm, out_t);
+      turn_columns<typename Source::Raw, E5M2, false>(raw, sm);
     __syncthreads();
-    // 16 lanes write one 128-byte row of the transposed matrix
-    const int64_t rr = t.tile_r * kF8Block + tc * 8;
-    const int nr = left8(rows, rr);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int col = tr + 16 * k;
-      const int64_t c = t.tile_c * kF8Block + col;
-      if (c < cols && nr > 0)
-        store_q8(out_t.q + c * out_t.ld + rr, nr,
-                 *reinterpret_cast<const uint2*>(&sm.turned[col * 128 + ((tc ^ (col >> 3)) << 3)]));
-    }
+    // 8 lanes write one 128-byte row of the transposed matrix
+    const int64_t left = cols - t.tile_c * kF8Block;
+    write_turned(sm.turned, out_t.q + t.tile_c * kF8Block * out_t.ld, out_t.ld, t.tile_r * kF8Block, rows,
+                 left < kF8Block ? (int)left : kF8Block, kThreads);
   }
 }
 
-template <typename Source>
-cudaError_t run(const Source& src, int64_t rows, int64_t cols, const F8Out& out, const F8Out& out_t, bool pow2,
-                cudaStream_t st) {
+template <typename Source, bool E5M2>
+cudaError_t run_as(const Source& src, int64_t rows, int64_t cols, const F8Out& out, const F8Out& out_t, bool pow2,
+                   cudaStream_t st) {
   const int64_t nb = (cols + kF8Block - 1) / kF8Block;
   if (out_t.q == nullptr && !out.tiles) {
     const int64_t want = ((rows + R - 1) / R * nb + kThreads / 16 - 1) / (kThreads / 16);
     const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * 32;
-    quantize_rows_kernel<<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(src, rows, cols, out, pow2);
+    quantize_rows_kernel<Source, E5M2>
+        <<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(src, rows, cols, out, pow2);
   } else {
     const int64_t tiles = (rows + kF8Block - 1) / kF8Block * nb;
-    quantize_tile_kernel<<<(unsigned)tiles, kThreads, 0, st>>>(src, rows, cols, out, out_t, pow2);
+    quantize_tile_kernel<Source, E5M2><<<(unsigned)tiles, kThreads, 0, st>>>(src, rows, cols, out, out_t, pow2);
   }
   return cudaGetLastError();
 }
 
+template <typename Source>
+cudaError_t run(const Source& src, int64_t rows, int64_t cols, const F8Out& out, const F8Out& out_t, bool e5m2,
+                bool pow2, cudaStream_t st) {
+  return e5m2 ? run_as<Source, true>(src, rows, cols, out, out_t, pow2, st)
+              : run_as<Source, false>(src, rows, cols, out, out_t, pow2, st);
+}
+
 template <typename T>
 cudaError_t run_float(const void* x, int64_t rows, int64_t cols, int64_t ldx, const F8Out& out, const F8Out& out_t,
-                      bool pow2, cudaStream_t st) {
+                      bool e5m2, bool pow2, cudaStream_t st) {
   const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && ldx * sizeof(T) % 16 == 0;
-  return run(SourceFloat<T>{static_cast<const T*>(x), ldx, vec}, rows, cols, out, out_t, pow2, st);
+  return run(SourceFloat<T>{static_cast<const T*>(x), ldx, vec}, rows, cols, out, out_t, e5m2, pow2, st);
+}
+
+template <bool E5M2>
+cudaError_t run_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool e5m2, bool pow2,
+                   cudaStream_t st) {
+  return run(SourceF8<E5M2>{static_cast<const uint8_t*>(in->q), in->scale, in->ld, in->ld_scale,
+                            in->blocks == DS_F8_TILES},
+             in->rows, in->cols, out, out_t, e5m2, pow2, st);
 }
 
 // Shift weights as 8-bit tiles: s * 2^p = (s * 2^(p + 8)) * 2^-8, exact in e4m3 (2^-7, its smallest magnitude here, is a
@@ -333,7 +342,7 @@ __global__ void __launch_bounds__(kThreads) expand_f8_kernel(const uint8_t* __re
       const float mag = __uint_as_float((135u - ((nib >> (4 * i)) & 15u)) << 23);  // 2^(8 + p)
       v[i] = ((b.y >> (j + i)) & 1u) ? (((b.x >> (j + i)) & 1u) ? -mag : mag) : 0.f;
     }
-    const uint32_t q = f8x2(v[0], v[1], false) | (f8x2(v[2], v[3], false) << 16);
+    const uint32_t q = f8x2<false>(v[0], v[1]) | (f8x2<false>(v[2], v[3]) << 16);
     uint8_t* o = out.q + n * out.ld + k;
     if (k + 4 <= k_red) {
       *reinterpret_cast<uint32_t*>(o) = q;
@@ -347,17 +356,16 @@ __global__ void __launch_bounds__(kThreads) expand_f8_kernel(const uint8_t* __re
 }  // namespace
 
 cudaError_t launch_quantize_f8(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const F8Out& out,
-                               const F8Out& out_t, bool pow2, cudaStream_t st) {
-  if (type == DS_TYPE_F32) return run_float<float>(x, rows, cols, ldx, out, out_t, pow2, st);
-  if (type == DS_TYPE_BF16) return run_float<__nv_bfloat16>(x, rows, cols, ldx, out, out_t, pow2, st);
-  return run_float<__half>(x, rows, cols, ldx, out, out_t, pow2, st);
+                               const F8Out& out_t, bool e5m2, bool pow2, cudaStream_t st) {
+  if (type == DS_TYPE_F32) return run_float<float>(x, rows, cols, ldx, out, out_t, e5m2, pow2, st);
+  if (type == DS_TYPE_BF16) return run_float<__nv_bfloat16>(x, rows, cols, ldx, out, out_t, e5m2, pow2, st);
+  return run_float<__half>(x, rows, cols, ldx, out, out_t, e5m2, pow2, st);
 }
 
-cudaError_t launch_requantize_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool pow2,
+cudaError_t launch_requantize_f8(const ds_f8_matrix* in, const F8Out& out, const F8Out& out_t, bool e5m2, bool pow2,
                                  cudaStream_t st) {
-  const SourceF8 src{static_cast<const uint8_t*>(in->q), in->scale, in->ld, in->ld_scale, in->format == DS_F8_E5M2,
-                     in->blocks == DS_F8_TILES};
-  return run(src, in->rows, in->cols, out, out_t, pow2, st);
+  return in->format == DS_F8_E5M2 ? run_f8<true>(in, out, out_t, e5m2, pow2, st)
+                                  : run_f8<false>(in, out, out_t, e5m2, pow2, st);
 }
 
 cudaError_t launch_expand_f8(const uint8_t* blob, int64_t n_out, int64_t k_red, const F8Out& out, cudaStream_t st) {

@@ -266,3 +266,14 @@ def test_helpers_refuse_what_the_abi_cannot_see(ds):
         ds.gated_f8(torch.zeros(4, 400), 200)
     with pytest.raises(ValueError):
         ds.rmsnorm_f8_backward(torch.zeros(4, 256), torch.zeros(4, 255), torch.zeros(4), torch.zeros(256))
+
+
+def test_outputs_of_one_call_have_one_format(ds):
+    L, x = ds.lib(), 1 << 45
+    a, b = _m(ds, 4, 256, 1 << 40), _m(ds, 256, 4, 1 << 41, format=ds.DS_F8_E5M2)
+    assert L.ds_quantize_f8(x, 0, 4, 256, 256, a, b, 0, None) == ds.DS_ERR_INVALID_ARG and "format" in ds.ds_last_error()
+    assert L.ds_requantize_f8(_m(ds, 4, 256, 1 << 42), a, b, 0, None) == ds.DS_ERR_INVALID_ARG
+    out, kept = _m(ds, 4, 200, 1 << 40), _m(ds, 4, 456, 1 << 41, format=ds.DS_F8_E5M2)
+    assert L.ds_gated_f8(x, 0, 456, 4, 200, out, kept, 0, None) == ds.DS_ERR_INVALID_ARG
+    d, d_t = _m(ds, 4, 456, 1 << 46), _m(ds, 456, 4, 1 << 47, format=ds.DS_F8_E5M2)
+    assert L.ds_gated_f8_backward(kept, x, 0, 200, 200, d, d_t, None, 0, None) == ds.DS_ERR_INVALID_ARG
