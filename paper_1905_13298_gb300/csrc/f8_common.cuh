@@ -305,16 +305,21 @@ __device__ __forceinline__ void store_q16(uint8_t* p, int n, uint4 q) {
     if (n > 8) store_q8(p + 8, n - 8, make_uint2(q.z, q.w));
   }
 }
-// Column c's turned bytes to the transposed matrix: rows r0 + 16 k .. of `rows`, k = the thread's place among 8.
+// A turned tile to the transposed matrix: columns 0 .. cols - 1 from `to`, rows r0 .. of `rows`.  FULL: 128 of each.
+template <int THREADS, bool FULL>
 __device__ __forceinline__ void write_turned(const uint8_t* turned, uint8_t* to, int64_t ld, int64_t r0, int64_t rows,
-                                             int cols, int threads) {
-  const int k = threadIdx.x & 7;
+                                             int cols) {
+  const int k = threadIdx.x & 7, first = threadIdx.x >> 3;
   const int64_t left = rows - r0 - 16 * k;
-  const int n = left >= 16 ? 16 : (int)left;
-  if (left <= 0) return;
-  uint8_t* p = to + r0 + 16 * k + (int64_t)(threadIdx.x >> 3) * ld;
-  for (int col = threadIdx.x >> 3; col < cols; col += threads >> 3, p += (threads >> 3) * ld)
-    store_q16(p, n, turned16(turned, col, k));
+  uint8_t* p = to + r0 + 16 * k + first * ld;
+  if (FULL) {
+#pragma unroll
+    for (int i = 0; i < 1024 / THREADS; ++i, p += THREADS / 8 * ld)
+      *reinterpret_cast<uint4*>(p) = turned16(turned, first + THREADS / 8 * i, k);
+  } else if (left > 0) {
+    const int n = left >= 16 ? 16 : (int)left;
+    for (int col = first; col < cols; col += THREADS / 8, p += THREADS / 8 * ld) store_q16(p, n, turned16(turned, col, k));
+  }
 }
 
 __device__ __forceinline__ int left8(int64_t cols, int64_t c) {

@@ -134,7 +134,7 @@ __device__ __forceinline__ void column_maxima(float (*col_max)[128], const float
   *reinterpret_cast<float4*>(&col_max[warp][tc * 8 + (up ? 4 : 0)]) = make_float4(c[0], c[1], c[2], c[3]);
 }
 
-// The row form of a patch: m of its rows, n of its columns.
+// The row form of a patch: m of its rows, n of its columns.  CHECK: the tile is not whole, or holds infinities.
 template <bool E5M2, bool CHECK>
 __device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out, int64_t r0, int64_t c0, int64_t block,
                                            int m, int n, bool pow2) {
@@ -144,10 +144,16 @@ __device__ __forceinline__ void write_rows(const float v[4][8], const F8Out& out
   for (int i = 0; i < 4; ++i) rm[i] = CHECK ? amax8_finite(v[i]) : amax8(v[i]);
   const float b = lanes_max<4>(rm);  // lane l of 16: row l & 3
   const F8Scale s = f8_scale<E5M2>(b, pow2);
+  uint8_t* p = out.q + r0 * out.ld + c0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float inv = of_lane(s.inv, i);
-    if (i < m && n > 0) store_q8(out.q + (r0 + i) * out.ld + c0, n, f8x8<E5M2, CHECK>(v[i], inv));
+    const uint2 q = f8x8<E5M2, CHECK>(v[i], inv);
+    if (!CHECK)
+      *reinterpret_cast<uint2*>(p) = q;
+    else if (i < m && n > 0)
+      store_q8(p, n, q);
+    p += out.ld;
   }
   if (tc < m && tc < 4) out.s[(r0 + tc) * out.lds + block] = s.s;
 }
@@ -216,6 +222,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
     }
   }
   const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);
+  const bool full = cols == kF8Block && (tile_r + 1) * kF8Block <= rows;
   // a column's scale each: of dg, du and a; the gate half's columns go on to the up half with zeros
   const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
   const F8Out& out = which < 2 ? dgu_t : a_t;
@@ -257,16 +264,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(cons
     column_scales();
     __syncthreads();
     emit(std::true_type());
+  } else if (!full) {
+    emit(std::true_type());
   } else {
     emit(std::false_type());
   }
   __syncthreads();
   const int64_t first = tile_r * kF8Block;
-  if (dgu_t.q) {
-    write_turned(sm.turned[0], dgu_t.q + c_tile * dgu_t.ld, dgu_t.ld, first, rows, kF8Block, kTileThreads);
-    write_turned(sm.turned[1], dgu_t.q + (up + c_tile) * dgu_t.ld, dgu_t.ld, first, rows, cols, kTileThreads);
-  }
-  if (a_t.q) write_turned(sm.turned[2], a_t.q + c_tile * a_t.ld, a_t.ld, first, rows, cols, kTileThreads);
+  auto turn = [&](auto whole) {
+    constexpr bool FULL = decltype(whole)::value;
+    if (dgu_t.q) {
+      write_turned<kTileThreads, FULL>(sm.turned[0], dgu_t.q + c_tile * dgu_t.ld, dgu_t.ld, first, rows, kF8Block);
+      write_turned<kTileThreads, FULL>(sm.turned[1], dgu_t.q + (up + c_tile) * dgu_t.ld, dgu_t.ld, first, rows, cols);
+    }
+    if (a_t.q) write_turned<kTileThreads, FULL>(sm.turned[2], a_t.q + c_tile * a_t.ld, a_t.ld, first, rows, cols);
+  };
+  if (full)
+    turn(std::true_type());
+  else
+    turn(std::false_type());
 }
 
 template <typename T>

@@ -148,18 +148,24 @@ struct TileAt {
   int m, n;  // rows and columns of the patch that exist
 };
 
+// CHECK: the tile is not whole, or holds infinities.
 template <typename Raw, bool E5M2, bool CHECK>
 __device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, const F8Out& out, const TileAt& t,
                                            float tile_max, bool pow2) {
   const int lane = threadIdx.x & 31, tc = lane & 15;
   const F8Scale s = f8_scale<E5M2>(out.tiles ? tile_max : row_max, pow2);  // lane i of 16: row i's
+  uint8_t* p = out.q + t.r0 * out.ld + t.c0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float inv = of_lane(s.inv, i);
     float v[8];
     raw[i].get(v);
-    if (i < t.m && t.n > 0)
-      store_q8(out.q + (t.r0 + i) * out.ld + t.c0, t.n, f8x8<E5M2, CHECK>(v, inv));
+    const uint2 q = f8x8<E5M2, CHECK>(v, inv);
+    if (!CHECK)
+      *reinterpret_cast<uint2*>(p) = q;
+    else if (i < t.m && t.n > 0)
+      store_q8(p, t.n, q);
+    p += out.ld;
   }
   if (!out.tiles) {
     if (tc < t.m && tc < 8) out.s[(t.r0 + tc) * out.lds + t.tile_c] = s.s;
@@ -266,8 +272,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ?
       out_t.s[t.tile_c * out_t.lds + t.tile_r] = s.s;
     }
   }
+  // most tiles are whole and hold no infinity: their stores need no conditions
+  const bool full = (t.tile_r + 1) * kF8Block <= rows && (t.tile_c + 1) * kF8Block <= cols;
   if (out.q) {
-    if (check)
+    if (check || !full)
       write_rows<typename Source::Raw, E5M2, true>(raw, row_max, out, t, tile_max, pow2);
     else
       write_rows<typename Source::Raw, E5M2, false>(raw, row_max, out, t, tile_max, pow2);
@@ -281,8 +289,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ?
     __syncthreads();
     // 8 lanes write one 128-byte row of the transposed matrix
     const int64_t left = cols - t.tile_c * kF8Block;
-    write_turned(sm.turned, out_t.q + t.tile_c * kF8Block * out_t.ld, out_t.ld, t.tile_r * kF8Block, rows,
-                 left < kF8Block ? (int)left : kF8Block, kThreads);
+    uint8_t* to = out_t.q + t.tile_c * kF8Block * out_t.ld;
+    if (full)
+      write_turned<kThreads, true>(sm.turned, to, out_t.ld, t.tile_r * kF8Block, rows, kF8Block);
+    else
+      write_turned<kThreads, false>(sm.turned, to, out_t.ld, t.tile_r * kF8Block, rows,
+                                    left < kF8Block ? (int)left : kF8Block);
   }
 }
 
