@@ -611,7 +611,7 @@ ds_status ds_expand_shift_weights_f8(const ds_weights* w, const ds_f8_matrix* ou
 ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* bias, const float* add,
                        int64_t ld_add, void* y, int type, int64_t ldy, void* stream);
 
-/* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8. */
+/* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8 and ds_gated_f8_backward. */
 int ds_f8_fault_flag(void);
 void ds_f8_set_wait_limit(long long cycles);
 

@@ -218,7 +218,10 @@ ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float
   return cuda_check(launch_linear_f8(p, static_cast<cudaStream_t>(stream)), "linear_f8 launch");
 }
 
-int ds_f8_fault_flag(void) { return read_f8_fault_flag(); }
+int ds_f8_fault_flag(void) {
+  const int a = read_f8_fault_flag(), b = read_gated_f8_fault_flag();  // both are read, and so cleared
+  return a < 0 || b < 0 ? -1 : (a | b);
+}
 
 void ds_f8_set_wait_limit(long long cycles) { set_f8_wait_cycles(cycles); }
 

@@ -388,6 +388,8 @@ cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, i
                                      cudaStream_t st);
 cudaError_t launch_linear_f8(const LinearF8Params& p, cudaStream_t st);
 int read_f8_fault_flag();
+int read_gated_f8_fault_flag();
 void set_f8_wait_cycles(long long cycles);
+long long f8_wait_cycles();  // limit of a bounded wait of the next launches
 
 }  // namespace ds

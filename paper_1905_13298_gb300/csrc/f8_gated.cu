@@ -11,14 +11,20 @@
 // the 4 of a bf16 pair, and a is made again rather than kept.
 //
 // The forward pass streams: 16 lanes hold a block of each of g, u and a.  The
-// backward pass holds a 128 x 128 tile per CTA, 4 rows x 8 columns of it per
-// thread, and writes its five 8-bit outputs from registers, so the checkpoint
-// and da are read once.
+// backward pass walks 128 x 128 tiles, one CTA per SM, 4 rows x 8 columns of a
+// tile per thread, and writes its five 8-bit outputs from registers, so the
+// checkpoint and da are read once.  Three results of 16384 float32 fill most of
+// an SM's registers, so no second CTA can hide the first one's reads: TMA
+// brings the next tile to shared memory while this one is rounded and stored.
 #include <type_traits>
 
 #include "f8_common.cuh"
+#include "tensor_core.cuh"
 
 namespace ds {
+
+__device__ int g_gated_fault;  // set when a bounded wait of the backward pass gives up
+
 namespace {
 
 constexpr int kThreads = 256;
@@ -106,11 +112,18 @@ __global__ void __launch_bounds__(kThreads) gated_f8_kernel(const T* gu, int64_t
   }
 }
 
-// Each result has its turned tile and column maxima, so that one pass of barriers serves all three.
+// The tile that TMA brings (rows as they lie in memory), its scales, and the results: each has its turned tile and
+// column maxima, so that one pass of barriers serves all three.
+template <typename T>
 struct TileSmem {
+  T da[128][128];
+  uint8_t g[128][128], u[128][128];
   uint8_t turned[3][128 * 128];
   float col_max[3][kTileWarps][128];
   float col_inv[3][128];
+  float scale[2][2][128];  // of g's and u's rows, of this tile and the next
+  uint64_t full;
+  int abort;
 };
 
 // A 4 x 8 patch of a result, its largest magnitudes by columns (the warp's 8 rows together) to shared memory.
@@ -170,119 +183,158 @@ __device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv
   for (int j = 0; j < 8; ++j) to[j * 32] = f8x4<E5M2, CHECK>(v[0][j], v[1][j], v[2][j], v[3][j], inv[j]);
 }
 
-struct GatedIn {
-  const uint8_t* q;
-  const float* s;
-  int64_t ld, lds;
+template <typename T>
+struct BackwardIn {
+  const float* scale;  // of the checkpoint
+  int64_t lds;
+  const T* da;
+  int64_t ld;
+  bool vec;  // da's rows are aligned for TMA; otherwise a thread reads its own patch
+  int64_t rows, features;
+  long long wait_cycles;
 };
 
 // IN5, E5M2: the formats of the checkpoint and of what is written.
 template <typename T, bool IN5, bool E5M2>
-__global__ void __launch_bounds__(kTileThreads, 1) gated_f8_backward_kernel(const GatedIn in, const T* da, int64_t ld,
-                                                                            bool vec, int64_t rows, int64_t features,
-                                                                            const F8Out dgu, const F8Out dgu_t,
-                                                                            const F8Out a_t, bool pow2) {
-  extern __shared__ __align__(16) unsigned char smem_raw[];
-  TileSmem& sm = *reinterpret_cast<TileSmem*>(smem_raw);
+__global__ void __launch_bounds__(kTileThreads, 1)
+    gated_f8_backward_kernel(const __grid_constant__ CUtensorMap map_ckpt, const __grid_constant__ CUtensorMap map_da,
+                             const BackwardIn<T> B, const F8Out dgu, const F8Out dgu_t, const F8Out a_t, bool pow2) {
+  extern __shared__ __align__(128) unsigned char smem_raw[];
+  TileSmem<T>& sm = *reinterpret_cast<TileSmem<T>*>(smem_raw);
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;
-  const int64_t nb = (features + kF8Block - 1) / kF8Block, up = nb * kF8Block;
-  const int64_t tile_r = blockIdx.x / nb, tile_c = blockIdx.x - tile_r * nb;
-  const int64_t r0 = tile_r * kF8Block + tr * 4, c_tile = tile_c * kF8Block, c0 = c_tile + tc * 8;
-  const int n = left8(features, c0);
-  const int m = rows - r0 >= 4 ? 4 : (rows - r0 < 0 ? 0 : (int)(rows - r0));
-  const int64_t cc = n > 0 ? c0 : 0;
-
-  Raw8<T> rd[4];
-  uint2 qg[4], qu[4];
-  float sg[4], su[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t r = i < m ? r0 + i : 0;
-    const int ni = i < m ? n : 0;
-    rd[i].load(da + r * ld + cc, ni, vec);
-    qg[i] = load_q8(in.q + r * in.ld + cc, ni);
-    qu[i] = load_q8(in.q + r * in.ld + up + cc, ni);
-    sg[i] = ni > 0 ? in.s[r * in.lds + tile_c] : 0.f;
-    su[i] = ni > 0 ? in.s[r * in.lds + nb + tile_c] : 0.f;
+  const int64_t rows = B.rows, features = B.features;
+  const uint32_t nb = (uint32_t)((features + kF8Block - 1) / kF8Block);
+  const uint32_t tiles = (uint32_t)((rows + kF8Block - 1) / kF8Block) * nb;
+  const int64_t up = (int64_t)nb * kF8Block;
+  // one thread: the copies of tile t
+  auto bring = [&](uint32_t t) {
+    const uint32_t r = t / nb, c = t - r * nb;
+    mbar_expect_tx(&sm.full, sizeof(sm.g) + sizeof(sm.u) + (B.vec ? sizeof(sm.da) : 0));
+    tma_load_2d(sm.g, &map_ckpt, &sm.full, (int)(c * kF8Block), (int)(r * kF8Block));
+    tma_load_2d(sm.u, &map_ckpt, &sm.full, (int)(up + c * kF8Block), (int)(r * kF8Block));
+    if (B.vec) tma_load_2d(sm.da, &map_da, &sm.full, (int)(c * kF8Block), (int)(r * kF8Block));
+  };
+  // threads 0 .. 255: the scale of row (thread % 128) of g or u in tile t
+  auto scale_of = [&](uint32_t t) {
+    const uint32_t tile_r = t / nb, tile_c = t - tile_r * nb;
+    const int64_t r = (int64_t)tile_r * kF8Block + (threadIdx.x & 127);
+    return r < rows ? B.scale[r * B.lds + tile_c + (threadIdx.x >= 128 ? nb : 0)] : 0.f;
+  };
+  if (threadIdx.x == 0) {
+    mbar_init(&sm.full, 1);
+    sm.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    bring(blockIdx.x);
   }
-  float dg[4][8], du[4][8], a[4][8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float d[8], g[8], u[8];
-    rd[i].get(d);
-    f8x8_value<IN5>(qg[i], g);
-    f8x8_value<IN5>(qu[i], u);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gj = g[j] * sg[i], uj = u[j] * su[i];
-      const float sig = sigmoid(gj), act = gj * sig;
-      a[i][j] = act * uj;
-      du[i][j] = d[j] * act;
-      dg[i][j] = d[j] * uj * fmaf(act, 1.f - sig, sig);  // sig (1 + g (1 - sig))
-    }
-  }
-  const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);
-  const bool full = cols == kF8Block && (tile_r + 1) * kF8Block <= rows;
-  // a column's scale each: of dg, du and a; the gate half's columns go on to the up half with zeros
-  const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
-  const F8Out& out = which < 2 ? dgu_t : a_t;
-  auto column_scales = [&] {
-    float mx = 0.f;
-    if (which < 3) {
-#pragma unroll
-      for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[which][w][c]);
-      const F8Scale s = f8_scale<E5M2>(mx, pow2);
-      sm.col_inv[which][c] = s.inv;
-      if (out.q && mx < kInf && (which == 0 || c < cols))
-        out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
-    }
-    return mx;
-  };
-  auto maxima = [&](auto finite) {
-    column_maxima<decltype(finite)::value>(sm.col_max[0], dg);
-    column_maxima<decltype(finite)::value>(sm.col_max[1], du);
-    column_maxima<decltype(finite)::value>(sm.col_max[2], a);
-  };
-  auto emit = [&](auto finite) {
-    constexpr bool CHECK = decltype(finite)::value;
-    if (dgu.q) {
-      write_rows<E5M2, CHECK>(dg, dgu, r0, c0, tile_c, m, 8, pow2);
-      write_rows<E5M2, CHECK>(du, dgu, r0, up + c0, nb + tile_c, m, n, pow2);
-    }
-    if (dgu_t.q) {
-      turn_patch<E5M2, CHECK>(sm.turned[0], sm.col_inv[0], dg);
-      turn_patch<E5M2, CHECK>(sm.turned[1], sm.col_inv[1], du);
-    }
-    if (a_t.q) turn_patch<E5M2, CHECK>(sm.turned[2], sm.col_inv[2], a);
-  };
-  maxima(std::false_type());
+  if (threadIdx.x < 256) sm.scale[0][threadIdx.x >> 7][threadIdx.x & 127] = scale_of(blockIdx.x);
   __syncthreads();
-  // an infinity anywhere is some column's largest magnitude
-  if (__syncthreads_or(!(column_scales() < kInf))) {
-    maxima(std::true_type());
-    __syncthreads();
-    column_scales();
-    __syncthreads();
-    emit(std::true_type());
-  } else if (!full) {
-    emit(std::true_type());
-  } else {
-    emit(std::false_type());
-  }
-  __syncthreads();
-  const int64_t first = tile_r * kF8Block;
-  auto turn = [&](auto whole) {
-    constexpr bool FULL = decltype(whole)::value;
-    if (dgu_t.q) {
-      write_turned<kTileThreads, FULL>(sm.turned[0], dgu_t.q + c_tile * dgu_t.ld, dgu_t.ld, first, rows, kF8Block);
-      write_turned<kTileThreads, FULL>(sm.turned[1], dgu_t.q + (up + c_tile) * dgu_t.ld, dgu_t.ld, first, rows, cols);
+  uint32_t turn = 0;
+  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1u) {
+    const uint32_t tile_r = tile / nb, tile_c = tile - tile_r * nb;
+    const int64_t r0 = (int64_t)tile_r * kF8Block + tr * 4, c_tile = (int64_t)tile_c * kF8Block, c0 = c_tile + tc * 8;
+    const int n = left8(features, c0);
+    const int m = rows - r0 >= 4 ? 4 : (rows - r0 < 0 ? 0 : (int)(rows - r0));
+    const bool more = tile + gridDim.x < tiles;
+    float next_scale = 0.f;
+    if (more && threadIdx.x < 256) next_scale = scale_of(tile + gridDim.x);
+    const bool ok = mbar_wait(&sm.full, turn, &sm.abort, B.wait_cycles, &g_gated_fault);
+    float dg[4][8], du[4][8], a[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float d[8], g[8], u[8];
+      const int row = tr * 4 + i;
+      Raw8<T> rd;
+      if (B.vec)
+        rd.load(&sm.da[row][tc * 8], 8, true);
+      else
+        rd.load(B.da + (i < m ? r0 + i : 0) * B.ld + (n > 0 ? c0 : 0), i < m ? n : 0, false);
+      rd.get(d);
+      f8x8_value<IN5>(*reinterpret_cast<const uint2*>(&sm.g[row][tc * 8]), g);
+      f8x8_value<IN5>(*reinterpret_cast<const uint2*>(&sm.u[row][tc * 8]), u);
+      if (n < 8) {  // what lies between the halves is not read
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = j < n ? g[j] : 0.f;
+      }
+      const float sg = sm.scale[turn][0][row], su = sm.scale[turn][1][row];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float gj = g[j] * sg, uj = u[j] * su;
+        const float sig = sigmoid(gj), act = gj * sig;
+        a[i][j] = act * uj;
+        du[i][j] = d[j] * act;
+        dg[i][j] = d[j] * uj * fmaf(act, 1.f - sig, sig);  // sig (1 + g (1 - sig))
+      }
     }
-    if (a_t.q) write_turned<kTileThreads, FULL>(sm.turned[2], a_t.q + c_tile * a_t.ld, a_t.ld, first, rows, cols);
-  };
-  if (full)
-    turn(std::true_type());
-  else
-    turn(std::false_type());
+    const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);
+    const bool full = cols == kF8Block && (int64_t)(tile_r + 1) * kF8Block <= rows;
+    // a column's scale each: of dg, du and a; the gate half's columns go on to the up half with zeros
+    const int which = threadIdx.x >> 7, c = threadIdx.x & 127;
+    const F8Out& out = which < 2 ? dgu_t : a_t;
+    auto column_scales = [&] {
+      float mx = 0.f;
+      if (which < 3) {
+#pragma unroll
+        for (int w = 0; w < kTileWarps; ++w) mx = fmaxf(mx, sm.col_max[which][w][c]);
+        const F8Scale s = f8_scale<E5M2>(mx, pow2);
+        sm.col_inv[which][c] = s.inv;
+        if (out.q && mx < kInf && (which == 0 || c < cols))
+          out.s[((which == 1 ? up : 0) + c_tile + c) * out.lds + tile_r] = s.s;
+      }
+      return mx;
+    };
+    auto maxima = [&](auto finite) {
+      column_maxima<decltype(finite)::value>(sm.col_max[0], dg);
+      column_maxima<decltype(finite)::value>(sm.col_max[1], du);
+      column_maxima<decltype(finite)::value>(sm.col_max[2], a);
+    };
+    auto emit = [&](auto finite) {
+      constexpr bool CHECK = decltype(finite)::value;
+      if (dgu.q) {
+        write_rows<E5M2, CHECK>(dg, dgu, r0, c0, tile_c, m, 8, pow2);
+        write_rows<E5M2, CHECK>(du, dgu, r0, up + c0, nb + tile_c, m, n, pow2);
+      }
+      if (dgu_t.q) {
+        turn_patch<E5M2, CHECK>(sm.turned[0], sm.col_inv[0], dg);
+        turn_patch<E5M2, CHECK>(sm.turned[1], sm.col_inv[1], du);
+      }
+      if (a_t.q) turn_patch<E5M2, CHECK>(sm.turned[2], sm.col_inv[2], a);
+    };
+    maxima(std::false_type());
+    if (__syncthreads_or(!ok)) {
+      if (threadIdx.x == 0) mbar_drain(&sm.full, turn);  // the copies land before the CTA leaves
+      break;
+    }
+    // the tile is in registers: the next one may come
+    if (more && threadIdx.x == 0) bring(tile + gridDim.x);
+    if (more && threadIdx.x < 256) sm.scale[turn ^ 1u][threadIdx.x >> 7][threadIdx.x & 127] = next_scale;
+    // an infinity anywhere is some column's largest magnitude
+    if (__syncthreads_or(!(column_scales() < kInf))) {
+      maxima(std::true_type());
+      __syncthreads();
+      column_scales();
+      __syncthreads();
+      emit(std::true_type());
+    } else if (!full) {
+      emit(std::true_type());
+    } else {
+      emit(std::false_type());
+    }
+    __syncthreads();
+    const int64_t first = (int64_t)tile_r * kF8Block;
+    auto write = [&](auto whole) {
+      constexpr bool FULL = decltype(whole)::value;
+      if (dgu_t.q) {
+        write_turned<kTileThreads, FULL>(sm.turned[0], dgu_t.q + c_tile * dgu_t.ld, dgu_t.ld, first, rows, kF8Block);
+        write_turned<kTileThreads, FULL>(sm.turned[1], dgu_t.q + (up + c_tile) * dgu_t.ld, dgu_t.ld, first, rows, cols);
+      }
+      if (a_t.q) write_turned<kTileThreads, FULL>(sm.turned[2], a_t.q + c_tile * a_t.ld, a_t.ld, first, rows, cols);
+    };
+    if (full)
+      write(std::true_type());
+    else
+      write(std::false_type());
+    // the next tile's maxima are written before a barrier, its turned tiles after two: nobody still reads these
+  }
 }
 
 template <typename T>
@@ -301,16 +353,27 @@ cudaError_t forward(const void* gu, int64_t ld, int64_t rows, int64_t features, 
 template <typename T, bool IN5, bool E5M2>
 cudaError_t backward_as(const ds_f8_matrix* ckpt, const void* da, int64_t ld, int64_t features, const F8Out& dgu,
                         const F8Out& dgu_t, const F8Out& a_t, bool pow2, cudaStream_t st) {
-  const GatedIn in{static_cast<const uint8_t*>(ckpt->q), ckpt->scale, ckpt->ld, ckpt->ld_scale};
   const int64_t tiles = (ckpt->rows + kF8Block - 1) / kF8Block * ((features + kF8Block - 1) / kF8Block);
   const bool vec = (reinterpret_cast<uintptr_t>(da) & 15) == 0 && ld * sizeof(T) % 16 == 0;
   // once per process, thread-safe (function-local static)
   static const cudaError_t attr =
       cudaFuncSetAttribute(gated_f8_backward_kernel<T, IN5, E5M2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)sizeof(TileSmem));
+                           (int)sizeof(TileSmem<T>));
   if (attr != cudaSuccess) return attr;
-  gated_f8_backward_kernel<T, IN5, E5M2><<<(unsigned)tiles, kTileThreads, sizeof(TileSmem), st>>>(
-      in, static_cast<const T*>(da), ld, vec, ckpt->rows, features, dgu, dgu_t, a_t, pow2);
+  const CUtensorMapDataType type = std::is_same<T, float>::value    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                                    : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  CUtensorMap map_ckpt, map_da = {};
+  if (!make_map_2d(&map_ckpt, CU_TENSOR_MAP_DATA_TYPE_UINT8, ckpt->q, ckpt->cols, ckpt->rows, ckpt->ld, kF8Block,
+                   kF8Block, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      (vec && !make_map_2d(&map_da, type, da, features, ckpt->rows, ld * (int64_t)sizeof(T), kF8Block, kF8Block,
+                           CU_TENSOR_MAP_SWIZZLE_NONE)))
+    return cudaErrorInvalidValue;
+  const BackwardIn<T> in{ckpt->scale, ckpt->ld_scale, static_cast<const T*>(da), ld, vec, ckpt->rows, features,
+                         f8_wait_cycles()};
+  const int64_t sms = sm_count() > 0 ? sm_count() : 1;
+  gated_f8_backward_kernel<T, IN5, E5M2><<<(unsigned)(tiles < sms ? tiles : sms), kTileThreads, sizeof(TileSmem<T>),
+                                           st>>>(map_ckpt, map_da, in, dgu, dgu_t, a_t, pow2);
   return cudaGetLastError();
 }
 
@@ -337,6 +400,14 @@ cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, i
   if (type == DS_TYPE_F32) return backward<float>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
   if (type == DS_TYPE_BF16) return backward<__nv_bfloat16>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
   return backward<__half>(ckpt, da, ld, features, dgu, dgu_t, a_t, e5m2, pow2, st);
+}
+
+int read_gated_f8_fault_flag() {
+  int v = 0;
+  if (cudaMemcpyFromSymbol(&v, g_gated_fault, sizeof(int)) != cudaSuccess) return -1;
+  const int zero = 0;
+  if (v != 0 && cudaMemcpyToSymbol(g_gated_fault, &zero, sizeof(int)) != cudaSuccess) return -1;
+  return v;
 }
 
 }  // namespace ds

@@ -889,7 +889,7 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   p.sectors = p.vec && reinterpret_cast<uintptr_t>(l.y) % 32 == 0 && l.ldy * (int64_t)size % 32 == 0;
   p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
              reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;
-  p.wait_cycles = g_wait_cycles.load(std::memory_order_relaxed);
+  p.wait_cycles = f8_wait_cycles();
   const Plan plan = plan_of(p);
   CUtensorMap mw = {}, mx = {};  // an empty reduction loads nothing
   if (p.nk > 0 && (!make_map(&mw, l.w, plan.bn ? ROWS : BIG_N) || !make_map(&mx, l.x, plan.bn ? plan.bn : ROWS)))
@@ -908,6 +908,8 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
 void set_f8_wait_cycles(long long cycles) {
   g_wait_cycles.store(cycles > 0 ? cycles : kTimeoutCycles, std::memory_order_relaxed);
 }
+
+long long f8_wait_cycles() { return g_wait_cycles.load(std::memory_order_relaxed); }
 
 int read_f8_fault_flag() {
   int v = 0;

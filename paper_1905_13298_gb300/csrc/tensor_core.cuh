@@ -112,9 +112,11 @@ inline PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
   return fn;
 }
 
-// A row-major matrix read in boxes of 128 bytes (box_inner elements) x box_outer rows, 128-byte swizzled.
+// A row-major matrix read in boxes of box_inner elements x box_outer rows (128 bytes x box_outer where they are 128-byte
+// swizzled); what lies outside the matrix reads as zeros.
 inline bool make_map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* ptr, int64_t inner, int64_t outer,
-                        int64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer) {
+                        int64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer,
+                        CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   PFN_cuTensorMapEncodeTiled_v12000 enc = get_encode();
   if (enc == nullptr) return false;
   cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
@@ -122,7 +124,7 @@ inline bool make_map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* 
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t estr[2] = {1, 1};
   return enc(map, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

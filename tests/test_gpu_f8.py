@@ -510,6 +510,56 @@ def test_gate_gradient_against_differences(dslib):
     assert np.all(np.abs(_np(d.q) * each - slope) <= F.rounding_bound(slope, each) * (1 + TOL) + 2 * TOL * np.abs(da).max() * 8)
 
 
+def test_gate_backward_with_the_shortest_wait_limit(dslib):
+    """With the wait limit cut to one cycle a launch whose copies are not there yet gives up and sets the flag (one whose
+    copies are there need not wait, and is correct); the context stays usable and the next call is correct."""
+    ds = dslib
+    r = torch.Generator(device="cuda").manual_seed(4)
+    kept, _ = ds.quantize_f8(torch.randn((4096, 4096), generator=r, device="cuda"))
+    da = torch.randn((4096, 2048), generator=r, device="cuda")
+    want = ds.gated_f8_backward(kept, da)
+    equal = lambda got: all(torch.equal(m.q.float(), n.q.float()) and torch.equal(m.scale, n.scale) for m, n in zip(got, want))
+    assert ds.ds_f8_fault_flag() == 0
+    try:
+        ds.ds_f8_set_wait_limit(1)
+        got = ds.gated_f8_backward(kept, da)
+        torch.cuda.synchronize()
+    finally:
+        ds.ds_f8_set_wait_limit(0)
+    assert ds.ds_f8_fault_flag() == 1 or equal(got)
+    assert ds.ds_f8_fault_flag() == 0
+    assert equal(ds.gated_f8_backward(kept, da)) and ds.ds_f8_fault_flag() == 0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_gate_backward_many_tiles_by_every_path(dslib, kind):
+    """More tiles than SMs, ragged edges; rows of da that TMA can and cannot read, and a tile with an infinity."""
+    r = torch.Generator(device="cuda").manual_seed(5)
+    rows, features = 2100, 2000
+    up = F.blocks(features) * 128
+    kept, _ = dslib.quantize_f8(torch.randn((rows, up + features), generator=r, device="cuda"))
+    da = torch.randn((rows, features), generator=r, device="cuda").to(TYPES[kind])
+    first = dslib.gated_f8_backward(kept, da)
+    for extra in (8, 1):
+        again = dslib.gated_f8_backward(kept, _strided(da, extra))
+        for m, n in zip(first, again):
+            assert torch.equal(m.q.float(), n.q.float()) and torch.equal(m.scale, n.scale)
+    for sample in (slice(0, 128), slice(1920, 2048), slice(2048, 2100)):  # rows of these blocks as if alone
+        part = dslib.F8Matrix(kept.q[sample], kept.scale[sample])
+        d, d_t, a_t = dslib.gated_f8_backward(part, da[sample])
+        assert torch.equal(d.q.float(), first[0].q[sample].float()) and torch.equal(d.scale, first[0].scale[sample])
+        for m, n in zip((d_t, a_t), first[1:]):
+            assert torch.equal(m.q.float(), n.q[:, sample].float())
+            assert torch.equal(m.scale[:, 0], n.scale[:, sample.start // 128])
+    da[1500, 1000] = float("inf")
+    d, d_t, _ = dslib.gated_f8_backward(kept, da)
+    assert d.q[1500, 1000].isnan() and d_t.q[1000, 1500].isnan() and d.scale.isfinite().all()
+    hit = torch.zeros((rows, up + features), dtype=torch.bool, device="cuda")
+    hit[1500, 1000] = hit[1500, up + 1000] = True
+    same = d.q.float() == first[0].q.float()
+    assert (same | hit | (torch.arange(rows, device="cuda")[:, None] == 1500)).all()
+
+
 def test_gate_without_rows(dslib):
     a, kept = dslib.gated_f8(torch.empty((0, 456), device="cuda"), 200)
     assert a.q.shape == (0, 200) and kept.q.shape == (0, 456)
