@@ -21,7 +21,8 @@ constexpr int kThreads = 256;
 template <typename T>
 struct SourceFloat {
   using Raw = Raw8<T>;
-  static constexpr bool PACKED = sizeof(T) == 2;  // 16-bit values: maxima of their bits, two at a time
+  static constexpr bool PACKED = sizeof(T) == 2;    // 16-bit values: maxima of their bits, two at a time
+  static constexpr int CTAS = sizeof(T) == 2 ? 4 : 2;  // that the registers of a tile's patches let share an SM
   const T* p;
   int64_t ld;
   bool vec;
@@ -44,6 +45,7 @@ template <bool E5M2>
 struct SourceF8 {
   using Raw = RawF8<E5M2>;
   static constexpr bool PACKED = false;
+  static constexpr int CTAS = 3;
   const uint8_t* q;
   const float* s;
   int64_t ld, lds;
@@ -202,7 +204,7 @@ __device__ __forceinline__ void turn_columns(const Raw (&raw)[8], TileSmem& sm) 
 }
 
 template <typename Source, bool E5M2>
-__global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, Source::CTAS)
     quantize_tile_kernel(const Source src, int64_t rows, int64_t cols, const F8Out out, const F8Out out_t, bool pow2) {
   __shared__ __align__(16) TileSmem sm;
   const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15, warp = threadIdx.x >> 5;
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(typename Source::Raw) <= 16 ?
       c[j] = fmaxf(up ? cm[j + 4] : cm[j], __shfl_xor_sync(0xFFFFFFFFu, up ? cm[j] : cm[j + 4], 16));
     *reinterpret_cast<float4*>(&sm.col_max[warp][tc * 8 + (up ? 4 : 0)]) = make_float4(c[0], c[1], c[2], c[3]);
   }
-  const float row_max = lanes_max<8>(rm);  // lane l of 16: row l & 7
+  const float row_max = out.q || out_t.tiles ? lanes_max<8>(rm) : 0.f;  // lane l of 16: row l & 7
   float tile_max = 0.f;
   if (out.tiles || out_t.tiles) {
     float m = row_max;

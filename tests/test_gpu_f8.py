@@ -599,3 +599,46 @@ def test_outputs_stay_inside_their_rows(dslib, rows, cols):
         assert (q[0] == 0xA5).all() and (q[-1] == 0xA5).all() and (q[1:-1, c:] == 0xA5).all()
         assert (s[0] == -7).all() and (s[-1] == -7).all() and (s[1:-1, F.blocks(c):] == -7).all()
         assert (s[1:-1, :F.blocks(c)] != -7).all()
+
+
+# ---------------------------------------------------------------------------------------------------- the block
+
+def test_feed_forward_block_against_float64(dslib):
+    """Outputs and gradients of the 8-bit block against the float64 block with the same weights.  A value rounded to
+    e4m3 is off by at most 2^-4 of itself, 2^-4 / sqrt(3) = 3.6% in the mean; at most six such roundings stand between
+    the inputs and a gradient, so its 2-norm is off by sqrt(6) 3.6% = 9%, and the bound is a little more."""
+    from paper_1905_13298_gb300.feed_forward import GatedFeedForward
+    r = torch.Generator(device="cuda").manual_seed(6)
+    T, H, Fe = 384, 256, 200
+    b = GatedFeedForward(H, Fe, seed=7)
+    x, s, dy, dh = (torch.randn((T, H), generator=r, device="cuda").to(torch.bfloat16) for _ in range(4))
+    y, h, saved = b.forward(x, s)
+    dx, grads = b.backward(dy, dh, saved)
+    xd, sd = (t.double().requires_grad_() for t in (x, s))
+    norm = b.norm.double().requires_grad_()
+    gate = b.gate_up[:Fe].double().requires_grad_()
+    up = b.gate_up[b.up_at:].double().requires_grad_()
+    down = b.down.double().requires_grad_()
+    hd = xd + sd
+    n = hd * (hd.square().mean(1, keepdim=True) + 1e-5).rsqrt() * norm
+    yd = (torch.nn.functional.silu(n @ gate.t()) * (n @ up.t())) @ down.t()
+    ((yd * dy.double()).sum() + (hd * dh.double()).sum()).backward()
+    rel = lambda a, want: float((a.double() - want.detach()).norm() / want.detach().norm())
+    assert rel(y, yd) < 0.12 and rel(h, hd) < 2.0**-8
+    assert rel(dx, xd.grad) < 0.12
+    assert rel(grads["norm"], norm.grad) < 0.12 and rel(grads["down"], down.grad) < 0.12
+    assert rel(grads["gate_up"][:Fe], gate.grad) < 0.12 and rel(grads["gate_up"][b.up_at:], up.grad) < 0.12
+    assert not grads["gate_up"][Fe : b.up_at].any()
+    again = {k: v.clone() for k, v in grads.items()}
+    b.backward(dy, dh, saved, again)  # a second micro-batch adds to the sums
+    for k, v in again.items():
+        assert rel(v, 2 * grads[k].double()) < 1e-6
+    t, ht = b.token(x[:3], s[:3])
+    assert torch.equal(ht, h[:3]) and rel(t, y[:3].double()) < 2.0**-7  # another kernel, another order of sums
+
+
+def test_feed_forward_example_learns(dslib, capsys):
+    from paper_1905_13298_gb300 import feed_forward
+    losses = feed_forward.main(["--tokens", "512", "--hidden", "256", "--features", "384", "--steps", "12", "--shift"])
+    assert losses[-1] < 0.9 * losses[0]
+    assert "one token" in capsys.readouterr().out
