@@ -538,8 +538,9 @@ void ds_specialized_destroy(ds_specialized* h);
  *
  * Writing a block: with amax the largest finite magnitude in it and MAX the
  * largest value of the format (448, 57344),
- *   scale = max(amax / MAX, 2^-126), rounded up to a power of two with
- *   DS_F8_POW2;  q = value * (1 / scale) rounded to nearest, ties to even.
+ *   scale = max(amax / MAX, 2^-126),  q = value * min(MAX / amax, 2^126)
+ * (each a float32 operation) rounded to nearest, ties to even; with DS_F8_POW2
+ * the scale is rounded up to a power of two and q = value / scale.
  * Infinities and NaN become the 8-bit NaN.  With DS_F8_POW2 q * scale needs no
  * rounding in float32, and changing the blocks of such a matrix later changes
  * only values that fall below the format's range.

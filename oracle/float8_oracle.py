@@ -68,11 +68,15 @@ def spread(s, rows, cols, tiles):
 def quantize(x, tiles=False, pow2=False, fmt="e4m3"):
     """(q values, scales) of a float32 matrix: the float32 steps of the conversion's definition."""
     x = np.asarray(x, dtype=np.float32)
-    s = np.maximum(amax(x, tiles) / np.float32(MAX[fmt]), np.float32(2.0**-126)).astype(np.float32)
+    most = amax(x, tiles)
+    s = np.maximum(most / np.float32(MAX[fmt]), np.float32(2.0**-126)).astype(np.float32)
     if pow2:
         m, e = np.frexp(s.astype(np.float64))
         s = np.ldexp(1.0, np.where(m == 0.5, e - 1, e)).astype(np.float32)
-    inv = (np.float32(1) / s).astype(np.float32)
+        inv = (np.float32(1) / s).astype(np.float32)
+    else:
+        with np.errstate(divide="ignore", over="ignore"):
+            inv = np.minimum(np.float32(MAX[fmt]) / most, np.float32(2.0**126)).astype(np.float32)
     with np.errstate(invalid="ignore", over="ignore"):
         u = (x * spread(inv, *x.shape, tiles)).astype(np.float32)
     return round8(np.where(np.isfinite(x), u, np.nan), fmt), s

@@ -3,11 +3,11 @@
 // to 8 bits.
 //
 // A block of 128 values (one row, or 128 x 128 for a tile) is held as
-//     q = round8(v * (1 / s)),   s = max(amax / MAX, 2^-126),
+//     q = round8(v * min(MAX / amax, 2^126)),   s = max(amax / MAX, 2^-126),
 // amax its largest finite magnitude and MAX the format's largest value (448
 // for e4m3, 57344 for e5m2); with DS_F8_POW2 s is rounded up to a power of
-// two, so that q * s is exact in the source's type range and a later change of
-// blocks rounds nothing but values that leave the format's range.  A
+// two and q = round8(v / s), so that a later change of blocks rounds nothing
+// but values that leave the format's range.  A
 // non-finite value becomes the 8-bit NaN, and does not enter the scale.
 #pragma once
 
@@ -167,11 +167,16 @@ struct F8Scale {
 };
 template <bool E5M2>
 __device__ __forceinline__ F8Scale f8_scale(float amax, bool pow2) {
-  float s = fmaxf(__fdiv_rn(amax, E5M2 ? 57344.f : 448.f), 1.17549435e-38f);
-  if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
-  return F8Scale{s, __frcp_rn(s)};
+  constexpr float kMax = E5M2 ? 57344.f : 448.f;
+  float s = fmaxf(__fdiv_rn(amax, kMax), 1.17549435e-38f);
+  if (pow2) {
+    s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
+    return F8Scale{s, __frcp_rn(s)};
+  }
+  // not 1 / s: one rounding instead of two
+  return F8Scale{s, fminf(__fdiv_rn(kMax, amax), 8.50705917e37f)};
 }
-// Values by 1 / s.  CHECK: the values may hold infinities, which have to become NaN and not the largest value (v * 0 is
+// Values in units of the scale.  CHECK: the values may hold infinities, which have to become NaN and not the largest value (v * 0 is
 // NaN for them and 0 otherwise); NaN stays NaN by itself.
 template <bool CHECK>
 __device__ __forceinline__ float f8_unit(float v, float inv) {

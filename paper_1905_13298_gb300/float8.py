@@ -14,7 +14,7 @@ A training step of a gated feed-forward block reads::
     da = linear_f8(d, w_down_t)
     dgu, dgu_t, a_t = gated_f8_backward(kept, da)
     grad_down = linear_f8(d_t, a_t, add=grad_down, out=grad_down, dtype=torch.float32)
-    n_t = quantize_f8(n, None, "rows")[1]
+    n_t = quantize_f8(n, None, "tiles")[1]
     grad_gu = linear_f8(dgu_t, n_t, add=grad_gu, out=grad_gu, dtype=torch.float32)
     dx, grad_norm = rmsnorm_f8_backward(linear_f8(dgu, w_gu_t), h, rstd, norm_w, dh=dy)
 """
