@@ -494,18 +494,31 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // lanes) by 256 rows of w (the columns).  Warp 0 loads, warp 1 multiplies block
 // after block into two accumulators of 256 columns in turn, and eight warps
 // read each block back and add it, scaled, to the tile's sums: 128 float32 per
-// thread.  Warps 2 and 3 write a block's scales to shared memory as part of
+// thread.  Further warps write a block's scales to shared memory as part of
 // its stage (the stage's barrier counts them with the copies), so the warps
 // that add wait for one barrier per block.
 //
 // A block's products take 512 cycles; what the adding warps do for it has to
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
 // shared memory 40: a second barrier per block for the scales made it 1100.
+// Measured at 8192 x 4096 x 4096: 140 us (1.96 PFLOP/s) with a scale per 128
+// rows of w, 207 us (1.33) with one per row, where the adding warps' two
+// multiplications and the reads of the columns' scales are what takes long
+// (203 us without those reads).
 // ---------------------------------------------------------------------------
 constexpr int BIG_N = 256, BIG_STAGES = 4, BIG_ACC = 2;
 constexpr int kBigEpiWarps = 8;
 constexpr int kBigCols = BIG_N / (kBigEpiWarps / 4);  // columns of a tile that a warp adds up
-constexpr int kBigThreads = 32 * (4 + kBigEpiWarps);
+// Warps for scales: with a scale per row of w two of them kept up with a block per 2400 cycles only (239 us at 8192 x
+// 4096 x 4096), six keep up with the adding warps; two suffice for the 130 scales of the other case and leave more
+// registers.  All threads are launched with the mean of the registers that the adding warps and the others then take.
+template <bool COLS>
+struct BigCfg {
+  static constexpr int SCALE_WARPS = COLS ? 6 : 2, OTHERS = 2 + SCALE_WARPS;
+  static constexpr int THREADS = 32 * (OTHERS + kBigEpiWarps);
+  static constexpr int REGS = COLS ? 208 : 216, REGS_OTHERS = COLS ? 48 : 72;
+  static_assert(OTHERS * REGS_OTHERS + kBigEpiWarps * REGS <= (65536 / THREADS / 8 * 8) * (THREADS / 32), "registers");
+};
 // Slots of the scales' ring.  A slot of the data ring is free when the products of the block 4 before are done, which
 // needed the accumulator of the block 6 before, whose readers were done with the block 7 before: so a slot of the
 // scales' ring may be written again 8 blocks later without a wait of its own.
@@ -544,9 +557,10 @@ struct TileOrder {
 
 // COLS: w has a scale per row, so the columns of a tile differ; otherwise a warp's 128 columns share one.
 template <bool COLS>
-__global__ void __launch_bounds__(kBigThreads, 1)
+__global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
     linear_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
                          const Params P, const TileOrder tiles) {
+  using Cfg = BigCfg<COLS>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -558,7 +572,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < BIG_STAGES; ++s) {
-      mbar_init(&sh->full[s], 3);  // the copies, and two warps with scales
+      mbar_init(&sh->full[s], 1 + Cfg::SCALE_WARPS);  // the copies, and the warps with scales
       mbar_init(&sh->mult[s], 1);
     }
     for (int b = 0; b < BIG_ACC; ++b) mbar_init(&sh->tempty[b], kBigEpiWarps);
@@ -577,9 +591,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = sh->tmem_base;
 
-  // 384 threads are launched with 168 registers each; 4 warps keep 72 and 8 warps take 216: 4 * 72 + 8 * 216 = 12 * 168
-  if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  if (warp < Cfg::OTHERS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Cfg::REGS_OTHERS));
     if (warp == 0 && lane == 0) {
       // A slot's first use waits for the phase before the first one, which a fresh barrier reports as complete.
       Ring<BIG_STAGES> st;
@@ -628,9 +641,10 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       umma_commit(&sh->done);
       mbar_drain(&sh->done, 0u);
     } else if (warp >= 2) {
-      // Scales: thread j holds rows j, j + 64 of x and j, .. j + 192 of w (one of each 128 where they share), of GROUP
-      // blocks at a time; the next group is on its way while this one is written.
-      constexpr int PER = COLS ? 6 : 3, GROUP = COLS ? 2 : 4;
+      // Scales: thread j holds rows j, j + SPAN .. of the tile's 128 rows of x and 256 of w (or the 2 scales that these
+      // share), of four blocks at a time; the next four are on their way while these are written.
+      constexpr int SPAN = 32 * Cfg::SCALE_WARPS, USED = COLS ? kScaleRows : ROWS + 2, GROUP = 4;
+      constexpr int PER = (USED + SPAN - 1) / SPAN;
       const int j = threadIdx.x - 64;
       ScaleFeed<PER, GROUP> feed;
       auto point = [&](uint32_t t) {  // at the scales of a tile's rows
@@ -638,16 +652,13 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         tiles.at(t, m0, n0);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
+          const int r = j + SPAN * i;
+          const int64_t m = m0 + r, n = n0 + (COLS ? r - ROWS : (r - ROWS) * 128);
           feed.src[i] = nullptr;
-          if (i < 2) {
-            const int64_t m = m0 + j + 64 * i;
+          if (r < ROWS) {
             if (m < P.M) feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld;
-          } else if (COLS) {
-            const int64_t n = n0 + j + 64 * (i - 2);
-            if (n < P.N) feed.src[i] = P.w.s + n * P.w.ld;
-          } else {
-            const int64_t n = n0 + 128 * j;
-            if (j < 2 && n < P.N) feed.src[i] = P.w.s + (n >> 7) * P.w.ld;
+          } else if ((COLS || r < ROWS + 2) && n < P.N) {
+            feed.src[i] = P.w.s + (COLS ? n : n >> 7) * P.w.ld;
           }
         }
       };
@@ -678,7 +689,7 @@ __global__ void __launch_bounds__(kBigThreads, 1)
             float* to = sh->scale[it % kScaleSlots] + j;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-              if (i < 2 || COLS || j < 2) to[64 * i] = v[i][b];
+              if (USED % SPAN == 0 || j + SPAN * i < USED) to[SPAN * i] = v[i][b];
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->full[st.slot]);
             st.next();
@@ -688,62 +699,57 @@ __global__ void __launch_bounds__(kBigThreads, 1)
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const int q = warp & 3, e = warp - 4, col0 = (e >> 2) * kBigCols;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Cfg::REGS));
+    const int q = warp & 3, e = warp - Cfg::OTHERS, col0 = (e >> 2) * kBigCols;
     const uint32_t tmem = tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)col0;
     Ring<BIG_STAGES> st;
     Ring<BIG_ACC> ac;
     uint32_t it = 0;
     bool ok = true;
+    auto wait_block = [&] {
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait(&sh->mult[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault));
+      st.next();
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      return ok;
+    };
+    auto release = [&] {  // the block is in registers: the accumulator may be written again
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
+      ac.next();
+    };
     for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
       float acc[kBigCols];
 #pragma unroll
       for (int j = 0; j < kBigCols; ++j) acc[j] = 0.f;
       for (int i = 0; i < nk; ++i, ++it) {
-        ok = __all_sync(0xFFFFFFFFu,
-                        mbar_wait(&sh->mult[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault));
-        if (!ok) break;
-        st.next();
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (!wait_block()) break;
         const uint32_t taddr = tmem + ac.slot * BIG_N;
         const float* scale = sh->scale[it % kScaleSlots];
         const float* col = scale + ROWS + col0;
-        auto release = [&] {  // the block is in registers: the accumulator may be written again
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
-          ac.next();
-        };
-        if constexpr (COLS) {
-          const float s = scale[32 * q + lane];
-          const uint64_t row2 = pair(__float_as_uint(s), __float_as_uint(s));
+        const float s = COLS ? scale[32 * q + lane] : scale[32 * q + lane] * scale[ROWS + col0 / 128];
+        uint32_t r[2][16];
+        tmem_ld16(taddr, r[0]);
 #pragma unroll
-          for (int c = 0; c < kBigCols / 16; ++c) {
-            uint32_t v[16];
-            tmem_ld16(taddr + 16 * c, v);
-            tmem_wait_ld();
-            if (c == kBigCols / 16 - 1) release();
+        for (int c = 0; c < kBigCols / 16; ++c) {
+          tmem_wait_ld();
+          if (c < kBigCols / 16 - 1)
+            tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
+          else
+            release();
+          const uint32_t* v = r[c & 1];
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
+          for (int j = 0; j < 16; j += 4) {
+            float* o = &acc[16 * c + j];
+            if constexpr (COLS) {
+              // two multiplications per value: in pairs they take 20% less time (one per value does not gain from it)
               const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(&col[16 * c + j]);
-              float* o = &acc[16 * c + j];
-              unpair(fma2(mul2(pair(v[j], v[j + 1]), row2), f.x, pair(o[0], o[1])), o[0], o[1]);
-              unpair(fma2(mul2(pair(v[j + 2], v[j + 3]), row2), f.y, pair(o[2], o[3])), o[2], o[3]);
+              unpair(fma2(mul2(pair(v[j], v[j + 1]), pair(s, s)), f.x, pair(o[0], o[1])), o[0], o[1]);
+              unpair(fma2(mul2(pair(v[j + 2], v[j + 3]), pair(s, s)), f.y, pair(o[2], o[3])), o[2], o[3]);
+            } else {
+#pragma unroll
+              for (int l = 0; l < 4; ++l) o[l] = fmaf(__uint_as_float(v[j + l]), s, o[l]);
             }
-          }
-        } else {
-          const float s = scale[32 * q + lane] * scale[ROWS + col0 / 128];
-          uint32_t r[2][16];
-          tmem_ld16(taddr, r[0]);
-#pragma unroll
-          for (int c = 0; c < kBigCols / 16; ++c) {
-            tmem_wait_ld();
-            if (c < kBigCols / 16 - 1)
-              tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
-            else
-              release();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(r[c & 1][j]), s, acc[16 * c + j]);
           }
         }
       }
@@ -753,8 +759,8 @@ __global__ void __launch_bounds__(kBigThreads, 1)
         if (m0 + 32 * q + lane < P.M) store_row<kBigCols>(P, m0 + 32 * q + lane, n0 + col0, acc);
         continue;
       }
-      // Rows that are not aligned, and the last columns: 16 rows x 16 columns at a time through shared memory, so that
-      // neighbouring threads write neighbouring columns.
+      // Rows that are not aligned, and the last columns: 16 rows x 16 columns at a time through shared memory, so
+      // that neighbouring threads write neighbouring columns.
       float* out = sh->out[e];
 #pragma unroll
       for (int c = 0; c < kBigCols / 16; ++c) {
@@ -798,7 +804,7 @@ cudaError_t launch_big(const CUtensorMap& mx, const CUtensorMap& mw, const Param
   const uint32_t sms = sm_count() > 0 ? sm_count() : 1, grid = t.tiles_m * t.tiles_n < sms ? t.tiles_m * t.tiles_n : sms;
   t.G = (grid + t.tiles_n - 1) / t.tiles_n;  // about one wave of tiles per group
   if (t.G > t.tiles_m) t.G = t.tiles_m;
-  linear_f8_big_kernel<COLS><<<grid, kBigThreads, kBigSmem, st>>>(mx, mw, p, t);
+  linear_f8_big_kernel<COLS><<<grid, BigCfg<COLS>::THREADS, kBigSmem, st>>>(mx, mw, p, t);
   return cudaGetLastError();
 }
 
@@ -832,7 +838,7 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
 
 // Which kernel: a product's time is about its waves of CTAs times what one CTA takes.  Measured on one GB300 (bf16
 // results; N 512 .. 8192, K 512 .. 8192, M 1 .. 4096), in microseconds: a CTA of the small kernel takes 3 + 0.30, 0.32,
-// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.95 with a scale per row
+// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.85 with a scale per row
 // of w).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for
 // 27 / 32 of the CTAs that would fit one by one, 24 / 32 where an SM holds one CTA.
 struct Plan {
@@ -854,7 +860,7 @@ Plan plan_of(const Params& p) {
     }
   }
   const int64_t big = (p.M + ROWS - 1) / ROWS * ((p.N + BIG_N - 1) / BIG_N);
-  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.95) * p.nk < time) best.bn = 0;
+  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.85) * p.nk < time) best.bn = 0;
   return best;
 }
 
