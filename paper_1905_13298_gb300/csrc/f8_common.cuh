@@ -176,8 +176,8 @@ __device__ __forceinline__ F8Scale f8_scale(float amax, bool pow2) {
   // not 1 / s: one rounding instead of two
   return F8Scale{s, fminf(__fdiv_rn(kMax, amax), 8.50705917e37f)};
 }
-// Values in units of the scale.  CHECK: the values may hold infinities, which have to become NaN and not the largest value (v * 0 is
-// NaN for them and 0 otherwise); NaN stays NaN by itself.
+// Values in units of the scale.  CHECK: the values may hold infinities, which have to become NaN and not the largest
+// value (v * 0 is NaN for them and 0 otherwise); NaN stays NaN by itself.
 template <bool CHECK>
 __device__ __forceinline__ float f8_unit(float v, float inv) {
   return CHECK ? fmaf(v, 0.f, v * inv) : v * inv;
@@ -323,7 +323,8 @@ __device__ __forceinline__ void write_turned(const uint8_t* turned, uint8_t* to,
       *reinterpret_cast<uint4*>(p) = turned16(turned, first + THREADS / 8 * i, k);
   } else if (left > 0) {
     const int n = left >= 16 ? 16 : (int)left;
-    for (int col = first; col < cols; col += THREADS / 8, p += THREADS / 8 * ld) store_q16(p, n, turned16(turned, col, k));
+    for (int col = first; col < cols; col += THREADS / 8, p += THREADS / 8 * ld)
+      store_q16(p, n, turned16(turned, col, k));
   }
 }
 

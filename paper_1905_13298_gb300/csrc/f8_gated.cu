@@ -46,9 +46,9 @@ __device__ __forceinline__ float sigmoid(float g) {
 constexpr int R = 2;
 
 template <typename T, bool E5M2>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6) gated_f8_kernel(const T* gu, int64_t ld, bool vec, int64_t rows,
-                                                            int64_t features, const F8Out out, const F8Out ckpt,
-                                                            bool pow2) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6)
+    gated_f8_kernel(const T* gu, int64_t ld, bool vec, int64_t rows, int64_t features, const F8Out out, const F8Out ckpt,
+                    bool pow2) {
   const int64_t nb = (features + kF8Block - 1) / kF8Block, up = nb * kF8Block, groups = (rows + R - 1) / R;
   const int sub = threadIdx.x & 15;
   Units at(((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 4, (int64_t)gridDim.x * (kThreads / 16), nb);

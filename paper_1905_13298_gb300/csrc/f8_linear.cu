@@ -67,6 +67,18 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t r[16]) {
       : "r"(addr)
       : "memory");
 }
+// 16 lanes x 64 columns: of each 8 columns thread 4 a + b holds columns 2 b and 2 b + 1 of lane a, then of lane a + 8.
+__device__ __forceinline__ void tmem_ld_fragment(uint32_t addr, uint32_t r[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+      "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Pairs of float32 in one 64-bit register: two multiplications per instruction.
@@ -145,7 +157,8 @@ __device__ __forceinline__ void finish4(const Params& P, int64_t m, int64_t n, f
       *reinterpret_cast<float4*>(static_cast<float*>(P.y) + at) = make_float4(o[0], o[1], o[2], o[3]);
     else if (P.type == DS_TYPE_BF16)
       *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.y) + at) =
-          make_uint2(pack2(o[0], o[1], (const __nv_bfloat16*)nullptr), pack2(o[2], o[3], (const __nv_bfloat16*)nullptr));
+          make_uint2(pack2(o[0], o[1], (const __nv_bfloat16*)nullptr),
+                     pack2(o[2], o[3], (const __nv_bfloat16*)nullptr));
     else
       *reinterpret_cast<uint2*>(static_cast<__half*>(P.y) + at) =
           make_uint2(pack2(o[0], o[1], (const __half*)nullptr), pack2(o[2], o[3], (const __half*)nullptr));
@@ -202,6 +215,98 @@ __device__ __forceinline__ void store_row(const Params& P, int64_t m, int64_t n,
 #pragma unroll
       for (int l = 0; l < 8; ++l) w[l] = pack2(v[j + 2 * l], v[j + 2 * l + 1], (const __half*)nullptr);
       store_sector(y + j, w);
+    }
+  }
+}
+
+// Thread 4 a + b holds values 2 b, 2 b + 1 of four groups of 8 (v[2 g + i]); afterwards it holds the whole group b.
+__device__ __forceinline__ void turn_quad(float v[8]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int bit = 1; bit <= 2; bit *= 2) {
+    const bool up = lane & bit;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g & bit) continue;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float &lo = v[2 * g + i], &hi = v[2 * (g | bit) + i];
+        const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? lo : hi, bit);
+        if (up)
+          lo = got;
+        else
+          hi = got;
+      }
+    }
+  }
+}
+// The sums of 32 rows from m, 128 columns from n, as tmem_ld_fragment spreads them: acc[64 c + 32 h + 4 g + 2 e + i] is
+// row 16 h + 8 e + lane / 4, column 64 c + 8 g + 2 (lane % 4) + i.  Turned so that a thread has 8 columns of
+// a row (stores of the pairs as they come took 6 us of a tile).
+__device__ __forceinline__ void store_fragments(const Params& P, int64_t m, int64_t n, const float acc[128]) {
+  const int lane = threadIdx.x & 31;
+  m += lane >> 2;
+  n += 8 * (lane & 3);
+#pragma unroll
+  for (int c = 0; c < 4; ++c, n += 32) {
+    float o[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        o[r][j] = acc[64 * (c >> 1) + 32 * (r >> 1) + 16 * (c & 1) + 4 * (j >> 1) + 2 * (r & 1) + (j & 1)];
+      turn_quad(o[r]);
+    }
+    if (!P.sectors || n + 8 > P.N) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; j += 4)
+          if (m + 8 * r < P.M && n + j < P.N)
+            finish4(P, m + 8 * r, n + j, make_float4(o[r][j], o[r][j + 1], o[r][j + 2], o[r][j + 3]));
+      continue;
+    }
+    if (P.bias) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float b = P.bias[n + j];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r][j] += b;
+      }
+    }
+    if (P.add) {  // four rows are loaded before any of them is stored
+      float4 f[4][2] = {};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (m + 8 * r >= P.M) continue;
+        const float4* a = reinterpret_cast<const float4*>(P.add + (m + 8 * r) * P.ld_add + n);
+        f[r][0] = a[0], f[r][1] = a[1];
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+          const float4 u = f[r][j / 4];
+          o[r][j] += u.x, o[r][j + 1] += u.y, o[r][j + 2] += u.z, o[r][j + 3] += u.w;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (m + 8 * r >= P.M) continue;
+      const int64_t at = (m + 8 * r) * P.ldy + n;
+      if (P.type == DS_TYPE_F32) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(o[r][j]);
+        store_sector(static_cast<float*>(P.y) + at, w);
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = P.type == DS_TYPE_BF16 ? pack2(o[r][2 * j], o[r][2 * j + 1], (const __nv_bfloat16*)nullptr)
+                                        : pack2(o[r][2 * j], o[r][2 * j + 1], (const __half*)nullptr);
+        *reinterpret_cast<uint4*>(static_cast<__half*>(P.y) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
   }
 }
@@ -291,8 +396,8 @@ constexpr size_t smem_bytes() {
   return (size_t)Cfg<BN>::STAGES * (ROWS + BN) * BK + sizeof(Shared<BN>) + 1024;
 }
 
-// One tile: 128 rows of w (n0 ..), BN rows of x (m0 ..).  blockIdx.x = tile * split + rank in the cluster; the rank takes
-// the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2 and 3
+// One tile: 128 rows of w (n0 ..), BN rows of x (m0 ..).  blockIdx.x = tile * split + rank in the cluster; the rank
+// takes the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2 and 3
 // bring scales (as in the large kernel below), warps 4-7 add.
 template <int BN>
 __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(const __grid_constant__ CUtensorMap tmap_w,
@@ -480,7 +585,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
     const uint32_t at = part_addr + (uint32_t)(c * ROWS + r4) * 4;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s = 0; s < split; ++s) {
-      const float4 u = split > 1 ? ld_cluster4(map_rank(at, s)) : *reinterpret_cast<const float4*>(&part[c * ROWS + r4]);
+      const float4 u =
+          split > 1 ? ld_cluster4(map_rank(at, s)) : *reinterpret_cast<const float4*>(&part[c * ROWS + r4]);
       v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
     }
     finish4(P, m0 + c, n0 + r4, v);
@@ -502,9 +608,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
 // shared memory 40: a second barrier per block for the scales made it 1100.
 // Measured at 8192 x 4096 x 4096: 140 us (1.96 PFLOP/s) with a scale per 128
-// rows of w, 207 us (1.33) with one per row, where the adding warps' two
-// multiplications and the reads of the columns' scales are what takes long
-// (203 us without those reads).
+// rows of w, 185 us (1.49) with one per row, where the adding warps multiply
+// twice and the scales' loads compete with them for the path to shared memory
+// (169 us without these loads, 139 with a scale per 128 rows in their place).
 // ---------------------------------------------------------------------------
 constexpr int BIG_N = 256, BIG_STAGES = 4, BIG_ACC = 2;
 constexpr int kBigEpiWarps = 8;
@@ -525,7 +631,7 @@ struct BigCfg {
 constexpr int kScaleSlots = 8;
 static_assert(kScaleSlots > BIG_STAGES + BIG_ACC, "scales in use");
 constexpr int kScaleRows = ROWS + BIG_N;
-constexpr int kStagePitch = 20;  // floats between the rows of a warp's 16 x 16 output patch: conflict-free 16-byte accesses
+constexpr int kStagePitch = 20;  // floats between the rows of a warp's 16 x 16 output patch: no bank conflicts
 
 struct __align__(16) BigShared {
   float out[kBigEpiWarps][16 * kStagePitch];
@@ -726,35 +832,56 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
         if (!wait_block()) break;
         const uint32_t taddr = tmem + ac.slot * BIG_N;
         const float* scale = sh->scale[it % kScaleSlots];
-        const float* col = scale + ROWS + col0;
-        const float s = COLS ? scale[32 * q + lane] : scale[32 * q + lane] * scale[ROWS + col0 / 128];
-        uint32_t r[2][16];
-        tmem_ld16(taddr, r[0]);
+        if constexpr (COLS) {
+          // Fragments of 16 rows x 64 columns: a thread has 32 of the warp's columns, so that a warp reads a quarter of
+          // the scales that it would with all 128 (a read of shared memory returns 128 bytes a cycle, also where all
+          // threads read the same; those of 128 columns took 1000 cycles of an SM).
+          const float* row = scale + 32 * q + (lane >> 2);
+          const float* col = scale + ROWS + col0 + 2 * (lane & 3);
+          uint64_t row2[4], col2[8];
 #pragma unroll
-        for (int c = 0; c < kBigCols / 16; ++c) {
-          tmem_wait_ld();
-          if (c < kBigCols / 16 - 1)
-            tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
-          else
-            release();
-          const uint32_t* v = r[c & 1];
+          for (int i = 0; i < 4; ++i) row2[i] = pair(row[8 * i], row[8 * i]);
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            float* o = &acc[16 * c + j];
-            if constexpr (COLS) {
+          for (int c = 0; c < kBigCols / 64; ++c) {
+#pragma unroll
+            for (int g = 0; g < 8; ++g) col2[g] = *reinterpret_cast<const uint64_t*>(&col[64 * c + 8 * g]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // rows 16 h ..
+              uint32_t v[32];
+              tmem_ld_fragment(taddr + 64 * c + ((uint32_t)h << 20), v);
+              tmem_wait_ld();
+              if (c == kBigCols / 64 - 1 && h == 1) release();
               // two multiplications per value: in pairs they take 20% less time (one per value does not gain from it)
-              const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(&col[16 * c + j]);
-              unpair(fma2(mul2(pair(v[j], v[j + 1]), pair(s, s)), f.x, pair(o[0], o[1])), o[0], o[1]);
-              unpair(fma2(mul2(pair(v[j + 2], v[j + 3]), pair(s, s)), f.y, pair(o[2], o[3])), o[2], o[3]);
-            } else {
 #pragma unroll
-              for (int l = 0; l < 4; ++l) o[l] = fmaf(__uint_as_float(v[j + l]), s, o[l]);
+              for (int j = 0; j < 32; j += 2) {
+                float* o = &acc[64 * c + 32 * h + j];
+                const uint64_t scaled = mul2(pair(v[j], v[j + 1]), row2[2 * h + (j / 2) % 2]);
+                unpair(fma2(scaled, col2[j / 4], pair(o[0], o[1])), o[0], o[1]);
+              }
             }
+          }
+        } else {
+          const float s = scale[32 * q + lane] * scale[ROWS + col0 / 128];
+          uint32_t r[2][16];
+          tmem_ld16(taddr, r[0]);
+#pragma unroll
+          for (int c = 0; c < kBigCols / 16; ++c) {
+            tmem_wait_ld();
+            if (c < kBigCols / 16 - 1)
+              tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
+            else
+              release();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(r[c & 1][j]), s, acc[16 * c + j]);
           }
         }
       }
       int m0, n0;
       tiles.at(t, m0, n0);
+      if constexpr (COLS) {
+        store_fragments(P, m0 + 32 * q, n0 + col0, acc);
+        continue;
+      }
       if (P.sectors && n0 + col0 + kBigCols <= P.N) {
         if (m0 + 32 * q + lane < P.M) store_row<kBigCols>(P, m0 + 32 * q + lane, n0 + col0, acc);
         continue;
@@ -801,7 +928,7 @@ cudaError_t launch_big(const CUtensorMap& mx, const CUtensorMap& mw, const Param
       cudaFuncSetAttribute(linear_f8_big_kernel<COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem);
   if (attr != cudaSuccess) return attr;
   TileOrder t{(uint32_t)((p.M + ROWS - 1) / ROWS), (uint32_t)((p.N + BIG_N - 1) / BIG_N), 1};
-  const uint32_t sms = sm_count() > 0 ? sm_count() : 1, grid = t.tiles_m * t.tiles_n < sms ? t.tiles_m * t.tiles_n : sms;
+  const uint32_t sms = sm_count() > 0 ? sm_count() : 1, count = t.tiles_m * t.tiles_n, grid = count < sms ? count : sms;
   t.G = (grid + t.tiles_n - 1) / t.tiles_n;  // about one wave of tiles per group
   if (t.G > t.tiles_m) t.G = t.tiles_m;
   linear_f8_big_kernel<COLS><<<grid, BigCfg<COLS>::THREADS, kBigSmem, st>>>(mx, mw, p, t);
@@ -838,7 +965,7 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
 
 // Which kernel: a product's time is about its waves of CTAs times what one CTA takes.  Measured on one GB300 (bf16
 // results; N 512 .. 8192, K 512 .. 8192, M 1 .. 4096), in microseconds: a CTA of the small kernel takes 3 + 0.30, 0.32,
-// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.85 with a scale per row
+// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.72 with a scale per row
 // of w).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for
 // 27 / 32 of the CTAs that would fit one by one, 24 / 32 where an SM holds one CTA.
 struct Plan {
@@ -860,7 +987,7 @@ Plan plan_of(const Params& p) {
     }
   }
   const int64_t big = (p.M + ROWS - 1) / ROWS * ((p.N + BIG_N - 1) / BIG_N);
-  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.85) * p.nk < time) best.bn = 0;
+  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.72) * p.nk < time) best.bn = 0;
   return best;
 }
 

@@ -306,7 +306,8 @@ cudaError_t backward(const RmsnormBackwardParams& p, cudaStream_t st) {
                    rows16(p.dx, p.lddx, sizeof(T))};
   const int nv = p.cols <= kThreads * 8 ? 1 : (p.cols <= 2 * kThreads * 8 ? 2 : (p.cols <= 4 * kThreads * 8 ? 4 : 0));
   // the CTAs that fit at once (of the 152 SMs; fewer SMs take them in turn), each with a partial row of dw
-  const int64_t fit = kF8NormPartials / 4 * (nv == 0 ? 4 : (nv == 1 ? (sizeof(T) == 2 ? 3 : 2) : (nv == 2 && sizeof(T) == 2 ? 2 : 1)));
+  const int of_sm = nv == 0 ? 4 : (nv == 1 ? (sizeof(T) == 2 ? 3 : 2) : (nv == 2 && sizeof(T) == 2 ? 2 : 1));
+  const int64_t fit = kF8NormPartials / 4 * of_sm;
   const int64_t n = p.rows < fit ? p.rows : fit;
   if (n > 0) {
     const unsigned grid = (unsigned)n;
