@@ -116,8 +116,7 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(addr)
-               : "memory");
+               : "r"(addr));  // stays behind the cluster's barrier, which is volatile too
   return v;
 }
 
@@ -374,10 +373,6 @@ template <>
 struct Cfg<64> {
   static constexpr int STAGES = 4, ACC = 4, CTAS = 2;
 };
-template <>
-struct Cfg<128> {
-  static constexpr int STAGES = 5, ACC = 4, CTAS = 1;
-};
 
 template <int BN>
 struct __align__(16) Shared {
@@ -397,8 +392,8 @@ constexpr size_t smem_bytes() {
 }
 
 // One tile: 128 rows of w (n0 ..), BN rows of x (m0 ..).  blockIdx.x = tile * split + rank in the cluster; the rank
-// takes the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2 and 3
-// bring scales (as in the large kernel below), warps 4-7 add.
+// takes the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2
+// and 3 bring scales (as in the large kernel below), warps 4-7 add.
 template <int BN>
 __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(const __grid_constant__ CUtensorMap tmap_w,
                                                              const __grid_constant__ CUtensorMap tmap_x,
@@ -583,12 +578,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
     const int c = i / (ROWS / 4), r4 = (i % (ROWS / 4)) * 4;
     if (m0 + c >= P.M || n0 + r4 >= P.N) continue;
     const uint32_t at = part_addr + (uint32_t)(c * ROWS + r4) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < split; ++s) {
-      const float4 u =
-          split > 1 ? ld_cluster4(map_rank(at, s)) : *reinterpret_cast<const float4*>(&part[c * ROWS + r4]);
-      v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
-    }
+    float4 u[8];  // all on their way before the first is added
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (s < split)
+        u[s] = split > 1 ? ld_cluster4(map_rank(at, s)) : *reinterpret_cast<const float4*>(&part[c * ROWS + r4]);
+    float4 v = u[0];
+#pragma unroll
+    for (int s = 1; s < 8; ++s)
+      if (s < split) v.x += u[s].x, v.y += u[s].y, v.z += u[s].z, v.w += u[s].w;
     finish4(P, m0 + c, n0 + r4, v);
   }
   __syncwarp();
@@ -963,31 +961,39 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
   return cudaLaunchKernelEx(&cfg, linear_f8_kernel<BN>, mw, mx, p, split);
 }
 
-// Which kernel: a product's time is about its waves of CTAs times what one CTA takes.  Measured on one GB300 (bf16
-// results; N 512 .. 8192, K 512 .. 8192, M 1 .. 4096), in microseconds: a CTA of the small kernel takes 3 + 0.30, 0.32,
-// 0.38 or 0.63 a block for BN = 16, 32, 64, 128; one of the large kernel 5 + 0.56 a block (0.72 with a scale per row
-// of w).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for
-// 27 / 32 of the CTAs that would fit one by one, 24 / 32 where an SM holds one CTA.
+// Which kernel: the time of each that could run is estimated, in microseconds, by a fit to its measured times on one
+// GB300 (312 products of N 512 .. 8192, K 512 .. 8192, M 1 .. 1024 in a stream; bf16 results).  A wave of the large kernel
+// takes 0.53 a block of the reduction (0.67 with a scale per row of w) and the launch 4.2.  A wave of the small kernel
+// takes 3.8, 4.0 or 4.1 and 0.21, 0.24 or 0.39 a block for BN = 16, 32, 64, 1.36 times the latter where two CTAs share an
+// SM; to that come 0.6 for each CTA of an SM in turn, and 0.5 (0.7) for a cluster (of 8).  Splitting a reduction divides
+// the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for 27 / 32 of the CTAs that would fit one by
+// one.  The choice takes 0.7% more than the best of all on average, 9% at most; BN by M alone took 13% and 51%.
 struct Plan {
   int bn, split;  // bn = 0: the large kernel
 };
 Plan plan_of(const Params& p) {
-  const int bn = p.M <= 16 ? 16 : (p.M <= 32 ? 32 : (p.M <= 64 ? 64 : 128));
-  const double per_block = bn == 16 ? 0.30 : (bn == 32 ? 0.32 : (bn == 64 ? 0.38 : 0.63));
   const int64_t sms = sm_count() > 0 ? sm_count() : 1;
-  const int64_t tiles = (p.M + bn - 1) / bn * ((p.N + ROWS - 1) / ROWS);
-  Plan best{bn, 1};
-  double time = 1e30;
-  for (int split = 1; split <= 8 && (split == 1 || split <= p.nk); split *= 2) {
-    const int64_t room = sms * (bn <= 64 ? 2 : 1) * (split < 8 ? 32 : (bn <= 64 ? 27 : 24)) / 32;
-    const double t = (double)((tiles * split + room - 1) / room) * (3.0 + per_block * ((p.nk + split - 1) / split));
-    if (t < 0.98 * time) {
-      time = t;
-      best.split = split;
+  auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+  Plan best{16, 1};
+  double least = 1e30;
+  auto consider = [&](int bn, int split, double time) {
+    if (time < 0.99 * least) best = Plan{bn, split}, least = time;
+  };
+  const struct {
+    int bn;
+    double wave, block;
+  } small[3] = {{16, 3.8, 0.21}, {32, 4.0, 0.24}, {64, 4.1, 0.39}};
+  for (const auto& k : small) {
+    for (int split = 1; split <= 8 && (split == 1 || split <= p.nk); split *= 2) {
+      const int64_t ctas = over(p.M, k.bn) * over(p.N, ROWS) * split, room = split < 8 ? sms : sms * 27 / 32;
+      const double block = k.block * (ctas > room ? 1.36 : 1.0);
+      consider(k.bn, split,
+               (double)over(ctas, 2 * room > 0 ? 2 * room : 1) * (k.wave + block * (double)over(p.nk, split)) +
+                   0.6 * (double)ctas / (double)sms + (split == 1 ? 0.0 : (split < 8 ? 0.5 : 0.7)));
     }
   }
-  const int64_t big = (p.M + ROWS - 1) / ROWS * ((p.N + BIG_N - 1) / BIG_N);
-  if (p.nk > 0 && 5.0 + (double)((big + sms - 1) / sms) * (p.w.shift ? 0.56 : 0.72) * p.nk < time) best.bn = 0;
+  if (p.nk > 0)
+    consider(0, 1, 4.2 + (double)over(over(p.M, ROWS) * over(p.N, BIG_N), sms) * (p.w.shift ? 0.53 : 0.67) * p.nk);
   return best;
 }
 
@@ -1033,8 +1039,7 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
       return p.w.shift ? launch_big<false>(mx, mw, p, st) : launch_big<true>(mx, mw, p, st);
     case 16: return launch<16>(mw, mx, p, plan.split, st);
     case 32: return launch<32>(mw, mx, p, plan.split, st);
-    case 64: return launch<64>(mw, mx, p, plan.split, st);
-    default: return launch<128>(mw, mx, p, plan.split, st);
+    default: return launch<64>(mw, mx, p, plan.split, st);
   }
 }
 
