@@ -44,7 +44,6 @@ struct Params {
   int type;       // of y
   int scale4;     // rows of scales are aligned for loads of four
   int vec;        // y's rows are aligned for stores of four values, add's for loads of four
-  int sectors;    // y's rows are aligned for stores of 32 bytes, add's for loads of four
   long long wait_cycles;
 };
 
@@ -68,7 +67,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t r[16]) {
       : "memory");
 }
 // 16 lanes x 64 columns: of each 8 columns thread 4 a + b holds columns 2 b and 2 b + 1 of lane a, then of lane a + 8.
-__device__ __forceinline__ void tmem_ld_fragment(uint32_t addr, uint32_t r[32]) {
+__device__ __forceinline__ void tmem_ld_fragment(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
       "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -174,62 +173,19 @@ __device__ __forceinline__ void store_sector(void* p, const uint32_t v[8]) {
                "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-// COLS consecutive sums of row m from column n, by one thread: bias and `add` added, rounded once, stored by sectors.
-// All columns exist and the rows of y (and add) are aligned to 32 bytes.
-template <int COLS>
-__device__ __forceinline__ void store_row(const Params& P, int64_t m, int64_t n, float v[COLS]) {
-  if (P.bias) {
-#pragma unroll
-    for (int j = 0; j < COLS; ++j) v[j] += P.bias[n + j];
-  }
-  if (P.add) {
-    const float4* a = reinterpret_cast<const float4*>(P.add + m * P.ld_add + n);
-#pragma unroll
-    for (int j = 0; j < COLS; j += 4) {
-      const float4 f = a[j / 4];
-      v[j] += f.x, v[j + 1] += f.y, v[j + 2] += f.z, v[j + 3] += f.w;
-    }
-  }
-  uint32_t w[8];
-  if (P.type == DS_TYPE_F32) {
-    float* y = static_cast<float*>(P.y) + m * P.ldy + n;
-#pragma unroll
-    for (int j = 0; j < COLS; j += 8) {
-#pragma unroll
-      for (int l = 0; l < 8; ++l) w[l] = __float_as_uint(v[j + l]);
-      store_sector(y + j, w);
-    }
-  } else if (P.type == DS_TYPE_BF16) {
-    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(P.y) + m * P.ldy + n;
-#pragma unroll
-    for (int j = 0; j < COLS; j += 16) {
-#pragma unroll
-      for (int l = 0; l < 8; ++l) w[l] = pack2(v[j + 2 * l], v[j + 2 * l + 1], (const __nv_bfloat16*)nullptr);
-      store_sector(y + j, w);
-    }
-  } else {
-    __half* y = static_cast<__half*>(P.y) + m * P.ldy + n;
-#pragma unroll
-    for (int j = 0; j < COLS; j += 16) {
-#pragma unroll
-      for (int l = 0; l < 8; ++l) w[l] = pack2(v[j + 2 * l], v[j + 2 * l + 1], (const __half*)nullptr);
-      store_sector(y + j, w);
-    }
-  }
-}
-
-// Thread 4 a + b holds values 2 b, 2 b + 1 of four groups of 8 (v[2 g + i]); afterwards it holds the whole group b.
-__device__ __forceinline__ void turn_quad(float v[8]) {
+// Four threads 4 a + b exchange the parts of their four units of N values each: v[u] of thread b goes to v[b] of thread u.
+template <int N>
+__device__ __forceinline__ void turn_quad(float (&v)[4][N]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int bit = 1; bit <= 2; bit *= 2) {
     const bool up = lane & bit;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g & bit) continue;
+    for (int u = 0; u < 4; ++u) {
+      if (u & bit) continue;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float &lo = v[2 * g + i], &hi = v[2 * (g | bit) + i];
+      for (int i = 0; i < N; ++i) {
+        float &lo = v[u][i], &hi = v[u | bit][i];
         const float got = __shfl_xor_sync(0xFFFFFFFFu, up ? lo : hi, bit);
         if (up)
           lo = got;
@@ -239,30 +195,50 @@ __device__ __forceinline__ void turn_quad(float v[8]) {
     }
   }
 }
-// The sums of 32 rows from m, 128 columns from n, as tmem_ld_fragment spreads them: acc[64 c + 32 h + 4 g + 2 e + i] is
-// row 16 h + 8 e + lane / 4, column 64 c + 8 g + 2 (lane % 4) + i.  Turned so that a thread has 8 columns of
-// a row (stores of the pairs as they come took 6 us of a tile).
-__device__ __forceinline__ void store_fragments(const Params& P, int64_t m, int64_t n, const float acc[128]) {
+// Columns 32 c .. of a warp's 32 x 128 sums, turned so that thread 4 a + b has columns 8 b .. of four rows.  What a store
+// costs is the rows that it touches: eight here, 32 where a thread has a row, which took 3 us of a tile.
+// LANES: thread i holds row i, and gets rows 4 a .. 4 a + 3.  Otherwise the sums lie as tmem_ld_fragment spreads them,
+// acc[64 c + 32 h + 4 g + 2 e + i] being row 16 h + 8 e + a, column 64 c + 8 g + 2 b + i, and it gets rows a, a + 8 ..
+template <bool LANES>
+__device__ __forceinline__ void turned_rows(const float acc[128], int c, float (&o)[4][8]) {
+  if constexpr (LANES) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[u][i] = acc[32 * c + 8 * u + i];
+    turn_quad(o);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float v[4][2];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j >> 1][j & 1] = acc[64 * (c >> 1) + 32 * (r >> 1) + 16 * (c & 1) + 4 * (j >> 1) + 2 * (r & 1) + (j & 1)];
+      turn_quad(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[r][j] = v[j >> 1][j & 1];
+    }
+  }
+}
+// Bias and `add` are added to the sums of 32 rows from m, 128 columns from n; these are rounded once to y's type and
+// stored.  For rows that are aligned for stores of eight values (and for loads of four from add).
+template <bool LANES>
+__device__ __forceinline__ void store_wide(const Params& P, int64_t m, int64_t n, const float acc[128]) {
+  constexpr int STEP = LANES ? 1 : 8;
   const int lane = threadIdx.x & 31;
-  m += lane >> 2;
+  m += LANES ? lane & ~3 : lane >> 2;
   n += 8 * (lane & 3);
 #pragma unroll
   for (int c = 0; c < 4; ++c, n += 32) {
     float o[4][8];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        o[r][j] = acc[64 * (c >> 1) + 32 * (r >> 1) + 16 * (c & 1) + 4 * (j >> 1) + 2 * (r & 1) + (j & 1)];
-      turn_quad(o[r]);
-    }
-    if (!P.sectors || n + 8 > P.N) {
+    turned_rows<LANES>(acc, c, o);
+    if (n + 8 > P.N) {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int j = 0; j < 8; j += 4)
-          if (m + 8 * r < P.M && n + j < P.N)
-            finish4(P, m + 8 * r, n + j, make_float4(o[r][j], o[r][j + 1], o[r][j + 2], o[r][j + 3]));
+          if (m + STEP * r < P.M && n + j < P.N)
+            finish4(P, m + STEP * r, n + j, make_float4(o[r][j], o[r][j + 1], o[r][j + 2], o[r][j + 3]));
       continue;
     }
     if (P.bias) {
@@ -277,8 +253,8 @@ __device__ __forceinline__ void store_fragments(const Params& P, int64_t m, int6
       float4 f[4][2] = {};
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if (m + 8 * r >= P.M) continue;
-        const float4* a = reinterpret_cast<const float4*>(P.add + (m + 8 * r) * P.ld_add + n);
+        if (m + STEP * r >= P.M) continue;
+        const float4* a = reinterpret_cast<const float4*>(P.add + (m + STEP * r) * P.ld_add + n);
         f[r][0] = a[0], f[r][1] = a[1];
       }
 #pragma unroll
@@ -291,8 +267,8 @@ __device__ __forceinline__ void store_fragments(const Params& P, int64_t m, int6
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      if (m + 8 * r >= P.M) continue;
-      const int64_t at = (m + 8 * r) * P.ldy + n;
+      if (m + STEP * r >= P.M) continue;
+      const int64_t at = (m + STEP * r) * P.ldy + n;
       if (P.type == DS_TYPE_F32) {
         uint32_t w[8];
 #pragma unroll
@@ -306,6 +282,44 @@ __device__ __forceinline__ void store_fragments(const Params& P, int64_t m, int6
                                         : pack2(o[r][2 * j], o[r][2 * j + 1], (const __half*)nullptr);
         *reinterpret_cast<uint4*>(static_cast<__half*>(P.y) + at) = make_uint4(w[0], w[1], w[2], w[3]);
       }
+    }
+  }
+}
+constexpr int kPatchPitch = 36;  // floats between the rows of a patch of 8 x 32: no bank conflicts
+// The same for rows of any alignment: a patch of shared memory makes it 32 columns of one row per store (4096 x 4097 x
+// 4096 with add into bf16 121 us, 97 with rows that are aligned; by fours of a row's columns 247).
+template <bool LANES>
+__device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t n, const float acc[128], float* patch) {
+  const int lane = threadIdx.x & 31;
+  const int rows = (int)(P.M - m < 32 ? P.M - m : 32);
+  auto row = [](int r, int i) { return LANES ? 4 * i + r : 8 * r + i; };  // of the i-th row of the r-th patch
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int64_t col = n + 32 * c + lane;
+    const bool in = col < P.N;
+    float v[4][8];  // bias and add: the latter of 32 rows on their way at once
+    const float bias = P.bias && in ? P.bias[col] : 0.f;
+    const float* from = P.add + m * P.ld_add + col;
+    asm volatile("" : "+l"(from));  // addresses are found here, not all of them before the first use
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[r][i] = P.add && in && row(r, i) < rows ? from[row(r, i) * P.ld_add] : 0.f;
+    float o[4][8];
+    turned_rows<LANES>(acc, c, o);
+    int64_t at = m * P.ldy + col;
+    asm volatile("" : "+l"(at));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      __syncwarp();
+      float4* to = reinterpret_cast<float4*>(&patch[(lane >> 2) * kPatchPitch + 8 * (lane & 3)]);
+      to[0] = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+      to[1] = make_float4(o[r][4], o[r][5], o[r][6], o[r][7]);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (in && row(r, i) < rows)
+          store_one(P.y, P.type, at + row(r, i) * P.ldy, patch[i * kPatchPitch + lane] + bias + v[r][i]);
     }
   }
 }
@@ -605,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // A block's products take 512 cycles; what the adding warps do for it has to
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
 // shared memory 40: a second barrier per block for the scales made it 1100.
-// Measured at 8192 x 4096 x 4096: 140 us (1.96 PFLOP/s) with a scale per 128
+// Measured at 8192 x 4096 x 4096: 137 us (2.00 PFLOP/s) with a scale per 128
 // rows of w, 185 us (1.49) with one per row, where the adding warps multiply
 // twice and the scales' loads compete with them for the path to shared memory
 // (169 us without these loads, 139 with a scale per 128 rows in their place).
@@ -629,10 +643,9 @@ struct BigCfg {
 constexpr int kScaleSlots = 8;
 static_assert(kScaleSlots > BIG_STAGES + BIG_ACC, "scales in use");
 constexpr int kScaleRows = ROWS + BIG_N;
-constexpr int kStagePitch = 20;  // floats between the rows of a warp's 16 x 16 output patch: no bank conflicts
 
 struct __align__(16) BigShared {
-  float out[kBigEpiWarps][16 * kStagePitch];
+  float patch[kBigEpiWarps][8 * kPatchPitch];
   float scale[kScaleSlots][kScaleRows];  // rows of x, then rows of w
   uint64_t full[BIG_STAGES];   // a stage's copies and scales have come
   uint64_t mult[BIG_STAGES];   // its products are done: the sums may be read, the stage written again
@@ -660,7 +673,7 @@ struct TileOrder {
 };
 
 // COLS: w has a scale per row, so the columns of a tile differ; otherwise a warp's 128 columns share one.
-template <bool COLS>
+template <bool COLS, bool WIDE>
 __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
     linear_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
                          const Params P, const TileOrder tiles) {
@@ -860,55 +873,26 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
           }
         } else {
           const float s = scale[32 * q + lane] * scale[ROWS + col0 / 128];
-          uint32_t r[2][16];
-          tmem_ld16(taddr, r[0]);
+          uint32_t v[2][16];
+          tmem_ld16(taddr, v[0]);
 #pragma unroll
           for (int c = 0; c < kBigCols / 16; ++c) {
             tmem_wait_ld();
             if (c < kBigCols / 16 - 1)
-              tmem_ld16(taddr + 16 * (c + 1), r[(c + 1) & 1]);
+              tmem_ld16(taddr + 16 * (c + 1), v[(c + 1) & 1]);
             else
               release();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(r[c & 1][j]), s, acc[16 * c + j]);
+            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(v[c & 1][j]), s, acc[16 * c + j]);
           }
         }
       }
       int m0, n0;
       tiles.at(t, m0, n0);
-      if constexpr (COLS) {
-        store_fragments(P, m0 + 32 * q, n0 + col0, acc);
-        continue;
-      }
-      if (P.sectors && n0 + col0 + kBigCols <= P.N) {
-        if (m0 + 32 * q + lane < P.M) store_row<kBigCols>(P, m0 + 32 * q + lane, n0 + col0, acc);
-        continue;
-      }
-      // Rows that are not aligned, and the last columns: 16 rows x 16 columns at a time through shared memory, so
-      // that neighbouring threads write neighbouring columns.
-      float* out = sh->out[e];
-#pragma unroll
-      for (int c = 0; c < kBigCols / 16; ++c) {
-        const int64_t n = n0 + col0 + 16 * c + 4 * (lane & 3);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          __syncwarp();
-          if ((lane >> 4) == h) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              *reinterpret_cast<float4*>(&out[(lane & 15) * kStagePitch + 4 * j]) = make_float4(
-                  acc[16 * c + 4 * j], acc[16 * c + 4 * j + 1], acc[16 * c + 4 * j + 2], acc[16 * c + 4 * j + 3]);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int row = 8 * i + (lane >> 2);
-            const int64_t m = m0 + 32 * q + 16 * h + row;
-            const float4 v = *reinterpret_cast<const float4*>(&out[row * kStagePitch + 4 * (lane & 3)]);
-            if (m < P.M && n < P.N) finish4(P, m, n, v);
-          }
-        }
-      }
+      if constexpr (WIDE)
+        store_wide<!COLS>(P, m0 + 32 * q, n0 + col0, acc);
+      else
+        store_narrow<!COLS>(P, m0 + 32 * q, n0 + col0, acc, sh->patch[e]);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -920,16 +904,16 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
   }
 }
 
-template <bool COLS>
+template <bool COLS, bool WIDE>
 cudaError_t launch_big(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, cudaStream_t st) {
   static const cudaError_t attr =
-      cudaFuncSetAttribute(linear_f8_big_kernel<COLS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem);
+      cudaFuncSetAttribute(linear_f8_big_kernel<COLS, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem);
   if (attr != cudaSuccess) return attr;
   TileOrder t{(uint32_t)((p.M + ROWS - 1) / ROWS), (uint32_t)((p.N + BIG_N - 1) / BIG_N), 1};
   const uint32_t sms = sm_count() > 0 ? sm_count() : 1, count = t.tiles_m * t.tiles_n, grid = count < sms ? count : sms;
   t.G = (grid + t.tiles_n - 1) / t.tiles_n;  // about one wave of tiles per group
   if (t.G > t.tiles_m) t.G = t.tiles_m;
-  linear_f8_big_kernel<COLS><<<grid, BigCfg<COLS>::THREADS, kBigSmem, st>>>(mx, mw, p, t);
+  linear_f8_big_kernel<COLS, WIDE><<<grid, BigCfg<COLS>::THREADS, kBigSmem, st>>>(mx, mw, p, t);
   return cudaGetLastError();
 }
 
@@ -1025,7 +1009,7 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   const size_t size = l.type == DS_TYPE_F32 ? 4 : 2;
   p.vec = reinterpret_cast<uintptr_t>(l.y) % (4 * size) == 0 && l.ldy % 4 == 0 &&
           (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 16 == 0 && l.ld_add % 4 == 0));
-  p.sectors = p.vec && reinterpret_cast<uintptr_t>(l.y) % 32 == 0 && l.ldy * (int64_t)size % 32 == 0;
+  const bool wide = p.vec && reinterpret_cast<uintptr_t>(l.y) % (8 * size) == 0 && l.ldy % 8 == 0;
   p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
              reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;
   p.wait_cycles = f8_wait_cycles();
@@ -1036,7 +1020,8 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   switch (plan.bn) {
     case 0:
       p.idesc = idesc_of(l.x, l.w);  // x along the lanes
-      return p.w.shift ? launch_big<false>(mx, mw, p, st) : launch_big<true>(mx, mw, p, st);
+      if (p.w.shift) return wide ? launch_big<false, true>(mx, mw, p, st) : launch_big<false, false>(mx, mw, p, st);
+      return wide ? launch_big<true, true>(mx, mw, p, st) : launch_big<true, false>(mx, mw, p, st);
     case 16: return launch<16>(mw, mx, p, plan.split, st);
     case 32: return launch<32>(mw, mx, p, plan.split, st);
     default: return launch<64>(mw, mx, p, plan.split, st);
