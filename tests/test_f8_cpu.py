@@ -282,8 +282,8 @@ def test_outputs_of_one_call_have_one_format(ds):
 @pytest.mark.parametrize("rows,cols,tiles", [(0, 5, False), (5, 0, False), (0, 0, True), (1, 1, True), (3, 130, False),
                                              (129, 260, True), (256, 128, False)])
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
-def test_a_matrix_is_one_allocation(ds, rows, cols, tiles, fmt):
-    m = ds.F8Matrix.empty(rows, cols, "cpu", dtype=FORMATS[fmt], tiles=tiles)
+def test_a_matrix_is_one_allocation(dslib, rows, cols, tiles, fmt):
+    m = dslib.F8Matrix.empty(rows, cols, "cpu", dtype=FORMATS[fmt], tiles=tiles)
     nb = (cols + 127) // 128
     assert m.q.shape == (rows, cols) and m.q.dtype == FORMATS[fmt]
     assert m.scale.shape == ((rows + 127) // 128 if tiles else rows, nb) and m.scale.dtype == torch.float32
