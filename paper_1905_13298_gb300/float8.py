@@ -28,20 +28,14 @@ from . import (DS_F8_E4M3, DS_F8_E5M2, DS_F8_POW2, DS_F8_ROWS, DS_F8_TILES, DS_T
 _TYPES = {torch.float32: DS_TYPE_F32, torch.bfloat16: DS_TYPE_BF16, torch.float16: DS_TYPE_F16}
 _FORMATS = {torch.float8_e4m3fn: DS_F8_E4M3, torch.float8_e5m2: DS_F8_E5M2}
 _BLOCKS = {"rows": DS_F8_ROWS, "tiles": DS_F8_TILES}
-_DTYPES = {v: k for k, v in _FORMATS.items()}
 BLOCK = 128
-
-
-def _scale_offset(rows: int, ld: int) -> int:
-    """Bytes before the scales of a matrix that is one allocation."""
-    return (rows * ld + 255) // 256 * 256
 
 
 class F8Matrix:
     """8-bit values ``q`` [rows, cols] (``torch.float8_e4m3fn`` or ``float8_e5m2``, rows a multiple of 16 bytes apart)
     and float32 scales: ``scale`` [rows, ceil(cols / 128)], or with ``tiles`` [ceil(rows / 128), ceil(cols / 128)]."""
 
-    __slots__ = ("_q", "_scale", "_memory", "device", "desc")
+    __slots__ = ("q", "scale", "desc")
 
     def __init__(self, q, scale, tiles: bool = False):
         fmt = _FORMATS.get(q.dtype)
@@ -60,7 +54,7 @@ class F8Matrix:
             raise ValueError(f"scale has shape {tuple(scale.shape)}, expected {want}")
         if q.get_device() < 0 or q.get_device() != scale.get_device():
             raise ValueError("q and scale must be CUDA tensors of one device")
-        self._q, self._scale, self._memory, self.device = q, scale, None, q.device
+        self.q, self.scale = q, scale
         self.desc = ds_f8_matrix(q.data_ptr(), scale.data_ptr(), rows, cols, ld, ld_scale, fmt,
                                  DS_F8_TILES if tiles else DS_F8_ROWS)
 
@@ -72,34 +66,13 @@ class F8Matrix:
             raise ValueError(f"dtype must be torch.float8_e4m3fn or torch.float8_e5m2, got {dtype}")
         m = cls.__new__(cls)
         ld, nb = (cols + 15) // 16 * 16, (cols + BLOCK - 1) // BLOCK
-        # one allocation, the scales behind the values: a tensor costs more than what a small call does with it, so the
-        # two are made when they are asked for
-        at = _scale_offset(rows, ld)
-        memory = torch.empty(at + 4 * nb * ((rows + BLOCK - 1) // BLOCK if tiles else rows), dtype=torch.uint8,
-                             device=device)
-        address = memory.data_ptr()
-        m._q = m._scale = None
-        m._memory, m.device = memory, memory.device
-        m.desc = ds_f8_matrix(address, address + at, rows, cols, ld, nb, fmt, DS_F8_TILES if tiles else DS_F8_ROWS)
+        m.q = torch.empty((rows, ld), dtype=dtype, device=device)
+        if ld != cols:
+            m.q = m.q[:, :cols]
+        m.scale = torch.empty(((rows + BLOCK - 1) // BLOCK if tiles else rows, nb), dtype=torch.float32, device=device)
+        m.desc = ds_f8_matrix(m.q.data_ptr(), m.scale.data_ptr(), rows, cols, ld, nb, fmt,
+                              DS_F8_TILES if tiles else DS_F8_ROWS)
         return m
-
-    @property
-    def q(self):
-        """The 8-bit values."""
-        if self._q is None:
-            d = self.desc
-            q = self._memory[: d.rows * d.ld].view(_DTYPES[d.format]).view(d.rows, d.ld)
-            self._q = q[:, : d.cols] if d.ld != d.cols else q
-        return self._q
-
-    @property
-    def scale(self):
-        """The scales of the blocks."""
-        if self._scale is None:
-            d = self.desc
-            rows = (d.rows + BLOCK - 1) // BLOCK if self.tiles else d.rows
-            self._scale = self._memory[_scale_offset(d.rows, d.ld):].view(torch.float32).view(rows, d.ld_scale)
-        return self._scale
 
     @property
     def rows(self) -> int:
@@ -212,7 +185,7 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
         raise ValueError("neither the matrix nor its transpose is asked for")
     is_f8 = isinstance(x, F8Matrix)
     if is_f8:
-        rows, cols, device = x.desc.rows, x.desc.cols, x.device
+        rows, cols, device = x.desc.rows, x.desc.cols, x.q.device
     else:
         ld = _matrix(x, "x")
         _on_gpu(x, "x")
@@ -243,14 +216,13 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
     ``bias`` is float32 [N], ``add`` float32 [M, N]; ``out`` may be ``add`` itself, which then accumulates."""
     dx, dw = _f8(x, "x"), _f8(w, "w")
     M, N = dx.rows, dw.rows
-    device = x.device.index
-    if w.device.index != device:
-        raise ValueError(f"w is on cuda:{w.device.index}, the input on cuda:{device}")
+    device = x.q.get_device()
+    _on_gpu(w.q, "w", device)
     y = out
     if y is None:
         if dtype not in _TYPES:
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        y = torch.empty((M, N), dtype=dtype, device=x.device)
+        y = torch.empty((M, N), dtype=dtype, device=x.q.device)
         py, ldy = y.data_ptr(), N
     else:
         if y.dtype not in _TYPES:
@@ -341,7 +313,7 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     rows, features = da.shape
     if features == 0 or dk.rows != rows or dk.cols != _gate_width(features):
         raise ValueError(f"kept is {dk.rows} x {dk.cols}, expected {rows} x {_gate_width(features)}")
-    device = _on_gpu(da, "da", kept.device.index)
+    device = _on_gpu(da, "da", kept.q.get_device())
     dgu = F8Matrix.empty(rows, dk.cols, da.device, dtype)
     dgu_t = F8Matrix.empty(dk.cols, rows, da.device, dtype) if transposed else None
     a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None

@@ -277,18 +277,3 @@ def test_outputs_of_one_call_have_one_format(ds):
     assert L.ds_gated_f8(x, 0, 456, 4, 200, out, kept, 0, None) == ds.DS_ERR_INVALID_ARG
     d, d_t = _m(ds, 4, 456, 1 << 46), _m(ds, 456, 4, 1 << 47, format=ds.DS_F8_E5M2)
     assert L.ds_gated_f8_backward(kept, x, 0, 200, 200, d, d_t, None, 0, None) == ds.DS_ERR_INVALID_ARG
-
-
-@pytest.mark.parametrize("rows,cols,tiles", [(0, 5, False), (5, 0, False), (0, 0, True), (1, 1, True), (3, 130, False),
-                                             (129, 260, True), (256, 128, False)])
-@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
-def test_a_matrix_is_one_allocation(dslib, rows, cols, tiles, fmt):
-    m = dslib.F8Matrix.empty(rows, cols, "cpu", dtype=FORMATS[fmt], tiles=tiles)
-    nb = (cols + 127) // 128
-    assert m.q.shape == (rows, cols) and m.q.dtype == FORMATS[fmt]
-    assert m.scale.shape == ((rows + 127) // 128 if tiles else rows, nb) and m.scale.dtype == torch.float32
-    assert m.q is m.q and m.scale is m.scale and m.tiles == tiles and (m.rows, m.cols) == (rows, cols)
-    assert (m.desc.q or 0) == m.q.data_ptr() and (m.desc.scale or 0) == m.scale.data_ptr()
-    if rows > 1 and cols:
-        assert m.q.stride() == (m.desc.ld, 1) and m.desc.ld % 16 == 0
-        assert m.desc.q + (rows - 1) * m.desc.ld + cols <= m.desc.scale
