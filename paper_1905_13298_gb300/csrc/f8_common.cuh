@@ -60,14 +60,51 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, const __half*) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Eight 16-bit values at any address: by the widest accesses that it allows.  Rows an odd number of values apart start
+// anywhere; the branches go the same way for a whole row.
+__device__ __forceinline__ uint4 load16(const void* p) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  if (a % 8 == 0) {
+    const uint2 *w = static_cast<const uint2*>(p), lo = w[0], hi = w[1];
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+  }
+  if (a % 4 == 0) {
+    const uint32_t* w = static_cast<const uint32_t*>(p);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  const uint16_t* h = static_cast<const uint16_t*>(p);
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(h + 1);
+  const uint32_t a0 = h[0], a1 = w[0], a2 = w[1], a3 = w[2], a4 = h[7];
+  return make_uint4(a0 | a1 << 16, a1 >> 16 | a2 << 16, a2 >> 16 | a3 << 16, a3 >> 16 | a4 << 16);
+}
+__device__ __forceinline__ void store16(void* p, uint4 u) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  if (a % 8 == 0) {
+    uint2* w = static_cast<uint2*>(p);
+    w[0] = make_uint2(u.x, u.y), w[1] = make_uint2(u.z, u.w);
+  } else if (a % 4 == 0) {
+    uint32_t* w = static_cast<uint32_t*>(p);
+    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+  } else {
+    uint16_t* h = static_cast<uint16_t*>(p);
+    uint32_t* w = reinterpret_cast<uint32_t*>(h + 1);
+    h[0] = (uint16_t)u.x, w[0] = u.x >> 16 | u.y << 16, w[1] = u.y >> 16 | u.z << 16;
+    w[2] = u.z >> 16 | u.w << 16, h[7] = (uint16_t)(u.w >> 16);
+  }
+}
+
 // Eight consecutive values as they lie in memory; `vec` says that p is 16-byte aligned.  The `n` first exist, the
-// others read as zero.
+// others read as zero.  ODD: eight 16-bit values that are not aligned are loaded by load16; otherwise one by one, which
+// is less code.
 template <typename T>
 struct Raw8 {
   uint4 u;
+  template <bool ODD = false>
   __device__ __forceinline__ void load(const T* p, int n, bool vec) {
     if (vec && n >= 8) {
       u = *reinterpret_cast<const uint4*>(p);
+    } else if (ODD && n >= 8) {
+      u = load16(p);
     } else {
       const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
       uint32_t w[4];
@@ -87,6 +124,7 @@ struct Raw8 {
 template <>
 struct Raw8<float> {
   float4 a, b;
+  template <bool ODD = false>
   __device__ __forceinline__ void load(const float* p, int n, bool vec) {
     if (vec && n >= 8) {
       a = reinterpret_cast<const float4*>(p)[0];
@@ -105,20 +143,23 @@ struct Raw8<float> {
   }
 };
 
-template <typename T>
+template <bool ODD, typename T>
 __device__ __forceinline__ void store8(T* p, int n, bool vec, const float v[8]) {
-  if (vec && n >= 8) {
-    *reinterpret_cast<uint4*>(p) =
-        make_uint4(pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr),
-                   pack2(v[4], v[5], (const T*)nullptr), pack2(v[6], v[7], (const T*)nullptr));
+  if ((vec || ODD) && n >= 8) {
+    const uint4 u = make_uint4(pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr),
+                               pack2(v[4], v[5], (const T*)nullptr), pack2(v[6], v[7], (const T*)nullptr));
+    if (vec)
+      *reinterpret_cast<uint4*>(p) = u;
+    else
+      store16(p, u);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) from_float(v[i], p[i]);
   }
 }
-template <>
-__device__ __forceinline__ void store8<float>(float* p, int n, bool vec, const float v[8]) {
+template <bool ODD>
+__device__ __forceinline__ void store8(float* p, int n, bool vec, const float v[8]) {
   if (vec && n >= 8) {
     reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);

@@ -61,8 +61,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const T* p = gu + (i < m ? r0 + i : 0) * ld + (n > 0 ? c : 0);
-      rg[i].load(p, i < m ? n : 0, vec);
-      ru[i].load(p + up, i < m ? n : 0, vec);
+      rg[i].template load<true>(p, i < m ? n : 0, vec);
+      ru[i].template load<true>(p + up, i < m ? n : 0, vec);
     }
     float a[R][8], mx[8];  // maxima of a, g and u of each row
     mx[6] = mx[7] = 0.f;

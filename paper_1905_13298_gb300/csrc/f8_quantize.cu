@@ -27,7 +27,7 @@ struct SourceFloat {
   int64_t ld;
   bool vec;
   __device__ __forceinline__ void load(int64_t r, int64_t c, int n, Raw& raw) const {
-    raw.load(p + r * ld + c, n, vec);
+    raw.template load<true>(p + r * ld + c, n, vec);
   }
 };
 // Eight 8-bit values and their scale, decoded where they are used: an eighth of the registers of the values.

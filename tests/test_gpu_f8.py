@@ -642,3 +642,42 @@ def test_feed_forward_example_learns(dslib, capsys):
     losses = feed_forward.main(["--tokens", "512", "--hidden", "256", "--features", "384", "--steps", "12", "--shift"])
     assert losses[-1] < 0.9 * losses[0]
     assert "one token" in capsys.readouterr().out
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("cols", [136, 1000, 1027, 2056, 4100, 8200])
+@pytest.mark.parametrize("first,pad", [(1, 0), (0, 1), (2, 2), (4, 4), (3, 5)])
+def test_rows_at_any_address_give_the_same_bits(dslib, dtype, cols, first, pad):
+    """Rows that start at any element take other loads and stores, and the same sums and roundings."""
+    rows, width = 9, (cols + 127) // 128 * 128 + cols
+    g = torch.Generator(device="cuda").manual_seed(cols + first)
+
+    def apart(t):  # the same values, the rows `pad` elements further apart, the first one `first` elements in
+        r, c = t.shape
+        flat = torch.full((first + r * (c + pad),), float("nan"), dtype=t.dtype, device="cuda")
+        view = flat[first:].view(r, c + pad)[:, :c]
+        view.copy_(t)
+        return view
+
+    x, res, dy, dh = (torch.randn(rows, cols, device="cuda", generator=g).to(dtype) for _ in range(4))
+    gu = torch.randn(rows, width, device="cuda", generator=g).to(dtype)
+    w = torch.rand(cols, device="cuda", generator=g) + 0.5
+
+    def same(a, b):
+        assert torch.equal(a.q.float(), b.q.float()) and torch.equal(a.scale, b.scale)
+
+    for a, b in zip(dslib.quantize_f8(x, "rows", "rows"), dslib.quantize_f8(apart(x), "rows", "rows")):
+        same(a, b)
+    same(dslib.quantize_f8(x)[0], dslib.quantize_f8(apart(x))[0])
+    n, h, rstd = dslib.rmsnorm_f8(x, w, residual=res)
+    n2, h2, rstd2 = dslib.rmsnorm_f8(apart(x), w, residual=apart(res), h=apart(torch.zeros_like(x)))
+    same(n, n2)
+    assert torch.equal(h, h2) and torch.equal(rstd, rstd2)
+    dx, dw = dslib.rmsnorm_f8_backward(dy, h, rstd, w, dh=dh)
+    dx2, dw2 = dslib.rmsnorm_f8_backward(apart(dy), apart(h), rstd, w, dh=apart(dh), out=apart(torch.zeros_like(dy)))
+    assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    a, kept = dslib.gated_f8(gu, cols)
+    a2, kept2 = dslib.gated_f8(apart(gu), cols)
+    same(a, a2), same(kept, kept2)
+    for one, two in zip(dslib.gated_f8_backward(kept, dy), dslib.gated_f8_backward(kept, apart(dy))):
+        same(one, two)
