@@ -9,6 +9,12 @@
 // whatever is written from it.  Both are bound by HBM where their instructions
 // fit beside it: a tile's are about 10 per value and direction, and infinities
 // (the only values that need more) send the tile down a second path.
+//
+// Measured at 8192 x 4096: bf16 to rows 20.7 us (4.9 TB/s), to tiles 18.9
+// (5.3), to rows and transposed rows 25.4 (5.4), float32 to rows 26.5 (6.4).
+// 8-bit rows to transposed rows, 4096 x 8192: 24.4 us (2.8 TB/s), bound by
+// instructions: each value is decoded twice, once for its column's maximum and
+// once to be rounded, since decoded tiles would leave room for one CTA of an SM.
 #include "f8_common.cuh"
 
 namespace ds {
