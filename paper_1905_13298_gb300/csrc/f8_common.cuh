@@ -209,7 +209,11 @@ struct F8Scale {
 template <bool E5M2>
 __device__ __forceinline__ F8Scale f8_scale(float amax, bool pow2) {
   constexpr float kMax = E5M2 ? 57344.f : 448.f;
-  float s = fmaxf(__fdiv_rn(amax, kMax), 1.17549435e-38f);
+  // amax / kMax, correctly rounded, by a multiplication and the correction of its remainder (the division by a constant
+  // of P. Markstein, IBM J. Res. Dev. 34 (1), 1990; exact remainders down to quotients of 2^-126, below which s is set)
+  constexpr float kPart = 1.f / kMax;
+  const float near = amax * kPart;
+  float s = fmaxf(fmaf(fmaf(-near, kMax, amax), kPart, near), 1.17549435e-38f);
   if (pow2) {
     s = __uint_as_float((__float_as_uint(s) + 0x7FFFFFu) & 0xFF800000u);
     return F8Scale{s, __frcp_rn(s)};
