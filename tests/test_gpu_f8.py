@@ -681,3 +681,16 @@ def test_rows_at_any_address_give_the_same_bits(dslib, dtype, cols, first, pad):
     same(a, a2), same(kept, kept2)
     for one, two in zip(dslib.gated_f8_backward(kept, dy), dslib.gated_f8_backward(kept, apart(dy))):
         same(one, two)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("low,high", [(1, 1 << 23), (1 << 23, 0x7F7FFFFF), (0x3F000000, 0x40000000), (0x7E000000, 0x7F7FFFFF)])
+def test_scales_over_the_range_of_float32(dslib, fmt, low, high):
+    """Blocks whose largest magnitude has any bits: the scale and the factor to its units are correctly rounded."""
+    rng = _rng(fmt, low)
+    amax = rng.integers(low, high, size=(20000, 1)).astype(np.uint32).view(np.float32)
+    x = (rng.uniform(-1, 1, (20000, 128)).astype(np.float32) * amax).astype(np.float32)
+    x[np.arange(20000), rng.integers(0, 128, 20000)] = amax[:, 0] * rng.choice([-1, 1], 20000).astype(np.float32)
+    m, _ = dslib.quantize_f8(torch.from_numpy(x).cuda(), dtype=FORMATS[fmt])
+    q, s = F.quantize(x, False, False, fmt)
+    assert np.array_equal(_np(m.scale), s) and np.array_equal(_np(m.q), q)
