@@ -17,9 +17,9 @@
 // an SM's registers, so no second CTA can hide the first one's reads: TMA
 // brings the next tile to shared memory while this one is rounded and stored.
 //
-// Measured in bf16: forward 4095 x 8200 with the checkpoint 53 us (4.5 TB/s;
-// 66% of the issue slots, half of them conversions and maxima), 8192 x 4096
-// without it 42 us (4.0 TB/s); backward 8192 x 8192 144 us (4.3 TB/s, 57% of
+// Measured in bf16: forward 4095 x 8200 with the checkpoint 47 us (5.0 TB/s;
+// most of the rest is instructions, half of them conversions and maxima), 8192
+// x 4096 without it 37 us (4.6 TB/s); backward 8192 x 8192 142 us (4.4 TB/s, 57% of
 // the issue slots: a tile's phases, maxima, scales, rounding and turning, are
 // parted by barriers that nothing else on the SM fills).
 #include <type_traits>

@@ -10,8 +10,8 @@
 // fit beside it: a tile's are about 10 per value and direction, and infinities
 // (the only values that need more) send the tile down a second path.
 //
-// Measured at 8192 x 4096: bf16 to rows 20.7 us (4.9 TB/s), to tiles 18.9
-// (5.3), to rows and transposed rows 25.4 (5.4), float32 to rows 26.5 (6.4).
+// Measured at 8192 x 4096: bf16 to rows 18.8 us (5.4 TB/s), to tiles 19.1
+// (5.3), to rows and transposed rows 25.4 (5.4), float32 to rows 26.4 (6.4).
 // 8-bit rows to transposed rows, 4096 x 8192: 24.4 us (2.8 TB/s), bound by
 // instructions: each value is decoded twice, once for its column's maximum and
 // once to be rounded, since decoded tiles would leave room for one CTA of an SM.
@@ -312,7 +312,9 @@ cudaError_t run_as(const Source& src, int64_t rows, int64_t cols, const F8Out& o
   const int64_t nb = (cols + kF8Block - 1) / kF8Block;
   if (out_t.q == nullptr && !out.tiles) {
     const int64_t want = ((rows + R - 1) / R * nb + kThreads / 16 - 1) / (kThreads / 16);
-    const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * 32;
+    // 16-bit values are walked by the CTAs that fit at once (18.8 us at 8192 x 4096, 20.8 with one unit per CTA); of
+    // float32, twice the bytes, more CTAs in turn keep more in flight (26.4 us, 27.1 walked)
+    const int64_t cap = (int64_t)(sm_count() > 0 ? sm_count() : 1) * (Source::PACKED ? 4 : 32);
     quantize_rows_kernel<Source, E5M2>
         <<<(unsigned)(want < cap ? want : cap), kThreads, 0, st>>>(src, rows, cols, out, pow2);
   } else {
