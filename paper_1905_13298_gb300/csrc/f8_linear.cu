@@ -197,12 +197,12 @@ __device__ __forceinline__ void turn_quad(float (&v)[4][N]) {
     }
   }
 }
-// Columns 32 c .. of a warp's 32 x 128 sums, turned so that thread 4 a + b has columns 8 b .. of four rows.  What a store
+// Columns 32 c .. of a warp's 32 rows of sums, turned so that thread 4 a + b has columns 8 b .. of four rows.  What a store
 // costs is the rows that it touches: eight here, 32 where a thread has a row, which took 3 us of a tile.
 // LANES: thread i holds row i, and gets rows 4 a .. 4 a + 3.  Otherwise the sums lie as tmem_ld_fragment spreads them,
 // acc[64 c + 32 h + 4 g + 2 e + i] being row 16 h + 8 e + a, column 64 c + 8 g + 2 b + i, and it gets rows a, a + 8 ..
 template <bool LANES>
-__device__ __forceinline__ void turned_rows(const float acc[128], int c, float (&o)[4][8]) {
+__device__ __forceinline__ void turned_rows(const float* acc, int c, float (&o)[4][8]) {
   if constexpr (LANES) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
@@ -222,16 +222,16 @@ __device__ __forceinline__ void turned_rows(const float acc[128], int c, float (
     }
   }
 }
-// Bias and `add` are added to the sums of 32 rows from m, 128 columns from n; these are rounded once to y's type and
+// Bias and `add` are added to the sums of 32 rows from m, NC columns from n; these are rounded once to y's type and
 // stored.  For rows that are aligned for stores of eight values (and for loads of four from add).
-template <bool LANES>
-__device__ __forceinline__ void store_wide(const Params& P, int64_t m, int64_t n, const float acc[128]) {
+template <bool LANES, int NC>
+__device__ __forceinline__ void store_wide(const Params& P, int64_t m, int64_t n, const float (&acc)[NC]) {
   constexpr int STEP = LANES ? 1 : 8;
   const int lane = threadIdx.x & 31;
   m += LANES ? lane & ~3 : lane >> 2;
   n += 8 * (lane & 3);
 #pragma unroll
-  for (int c = 0; c < 4; ++c, n += 32) {
+  for (int c = 0; c < NC / 32; ++c, n += 32) {
     float o[4][8];
     turned_rows<LANES>(acc, c, o);
     if (n + 8 > P.N) {
@@ -289,14 +289,15 @@ __device__ __forceinline__ void store_wide(const Params& P, int64_t m, int64_t n
 }
 constexpr int kPatchPitch = 36;  // floats between the rows of a patch of 8 x 32: no bank conflicts
 // The same for rows of any alignment: a patch of shared memory makes it 32 columns of one row per store (4096 x 4097 x
-// 4096 with add into bf16 121 us, 97 with rows that are aligned; by fours of a row's columns 247).
-template <bool LANES>
-__device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t n, const float acc[128], float* patch) {
+// 4096 with add into bf16 115 us, 98 with rows that are aligned; by fours of a row's columns 247).
+template <bool LANES, typename T, int NC>
+__device__ __forceinline__ void store_narrow_as(const Params& P, int64_t m, int64_t n, const float (&acc)[NC],
+                                                float* patch) {
   const int lane = threadIdx.x & 31;
   const int rows = (int)(P.M - m < 32 ? P.M - m : 32);
   auto row = [](int r, int i) { return LANES ? 4 * i + r : 8 * r + i; };  // of the i-th row of the r-th patch
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
+  for (int c = 0; c < NC / 32; ++c) {
     const int64_t col = n + 32 * c + lane;
     const bool in = col < P.N;
     float v[4][8];  // bias and add: the latter of 32 rows on their way at once
@@ -309,8 +310,8 @@ __device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t
       for (int i = 0; i < 8; ++i) v[r][i] = P.add && in && row(r, i) < rows ? from[row(r, i) * P.ld_add] : 0.f;
     float o[4][8];
     turned_rows<LANES>(acc, c, o);
-    int64_t at = m * P.ldy + col;
-    asm volatile("" : "+l"(at));
+    T* to_y = static_cast<T*>(P.y) + m * P.ldy + col;
+    asm volatile("" : "+l"(to_y));
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       __syncwarp();
@@ -321,9 +322,20 @@ __device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if (in && row(r, i) < rows)
-          store_one(P.y, P.type, at + row(r, i) * P.ldy, patch[i * kPatchPitch + lane] + bias + v[r][i]);
+          from_float(patch[i * kPatchPitch + lane] + bias + v[r][i], to_y[row(r, i) * P.ldy]);
     }
   }
+}
+// One branch by the type for all of them: one per value made the code of a tile miss in the instruction cache.
+template <bool LANES, int NC>
+__device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t n, const float (&acc)[NC],
+                                             float* patch) {
+  if (P.type == DS_TYPE_F32)
+    store_narrow_as<LANES, float>(P, m, n, acc, patch);
+  else if (P.type == DS_TYPE_BF16)
+    store_narrow_as<LANES, __nv_bfloat16>(P, m, n, acc, patch);
+  else
+    store_narrow_as<LANES, __half>(P, m, n, acc, patch);
 }
 
 constexpr int BK = 128;    // bytes of a row per stage: one block of the reduction
@@ -611,12 +623,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 
 // ---------------------------------------------------------------------------
 // Large products: one persistent CTA per SM walks tiles of 128 rows of x (the
-// lanes) by 256 rows of w (the columns).  Warp 0 loads, warp 1 multiplies block
-// after block into two accumulators of 256 columns in turn, and eight warps
-// read each block back and add it, scaled, to the tile's sums: 128 float32 per
-// thread.  Further warps write a block's scales to shared memory as part of
-// its stage (the stage's barrier counts them with the copies), so the warps
-// that add wait for one barrier per block.
+// lanes) by N = 256 or 128 rows of w (the columns).  Warp 0 loads, warp 1
+// multiplies block after block into two (four) accumulators in turn, and eight
+// warps read each block back and add it, scaled, to the tile's sums: N / 2
+// float32 per thread.  Further warps write a block's scales to shared memory
+// as part of its stage (the stage's barrier counts them with the copies), so
+// the warps that add wait for one barrier per block.
 //
 // A block's products take 512 cycles; what the adding warps do for it has to
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
@@ -625,43 +637,46 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // rows of w, 185 us (1.49) with one per row, where the adding warps multiply
 // twice and the scales' loads compete with them for the path to shared memory
 // (169 us without these loads, 139 with a scale per 128 rows in their place).
+// Tiles of half the width take two thirds of the time: 512 x 2048 x 4096 with a
+// scale per 128 rows, 128 of them, 11.0 us, 64 of the others 13.7.
 // ---------------------------------------------------------------------------
-constexpr int BIG_N = 256, BIG_STAGES = 4, BIG_ACC = 2;
 constexpr int kBigEpiWarps = 8;
-constexpr int kBigCols = BIG_N / (kBigEpiWarps / 4);  // columns of a tile that a warp adds up
+// N: rows of w per tile.  Tiles of 256 read less; of 128 they leave fewer SMs without work where there are few, and room
+// for more stages and accumulators.
 // Warps for scales: with a scale per row of w two of them kept up with a block per 2400 cycles only (239 us at 8192 x
 // 4096 x 4096), six keep up with the adding warps; two suffice for the 130 scales of the other case and leave more
 // registers.  All threads are launched with the mean of the registers that the adding warps and the others then take.
-template <bool COLS>
+template <bool COLS, int N>
 struct BigCfg {
+  static constexpr int STAGES = N == 256 ? 4 : 6, ACC = 512 / N;
+  static constexpr int EACH = N / (kBigEpiWarps / 4);  // columns of a tile that a warp adds up
   static constexpr int SCALE_WARPS = COLS ? 6 : 2, OTHERS = 2 + SCALE_WARPS;
   static constexpr int THREADS = 32 * (OTHERS + kBigEpiWarps);
   static constexpr int REGS = COLS ? 208 : 216, REGS_OTHERS = COLS ? 48 : 72;
   static_assert(OTHERS * REGS_OTHERS + kBigEpiWarps * REGS <= (65536 / THREADS / 8 * 8) * (THREADS / 32), "registers");
+  // Slots of the scales' ring.  A slot of the data ring is free when the products of the block STAGES before are done,
+  // which needed the accumulator of the block STAGES + ACC before, whose readers were done with the block before that:
+  // so a slot of the scales' ring may be written again SLOTS blocks later without a wait of its own.
+  static constexpr int SLOTS = N == 256 ? 8 : 16;
+  static_assert(SLOTS > STAGES + ACC, "scales in use");
+  static constexpr int SCALE_ROWS = ROWS + N, STAGE_BYTES = (ROWS + N) * BK;
+  struct __align__(16) Shared {
+    float patch[kBigEpiWarps][8 * kPatchPitch];
+    float scale[SLOTS][SCALE_ROWS];  // rows of x, then rows of w
+    uint64_t full[STAGES];   // a stage's copies and scales have come
+    uint64_t mult[STAGES];   // its products are done: the sums may be read, the stage written again
+    uint64_t tempty[ACC];    // an accumulator has been read
+    uint64_t done;
+    uint32_t tmem_base;
+    int abort;
+  };
+  static constexpr size_t SMEM = (size_t)STAGES * STAGE_BYTES + sizeof(Shared) + 1024;
+  static_assert(SMEM <= 232448, "shared memory of a CTA");
 };
-// Slots of the scales' ring.  A slot of the data ring is free when the products of the block 4 before are done, which
-// needed the accumulator of the block 6 before, whose readers were done with the block 7 before: so a slot of the
-// scales' ring may be written again 8 blocks later without a wait of its own.
-constexpr int kScaleSlots = 8;
-static_assert(kScaleSlots > BIG_STAGES + BIG_ACC, "scales in use");
-constexpr int kScaleRows = ROWS + BIG_N;
-
-struct __align__(16) BigShared {
-  float patch[kBigEpiWarps][8 * kPatchPitch];
-  float scale[kScaleSlots][kScaleRows];  // rows of x, then rows of w
-  uint64_t full[BIG_STAGES];   // a stage's copies and scales have come
-  uint64_t mult[BIG_STAGES];   // its products are done: the sums may be read, the stage written again
-  uint64_t tempty[BIG_ACC];    // an accumulator has been read
-  uint64_t done;
-  uint32_t tmem_base;
-  int abort;
-};
-constexpr int kBigStageBytes = (ROWS + BIG_N) * BK;
-constexpr size_t kBigSmem = (size_t)BIG_STAGES * kBigStageBytes + sizeof(BigShared) + 1024;
-static_assert(kBigSmem <= 232448, "shared memory of a CTA");
 
 // Tile t in grouped order: G row tiles, columns slowest inside a group, so that the tiles in flight share rows of both
 // operands in L2.
+template <int N>
 struct TileOrder {
   uint32_t tiles_m, tiles_n, G;
   __device__ __forceinline__ uint32_t count() const { return tiles_m * tiles_n; }
@@ -670,20 +685,22 @@ struct TileOrder {
     const uint32_t size = tiles_m - first < G ? tiles_m - first : G;
     const uint32_t r = t - g * per_group;
     m0 = (int)((first + r % size) * ROWS);
-    n0 = (int)((r / size) * BIG_N);
+    n0 = (int)((r / size) * N);
   }
 };
 
 // COLS: w has a scale per row, so the columns of a tile differ; otherwise a warp's 128 columns share one.
-template <bool COLS, bool WIDE>
-__global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
+template <bool COLS, bool WIDE, int N>
+__global__ void __launch_bounds__(BigCfg<COLS, N>::THREADS, 1)
     linear_f8_big_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w,
-                         const Params P, const TileOrder tiles) {
-  using Cfg = BigCfg<COLS>;
+                         const Params P, const TileOrder<N> tiles) {
+  using Cfg = BigCfg<COLS, N>;
+  using BigShared = typename Cfg::Shared;
+  constexpr int BIG_STAGES = Cfg::STAGES, BIG_ACC = Cfg::ACC, kBigCols = Cfg::EACH;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  BigShared* sh = reinterpret_cast<BigShared*>(ring + BIG_STAGES * kBigStageBytes);
+  BigShared* sh = reinterpret_cast<BigShared*>(ring + BIG_STAGES * Cfg::STAGE_BYTES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t ntiles = tiles.count();
   const int nk = P.nk;
@@ -701,7 +718,7 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
-                 "r"(BIG_ACC * BIG_N)
+                 "r"(BIG_ACC * N)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -723,8 +740,8 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
         for (int i = 0; i < nk; ++i, ++issued, st.next()) {
           ok = mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault);
           if (!ok) break;
-          unsigned char* a = ring + st.slot * kBigStageBytes;
-          mbar_expect_tx(&sh->full[st.slot], kBigStageBytes);
+          unsigned char* a = ring + st.slot * Cfg::STAGE_BYTES;
+          mbar_expect_tx(&sh->full[st.slot], Cfg::STAGE_BYTES);
           tma_load_2d(a, &tmap_x, &sh->full[st.slot], i * BK, m0);
           tma_load_2d(a + ROWS * BK, &tmap_w, &sh->full[st.slot], i * BK, n0);
         }
@@ -733,7 +750,7 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
       for (uint32_t j = issued > BIG_STAGES ? issued - BIG_STAGES : 0; j < issued; ++j)
         mbar_drain(&sh->full[j % BIG_STAGES], (j / BIG_STAGES) & 1u, *abort ? kLandedCycles : kTimeoutCycles);
     } else if (warp == 1 && lane == 0) {
-      const uint32_t idesc = P.idesc | ((uint32_t)(BIG_N >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
+      const uint32_t idesc = P.idesc | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
       const uint64_t adesc = sw128_desc(smem_u32(ring)), bdesc = sw128_desc(smem_u32(ring) + ROWS * BK);
       const uint32_t mine = blockIdx.x < ntiles ? (ntiles - blockIdx.x - 1) / gridDim.x + 1 : 0;
       const int64_t total = (int64_t)mine * nk;
@@ -743,8 +760,8 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
       bool ok = total > 0 && mbar_wait(&sh->full[0], 0u, abort, P.wait_cycles, &g_f8_fault);
       for (int64_t n = 0; n < total && ok; ++n) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t at = (uint64_t)(st.slot * (kBigStageBytes >> 4));
-        const uint32_t d = tmem_base + ac.slot * BIG_N;
+        const uint64_t at = (uint64_t)(st.slot * (Cfg::STAGE_BYTES >> 4));
+        const uint32_t d = tmem_base + ac.slot * N;
         uint64_t* const mult = &sh->mult[st.slot];
         umma_f8(d, adesc + at, bdesc + at, idesc, 0u);
         umma_f8(d, adesc + at + 2, bdesc + at + 2, idesc, 1u);
@@ -762,7 +779,7 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
     } else if (warp >= 2) {
       // Scales: thread j holds rows j, j + SPAN .. of the tile's 128 rows of x and 256 of w (or the 2 scales that these
       // share), of four blocks at a time; the next four are on their way while these are written.
-      constexpr int SPAN = 32 * Cfg::SCALE_WARPS, USED = COLS ? kScaleRows : ROWS + 2, GROUP = 4;
+      constexpr int SPAN = 32 * Cfg::SCALE_WARPS, USED = COLS ? Cfg::SCALE_ROWS : ROWS + N / 128, GROUP = 4;
       constexpr int PER = (USED + SPAN - 1) / SPAN;
       const int j = threadIdx.x - 64;
       ScaleFeed<PER, GROUP> feed;
@@ -776,7 +793,7 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
           feed.src[i] = nullptr;
           if (r < ROWS) {
             if (m < P.M) feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld;
-          } else if ((COLS || r < ROWS + 2) && n < P.N) {
+          } else if ((COLS || r < USED) && n < P.N) {
             feed.src[i] = P.w.s + (COLS ? n : n >> 7) * P.w.ld;
           }
         }
@@ -805,7 +822,7 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
             ok = __all_sync(0xFFFFFFFFu,
                             mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault));
             if (!ok) break;
-            float* to = sh->scale[it % kScaleSlots] + j;
+            float* to = sh->scale[it % Cfg::SLOTS] + j;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
               if (USED % SPAN == 0 || j + SPAN * i < USED) to[SPAN * i] = v[i][b];
@@ -843,8 +860,8 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
       for (int j = 0; j < kBigCols; ++j) acc[j] = 0.f;
       for (int i = 0; i < nk; ++i, ++it) {
         if (!wait_block()) break;
-        const uint32_t taddr = tmem + ac.slot * BIG_N;
-        const float* scale = sh->scale[it % kScaleSlots];
+        const uint32_t taddr = tmem + ac.slot * N;
+        const float* scale = sh->scale[it % Cfg::SLOTS];
         if constexpr (COLS) {
           // Fragments of 16 rows x 64 columns: a thread has 32 of the warp's columns, so that a warp reads a quarter of
           // the scales that it would with all 128 (a read of shared memory returns 128 bytes a cycle, also where all
@@ -901,22 +918,29 @@ __global__ void __launch_bounds__(BigCfg<COLS>::THREADS, 1)
   __syncthreads();
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(BIG_ACC * BIG_N)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(BIG_ACC * N)
                  : "memory");
   }
 }
 
-template <bool COLS, bool WIDE>
+template <bool COLS, bool WIDE, int N>
 cudaError_t launch_big(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, cudaStream_t st) {
-  static const cudaError_t attr =
-      cudaFuncSetAttribute(linear_f8_big_kernel<COLS, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBigSmem);
+  using Cfg = BigCfg<COLS, N>;
+  static const cudaError_t attr = cudaFuncSetAttribute(
+      linear_f8_big_kernel<COLS, WIDE, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg::SMEM);
   if (attr != cudaSuccess) return attr;
-  TileOrder t{(uint32_t)((p.M + ROWS - 1) / ROWS), (uint32_t)((p.N + BIG_N - 1) / BIG_N), 1};
+  TileOrder<N> t{(uint32_t)((p.M + ROWS - 1) / ROWS), (uint32_t)((p.N + N - 1) / N), 1};
   const uint32_t sms = sm_count() > 0 ? sm_count() : 1, count = t.tiles_m * t.tiles_n, grid = count < sms ? count : sms;
   t.G = (grid + t.tiles_n - 1) / t.tiles_n;  // about one wave of tiles per group
   if (t.G > t.tiles_m) t.G = t.tiles_m;
-  linear_f8_big_kernel<COLS, WIDE><<<grid, BigCfg<COLS>::THREADS, kBigSmem, st>>>(mx, mw, p, t);
+  linear_f8_big_kernel<COLS, WIDE, N><<<grid, Cfg::THREADS, Cfg::SMEM, st>>>(mx, mw, p, t);
   return cudaGetLastError();
+}
+
+template <int N>
+cudaError_t start_big(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, bool wide, cudaStream_t st) {
+  if (p.w.shift) return wide ? launch_big<false, true, N>(mx, mw, p, st) : launch_big<false, false, N>(mx, mw, p, st);
+  return wide ? launch_big<true, true, N>(mx, mw, p, st) : launch_big<true, false, N>(mx, mw, p, st);
 }
 
 bool make_map(CUtensorMap* map, const ds_f8_matrix* m, uint32_t box_rows) {
@@ -948,38 +972,46 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
 }
 
 // Which kernel: the time of each that could run is estimated, in microseconds, by a fit to its measured times on one
-// GB300 (312 products of N 512 .. 8192, K 512 .. 8192, M 1 .. 1024 in a stream; bf16 results).  A wave of the large kernel
-// takes 0.53 a block of the reduction (0.67 with a scale per row of w) and the launch 4.2.  A wave of the small kernel
-// takes 3.8, 4.0 or 4.1 and 0.21, 0.24 or 0.39 a block for BN = 16, 32, 64, 1.36 times the latter where two CTAs share an
-// SM; to that come 0.6 for each CTA of an SM in turn, and 0.5 (0.7) for a cluster (of 8).  Splitting a reduction divides
-// the blocks of a CTA and multiplies the CTAs; a cluster of 8 finds room for 27 / 32 of the CTAs that would fit one by
-// one.  The choice takes 0.7% more than the best of all on average, 9% at most; BN by M alone took 13% and 51%.
+// GB300 (720 products of N 512 .. 8192, K 512 .. 5632, M 1 .. 3000 in a stream; bf16 results).  The large kernel takes
+// 3.5 to start, and a wave of its tiles 1.3 and 0.60 a block of the reduction (0.79 with a scale per row of w), of half
+// tiles 0.7 and 0.40 (0.53).  A wave of the small kernel takes 3.8, 4.0 or 4.2 and 0.23, 0.24 or 0.38 a block for BN =
+// 16, 32, 64, 1.6 times the latter where two CTAs share an SM; to that come 0.6 for each CTA of an SM in turn, and 0.4
+// (0.6) for a cluster (of 8).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8
+// finds room for 27 / 32 of the CTAs that would fit one by one.  Stores of rows that are not aligned add 0.02 for each
+// row of x or w that the CTA's columns are (4096 x 1024 x 4097: 50 us, 31 for 4096 columns).  The choice takes 0.6% more than the best of all on
+// average, 21% at most.
 struct Plan {
-  int bn, split;  // bn = 0: the large kernel
+  int bn, split, big;  // big: rows of w per tile of the large kernel, or 0
 };
-Plan plan_of(const Params& p) {
+Plan plan_of(const Params& p, bool wide) {
   const int64_t sms = sm_count() > 0 ? sm_count() : 1;
   auto over = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-  Plan best{16, 1};
+  Plan best{16, 1, 0};
   double least = 1e30;
-  auto consider = [&](int bn, int split, double time) {
-    if (time < 0.99 * least) best = Plan{bn, split}, least = time;
+  auto consider = [&](int bn, int split, int big, double time) {
+    if (time < 0.99 * least) best = Plan{bn, split, big}, least = time;
   };
   const struct {
     int bn;
     double wave, block;
-  } small[3] = {{16, 3.8, 0.21}, {32, 4.0, 0.24}, {64, 4.1, 0.39}};
+  } small[3] = {{16, 3.8, 0.23}, {32, 4.0, 0.24}, {64, 4.2, 0.38}};
   for (const auto& k : small) {
     for (int split = 1; split <= 8 && (split == 1 || split <= p.nk); split *= 2) {
       const int64_t ctas = over(p.M, k.bn) * over(p.N, ROWS) * split, room = split < 8 ? sms : sms * 27 / 32;
-      const double block = k.block * (ctas > room ? 1.36 : 1.0);
-      consider(k.bn, split,
-               (double)over(ctas, 2 * room > 0 ? 2 * room : 1) * (k.wave + block * (double)over(p.nk, split)) +
-                   0.6 * (double)ctas / (double)sms + (split == 1 ? 0.0 : (split < 8 ? 0.5 : 0.7)));
+      const double wave = k.wave + k.block * (ctas > room ? 1.6 : 1.0) * (double)over(p.nk, split) +
+                          (p.vec ? 0.0 : 0.02 * k.bn / split);
+      consider(k.bn, split, 0,
+               (double)over(ctas, 2 * room > 0 ? 2 * room : 1) * wave + 0.6 * (double)ctas / (double)sms +
+                   (split == 1 ? 0.0 : (split < 8 ? 0.4 : 0.6)));
     }
   }
-  if (p.nk > 0)
-    consider(0, 1, 4.2 + (double)over(over(p.M, ROWS) * over(p.N, BIG_N), sms) * (p.w.shift ? 0.53 : 0.67) * p.nk);
+  if (p.nk > 0) {
+    for (int big = 256; big >= 128; big /= 2) {
+      const double block = big == 256 ? (p.w.shift ? 0.60 : 0.79) : (p.w.shift ? 0.40 : 0.53);
+      const double wave = (big == 256 ? 1.3 : 0.7) + (wide ? 0.0 : 0.02 * big) + block * p.nk;
+      consider(0, 1, big, 3.5 + (double)over(over(p.M, ROWS) * over(p.N, big), sms) * wave);
+    }
+  }
   return best;
 }
 
@@ -1015,15 +1047,14 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
              reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;
   p.wait_cycles = f8_wait_cycles();
-  const Plan plan = plan_of(p);
+  const Plan plan = plan_of(p, wide);
   CUtensorMap mw = {}, mx = {};  // an empty reduction loads nothing
-  if (p.nk > 0 && (!make_map(&mw, l.w, plan.bn ? ROWS : BIG_N) || !make_map(&mx, l.x, plan.bn ? plan.bn : ROWS)))
+  if (p.nk > 0 && (!make_map(&mw, l.w, plan.big ? plan.big : ROWS) || !make_map(&mx, l.x, plan.big ? ROWS : plan.bn)))
     return cudaErrorInvalidValue;
+  if (plan.big) p.idesc = idesc_of(l.x, l.w);  // x along the lanes
+  if (plan.big == 256) return start_big<256>(mx, mw, p, wide, st);
+  if (plan.big == 128) return start_big<128>(mx, mw, p, wide, st);
   switch (plan.bn) {
-    case 0:
-      p.idesc = idesc_of(l.x, l.w);  // x along the lanes
-      if (p.w.shift) return wide ? launch_big<false, true>(mx, mw, p, st) : launch_big<false, false>(mx, mw, p, st);
-      return wide ? launch_big<true, true>(mx, mw, p, st) : launch_big<true, false>(mx, mw, p, st);
     case 16: return launch<16>(mw, mx, p, plan.split, st);
     case 32: return launch<32>(mw, mx, p, plan.split, st);
     default: return launch<64>(mw, mx, p, plan.split, st);
