@@ -46,6 +46,7 @@ struct Params {
   int type;       // of y
   int scale4;     // rows of scales are aligned for loads of four
   int vec;        // y's rows are aligned for stores of four values, add's for loads of four
+  int pairs;      // ... of two
   long long wait_cycles;
 };
 
@@ -175,7 +176,7 @@ __device__ __forceinline__ void store_sector(void* p, const uint32_t v[8]) {
                "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
-// Four threads 4 a + b exchange the parts of their four units of N values each: v[u] of thread b goes to v[b] of thread u.
+// Four threads 4 a + b exchange the parts of their four units of N values: v[u] of thread b goes to v[b] of thread u.
 template <int N>
 __device__ __forceinline__ void turn_quad(float (&v)[4][N]) {
   const int lane = threadIdx.x & 31;
@@ -197,8 +198,8 @@ __device__ __forceinline__ void turn_quad(float (&v)[4][N]) {
     }
   }
 }
-// Columns 32 c .. of a warp's 32 rows of sums, turned so that thread 4 a + b has columns 8 b .. of four rows.  What a store
-// costs is the rows that it touches: eight here, 32 where a thread has a row, which took 3 us of a tile.
+// Columns 32 c .. of a warp's 32 rows of sums, turned so that thread 4 a + b has columns 8 b .. of four rows.  What a
+// store costs is the rows that it touches: eight here, 32 where a thread has a row, which took 3 us of a tile.
 // LANES: thread i holds row i, and gets rows 4 a .. 4 a + 3.  Otherwise the sums lie as tmem_ld_fragment spreads them,
 // acc[64 c + 32 h + 4 g + 2 e + i] being row 16 h + 8 e + a, column 64 c + 8 g + 2 b + i, and it gets rows a, a + 8 ..
 template <bool LANES>
@@ -288,30 +289,53 @@ __device__ __forceinline__ void store_wide(const Params& P, int64_t m, int64_t n
   }
 }
 constexpr int kPatchPitch = 36;  // floats between the rows of a patch of 8 x 32: no bank conflicts
-// The same for rows of any alignment: a patch of shared memory makes it 32 columns of one row per store (4096 x 4097 x
-// 4096 with add into bf16 115 us, 98 with rows that are aligned; by fours of a row's columns 247).
-template <bool LANES, typename T, int NC>
+// The same for rows of any alignment: a patch of shared memory makes it 32 columns of one row per store (4096 x 4096 x
+// 4097 into bf16 93 us, with add 114; 79 and 97 for 4096 columns; by fours of a row's columns 129 and 247).
+// COUNT = 2: rows are aligned for pairs of values, and a store takes 32 columns of two rows.
+template <bool LANES, typename T, int COUNT, int NC>
 __device__ __forceinline__ void store_narrow_as(const Params& P, int64_t m, int64_t n, const float (&acc)[NC],
                                                 float* patch) {
-  const int lane = threadIdx.x & 31;
+  struct alignas(sizeof(T) * COUNT) Some {
+    T v[COUNT];
+  };
+  struct alignas(4 * COUNT) Floats {
+    float v[COUNT];
+  };
+  const int lane = threadIdx.x & 31, half = COUNT * lane / 32, mine = COUNT * lane % 32;
   const int rows = (int)(P.M - m < 32 ? P.M - m : 32);
-  auto row = [](int r, int i) { return LANES ? 4 * i + r : 8 * r + i; };  // of the i-th row of the r-th patch
+  // of the i-th row of the r-th patch, as this thread stores it
+  auto place = [&](int i) { return COUNT * i + half; };
+  auto row = [&](int r, int i) { return LANES ? 4 * place(i) + r : 8 * r + place(i); };
 #pragma unroll
   for (int c = 0; c < NC / 32; ++c) {
-    const int64_t col = n + 32 * c + lane;
-    const bool in = col < P.N;
-    float v[4][8];  // bias and add: the latter of 32 rows on their way at once
-    const float bias = P.bias && in ? P.bias[col] : 0.f;
-    const float* from = P.add + m * P.ld_add + col;
-    asm volatile("" : "+l"(from));  // addresses are found here, not all of them before the first use
+    const int64_t col = n + 32 * c + mine;
+    const int left = (int)(P.N - col < COUNT ? P.N - col : COUNT);
+    auto exists = [&](int r, int i) { return left > 0 && row(r, i) < rows; };
+    Floats bias = {}, v[4][8 / COUNT] = {};  // v: of add, the values of 32 rows on their way at once
+    if (P.bias) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+      for (int k = 0; k < COUNT; ++k)
+        if (k < left) bias.v[k] = P.bias[col + k];
+    }
+    if (P.add) {
+      const float* from = P.add + m * P.ld_add + col;
+      asm volatile("" : "+l"(from));  // addresses are found here, not all of them before the first use
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[r][i] = P.add && in && row(r, i) < rows ? from[row(r, i) * P.ld_add] : 0.f;
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 8 / COUNT; ++i) {
+          if (!exists(r, i)) continue;
+          const float* a = from + row(r, i) * P.ld_add;
+          if (left == COUNT)
+            v[r][i] = *reinterpret_cast<const Floats*>(a);
+          else
+            v[r][i].v[0] = a[0];
+        }
+    }
     float o[4][8];
     turned_rows<LANES>(acc, c, o);
-    T* to_y = static_cast<T*>(P.y) + m * P.ldy + col;
-    asm volatile("" : "+l"(to_y));
+    T* y = static_cast<T*>(P.y) + m * P.ldy + col;
+    asm volatile("" : "+l"(y));
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       __syncwarp();
@@ -320,22 +344,39 @@ __device__ __forceinline__ void store_narrow_as(const Params& P, int64_t m, int6
       to[1] = make_float4(o[r][4], o[r][5], o[r][6], o[r][7]);
       __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (in && row(r, i) < rows)
-          from_float(patch[i * kPatchPitch + lane] + bias + v[r][i], to_y[row(r, i) * P.ldy]);
+      for (int i = 0; i < 8 / COUNT; ++i) {
+        if (!exists(r, i)) continue;
+        const Floats f = *reinterpret_cast<const Floats*>(&patch[place(i) * kPatchPitch + mine]);
+        Some out;
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) from_float(f.v[k] + bias.v[k] + v[r][i].v[k], out.v[k]);
+        T* at = y + row(r, i) * P.ldy;
+        if (left == COUNT)
+          *reinterpret_cast<Some*>(at) = out;
+        else
+          at[0] = out.v[0];
+      }
     }
   }
+}
+template <bool LANES, typename T, int NC>
+__device__ __forceinline__ void store_narrow_of(const Params& P, int64_t m, int64_t n, const float (&acc)[NC],
+                                                float* patch) {
+  if (P.pairs)
+    store_narrow_as<LANES, T, 2>(P, m, n, acc, patch);
+  else
+    store_narrow_as<LANES, T, 1>(P, m, n, acc, patch);
 }
 // One branch by the type for all of them: one per value made the code of a tile miss in the instruction cache.
 template <bool LANES, int NC>
 __device__ __forceinline__ void store_narrow(const Params& P, int64_t m, int64_t n, const float (&acc)[NC],
                                              float* patch) {
   if (P.type == DS_TYPE_F32)
-    store_narrow_as<LANES, float>(P, m, n, acc, patch);
+    store_narrow_of<LANES, float>(P, m, n, acc, patch);
   else if (P.type == DS_TYPE_BF16)
-    store_narrow_as<LANES, __nv_bfloat16>(P, m, n, acc, patch);
+    store_narrow_of<LANES, __nv_bfloat16>(P, m, n, acc, patch);
   else
-    store_narrow_as<LANES, __half>(P, m, n, acc, patch);
+    store_narrow_of<LANES, __half>(P, m, n, acc, patch);
 }
 
 constexpr int BK = 128;    // bytes of a row per stage: one block of the reduction
@@ -977,9 +1018,9 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
 // tiles 0.7 and 0.40 (0.53).  A wave of the small kernel takes 3.8, 4.0 or 4.2 and 0.23, 0.24 or 0.38 a block for BN =
 // 16, 32, 64, 1.6 times the latter where two CTAs share an SM; to that come 0.6 for each CTA of an SM in turn, and 0.4
 // (0.6) for a cluster (of 8).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8
-// finds room for 27 / 32 of the CTAs that would fit one by one.  Stores of rows that are not aligned add 0.02 for each
-// row of x or w that the CTA's columns are (4096 x 1024 x 4097: 50 us, 31 for 4096 columns).  The choice takes 0.6% more than the best of all on
-// average, 21% at most.
+// finds room for 27 / 32 of the CTAs that would fit one by one.  Stores of rows that are not aligned add 0.013 a column
+// of a tile (0.02 in the small kernel; 4096 x 1024 x 4097 takes 44 us, 31 with 4096 columns).  The choice takes 0.6%
+// more than the best of all on average, 21% at most.
 struct Plan {
   int bn, split, big;  // big: rows of w per tile of the large kernel, or 0
 };
@@ -1008,7 +1049,7 @@ Plan plan_of(const Params& p, bool wide) {
   if (p.nk > 0) {
     for (int big = 256; big >= 128; big /= 2) {
       const double block = big == 256 ? (p.w.shift ? 0.60 : 0.79) : (p.w.shift ? 0.40 : 0.53);
-      const double wave = (big == 256 ? 1.3 : 0.7) + (wide ? 0.0 : 0.02 * big) + block * p.nk;
+      const double wave = (big == 256 ? 1.3 : 0.7) + (wide ? 0.0 : 0.013 * big) + block * p.nk;
       consider(0, 1, big, 3.5 + (double)over(over(p.M, ROWS) * over(p.N, big), sms) * wave);
     }
   }
@@ -1043,6 +1084,8 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   const size_t size = l.type == DS_TYPE_F32 ? 4 : 2;
   p.vec = reinterpret_cast<uintptr_t>(l.y) % (4 * size) == 0 && l.ldy % 4 == 0 &&
           (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 16 == 0 && l.ld_add % 4 == 0));
+  p.pairs = reinterpret_cast<uintptr_t>(l.y) % (2 * size) == 0 && l.ldy % 2 == 0 &&
+            (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 8 == 0 && l.ld_add % 2 == 0));
   const bool wide = p.vec && reinterpret_cast<uintptr_t>(l.y) % (8 * size) == 0 && l.ldy % 8 == 0;
   p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
              reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;

@@ -694,3 +694,33 @@ def test_scales_over_the_range_of_float32(dslib, fmt, low, high):
     m, _ = dslib.quantize_f8(torch.from_numpy(x).cuda(), dtype=FORMATS[fmt])
     q, s = F.quantize(x, False, False, fmt)
     assert np.array_equal(_np(m.scale), s) and np.array_equal(_np(m.q), q)
+
+
+@pytest.mark.parametrize("M,N,K", [(1301, 517, 256), (1300, 518, 256), (2000, 1029, 130), (1100, 1152, 256), (130, 70, 300)])
+@pytest.mark.parametrize("pad,first", [(0, 0), (1, 0), (2, 0), (3, 1), (6, 2), (8, 0)])
+@pytest.mark.parametrize("tiles", [False, True])
+def test_product_into_rows_of_any_alignment_is_exact(dslib, M, N, K, pad, first, tiles):
+    """Small integers, whose sums are exact in any order, into rows that start at any element, with bias and add."""
+    g = torch.Generator(device="cuda").manual_seed(M + N + pad)
+    ints = lambda r, c, n: torch.randint(-n, n + 1, (r, c), device="cuda", generator=g).float()
+    x, w, bias, add = ints(M, K, 2), ints(N, K, 2), ints(1, N, 9)[0].contiguous(), ints(M, N, 9)
+    want = x.double() @ w.double().t()
+    ld = (K + 15) // 16 * 16
+
+    def matrix(v, tiled):
+        q = torch.zeros(v.shape[0], ld, device="cuda").to(torch.float8_e4m3fn)
+        q[:, :K] = v.to(torch.float8_e4m3fn)
+        blocks = (-(-v.shape[0] // 128) if tiled else v.shape[0], -(-K // 128))
+        return dslib.F8Matrix(q[:, :K], torch.ones(blocks, device="cuda"), tiles=tiled)
+
+    a, b = matrix(x, False), matrix(w, tiles)
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        for with_bias, with_add in ((False, False), (True, False), (True, True)):
+            room = torch.full((first + M * (N + pad),), 77.0, dtype=dtype, device="cuda")
+            out = room[first:].view(M, N + pad)[:, :N]
+            plus = torch.zeros(first + M * (N + pad), device="cuda")[first:].view(M, N + pad)[:, :N]
+            plus.copy_(add)
+            y = dslib.linear_f8(a, b, bias=bias if with_bias else None, add=plus if with_add else None, out=out)
+            exact = want + (bias if with_bias else 0) + (add if with_add else 0)
+            assert torch.equal(y, exact.to(dtype))
+            assert bool((room[:first] == 77).all()) and bool((room[first:].view(M, N + pad)[:, N:] == 77).all())
