@@ -44,7 +44,7 @@ struct Params {
   int nk;         // blocks of the reduction
   uint32_t idesc;  // formats of the operands, without the tile's shape
   int type;       // of y
-  int scale4;     // rows of scales are aligned for loads of four
+  int aligned;    // how many scales of a row a load may take: 8, 4 or 1
   int vec;        // y's rows are aligned for stores of four values, add's for loads of four
   int pairs;      // ... of two
   long long wait_cycles;
@@ -393,29 +393,36 @@ struct Ring {
   }
 };
 
-// The scales of PER rows on their way to shared memory, GROUP blocks of the reduction at a time.
+// The scales of PER rows on their way to shared memory, GROUP blocks of the reduction at a time (4 or 8).
 template <int PER, int GROUP>
 struct ScaleFeed {
   const float* src[PER];  // at a row's first block; NULL: no such row, and zeros in its products
   float next[PER][GROUP];
-  __device__ __forceinline__ void load(int i0, int nk, bool vec) {
+  // aligned: how many scales a load may take, 8, 4 or 1
+  __device__ __forceinline__ void load(int i0, int nk, int aligned) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
 #pragma unroll
       for (int b = 0; b < GROUP; ++b) next[i][b] = 0.f;
       if (src[i] == nullptr) continue;
-      if (vec && nk - i0 >= GROUP) {
-        if constexpr (GROUP == 4) {
-          const float4 f = *reinterpret_cast<const float4*>(src[i] + i0);
-          next[i][0] = f.x, next[i][1] = f.y, next[i][2] = f.z, next[i][3] = f.w;
-        } else {
-          const float2 f = *reinterpret_cast<const float2*>(src[i] + i0);
-          next[i][0] = f.x, next[i][1] = f.y;
-        }
-      } else {
+      if (GROUP == 8 && aligned == 8 && nk - i0 >= 8) {
+        float* v = next[i];
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[GROUP - 4]), "=f"(v[GROUP - 3]),
+                       "=f"(v[GROUP - 2]), "=f"(v[GROUP - 1])
+                     : "l"(src[i] + i0));
+        continue;
+      }
 #pragma unroll
-        for (int b = 0; b < GROUP; ++b)
-          if (i0 + b < nk) next[i][b] = src[i][i0 + b];
+      for (int h = 0; h < GROUP; h += 4) {
+        if (aligned >= 4 && nk - i0 >= h + 4) {
+          const float4 f = *reinterpret_cast<const float4*>(src[i] + i0 + h);
+          next[i][h] = f.x, next[i][h + 1] = f.y, next[i][h + 2] = f.z, next[i][h + 3] = f.w;
+        } else {
+#pragma unroll
+          for (int b = h; b < h + 4; ++b)
+            if (i0 + b < nk) next[i][b] = src[i][i0 + b];
+        }
       }
     }
   }
@@ -561,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
         feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld + kb0;
       }
     }
-    const bool vec = P.scale4 && kb0 % 4 == 0;
+    const int vec = kb0 % 4 == 0 ? P.aligned : 1;
     feed.load(0, nk, vec);
     Ring<STAGES> st;
     Ring<Shared<BN>::SLOTS> sc;
@@ -674,8 +681,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // A block's products take 512 cycles; what the adding warps do for it has to
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
 // shared memory 40: a second barrier per block for the scales made it 1100.
-// Measured at 8192 x 4096 x 4096: 137 us (2.00 PFLOP/s) with a scale per 128
-// rows of w, 185 us (1.49) with one per row, where the adding warps multiply
+// Measured at 8192 x 4096 x 4096: 136 us (2.02 PFLOP/s) with a scale per 128
+// rows of w, 175 us (1.57) with one per row, where the adding warps multiply
 // twice and the scales' loads compete with them for the path to shared memory
 // (169 us without these loads, 139 with a scale per 128 rows in their place).
 // Tiles of half the width take two thirds of the time: 512 x 2048 x 4096 with a
@@ -818,9 +825,11 @@ __global__ void __launch_bounds__(BigCfg<COLS, N>::THREADS, 1)
       umma_commit(&sh->done);
       mbar_drain(&sh->done, 0u);
     } else if (warp >= 2) {
-      // Scales: thread j holds rows j, j + SPAN .. of the tile's 128 rows of x and 256 of w (or the 2 scales that these
-      // share), of four blocks at a time; the next four are on their way while these are written.
-      constexpr int SPAN = 32 * Cfg::SCALE_WARPS, USED = COLS ? Cfg::SCALE_ROWS : ROWS + N / 128, GROUP = 4;
+      // Scales: thread j holds rows j, j + SPAN .. of the tile's 128 rows of x and N of w (or the scales that these
+      // share), of four blocks at a time; the next four are on their way while these are written.  Where the rows of w
+      // have their own, a load of eight costs the path to shared memory half as much; it is waited for, which the
+      // blocks ahead in the ring hide (175 us at 8192 x 4096 x 4096, 182 with four).
+      constexpr int SPAN = 32 * Cfg::SCALE_WARPS, USED = COLS ? Cfg::SCALE_ROWS : ROWS + N / 128, GROUP = COLS ? 8 : 4;
       constexpr int PER = (USED + SPAN - 1) / SPAN;
       const int j = threadIdx.x - 64;
       ScaleFeed<PER, GROUP> feed;
@@ -842,20 +851,26 @@ __global__ void __launch_bounds__(BigCfg<COLS, N>::THREADS, 1)
       Ring<BIG_STAGES> st;
       uint32_t it = 0;
       bool ok = true;
-      point(blockIdx.x);
-      feed.load(0, nk, P.scale4);
+      if constexpr (!COLS) {
+        point(blockIdx.x);
+        feed.load(0, nk, P.aligned);
+      }
       for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+        if constexpr (COLS) point(t);
         for (int i0 = 0; i0 < nk && ok; i0 += GROUP) {
           float v[PER][GROUP];
+          if constexpr (COLS) feed.load(i0, nk, P.aligned);
 #pragma unroll
           for (int i = 0; i < PER; ++i)
 #pragma unroll
             for (int b = 0; b < GROUP; ++b) v[i][b] = feed.next[i][b];
-          if (i0 + GROUP < nk) {
-            feed.load(i0 + GROUP, nk, P.scale4);
-          } else if (t + gridDim.x < ntiles) {
-            point(t + gridDim.x);
-            feed.load(0, nk, P.scale4);
+          if constexpr (!COLS) {
+            if (i0 + GROUP < nk) {
+              feed.load(i0 + GROUP, nk, P.aligned);
+            } else if (t + gridDim.x < ntiles) {
+              point(t + gridDim.x);
+              feed.load(0, nk, P.aligned);
+            }
           }
 #pragma unroll
           for (int b = 0; b < GROUP; ++b) {
@@ -1087,8 +1102,11 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
   p.pairs = reinterpret_cast<uintptr_t>(l.y) % (2 * size) == 0 && l.ldy % 2 == 0 &&
             (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 8 == 0 && l.ld_add % 2 == 0));
   const bool wide = p.vec && reinterpret_cast<uintptr_t>(l.y) % (8 * size) == 0 && l.ldy % 8 == 0;
-  p.scale4 = reinterpret_cast<uintptr_t>(p.x.s) % 16 == 0 && p.x.ld % 4 == 0 &&
-             reinterpret_cast<uintptr_t>(p.w.s) % 16 == 0 && p.w.ld % 4 == 0;
+  auto aligned = [&](int n) {
+    return reinterpret_cast<uintptr_t>(p.x.s) % (4 * n) == 0 && p.x.ld % n == 0 &&
+           reinterpret_cast<uintptr_t>(p.w.s) % (4 * n) == 0 && p.w.ld % n == 0;
+  };
+  p.aligned = aligned(8) ? 8 : (aligned(4) ? 4 : 1);
   p.wait_cycles = f8_wait_cycles();
   const Plan plan = plan_of(p, wide);
   CUtensorMap mw = {}, mx = {};  // an empty reduction loads nothing
