@@ -60,6 +60,28 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, const __half*) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Pairs of float32 in one 64-bit register: two multiplications per instruction.
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float& lo, float& hi) {
+  lo = __uint_as_float((uint32_t)v);
+  hi = __uint_as_float((uint32_t)(v >> 32));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Eight 16-bit values at any address: by the widest accesses that it allows.  Rows an odd number of values apart start
 // anywhere; the branches go the same way for a whole row.
 __device__ __forceinline__ uint4 load16(const void* p) {
@@ -98,6 +120,7 @@ __device__ __forceinline__ void store16(void* p, uint4 u) {
 // is less code.
 template <typename T>
 struct Raw8 {
+  static constexpr bool PAIRS = true;
   uint4 u;
   template <bool ODD = false>
   __device__ __forceinline__ void load(const T* p, int n, bool vec) {
@@ -123,6 +146,7 @@ struct Raw8 {
 };
 template <>
 struct Raw8<float> {
+  static constexpr bool PAIRS = true;
   float4 a, b;
   template <bool ODD = false>
   __device__ __forceinline__ void load(const float* p, int n, bool vec) {
@@ -238,8 +262,37 @@ __device__ __forceinline__ uint32_t f8x4(float a, float b, float c, float d, flo
   return f8x2<E5M2>(f8_unit<CHECK>(a, inv), f8_unit<CHECK>(b, inv)) |
          (f8x2<E5M2>(f8_unit<CHECK>(c, inv), f8_unit<CHECK>(d, inv)) << 16);
 }
+// Two rows' 8-bit values of eight columns with a factor each, by columns: the low half of two[j] is column j.
 template <bool E5M2, bool CHECK>
+__device__ __forceinline__ void f8_columns(const float a[8], const float b[8], const float inv[8], uint32_t two[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    if constexpr (CHECK) {
+#pragma unroll
+      for (int k = j; k < j + 2; ++k) two[k] = f8x2<E5M2>(f8_unit<true>(a[k], inv[k]), f8_unit<true>(b[k], inv[k]));
+    } else {
+      const uint64_t f = pair(inv[j], inv[j + 1]);
+      float a0, a1, b0, b1;
+      unpair(mul2(pair(a[j], a[j + 1]), f), a0, a1);
+      unpair(mul2(pair(b[j], b[j + 1]), f), b0, b1);
+      two[j] = f8x2<E5M2>(a0, b0);
+      two[j + 1] = f8x2<E5M2>(a1, b1);
+    }
+  }
+}
+// PAIRS: two multiplications per instruction, for which values lie in pairs of registers.
+template <bool E5M2, bool CHECK, bool PAIRS = true>
 __device__ __forceinline__ uint2 f8x8(const float v[8], float inv) {
+  if constexpr (!CHECK && PAIRS) {
+    uint32_t q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      unpair(mul2(pair(v[2 * j], v[2 * j + 1]), pair(inv, inv)), lo, hi);
+      q[j] = f8x2<E5M2>(lo, hi);
+    }
+    return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+  }
   return make_uint2(f8x4<E5M2, CHECK>(v[0], v[1], v[2], v[3], inv), f8x4<E5M2, CHECK>(v[4], v[5], v[6], v[7], inv));
 }
 // The address is 8-byte aligned: rows start 16 bytes apart or a multiple of it.

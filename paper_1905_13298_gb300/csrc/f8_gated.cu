@@ -17,9 +17,9 @@
 // an SM's registers, so no second CTA can hide the first one's reads: TMA
 // brings the next tile to shared memory while this one is rounded and stored.
 //
-// Measured in bf16: forward 4095 x 8200 with the checkpoint 47 us (5.0 TB/s;
+// Measured in bf16: forward 4095 x 8200 with the checkpoint 46 us (5.2 TB/s;
 // most of the rest is instructions, half of them conversions and maxima), 8192
-// x 4096 without it 37 us (4.6 TB/s); backward 8192 x 8192 142 us (4.4 TB/s, 57% of
+// x 4096 without it 37 us (4.6 TB/s); backward 8192 x 8192 140 us (4.4 TB/s, 57% of
 // the issue slots: a tile's phases, maxima, scales, rounding and turning, are
 // parted by barriers that nothing else on the SM fills).
 #include <type_traits>
@@ -44,6 +44,11 @@ __device__ __forceinline__ float sigmoid(float g) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
   return r;
+}
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
+  float a, b;
+  unpair(g, a, b);
+  return pair(sigmoid(a), sigmoid(b));
 }
 
 // Two rows of a unit (a block of 128 features) at a time: with the checkpoint six blocks, whose scales six lanes make.
@@ -78,7 +83,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 8 : 6)
       rg[i].get(g);
       ru[i].get(u);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a[i][j] = g[j] * sigmoid(g[j]) * u[j];
+      for (int j = 0; j < 8; j += 2) {
+        const uint64_t gj = pair(g[j], g[j + 1]);
+        unpair(mul2(mul2(gj, sigmoid2(gj)), pair(u[j], u[j + 1])), a[i][j], a[i][j + 1]);
+      }
       mx[i] = amax8(a[i]);
       mx[2 + i] = ckpt.q ? amax8(g) : 0.f;
       mx[4 + i] = ckpt.q ? amax8(u) : 0.f;
@@ -187,8 +195,11 @@ __device__ __forceinline__ void turn_patch(uint8_t* turned, const float* col_inv
   const float4 hi = *reinterpret_cast<const float4*>(&col_inv[tc * 8 + 4]);
   const float inv[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
   uint32_t* to = reinterpret_cast<uint32_t*>(&turned[tc * 8 * 128 + (((tr >> 1) ^ tc) << 3) + ((tr & 1) << 2)]);
+  uint32_t low[8], high[8];
+  f8_columns<E5M2, CHECK>(v[0], v[1], inv, low);
+  f8_columns<E5M2, CHECK>(v[2], v[3], inv, high);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) to[j * 32] = f8x4<E5M2, CHECK>(v[0][j], v[1][j], v[2][j], v[3][j], inv[j]);
+  for (int j = 0; j < 8; ++j) to[j * 32] = low[j] | high[j] << 16;
 }
 
 template <typename T>
@@ -265,12 +276,14 @@ __global__ void __launch_bounds__(kTileThreads, 1)
       }
       const float sg = sm.scale[turn][0][row], su = sm.scale[turn][1][row];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float gj = g[j] * sg, uj = u[j] * su;
-        const float sig = sigmoid(gj), act = gj * sig;
-        a[i][j] = act * uj;
-        du[i][j] = d[j] * act;
-        dg[i][j] = d[j] * uj * fmaf(act, 1.f - sig, sig);  // sig (1 + g (1 - sig))
+      for (int j = 0; j < 8; j += 2) {  // two columns per instruction
+        const uint64_t gj = mul2(pair(g[j], g[j + 1]), pair(sg, sg)), uj = mul2(pair(u[j], u[j + 1]), pair(su, su));
+        const uint64_t dj = pair(d[j], d[j + 1]), sig = sigmoid2(gj), act = mul2(gj, sig);
+        unpair(mul2(act, uj), a[i][j], a[i][j + 1]);
+        unpair(mul2(dj, act), du[i][j], du[i][j + 1]);
+        // sig (1 + g (1 - sig))
+        const uint64_t slope = fma2(act, fma2(sig, pair(-1.f, -1.f), pair(1.f, 1.f)), sig);
+        unpair(mul2(mul2(dj, uj), slope), dg[i][j], dg[i][j + 1]);
       }
     }
     const int cols = features - c_tile >= kF8Block ? kF8Block : (int)(features - c_tile);

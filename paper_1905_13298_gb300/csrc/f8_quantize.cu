@@ -39,6 +39,7 @@ struct SourceFloat {
 // Eight 8-bit values and their scale, decoded where they are used: an eighth of the registers of the values.
 template <bool E5M2>
 struct RawF8 {
+  static constexpr bool PAIRS = false;  // in tiles they would not fit in the registers (24 us, 27 with pairs)
   uint2 u;
   float s;
   __device__ __forceinline__ void get(float v[8]) const {
@@ -168,7 +169,7 @@ __device__ __forceinline__ void write_rows(const Raw (&raw)[8], float row_max, c
     const float inv = of_lane(s.inv, i);
     float v[8];
     raw[i].get(v);
-    const uint2 q = f8x8<E5M2, CHECK>(v, inv);
+    const uint2 q = f8x8<E5M2, CHECK, Raw::PAIRS>(v, inv);
     if (!CHECK)
       *reinterpret_cast<uint2*>(p) = q;
     else if (i < t.m && t.n > 0)
