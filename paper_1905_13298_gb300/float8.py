@@ -66,9 +66,10 @@ class F8Matrix:
             raise ValueError(f"dtype must be torch.float8_e4m3fn or torch.float8_e5m2, got {dtype}")
         m = cls.__new__(cls)
         ld, nb = (cols + 15) // 16 * 16, (cols + BLOCK - 1) // BLOCK
-        m.q = torch.empty((rows, ld), dtype=dtype, device=device)
-        if ld != cols:
-            m.q = m.q[:, :cols]
+        if ld == cols:
+            m.q = torch.empty((rows, cols), dtype=dtype, device=device)
+        else:
+            m.q = torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device)
         m.scale = torch.empty(((rows + BLOCK - 1) // BLOCK if tiles else rows, nb), dtype=torch.float32, device=device)
         m.desc = ds_f8_matrix(m.q.data_ptr(), m.scale.data_ptr(), rows, cols, ld, nb, fmt,
                               DS_F8_TILES if tiles else DS_F8_ROWS)
