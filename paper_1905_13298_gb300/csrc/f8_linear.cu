@@ -1012,8 +1012,8 @@ cudaError_t launch(const CUtensorMap& mw, const CUtensorMap& mx, const Params& p
 // 16, 32, 64, 1.6 times the latter where two CTAs share an SM; to that come 0.6 for each CTA of an SM in turn, and 0.4
 // (0.6) for a cluster (of 8).  Splitting a reduction divides the blocks of a CTA and multiplies the CTAs; a cluster of 8
 // finds room for 27 / 32 of the CTAs that would fit one by one.  Stores of rows that are not aligned add 0.013 a column
-// of a tile (0.02 in the small kernel; 4096 x 1024 x 4097 takes 44 us, 31 with 4096 columns).  The choice takes 0.6%
-// more than the best of all on average, 21% at most.
+// of a tile (0.02 in the small kernel; 4096 x 1024 x 4097 takes 44 us, 31 with 4096 columns).  The choice takes 0.5%
+// more than the best of all on average, 24% at most.
 struct Plan {
   int bn, split, big;  // big: rows of w per tile of the large kernel, or 0
 };
