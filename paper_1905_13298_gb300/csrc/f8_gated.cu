@@ -17,11 +17,11 @@
 // an SM's registers, so no second CTA can hide the first one's reads: TMA
 // brings the next tile to shared memory while this one is rounded and stored.
 //
-// Measured in bf16: forward 4095 x 8200 with the checkpoint 46 us (5.2 TB/s;
-// most of the rest is instructions, half of them conversions and maxima), 8192
-// x 4096 without it 37 us (4.6 TB/s); backward 8192 x 8192 140 us (4.4 TB/s, 57% of
-// the issue slots: a tile's phases, maxima, scales, rounding and turning, are
-// parted by barriers that nothing else on the SM fills).
+// Measured in bf16: forward 4095 x 8200 with the checkpoint 54 us (4.4 TB/s;
+// bound by instructions, a third of them the sigmoid's and half conversions
+// and maxima), 8192 x 4096 without it 44 us (3.8 TB/s); backward 8192 x 8192
+// 160 us (3.9 TB/s: a tile's phases, sigmoid, maxima, scales, rounding and
+// turning, are parted by barriers that nothing else on the SM fills).
 #include <type_traits>
 
 #include "f8_common.cuh"
@@ -37,19 +37,24 @@ constexpr int kThreads = 128;
 constexpr int kTileThreads = 512;
 constexpr int kTileWarps = kTileThreads / 32;
 
-// sig(g) = 1 / (1 + 2^(-g log2 e)) by the special-function unit (each within 2 steps of 2^-23, and the rounding of the
-// exponent adds |g| 2^-24): 2^x is inf or 0 far out, and the quotient then 0 or 1, as it should be.  The relative error
-// of g sig(g) is 5.7e-8 in the mean square over normal g; by expf and a division it is 5.0e-8.
-__device__ __forceinline__ float sigmoid(float g) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+__device__ __forceinline__ float rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+// sig(g) = z / (1 + z) or 1 / (1 + z) with z = e^-|g|, as exact as an exponential, a sum and a quotient in float32: 1 + z
+// is 1 .. 2, and the quotient by its approximate reciprocal is corrected by the remainder.  2^x of the special-function
+// unit alone would take 15% less time in all (gate 4095 x 8200 46 us), but the rounding of x = -|g| log2 e costs |g| 2^-24:
+// g sig(g) in the mean square 1.7e-6 off at g = -86 .. -60, 5e-8 here.
 __device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
-  float a, b;
-  unpair(g, a, b);
-  return pair(sigmoid(a), sigmoid(b));
+  float g0, g1, d0, d1;
+  unpair(g, g0, g1);
+  const float z0 = expf(-fabsf(g0)), z1 = expf(-fabsf(g1));
+  const uint64_t minus_d = fma2(pair(z0, z1), both(-1.f), both(-1.f));
+  unpair(minus_d, d0, d1);
+  const uint64_t n = pair(g0 < 0.f ? z0 : 1.f, g1 < 0.f ? z1 : 1.f), r = pair(rcp(-d0), rcp(-d1)), q = mul2(n, r);
+  return fma2(fma2(minus_d, q, n), r, q);
 }
 
 // Two rows of a unit (a block of 128 features) at a time: with the checkpoint six blocks, whose scales six lanes make.
