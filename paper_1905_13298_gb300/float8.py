@@ -1,5 +1,7 @@
 """Tensor-level helpers of the 8-bit floating-point operators (see the header's section on them).
 
+Calls run on the current stream, or on ``stream`` (a torch stream or a handle), to which what they return then belongs.
+
 An ``F8Matrix`` holds 8-bit values and their scales, one per block of 128.  The helpers check what the C ABI cannot
 see (dtype, shape, strides, device), allocate outputs with torch, and make one call each.
 
@@ -156,11 +158,19 @@ def _vector(t, name: str, n: int, device: int):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _on_stream(stream, device: int):
-    """The caller's stream, or the current one of the tensors' device (by torch's short way where it has one)."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(device)
-    return _stream(stream)
+def _on_stream(device: int):
+    """The current stream of the tensors' device (by torch's short way where it has one)."""
+    return _raw_stream(device) if _raw_stream is not None else _stream(None)
+
+
+def _given(stream):
+    """Makes the caller's stream (a torch stream, or a handle) current: a call's outputs and its workspace then belong to
+    it, so none of that memory is still in use, or used again, by the work of another stream.  As for anything made on a
+    stream, the caller orders the inputs before the call and the use of the results on other streams behind it."""
+    if isinstance(stream, int):
+        # 1 is CUDA's other name of the default stream
+        stream = torch.cuda.default_stream() if stream in (0, 1) else torch.cuda.ExternalStream(stream)
+    return torch.cuda.stream(stream)
 
 
 def _f8(m, name: str):
@@ -177,6 +187,9 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
     its transpose [cols, rows]; returns (result, transpose), made in one pass over x.  ``pow2`` rounds scales up to
     powers of two.
     """
+    if stream is not None:
+        with _given(stream):
+            return quantize_f8(x, blocks, transposed, pow2, dtype)
     for b in (blocks, transposed):
         if b is not None and b not in _BLOCKS:
             raise ValueError(f"blocks are 'rows', 'tiles' or None, got {b!r}")
@@ -196,7 +209,7 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
     out_t = F8Matrix.empty(cols, rows, device, dtype, transposed == "tiles") if transposed else None
     d, d_t = out.desc if out else None, out_t.desc if out_t else None
     flags = DS_F8_POW2 if pow2 else 0
-    stream = _on_stream(stream, device.index)
+    stream = _on_stream(device.index)
     if is_f8:
         _check(lib().ds_requantize_f8(x.desc, d, d_t, flags, stream))
     else:
@@ -206,8 +219,11 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
 
 def expand_shift_weights_f8(w, stream=None) -> F8Matrix:
     """The weights s * 2^p of a PackedShiftWeights as an e4m3 matrix in tiles (exact: q = s * 2^(p + 8), scales 2^-8)."""
+    if stream is not None:
+        with _given(stream):
+            return expand_shift_weights_f8(w)
     m = F8Matrix.empty(w.n_out, w.k_red, w.blob.device, tiles=True)
-    ds_expand_shift_weights_f8(w.desc, m.desc, stream)
+    ds_expand_shift_weights_f8(w.desc, m.desc)
     return m
 
 
@@ -215,6 +231,9 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
     """y = x @ w^T + bias + add for 8-bit x [M, K] and w [N, K]: a tensor [M, N] of ``dtype`` (or ``out``'s).
 
     ``bias`` is float32 [N], ``add`` float32 [M, N]; ``out`` may be ``add`` itself, which then accumulates."""
+    if stream is not None:
+        with _given(stream):
+            return linear_f8(x, w, bias, add, out, dtype)
     dx, dw = _f8(x, "x"), _f8(w, "w")
     M, N = dx.rows, dw.rows
     device = x.q.get_device()
@@ -231,7 +250,7 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
         py, ldy = _like(y, "out", M, N, y.dtype, device)
     pa, ld_add = _like(add, "add", M, N, torch.float32, device)
     _check(lib().ds_linear_f8(dx, dw, _vector(bias, "bias", N, device), pa, ld_add, py, _TYPES[y.dtype], ldy,
-                              _on_stream(stream, device)))
+                              _on_stream(device)))
     return y
 
 
@@ -241,6 +260,9 @@ def rmsnorm_f8(x, weight, residual=None, eps: float = 1e-5, pow2: bool = False, 
 
     Returns (n, h, rstd): the F8Matrix of h * rstd * weight, h in x's dtype (x itself without a residual, ``h`` where
     given; it may be x or residual), and the float32 reciprocal root mean squares that the backward pass reads."""
+    if stream is not None:
+        with _given(stream):
+            return rmsnorm_f8(x, weight, residual, eps, pow2, dtype, h)
     ldx = _matrix(x, "x")
     rows, cols = x.shape
     device, kind = _on_gpu(x, "x"), x.dtype
@@ -256,7 +278,7 @@ def rmsnorm_f8(x, weight, residual=None, eps: float = 1e-5, pow2: bool = False, 
     n = F8Matrix.empty(rows, cols, x.device, dtype)
     rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib().ds_rmsnorm_f8(x.data_ptr(), ldx, pr, ldr, pw, _TYPES[kind], rows, cols, eps, n.desc, ph, ldh,
-                               rstd.data_ptr(), DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
+                               rstd.data_ptr(), DS_F8_POW2 if pow2 else 0, _on_stream(device)))
     return n, h, rstd
 
 
@@ -264,6 +286,9 @@ def rmsnorm_f8_backward(dy, h, rstd, weight, dh=None, out=None, stream=None):
     """Backward pass of rmsnorm_f8: (dx, dweight) from the gradient dy of the norm (the rounding to 8 bits passes it
     unchanged), what the forward pass returned, and the gradient dh that the stream h brings (or None).  dx is the
     gradient of x and of residual alike; ``out`` may be dy, h or dh."""
+    if stream is not None:
+        with _given(stream):
+            return rmsnorm_f8_backward(dy, h, rstd, weight, dh, out)
     lddy = _matrix(dy, "dy")
     rows, cols = dy.shape
     device, kind = _on_gpu(dy, "dy"), dy.dtype
@@ -279,7 +304,7 @@ def rmsnorm_f8_backward(dy, h, rstd, weight, dh=None, out=None, stream=None):
     nbytes = lib().ds_rmsnorm_f8_backward_workspace_bytes(rows, cols)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dy.device)
     _check(lib().ds_rmsnorm_f8_backward(dy.data_ptr(), lddy, ph, ldh, pr, pw, pdh, lddh, _TYPES[kind], rows, cols, pdx,
-                                        lddx, dw.data_ptr(), ws.data_ptr(), nbytes, _on_stream(stream, device)))
+                                        lddx, dw.data_ptr(), ws.data_ptr(), nbytes, _on_stream(device)))
     return dx, dw
 
 
@@ -292,6 +317,9 @@ def gated_f8(gu, features: int, checkpoint: bool = True, pow2: bool = False, dty
     """a = silu(g) * u in 8 bits, for gu [rows, up + features] with g in columns [0, features) and u from column
     up = features rounded up to a multiple of 128.  Returns (a, kept): kept is the 8-bit checkpoint of gu that
     gated_f8_backward reads (None without ``checkpoint``)."""
+    if stream is not None:
+        with _given(stream):
+            return gated_f8(gu, features, checkpoint, pow2, dtype)
     ld = _matrix(gu, "gu")
     rows, width = gu.shape
     if features <= 0 or width != _gate_width(features):
@@ -300,7 +328,7 @@ def gated_f8(gu, features: int, checkpoint: bool = True, pow2: bool = False, dty
     a = F8Matrix.empty(rows, features, gu.device, dtype)
     kept = F8Matrix.empty(rows, width, gu.device, dtype) if checkpoint else None
     _check(lib().ds_gated_f8(gu.data_ptr(), _TYPES[gu.dtype], ld, rows, features, a.desc,
-                             kept.desc if kept else None, DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
+                             kept.desc if kept else None, DS_F8_POW2 if pow2 else 0, _on_stream(device)))
     return a, kept
 
 
@@ -309,6 +337,9 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     """Backward pass of gated_f8 from its checkpoint and the gradient da [rows, features] of a.  Returns
     (dgu, dgu_t, a_t) in 8 bits: the gradient of gu, its transpose, and the transpose of a made again from the
     checkpoint (the operands of the two weight gradients; None without ``transposed``)."""
+    if stream is not None:
+        with _given(stream):
+            return gated_f8_backward(kept, da, pow2, dtype, transposed)
     dk = _f8(kept, "kept")
     ld = _matrix(da, "da")
     rows, features = da.shape
@@ -320,5 +351,5 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None
     _check(lib().ds_gated_f8_backward(dk, da.data_ptr(), _TYPES[da.dtype], ld, features, dgu.desc,
                                       dgu_t.desc if dgu_t else None, a_t.desc if a_t else None,
-                                      DS_F8_POW2 if pow2 else 0, _on_stream(stream, device)))
+                                      DS_F8_POW2 if pow2 else 0, _on_stream(device)))
     return dgu, dgu_t, a_t
