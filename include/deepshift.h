@@ -53,9 +53,11 @@ typedef enum {
  * cluster sizes) are set once per process, on the device that is current at a
  * kernel's first launch: drive one GPU per process (one process per GPU, as
  * the multi-GPU replicas do).  A launch on a second device from the same
- * process is not supported; it fails with DS_ERR_CUDA rather than computing
- * anything wrong.  The device's SM count, which sizes grids, split
- * reductions and cluster choices, is likewise read once per process. */
+ * process is not supported: kernels that need such an attribute fail with
+ * DS_ERR_CUDA, and every launch goes to the device that is current, so that
+ * device has to be the memory's (the tensor helpers of the 8-bit operators
+ * check it).  The device's SM count, which sizes grids, split reductions and
+ * cluster choices, is likewise read once per process. */
 
 /* Size limits.  Every size the library forms from caller dimensions is
  * bounded before it can overflow 64 bits.  A code matrix holds at most 2^48

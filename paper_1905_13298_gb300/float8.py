@@ -113,11 +113,15 @@ def _row_stride(t, name: str) -> int:
 
 
 def _on_gpu(t, name: str, device: int = -1) -> int:
-    """The tensor's device index: a GPU, and `device` where given."""
+    """The tensor's device index: the current GPU, to which calls go, or `device` where an input has named it."""
     d = t.get_device()
     if d < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if device >= 0 and d != device:
+    if device < 0:
+        device = torch.cuda.current_device()
+        if d != device:
+            raise ValueError(f"{name} is on cuda:{d}, the current device is cuda:{device} (torch.cuda.set_device)")
+    elif d != device:
         raise ValueError(f"{name} is on cuda:{d}, the input on cuda:{device}")
     return d
 
@@ -200,11 +204,12 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
     is_f8 = isinstance(x, F8Matrix)
     if is_f8:
         rows, cols, device = x.desc.rows, x.desc.cols, x.q.device
+        _on_gpu(x.q, "x")
     else:
         ld = _matrix(x, "x")
-        _on_gpu(x, "x")
         rows, cols = x.shape
         device = x.device
+        _on_gpu(x, "x")
     out = F8Matrix.empty(rows, cols, device, dtype, blocks == "tiles") if blocks else None
     out_t = F8Matrix.empty(cols, rows, device, dtype, transposed == "tiles") if transposed else None
     d, d_t = out.desc if out else None, out_t.desc if out_t else None
@@ -222,6 +227,7 @@ def expand_shift_weights_f8(w, stream=None) -> F8Matrix:
     if stream is not None:
         with _given(stream):
             return expand_shift_weights_f8(w)
+    _on_gpu(w.blob, "w")
     m = F8Matrix.empty(w.n_out, w.k_red, w.blob.device, tiles=True)
     ds_expand_shift_weights_f8(w.desc, m.desc)
     return m
@@ -236,7 +242,7 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
             return linear_f8(x, w, bias, add, out, dtype)
     dx, dw = _f8(x, "x"), _f8(w, "w")
     M, N = dx.rows, dw.rows
-    device = x.q.get_device()
+    device = _on_gpu(x.q, "x")
     _on_gpu(w.q, "w", device)
     y = out
     if y is None:
@@ -345,7 +351,7 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     rows, features = da.shape
     if features == 0 or dk.rows != rows or dk.cols != _gate_width(features):
         raise ValueError(f"kept is {dk.rows} x {dk.cols}, expected {rows} x {_gate_width(features)}")
-    device = _on_gpu(da, "da", kept.q.get_device())
+    device = _on_gpu(da, "da", _on_gpu(kept.q, "kept"))
     dgu = F8Matrix.empty(rows, dk.cols, da.device, dtype)
     dgu_t = F8Matrix.empty(dk.cols, rows, da.device, dtype) if transposed else None
     a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None
