@@ -602,8 +602,9 @@ ds_status ds_expand_shift_weights_f8(const ds_weights* w, const ds_f8_matrix* ou
  * x [M][K] and w [N][K], on the tensor cores (tcgen05).  Each operand has its
  * own format and blocks.  Products within a block of 128 k are summed by the
  * tensor core; a block's sum is multiplied by its two scales and added in
- * float32.  So y = x w^T for a layer's forward pass, dy (w_t)^T for its input
- * gradient, and dy_t (x_t)^T for its weight gradient.
+ * float32 (a sum times either scale has to stay within the normal numbers; the
+ * scales' own product need not).  So y = x w^T for a layer's forward pass,
+ * dy (w_t)^T for its input gradient, and dy_t (x_t)^T for its weight gradient.
  *   bias  device float32 [N] or NULL
  *   add   device float32 [M][N], row stride ld_add, or NULL; may be y itself
  *         (DS_TYPE_F32, ldy == ld_add): gradients accumulate in place

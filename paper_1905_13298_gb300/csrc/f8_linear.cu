@@ -6,7 +6,8 @@
 // A block's inner sum is four tcgen05.mma of kind::f8f6f4 (K = 32 each) into
 // an accumulator of its own in tensor memory; it is then read back and added,
 // times its two scales, to float32 sums in registers.  So scales may be any
-// float32 and differ per row, and no sum is held in fewer than 32 bits.
+// float32 and differ per row (a sum times either scale has to stay within the
+// normal numbers), and no sum is held in fewer than 32 bits.
 //
 // linear_f8_kernel lays 128 rows of w along the lanes of tensor memory and BN
 // rows of x along its columns: with one token in flight the weights, which
@@ -17,6 +18,7 @@
 // launch of clusters takes 3), 300 x 1000 x 2050 8.8 us, 128 x 8192 x 4096
 // 15.7 us (2.1 TB/s).
 #include <atomic>
+#include <type_traits>
 
 #include "f8_common.cuh"
 #include "tensor_core.cuh"
@@ -659,10 +661,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(cons
 // A block's products take 512 cycles; what the adding warps do for it has to
 // fit there.  A wait that succeeds costs 85 cycles, an arrival 70, a load from
 // shared memory 40: a second barrier per block for the scales made it 1100.
-// Measured at 8192 x 4096 x 4096: 136 us (2.02 PFLOP/s) with a scale per 128
+// Measured at 8192 x 4096 x 4096: 140 us (1.96 PFLOP/s) with a scale per 128
 // rows of w, 175 us (1.57) with one per row, where the adding warps multiply
 // twice and the scales' loads compete with them for the path to shared memory
-// (169 us without these loads, 139 with a scale per 128 rows in their place).
+// (169 us without these loads).
 // Tiles of half the width take two thirds of the time: 512 x 2048 x 4096 with a
 // scale per 128 rows, 128 of them, 11.0 us, 64 of the others 13.7.
 // ---------------------------------------------------------------------------
@@ -925,19 +927,31 @@ __global__ void __launch_bounds__(BigCfg<COLS, N>::THREADS, 1)
             }
           }
         } else {
-          const float s = scale[32 * q + lane] * scale[ROWS + col0 / 128];
+          // One multiplication per value, by the product of the scales; by one after the other where that leaves the
+          // normal numbers (a sum times both may not), as the other kernels multiply.  The choice costs 2 us of 140.
           uint32_t v[2][16];
           tmem_ld16(taddr, v[0]);
+          const float sx = scale[32 * q + lane], sw = scale[ROWS + col0 / 128], s = sx * sw;
+          auto add_block = [&](auto apart) {
 #pragma unroll
-          for (int c = 0; c < kBigCols / 16; ++c) {
-            tmem_wait_ld();
-            if (c < kBigCols / 16 - 1)
-              tmem_ld16(taddr + 16 * (c + 1), v[(c + 1) & 1]);
-            else
-              release();
+            for (int c = 0; c < kBigCols / 16; ++c) {
+              tmem_wait_ld();
+              if (c < kBigCols / 16 - 1)
+                tmem_ld16(taddr + 16 * (c + 1), v[(c + 1) & 1]);
+              else
+                release();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(__uint_as_float(v[c & 1][j]), s, acc[16 * c + j]);
-          }
+              for (int j = 0; j < 16; ++j) {
+                const float f = __uint_as_float(v[c & 1][j]);
+                acc[16 * c + j] = decltype(apart)::value ? fmaf(f * sx, sw, acc[16 * c + j]) : fmaf(f, s, acc[16 * c + j]);
+              }
+            }
+          };
+          const uint32_t exponent = __float_as_uint(s) & 0x7F800000u;
+          if (__all_sync(0xFFFFFFFFu, exponent - 0x00800000u < 0x7F000000u))
+            add_block(std::false_type());
+          else
+            add_block(std::true_type());
         }
       }
       int m0, n0;
