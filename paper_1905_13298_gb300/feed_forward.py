@@ -51,7 +51,7 @@ class GatedFeedForward:
 
     def forward(self, x, stream):
         """(y, h, saved) for x and the residual stream, both [tokens, hidden]."""
-        n, h, rstd = rmsnorm_f8(x, self.norm, residual=stream)
+        n, h, rstd = rmsnorm_f8(x, self.norm, residual=stream, pow2=True)
         a, kept = gated_f8(linear_f8(n, self.w_gate_up, dtype=x.dtype), self.features)
         return linear_f8(a, self.w_down, dtype=x.dtype), h, (n, h, rstd, kept)
 
@@ -61,7 +61,8 @@ class GatedFeedForward:
         n, h, rstd, kept = saved
         d, d_t = quantize_f8(dy, "rows", "rows")
         dgu, dgu_t, a_t = gated_f8_backward(kept, linear_f8(d, self.w_down_t, dtype=dy.dtype))
-        _, n_t = quantize_f8(n, None, "tiles")  # a right operand in tiles takes the faster product
+        # a right operand in tiles takes the faster product; with scales that are powers of two the values stay as they are
+        _, n_t = quantize_f8(n, None, "tiles", pow2=True)
         g = grads or {}
         down = linear_f8(d_t, a_t, add=g.get("down"), out=g.get("down"), dtype=torch.float32)
         gate_up = linear_f8(dgu_t, n_t, add=g.get("gate_up"), out=g.get("gate_up"), dtype=torch.float32)
@@ -72,7 +73,7 @@ class GatedFeedForward:
 
     def token(self, x, stream):
         """(y, h) for a few tokens while serving."""
-        n, h, _ = rmsnorm_f8(x, self.norm, residual=stream)
+        n, h, _ = rmsnorm_f8(x, self.norm, residual=stream, pow2=True)
         a, _ = gated_f8(linear_f8(n, self.w_gate_up, dtype=x.dtype), self.features, checkpoint=False)
         return linear_f8(a, self.w_down, dtype=x.dtype), h
 

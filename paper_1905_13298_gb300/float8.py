@@ -7,7 +7,8 @@ see (dtype, shape, strides, device), allocate outputs with torch, and make one c
 
 A training step of a gated feed-forward block reads::
 
-    n, h, rstd = rmsnorm_f8(x, norm_w, residual=stream)        # 8-bit rows of the norm, the new residual stream
+    # 8-bit rows of the norm, the new residual stream; powers of two, since the blocks of n change below
+    n, h, rstd = rmsnorm_f8(x, norm_w, residual=stream, pow2=True)
     gu = linear_f8(n, w_gu)                                    # w_gu: quantize_f8(weight, "tiles", "tiles")[0]
     a, kept = gated_f8(gu, features)                           # only `kept` is needed again
     y = linear_f8(a, w_down)
@@ -16,7 +17,7 @@ A training step of a gated feed-forward block reads::
     da = linear_f8(d, w_down_t)
     dgu, dgu_t, a_t = gated_f8_backward(kept, da)
     grad_down = linear_f8(d_t, a_t, add=grad_down, out=grad_down, dtype=torch.float32)
-    n_t = quantize_f8(n, None, "tiles")[1]
+    n_t = quantize_f8(n, None, "tiles", pow2=True)[1]          # n's values, turned, not rounded again
     grad_gu = linear_f8(dgu_t, n_t, add=grad_gu, out=grad_gu, dtype=torch.float32)
     dx, grad_norm = rmsnorm_f8_backward(linear_f8(dgu, w_gu_t), h, rstd, norm_w, dh=dy)
 """

@@ -1,4 +1,4 @@
-"""The 8-bit gate against float32 arithmetic."""
+"""The 8-bit gate against float32 arithmetic, and what the feed-forward block built from the operators promises."""
 import pytest
 import torch
 
@@ -22,3 +22,31 @@ def test_gate_is_as_exact_as_the_formula_in_float32(dslib, low, high):
     rms = lambda got: float(((got.double() - want) / want)[big].square().mean().sqrt())
     assert float(big.float().mean()) > 0.8
     assert rms(a.scale) <= 1.03 * rms(plain)
+
+
+def test_block_rounds_the_norm_once(dslib, monkeypatch):
+    """The operand of the weight gradient holds the values of the forward pass, turned: changing the blocks of the norm's
+    output rounds nothing but values below the format's range."""
+    from paper_1905_13298_gb300 import feed_forward
+    seen = []
+
+    def watch(x, *args, **kw):
+        got = quantize(x, *args, **kw)
+        if isinstance(x, dslib.F8Matrix):
+            seen.append((x, got[1]))
+        return got
+
+    quantize = feed_forward.quantize_f8
+    r = torch.Generator(device="cuda").manual_seed(9)
+    T, H, Fe = 300, 264, 200
+    b = feed_forward.GatedFeedForward(H, Fe, seed=7)
+    monkeypatch.setattr(feed_forward, "quantize_f8", watch)
+    x, s, dy, dh = (torch.randn((T, H), generator=r, device="cuda").to(torch.bfloat16) for _ in range(4))
+    y, h, saved = b.forward(x, s)
+    b.backward(dy, dh, saved)
+    (n, n_t), = seen
+    v, v_t = n.dequantize(), n_t.dequantize().t()
+    # the smallest normal number of e4m3 in a tile's units
+    least = 2.0**-6 * n_t.scale.repeat_interleave(128, 0)[:H].repeat_interleave(128, 1)[:, :T].t()
+    assert bool((v.abs() >= least).float().mean() > 0.9)
+    assert bool(((v == v_t) | (v.abs() < least)).all())
