@@ -44,10 +44,13 @@ class GatedFeedForward:
         self.w_down, self.w_down_t = quantize_f8(self.down, "tiles", "tiles")
 
     def use_shift_weights(self) -> None:
-        """Serves with the weights s * 2^p of the power-of-two quantizer (Eq. 4-6; magnitudes above 1 become 1), which are
-        exact as 8-bit tiles.  The transposes, and so training, keep the float weights' rounding."""
+        """Takes the weights s * 2^p of the power-of-two quantizer (Eq. 4-6; magnitudes above 1 become 1), which are exact
+        as 8-bit tiles, and so are their transposes: gradients are those of the shift weights (passed on to the masters,
+        as the paper's straight-through estimate does).  ``refresh`` and ``step`` go back to rounded float weights."""
         self.w_gate_up = expand_shift_weights_f8(pack_shift_weights(*quantize_shift_weights(self.gate_up)))
         self.w_down = expand_shift_weights_f8(pack_shift_weights(*quantize_shift_weights(self.down)))
+        self.w_gate_up_t = quantize_f8(self.w_gate_up, None, "tiles", pow2=True)[1]
+        self.w_down_t = quantize_f8(self.w_down, None, "tiles", pow2=True)[1]
 
     def forward(self, x, stream):
         """(y, h, saved) for x and the residual stream, both [tokens, hidden]."""

@@ -50,3 +50,25 @@ def test_block_rounds_the_norm_once(dslib, monkeypatch):
     least = 2.0**-6 * n_t.scale.repeat_interleave(128, 0)[:H].repeat_interleave(128, 1)[:, :T].t()
     assert bool((v.abs() >= least).float().mean() > 0.9)
     assert bool(((v == v_t) | (v.abs() < least)).all())
+
+
+def test_block_with_shift_weights_has_their_gradients(dslib):
+    """After use_shift_weights the transposes are those of the shift weights, exactly, and so is the input's gradient."""
+    from paper_1905_13298_gb300.feed_forward import GatedFeedForward
+    T, H, Fe = 256, 256, 200
+    b = GatedFeedForward(H, Fe, seed=7)
+    b.use_shift_weights()
+    for m, m_t in ((b.w_gate_up, b.w_gate_up_t), (b.w_down, b.w_down_t)):
+        assert torch.equal(m.dequantize().t(), m_t.dequantize())
+    r = torch.Generator(device="cuda").manual_seed(6)
+    x, s, dy, dh = (torch.randn((T, H), generator=r, device="cuda").to(torch.bfloat16) for _ in range(4))
+    y, h, saved = b.forward(x, s)
+    dx, _ = b.backward(dy, dh, saved)
+    xd, sd = (t.double().requires_grad_() for t in (x, s))
+    w, down = b.w_gate_up.dequantize().double(), b.w_down.dequantize().double()
+    hd = xd + sd
+    n = hd * (hd.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    yd = (torch.nn.functional.silu(n @ w[:Fe].t()) * (n @ w[b.up_at :].t())) @ down.t()
+    ((yd * dy.double()).sum() + (hd * dh.double()).sum()).backward()
+    # weights are exact: at most five roundings to e4m3 of 3.6% each, sqrt(5) 3.6% = 8%
+    assert float((dx.double() - xd.grad).norm() / xd.grad.norm()) < 0.09
