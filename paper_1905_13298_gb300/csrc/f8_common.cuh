@@ -243,13 +243,13 @@ __device__ __forceinline__ F8Scale f8_scale(float amax, bool pow2) {
     return F8Scale{s, __frcp_rn(s)};
   }
   // kMax / amax (not 1 / s: one rounding instead of two) from an approximate reciprocal and the quotient's remainder.
-  // One correction gives the correctly rounded quotient for every amax (compared with __fdiv_rn over all 2^23 mantissas
-  // and 255 exponents; halves, so that the reciprocal of none is subnormal), or what fminf leaves out.
-  const float a = 0.5f * amax;
+  // Quarters, so that the reciprocal of none is subnormal.  One correction gives the correctly rounded quotient for every
+  // amax, or what fminf leaves out (compared with __fdiv_rn over all 2^23 mantissas of 255 exponents; the tests sample).
+  const float a = 0.25f * amax;
   float near_inv;
   asm("rcp.approx.f32 %0, %1;" : "=f"(near_inv) : "f"(a));
-  const float quot = 0.5f * kMax * near_inv;
-  return F8Scale{s, fminf(fmaf(fmaf(-quot, a, 0.5f * kMax), near_inv, quot), 8.50705917e37f)};
+  const float quot = 0.25f * kMax * near_inv;
+  return F8Scale{s, fminf(fmaf(fmaf(-quot, a, 0.25f * kMax), near_inv, quot), 8.50705917e37f)};
 }
 // Values in units of the scale.  CHECK: the values may hold infinities, which have to become NaN and not the largest
 // value (v * 0 is NaN for them and 0 otherwise); NaN stays NaN by itself.
