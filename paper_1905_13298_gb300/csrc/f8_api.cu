@@ -97,13 +97,13 @@ ds_status check_f8_out(const char* name, const ds_f8_matrix* m, int64_t rows, in
   return DS_OK;
 }
 
-// A [rows][cols] tensor of `size`-byte elements with row stride ld (NULL passes; no elements: the pointer is not used).
-ds_status check_tensor(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+// A [rows][cols] tensor aligned to `to` bytes with row stride ld (NULL passes; no elements: the pointer is not used).
+ds_status check_tensor(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t to) {
   if (!p) return DS_OK;
   if (ld < cols) return fail(DS_ERR_SHAPE, "%s: the row stride is shorter than a row", name);
   if (ld > ((int64_t)1 << 40) || (rows > 0 && ld > kMaxBytes / rows))
     return fail(DS_ERR_UNSUPPORTED, "%s: too large", name);
-  if (!aligned(p, size)) return fail(DS_ERR_ALIGNMENT, "%s must be aligned to its type", name);
+  if (!aligned(p, to)) return fail(DS_ERR_ALIGNMENT, "%s must be %d-byte aligned", name, (int)to);
   return DS_OK;
 }
 

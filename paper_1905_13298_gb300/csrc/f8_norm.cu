@@ -78,9 +78,9 @@ __device__ __forceinline__ void emit(const RmsnormParams& P, const Aligned& al, 
   }
 }
 
-__device__ __forceinline__ void load_weights(const RmsnormParams& P, const Aligned& al, int64_t c, int n, float w[8]) {
+__device__ __forceinline__ void load_weights(const RmsnormParams& P, int64_t c, int n, float w[8]) {
   Raw8<float> rw;
-  rw.load(P.weight + c, n, al.d);
+  rw.load(P.weight + c, n, true);
   rw.get(w);
 }
 
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(THREADS, kWalkers<T, NV> * (kThreads / THREADS
   load(blockIdx.x);
   float w[NV][8];
 #pragma unroll
-  for (int k = 0; k < NV; ++k) load_weights(P, al, c[k], n[k], w[k]);
+  for (int k = 0; k < NV; ++k) load_weights(P, c[k], n[k], w[k]);
   for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x, turn ^= 1) {
     float v[NV][8], sum = 0.f;
 #pragma unroll
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParam
       const int n = left8(P.cols, c);
       if (n <= 0) c = 0;
       float w[8];
-      load_weights(P, al, c, n, w);
+      load_weights(P, c, n, w);
       emit<T, E5M2, ODD>(P, al, r, c, n, v[k], w, rstd);
     }
   } else {
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) rmsnorm_f8_kernel(const RmsnormParam
       if (n <= 0) c = 0;
       float w[8];
       load_sum<T, ODD>(P, al, r, c, n, v[0]);
-      load_weights(P, al, c, n, w);
+      load_weights(P, c, n, w);
       emit<T, E5M2, ODD>(P, al, r, c, n, v[0], w, rstd);
     }
   }
@@ -386,7 +386,7 @@ cudaError_t forward_as(const RmsnormParams& p, const Aligned& al, cudaStream_t s
 template <typename T, bool E5M2>
 cudaError_t forward_of(const RmsnormParams& p, cudaStream_t st) {
   const Aligned al{rows16(p.x, p.ldx, sizeof(T)), rows16(p.residual, p.ldr, sizeof(T)), rows16(p.h, p.ldh, sizeof(T)),
-                   rows16(p.weight, 0, 4)};
+                   true};
   if constexpr (sizeof(T) == 2) {
     if (!(al.a && al.b && al.c)) return forward_as<T, E5M2, true>(p, al, st);
   }

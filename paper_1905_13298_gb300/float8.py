@@ -263,7 +263,7 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
 
 def rmsnorm_f8(x, weight, residual=None, eps: float = 1e-5, pow2: bool = False, dtype=torch.float8_e4m3fn, h=None,
                stream=None):
-    """Root-mean-square norm of h = x + residual, in 8 bits with a scale per row and 128 columns.
+    """Root-mean-square norm of h = x + residual, in 8 bits with a scale per row and 128 columns (weight: 16-byte aligned).
 
     Returns (n, h, rstd): the F8Matrix of h * rstd * weight, h in x's dtype (x itself without a residual, ``h`` where
     given; it may be x or residual), and the float32 reciprocal root mean squares that the backward pass reads."""

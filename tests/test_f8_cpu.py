@@ -277,3 +277,12 @@ def test_outputs_of_one_call_have_one_format(ds):
     assert L.ds_gated_f8(x, 0, 456, 4, 200, out, kept, 0, None) == ds.DS_ERR_INVALID_ARG
     d, d_t = _m(ds, 4, 456, 1 << 46), _m(ds, 456, 4, 1 << 47, format=ds.DS_F8_E5M2)
     assert L.ds_gated_f8_backward(kept, x, 0, 200, 200, d, d_t, None, 0, None) == ds.DS_ERR_INVALID_ARG
+
+
+def test_refusals_of_alignment_name_the_bytes(ds):
+    L, out = ds.lib(), _m(ds, 4, 256, 1 << 40)
+    fwd = lambda x=1 << 45, w=1 << 46, type_=0: L.ds_rmsnorm_f8(x, 256, None, 0, w, type_, 4, 256, 1e-5, out, None, 0, None, 0, None)
+    for call, what in ((lambda: fwd(w=(1 << 46) + 4), "weight must be 16-byte aligned"),
+                       (lambda: fwd(x=(1 << 45) + 2), "x must be 4-byte aligned"),
+                       (lambda: fwd(x=(1 << 45) + 1, type_=1), "x must be 2-byte aligned")):
+        assert call() == ds.DS_ERR_ALIGNMENT and ds.ds_last_error() == what
