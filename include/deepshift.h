@@ -615,6 +615,11 @@ ds_status ds_expand_shift_weights_f8(const ds_weights* w, const ds_f8_matrix* ou
 ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* bias, const float* add,
                        int64_t ld_add, void* y, int type, int64_t ldy, void* stream);
 
+/* Diagnostic: the tile that ds_linear_f8 takes for these arguments on the current device: 256 or 128 rows of w (the
+ * kernel of large products), or 64, 32 or 16 rows of x (the other one); 0 where it launches nothing or refuses them. */
+int ds_linear_f8_tile(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* add, int64_t ld_add, void* y, int type,
+                      int64_t ldy);
+
 /* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8 and ds_gated_f8_backward. */
 int ds_f8_fault_flag(void);
 void ds_f8_set_wait_limit(long long cycles);

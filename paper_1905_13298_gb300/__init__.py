@@ -146,6 +146,8 @@ _SIGNATURES = {
     "ds_expand_shift_weights_f8": (ctypes.c_int, [ctypes.POINTER(ds_weights), _F8, ctypes.c_void_p]),
     "ds_linear_f8": (ctypes.c_int, [_F8, _F8, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                     ctypes.c_int, ctypes.c_int64, ctypes.c_void_p]),
+    "ds_linear_f8_tile": (ctypes.c_int, [_F8, _F8, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int,
+                                         ctypes.c_int64]),
     "ds_f8_fault_flag": (ctypes.c_int, []),
     "ds_f8_set_wait_limit": (None, [ctypes.c_longlong]),
     "ds_rmsnorm_f8": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
@@ -406,6 +408,10 @@ def ds_expand_shift_weights_f8(w: ds_weights, out, stream=None) -> None:
 
 def ds_linear_f8(x, w, bias, add, ld_add: int, y, type_: int, ldy: int, stream=None) -> None:
     _check(lib().ds_linear_f8(x, w, _ptr(bias), _ptr(add), ld_add, _ptr(y), type_, ldy, _stream(stream)))
+
+
+def ds_linear_f8_tile(x, w, add, ld_add: int, y, type_: int, ldy: int) -> int:
+    return int(lib().ds_linear_f8_tile(x, w, _ptr(add), ld_add, _ptr(y), type_, ldy))
 
 
 def ds_f8_fault_flag() -> int:

@@ -135,6 +135,30 @@ ds_status check_quantize(const Span (&src)[2], int64_t rows, int64_t cols, const
 // An aliased output starts where its input does, with the same stride; anything else is an overlap.
 bool same(const void* a, int64_t lda, const void* b, int64_t ldb) { return a != nullptr && a == b && lda == ldb; }
 
+ds_status check_linear(const LinearF8Params& p) {
+  if (!p.x || !p.w) return fail(DS_ERR_INVALID_ARG, "NULL x or w");
+  ds_status r = check_type(p.type);
+  if (r != DS_OK) return r;
+  if ((r = check_f8("x", p.x)) != DS_OK) return r;
+  if ((r = check_f8("w", p.w)) != DS_OK) return r;
+  if (p.x->cols != p.w->cols)
+    return fail(DS_ERR_SHAPE, "x has %lld columns, w %lld", (long long)p.x->cols, (long long)p.w->cols);
+  const int64_t M = p.x->rows, N = p.w->rows, size = type_size(p.type);
+  if (!p.y && M > 0 && N > 0) return fail(DS_ERR_INVALID_ARG, "NULL y");
+  if ((r = check_tensor("y", p.y, M, N, p.ldy, size)) != DS_OK) return r;
+  if ((r = check_tensor("add", p.add, M, N, p.ld_add, 4)) != DS_OK) return r;
+  if ((r = check_tensor("bias", p.bias, 1, N, N, 4)) != DS_OK) return r;
+  const bool in_place = p.type == DS_TYPE_F32 && same(p.y, p.ldy, p.add, p.ld_add);
+  const Span outs[] = {span("y", p.y, strided(M, N, p.ldy, size))};
+  const Span ins[] = {values_of("x", p.x), scales_of("x's scales", p.x), values_of("w", p.w),
+                      scales_of("w's scales", p.w), span("bias", p.bias, 4 * N),
+                      span("add", in_place ? nullptr : p.add, strided(M, N, p.ld_add, 4))};
+  if ((r = check_apart(outs, ins)) != DS_OK) return r;
+  // the finest tiling (16 x 128, split 8 ways) stays inside a grid's 2^31 - 1 CTAs
+  if (blocks_of(N) * ((M + 15) / 16) > ((int64_t)1 << 28) - 1) return fail(DS_ERR_UNSUPPORTED, "M x N too large");
+  return DS_OK;
+}
+
 }  // namespace
 }  // namespace ds
 
@@ -194,29 +218,19 @@ ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float
                        int64_t ld_add, void* y, int type, int64_t ldy, void* stream) {
   NvtxRange nvtx_range("ds_linear_f8");
   clear_error();
-  if (!x || !w) return fail(DS_ERR_INVALID_ARG, "NULL x or w");
-  ds_status r = check_type(type);
-  if (r != DS_OK) return r;
-  if ((r = check_f8("x", x)) != DS_OK) return r;
-  if ((r = check_f8("w", w)) != DS_OK) return r;
-  if (x->cols != w->cols)
-    return fail(DS_ERR_SHAPE, "x has %lld columns, w %lld", (long long)x->cols, (long long)w->cols);
-  const int64_t M = x->rows, N = w->rows, size = type_size(type);
-  if (!y && M > 0 && N > 0) return fail(DS_ERR_INVALID_ARG, "NULL y");
-  if ((r = check_tensor("y", y, M, N, ldy, size)) != DS_OK) return r;
-  if ((r = check_tensor("add", add, M, N, ld_add, 4)) != DS_OK) return r;
-  if ((r = check_tensor("bias", bias, 1, N, N, 4)) != DS_OK) return r;
-  const bool in_place = type == DS_TYPE_F32 && same(y, ldy, add, ld_add);
-  const Span outs[] = {span("y", y, strided(M, N, ldy, size))};
-  const Span ins[] = {values_of("x", x), scales_of("x's scales", x), values_of("w", w), scales_of("w's scales", w),
-                      span("bias", bias, 4 * N),
-                      span("add", in_place ? nullptr : add, strided(M, N, ld_add, 4))};
-  if ((r = check_apart(outs, ins)) != DS_OK) return r;
-  if (M == 0 || N == 0) return DS_OK;
-  // the finest tiling (16 x 128, split 8 ways) stays inside a grid's 2^31 - 1 CTAs
-  if (blocks_of(N) * ((M + 15) / 16) > ((int64_t)1 << 28) - 1) return fail(DS_ERR_UNSUPPORTED, "M x N too large");
   const LinearF8Params p{x, w, bias, add, ld_add, y, type, ldy};
+  const ds_status r = check_linear(p);
+  if (r != DS_OK) return r;
+  if (x->rows == 0 || w->rows == 0) return DS_OK;
   return cuda_check(launch_linear_f8(p, static_cast<cudaStream_t>(stream)), "linear_f8 launch");
+}
+
+int ds_linear_f8_tile(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* add, int64_t ld_add, void* y, int type,
+                      int64_t ldy) {
+  clear_error();
+  const LinearF8Params p{x, w, nullptr, add, ld_add, y, type, ldy};
+  if (check_linear(p) != DS_OK || x->rows == 0 || w->rows == 0) return 0;
+  return linear_f8_tile(p);
 }
 
 int ds_f8_fault_flag(void) {

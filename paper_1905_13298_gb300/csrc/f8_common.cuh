@@ -497,6 +497,7 @@ cudaError_t launch_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, i
                                      const F8Out& dgu, const F8Out& dgu_t, const F8Out& a_t, bool e5m2, bool pow2,
                                      cudaStream_t st);
 cudaError_t launch_linear_f8(const LinearF8Params& p, cudaStream_t st);
+int linear_f8_tile(const LinearF8Params& p);  // rows of the tile that the launch would take
 int read_f8_fault_flag();
 int read_gated_f8_fault_flag();
 void set_f8_wait_cycles(long long cycles);

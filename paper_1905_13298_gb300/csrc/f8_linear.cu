@@ -1072,9 +1072,7 @@ uint32_t idesc_of(const ds_f8_matrix* a, const ds_f8_matrix* b) {
   return (1u << 4) | ((uint32_t)a->format << 7) | ((uint32_t)b->format << 10);
 }
 
-}  // namespace
-
-cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
+Params params_of(const LinearF8Params& l) {
   Params p = {};
   p.x = scales_of(l.x);
   p.w = scales_of(l.w);
@@ -1093,13 +1091,31 @@ cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
           (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 16 == 0 && l.ld_add % 4 == 0));
   p.pairs = reinterpret_cast<uintptr_t>(l.y) % (2 * size) == 0 && l.ldy % 2 == 0 &&
             (l.add == nullptr || (reinterpret_cast<uintptr_t>(l.add) % 8 == 0 && l.ld_add % 2 == 0));
-  const bool wide = p.vec && reinterpret_cast<uintptr_t>(l.y) % (8 * size) == 0 && l.ldy % 8 == 0;
   auto aligned = [&](int n) {
     return reinterpret_cast<uintptr_t>(p.x.s) % (4 * n) == 0 && p.x.ld % n == 0 &&
            reinterpret_cast<uintptr_t>(p.w.s) % (4 * n) == 0 && p.w.ld % n == 0;
   };
   p.aligned = aligned(8) ? 8 : (aligned(4) ? 4 : 1);
   p.wait_cycles = f8_wait_cycles();
+  return p;
+}
+// Whether the large kernel's stores of eight values are aligned.
+bool wide_of(const LinearF8Params& l, const Params& p) {
+  const size_t size = l.type == DS_TYPE_F32 ? 4 : 2;
+  return p.vec && reinterpret_cast<uintptr_t>(l.y) % (8 * size) == 0 && l.ldy % 8 == 0;
+}
+
+}  // namespace
+
+int linear_f8_tile(const LinearF8Params& l) {
+  const Params p = params_of(l);
+  const Plan plan = plan_of(p, wide_of(l, p));
+  return plan.big ? plan.big : plan.bn;
+}
+
+cudaError_t launch_linear_f8(const LinearF8Params& l, cudaStream_t st) {
+  Params p = params_of(l);
+  const bool wide = wide_of(l, p);
   const Plan plan = plan_of(p, wide);
   CUtensorMap mw = {}, mx = {};  // an empty reduction loads nothing
   if (p.nk > 0 && (!make_map(&mw, l.w, plan.big ? plan.big : ROWS) || !make_map(&mx, l.x, plan.big ? ROWS : plan.bn)))

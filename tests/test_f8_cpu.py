@@ -286,3 +286,10 @@ def test_refusals_of_alignment_name_the_bytes(ds):
                        (lambda: fwd(x=(1 << 45) + 2), "x must be 4-byte aligned"),
                        (lambda: fwd(x=(1 << 45) + 1, type_=1), "x must be 2-byte aligned")):
         assert call() == ds.DS_ERR_ALIGNMENT and ds.ds_last_error() == what
+
+
+def test_tile_of_refused_and_empty_products_is_zero(ds):
+    L, x, w = ds.lib(), _m(ds, 4, 256, 1 << 40), _m(ds, 8, 256, 1 << 41)
+    assert L.ds_linear_f8_tile(x, _m(ds, 8, 255, 1 << 41), None, 0, 1 << 50, 0, 8) == 0 and ds.ds_last_error()
+    assert L.ds_linear_f8_tile(None, w, None, 0, 1 << 50, 0, 8) == 0
+    assert L.ds_linear_f8_tile(_m(ds, 0, 256), w, None, 0, 1 << 50, 0, 8) == 0 and not ds.ds_last_error()

@@ -1,4 +1,4 @@
-"""Products of 8-bit matrices whose scales lie at the ends of float32."""
+"""Products of 8-bit matrices: scales at the ends of float32, and every instance of the large kernel on exact integers."""
 import numpy as np
 import pytest
 import torch
@@ -43,3 +43,54 @@ def test_product_with_scales_at_the_ends_of_float32(dslib, sx, sw, exponents, fm
     assert float(terms.max()) > 2.0**-124 and float(terms.max()) < 2.0**127
     assert bool(((y.double() - want).abs() <= 2.0**-24 * want.abs() + TOL * terms + 2.0**-148).all())
     assert not y[M // 2].any() and not y[:, N // 2].any()
+
+
+def _tile(ds, x, w, y, add=None):
+    kinds = {torch.float32: ds.DS_TYPE_F32, torch.bfloat16: ds.DS_TYPE_BF16, torch.float16: ds.DS_TYPE_F16}
+    return ds.ds_linear_f8_tile(x.desc, w.desc, add, 0 if add is None else add.stride(0), y, kinds[y.dtype], y.stride(0))
+
+
+@pytest.mark.parametrize("M,N,tile", [(2500, 3800, 256), (2500, 3801, 256), (2100, 2104, 128), (2100, 2103, 128)])
+@pytest.mark.parametrize("tiles_w", [False, True])
+@pytest.mark.parametrize("fx", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("fw", ["e4m3", "e5m2"])
+def test_large_products_of_small_integers_are_exact(dslib, M, N, tile, tiles_w, fx, fw):
+    """Every instance of the large kernel (width of a tile, scales of w, rows that are aligned or not) and every pair of
+    formats, over more tiles than SMs, 18 blocks of the reduction and ragged sides, with a bias, and accumulating in
+    place: integers times scales that are powers of two, whose sums fit 24 bits, so that every step is exact."""
+    K, r = 2200, torch.Generator(device="cuda").manual_seed(M + N)
+    tiles_x = (fx == fw) != tiles_w
+
+    def matrix(rows, fmt, tiled):
+        q = torch.zeros((rows, 2208), device="cuda").to(FORMATS[fmt])
+        q[:, :K] = torch.randint(-2, 3, (rows, K), generator=r, device="cuda").float().to(FORMATS[fmt])
+        s = torch.randint(-2, 3, (-(-rows // 128) if tiled else rows, 18), generator=r, device="cuda")
+        return dslib.F8Matrix(q[:, :K], torch.exp2(s.float()), tiles=tiled)
+
+    x, w = matrix(M, fx, tiles_x), matrix(N, fw, tiles_w)
+    assert -(-M // 128) * -(-N // tile) > torch.cuda.get_device_properties(0).multi_processor_count
+    bias = torch.randint(-9, 10, (N,), generator=r, device="cuda").float()
+    want = x.dequantize().double() @ w.dequantize().double().t()
+    for dtype in (torch.bfloat16, torch.float16):
+        y = torch.empty((M, N), dtype=dtype, device="cuda")
+        assert _tile(dslib, x, w, y) == tile
+        dslib.linear_f8(x, w, bias=bias if dtype == torch.bfloat16 else None, out=y)
+        assert torch.equal(y, (want + bias if dtype == torch.bfloat16 else want).to(dtype))
+    held = torch.randint(-9, 10, (M, N + 8), generator=r, device="cuda").float()
+    before, sums = held.clone(), held[:, :N]
+    assert _tile(dslib, x, w, sums, sums) == tile
+    dslib.linear_f8(x, w, bias=bias, add=sums, out=sums)
+    assert torch.equal(sums.double(), want + bias + before[:, :N]) and torch.equal(held[:, N:], before[:, N:])
+    assert dslib.ds_f8_fault_flag() == 0
+
+
+def test_sizes_at_the_ends_reach_every_kernel(dslib):
+    """The sizes of the test with scales at the ends of float32: the small kernel, and both widths of the large one."""
+    def tile(M, N, tiles):
+        x, w = dslib.F8Matrix.empty(M, 300, "cuda"), dslib.F8Matrix.empty(N, 300, "cuda", tiles=tiles)
+        return _tile(dslib, x, w, torch.empty((M, N), device="cuda"))
+
+    for tiles in (False, True):
+        assert tile(5, 260, tiles) == 16
+        assert tile(1100, 1152, tiles) == 128 and tile(1100, 1151, tiles) == 128
+        assert tile(2500, 3800, tiles) == 256
