@@ -169,12 +169,14 @@ def _on_stream(device: int):
 
 
 def _given(stream):
-    """Makes the caller's stream (a torch stream, or a handle) current: a call's outputs and its workspace then belong to
-    it, so none of that memory is still in use, or used again, by the work of another stream.  As for anything made on a
-    stream, the caller orders the inputs before the call and the use of the results on other streams behind it."""
-    if isinstance(stream, int):
+    """Makes the caller's stream (a torch stream, a handle, or what has one as ``cuda_stream``) current: a call's outputs
+    and its workspace then belong to it, so none of that memory is still in use, or used again, by the work of another
+    stream.  As for anything made on a stream, the caller orders the inputs before the call and the use of the results on
+    other streams behind it."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
         # 1 is CUDA's other name of the default stream
-        stream = torch.cuda.default_stream() if stream in (0, 1) else torch.cuda.ExternalStream(stream)
+        stream = torch.cuda.default_stream() if handle in (0, 1) else torch.cuda.ExternalStream(handle)
     return torch.cuda.stream(stream)
 
 

@@ -74,3 +74,20 @@ def test_outputs_are_not_memory_that_the_current_stream_still_reads(dslib, as_ha
         torch.cuda.synchronize()
         assert all(bool((t == 3).all()) for t in copies), name
         assert all(torch.equal(a, b) for a, b in zip(tensors(got), want)), name
+
+
+def test_every_name_of_a_stream_is_taken(dslib):
+    """A torch stream, its handle, an object with the handle as `cuda_stream`, and both handles of the default stream."""
+    x = torch.randn((5, 256), device="cuda")
+    want, _ = dslib.quantize_f8(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+
+    class Other:
+        cuda_stream = side.cuda_stream
+
+    before = torch.cuda.current_stream()
+    for name in (side, side.cuda_stream, Other(), 0, 1, torch.cuda.default_stream()):
+        m, _ = dslib.quantize_f8(x, stream=name)
+        torch.cuda.synchronize()
+        assert torch.equal(m.q.float(), want.q.float()) and torch.cuda.current_stream() == before
