@@ -112,6 +112,8 @@ def main(argv=None) -> list[float]:
     p.add_argument("--rate", type=float, default=0.3)
     p.add_argument("--shift", action="store_true", help="serve with power-of-two weights after training")
     a = p.parse_args(argv)
+    if min(a.tokens, a.hidden, a.features, a.steps) < 1:
+        p.error("--tokens, --hidden, --features and --steps must be at least 1")
     r = torch.Generator(device="cuda").manual_seed(1)
     shape = (a.tokens, a.hidden)
     block, teacher = GatedFeedForward(a.hidden, a.features, seed=2), GatedFeedForward(a.hidden, a.features, seed=3)

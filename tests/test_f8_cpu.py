@@ -293,3 +293,11 @@ def test_tile_of_refused_and_empty_products_is_zero(ds):
     assert L.ds_linear_f8_tile(x, _m(ds, 8, 255, 1 << 41), None, 0, 1 << 50, 0, 8) == 0 and ds.ds_last_error()
     assert L.ds_linear_f8_tile(None, w, None, 0, 1 << 50, 0, 8) == 0
     assert L.ds_linear_f8_tile(_m(ds, 0, 256), w, None, 0, 1 << 50, 0, 8) == 0 and not ds.ds_last_error()
+
+
+@pytest.mark.parametrize("what", ["--tokens", "--hidden", "--features", "--steps"])
+def test_feed_forward_example_refuses_empty_sizes(what, capsys):
+    from paper_1905_13298_gb300 import feed_forward
+    with pytest.raises(SystemExit):
+        feed_forward.main([what, "0"])
+    assert "must be at least 1" in capsys.readouterr().err
