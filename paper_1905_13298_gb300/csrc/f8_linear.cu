@@ -14,9 +14,9 @@
 // are all the traffic, still fill the tensor core's 128 lanes.  A
 // thread-block cluster splits the reduction of one tile and its CTAs add
 // their parts through distributed shared memory in rank order, so results do
-// not depend on timing.  Measured: 1 x 4096 x 4096 6.5 us (2.6 TB/s; an empty
-// launch of clusters takes 3), 300 x 1000 x 2050 8.8 us, 128 x 8192 x 4096
-// 15.7 us (2.1 TB/s).
+// not depend on timing.  Measured: 1 x 4096 x 4096 7.7 us (2.2 TB/s; 6.5 with
+// the weights in L2; an empty launch of clusters takes 3), 300 x 1000 x 2050
+// 8.7 us, 128 x 8192 x 4096 15.7 us (2.1 TB/s).
 #include <atomic>
 #include <type_traits>
 

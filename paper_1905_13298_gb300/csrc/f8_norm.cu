@@ -14,7 +14,7 @@
 // bound by HBM.  Rows too long for that (NV = 0) are read a second time.
 // Measured at 8192 x 4096 bf16 with the residual: forward 38.5 us (6.1 TB/s),
 // backward 47.7 us (5.6 TB/s, 5 of them the sum of dw's partial rows); without
-// a residual the forward pass is bound by its instructions (31.9 us, 3.2 TB/s:
+// a residual the forward pass is bound by its instructions (30 us, 3.3 TB/s:
 // about 30 per value, a third of them the blocks' maxima and scales).  4096 x
 // 8192 43 us, 2048 x 16384 (read twice) 58 us.  Rows that are not aligned to
 // 16 bytes have instances of their own (8192 x 4100 97 us; value by value 133;
