@@ -18,9 +18,10 @@
 // brings the next tile to shared memory while this one is rounded and stored.
 //
 // Measured in bf16: forward 4095 x 8200 with the checkpoint 54 us (4.4 TB/s;
-// bound by instructions: the sigmoid, conversions, maxima and scales), 8192 x 4096 without it 44 us (3.8 TB/s); backward 8192 x 8192
-// 160 us (3.9 TB/s: a tile's phases, sigmoid, maxima, scales, rounding and
-// turning, are parted by barriers that nothing else on the SM fills).
+// bound by instructions: the sigmoid, conversions, maxima and scales), 8192 x
+// 4096 without it 44 us (3.8 TB/s); backward 8192 x 8192 160 us (3.9 TB/s: a
+// tile's phases, sigmoid, maxima, scales, rounding and turning, are parted by
+// barriers that nothing else on the SM fills).
 #include <type_traits>
 
 #include "f8_common.cuh"
