@@ -73,8 +73,8 @@ const char* ds_last_error(void);
 /* Library version: major * 10000 + minor * 100 + patch (a library utility: no counterpart in the paper). */
 int ds_version(void);
 
-/* sizeof of the ABI structs as compiled into the library (0: ds_weights, 1: ds_layer, 2: ds_f8_matrix), so that
- * bindings can check their layout; 0 for any other argument (a library utility: no counterpart in the paper). */
+/* sizeof of the ABI structs as compiled into the library (0: ds_weights, 1: ds_layer, 2: ds_f8_matrix,
+ * 3: ds_expert_slots, 4: ds_adamw_tensor, 5: ds_adamw_options), so that bindings can check their layout; 0 for any other argument (a library utility: no counterpart in the paper). */
 size_t ds_abi_struct_size(int which);
 
 /* ---------------------------------------------------------------------------
@@ -620,7 +620,7 @@ ds_status ds_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const float
 int ds_linear_f8_tile(const ds_f8_matrix* x, const ds_f8_matrix* w, const float* add, int64_t ld_add, void* y, int type,
                       int64_t ldy);
 
-/* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8 and ds_gated_f8_backward. */
+/* As ds_bf16_fault_flag and ds_bf16_set_wait_limit, for ds_linear_f8, ds_gated_f8_backward and the experts' products. */
 int ds_f8_fault_flag(void);
 void ds_f8_set_wait_limit(long long cycles);
 
@@ -676,6 +676,158 @@ ds_status ds_gated_f8(const void* gu, int type, int64_t ld, int64_t rows, int64_
 ds_status ds_gated_f8_backward(const ds_f8_matrix* ckpt, const void* da, int type, int64_t ld, int64_t features,
                                const ds_f8_matrix* dgu, const ds_f8_matrix* dgu_t, const ds_f8_matrix* a_t,
                                uint32_t flags, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Experts: a feed-forward block of which each token takes `top_k` of `experts`
+ * parts.  Its slots s = t * top_k + j (choice j of token t) are put in order of
+ * their expert, tokens in their order within one; the operators of an expert's
+ * part then work on its segment of rows:
+ *   counts[e]    slots of expert e
+ *   offsets[e]   its first row; offsets[e + 1] = offsets[e] + counts[e] rounded
+ *                up to a multiple of `align` (offsets[experts]: the rows in use)
+ *   position[s]  the row of a slot, -1 where its expert is not in
+ *                [0, experts): such a slot (padding of a batch) goes nowhere
+ *   slot[r]      the slot of a row, -1 for rows that hold none (the gaps behind
+ *                segments, and the rows from offsets[experts] on)
+ * All of it is made and read on the device; `rows` is what the host knows of
+ * it, enough for any choice of experts: ds_expert_rows().  With align = 128 the
+ * segments start at blocks of the 8-bit matrices, so that these hold no two
+ * experts' rows also where they are transposed; with 1 there are no gaps.
+ *
+ * A ds_expert_slots describes this device memory (int32, 4-byte aligned; the
+ * library keeps no pointer to it).  What the calls below read of it has to be
+ * what ds_expert_order wrote; rows and slots out of range are passed over.
+ * Rows that hold no slot are written as zeros by the calls that write rows (the
+ * products take the gaps for rows of their expert: zeros, or the bias).
+ * Limits: rows below 2^31 - 256, 1 <= experts <= DS_EXPERTS_MAX, 1 <= align
+ * <= 2^20.  tokens = 0 is accepted.  Types, strides and alignment are as for
+ * the 8-bit operators; arithmetic is float32, in the order of j, and a value
+ * is rounded once, where it is stored.  No result depends on timing.
+ * ------------------------------------------------------------------------- */
+#define DS_EXPERTS_MAX 1024
+
+#define DS_INDEX_I32 0
+#define DS_INDEX_I64 1
+
+typedef struct ds_expert_slots {
+  int32_t* offsets;  /* device [experts + 1] */
+  int32_t* counts;   /* device [experts] */
+  int32_t* position; /* device [tokens * top_k] */
+  int32_t* slot;     /* device [rows] */
+  int64_t tokens, rows;
+  int32_t top_k, experts, align, reserved;
+} ds_expert_slots;
+
+/* Rows that hold the segments of any choice of experts: the largest multiple of align not above
+ * tokens * top_k + min(experts, tokens * top_k) * (align - 1); -1 for arguments out of range. */
+int64_t ds_expert_rows(int64_t tokens, int32_t top_k, int32_t experts, int32_t align);
+
+/* Writes all of `s` (its rows at least ds_expert_rows) from ids, device [tokens][top_k] of DS_INDEX_*, contiguous. */
+ds_status ds_expert_order(const void* ids, int id_type, const ds_expert_slots* s, void* stream);
+
+/* out[r] = x[slot[r] / top_k]: x [tokens][cols] and out [rows][cols] of `type`, or 8-bit matrices of one format with
+ * DS_F8_ROWS blocks, whose values and scales are copied as they are. */
+ds_status ds_expert_gather(const void* x, int type, int64_t ldx, int64_t cols, const ds_expert_slots* s, void* out,
+                           int64_t ldo, void* stream);
+ds_status ds_expert_gather_f8(const ds_f8_matrix* x, const ds_expert_slots* s, const ds_f8_matrix* out, void* stream);
+
+/*
+ * out[t] = add[t] + sum_j weights[t][j] * y[position[t][j]], over the slots that have a row
+ *   y        device [rows][cols] of `type`
+ *   weights  device float32 [tokens][top_k], contiguous, or NULL: all 1.  With these, the sum is the gradient of
+ *            ds_expert_gather's x, y being that of its rows.
+ *   add      device [tokens][cols] of `type`, or NULL; may be out itself (same stride)
+ *   out      device [tokens][cols] of `type`
+ * Backward, dout being the gradient of out (and of add):
+ *   dy[position[t][j]] = weights[t][j] * dout[t]     (zeros in the other rows)
+ *   dweights[t][j] = sum_c dout[t][c] * y[position[t][j]][c]     (0 for a slot without a row)
+ * dweights may be NULL, and y then too.  dy may be y itself (same stride).
+ */
+ds_status ds_expert_combine(const void* y, int type, int64_t ldy, int64_t cols, const ds_expert_slots* s,
+                            const float* weights, const void* add, int64_t ld_add, void* out, int64_t ldo,
+                            void* stream);
+ds_status ds_expert_combine_backward(const void* dout, int64_t ldd, const void* y, int64_t ldy, int type, int64_t cols,
+                                     const ds_expert_slots* s, const float* weights, void* dy, int64_t lddy,
+                                     float* dweights, void* stream);
+
+/*
+ * The products of the experts' parts, over 8-bit matrices as ds_linear_f8 takes them:
+ *   y[r] = bias[e] + x[r] w_e^T     for the rows r of each segment e (gaps too: x holds zeros there)
+ *   x     [rows][K], DS_F8_ROWS or DS_F8_TILES
+ *   w     [experts * N][K], w_e its rows [e N, (e + 1) N); in tiles only where N is a multiple of 128
+ *   bias  device float32 [experts][N], contiguous, or NULL
+ *   y     device [rows][N] of `type`; zeros from row offsets[experts] on
+ * and their weight gradients
+ *   dw_e[n][k] = add_e[n][k] + sum over the rows r of segment e of dy_t[n][r] x_t[k][r]
+ *   dy_t  [N][rows], x_t [K][rows]: transposed, so that blocks run along the rows; align a multiple of 128
+ *   dw    device float32 [experts * N][K], row stride lddw; add the same, ld_add, or NULL; may be dw itself
+ * A bounded wait that gives up is reported by ds_f8_fault_flag.
+ */
+ds_status ds_expert_linear_f8(const ds_f8_matrix* x, const ds_f8_matrix* w, const ds_expert_slots* s, const float* bias,
+                              void* y, int type, int64_t ldy, void* stream);
+ds_status ds_expert_weight_grad_f8(const ds_f8_matrix* dy_t, const ds_f8_matrix* x_t, const ds_expert_slots* s,
+                                   const float* add, int64_t ld_add, float* dw, int64_t lddw, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Optimizer: one step of Adam with decoupled weight decay over many tensors.
+ * For each value, with t the step's number (from 1) and each operation rounded
+ * to float32 (the factors are computed in float64 and rounded once):
+ *   g' = g * grad_scale
+ *   m  = beta1 * m + (1 - beta1) * g'
+ *   v  = beta2 * v + (1 - beta2) * (g' * g')
+ *   p  = p * (1 - lr * weight_decay)
+ *        - m * (lr / (1 - beta1^t)) / (sqrt(v) * (1 - beta2^t)^(-1/2) + eps)
+ * p is rounded once to its type; `copy` is p rounded to another.
+ *
+ * The states m and v are float32, or 8 bits: e4m3 values of m and of sqrt(v),
+ * with a float32 scale for each 128 consecutive values of a tensor,
+ *   scale = max(amax / 448, 2^-126),  u = value * min(448 / amax, 2^126),
+ * amax the block's largest finite magnitude.  u becomes one of its two e4m3
+ * neighbours, the one of larger magnitude with the probability of u's distance
+ * from the other one: the expected value of a state is then what the recurrence
+ * says.  (To the nearest it would stand still: a step changes v by 1 - beta2
+ * of itself, a rounding to 3 bits loses up to 12%.)  A positive sqrt(v) is held
+ * as at least the smallest value, 2^-9, so that no later step divides by eps
+ * alone what it should divide by a root; infinities and NaN become NaN.  The
+ * step itself takes m and v before they are rounded.  With i the index of a
+ * value in its tensor and n the tensor's number in the call, the random bits
+ * of m and sqrt(v) are the low and the high half of a hash of
+ *   x = i * 0x9E3779B1 + t * 0xBB67AE85 + n * 0x6A09E667 + seed    (mod 2^32):
+ *   x ^= x >> 16;  x *= 0x243F6A89;  x ^= x >> 15;  x *= 0xB7E15163;
+ *   x ^= x >> 16
+ * and the value is the upper neighbour where its distance plus (half + 1/2) /
+ * 2^16 reaches 1.
+ * ------------------------------------------------------------------------- */
+typedef struct ds_adamw_tensor {
+  void* p;            /* device [n] of p_type */
+  const void* g;      /* device [n] of g_type */
+  void *m, *v;        /* device [n]: float32, or e4m3 where the scales are given */
+  float *m_scale, *v_scale; /* device [ceil(n / 128)], or both NULL */
+  void* copy;         /* device [n] of copy_type, or NULL */
+  int64_t n;
+  float weight_decay;
+  int32_t p_type, g_type, copy_type; /* DS_TYPE_* */
+} ds_adamw_tensor;
+
+typedef struct ds_adamw_options {
+  double lr, beta1, beta2, eps;
+  int64_t step;            /* t, from 1; not read where step_dev is given */
+  const int64_t* step_dev; /* device: t, or NULL.  A captured call is replayed with the value that is there then */
+  const float* lr_dev;     /* device: lr, or NULL */
+  const float* grad_scale; /* device: a factor of all gradients (a clipped norm, a loss scale), or NULL */
+  uint32_t seed, reserved;
+} ds_adamw_options;
+
+/*
+ * Updates `count` tensors (a host array, read during the call): p, m, v, their
+ * scales and copy in place.  The tensors' memories are contiguous, aligned to
+ * their type (16 bytes take the vector path), and apart from each other; all
+ * states are of one kind.  n = 0 is accepted.  One launch for up to 400
+ * tensors.  Errors: DS_ERR_INVALID_ARG (NULL, a type, betas outside [0, 1),
+ * step below 1, overlap), DS_ERR_SHAPE, DS_ERR_ALIGNMENT, DS_ERR_UNSUPPORTED
+ * (n above 2^40).
+ */
+ds_status ds_adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_options* options, void* stream);
 
 #ifdef __cplusplus
 }

@@ -50,6 +50,10 @@ DS_F8_ROWS = 0
 DS_F8_TILES = 1
 DS_F8_POW2 = 1
 
+DS_EXPERTS_MAX = 1024
+DS_INDEX_I32 = 0
+DS_INDEX_I64 = 1
+
 DS_WEIGHTS_MAGIC = 0x31575344
 DS_FORMAT_PLANES6 = 1
 DS_FORMAT_CODES5 = 2
@@ -83,8 +87,30 @@ class ds_f8_matrix(ctypes.Structure):
                 ("format", ctypes.c_int32), ("blocks", ctypes.c_int32)]
 
 
+class ds_expert_slots(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("position", ctypes.c_void_p),
+                ("slot", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("top_k", ctypes.c_int32), ("experts", ctypes.c_int32), ("align", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class ds_adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float), ("p_type", ctypes.c_int32),
+                ("g_type", ctypes.c_int32), ("copy_type", ctypes.c_int32)]
+
+
+class ds_adamw_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("step_dev", ctypes.c_void_p),
+                ("lr_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
 _lib = None
 _F8 = ctypes.POINTER(ds_f8_matrix)
+_SLOTS = ctypes.POINTER(ds_expert_slots)
 
 _SIGNATURES = {
     "ds_last_error": (ctypes.c_char_p, []),
@@ -155,6 +181,24 @@ _SIGNATURES = {
                                      _F8, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_uint32,
                                      ctypes.c_void_p]),
     "ds_rmsnorm_f8_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64, ctypes.c_int64]),
+    "ds_expert_rows": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "ds_expert_order": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, _SLOTS, ctypes.c_void_p]),
+    "ds_expert_gather": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, _SLOTS,
+                                        ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "ds_expert_gather_f8": (ctypes.c_int, [_F8, _SLOTS, _F8, ctypes.c_void_p]),
+    "ds_expert_combine": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, _SLOTS,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                         ctypes.c_int64, ctypes.c_void_p]),
+    "ds_expert_combine_backward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                                  ctypes.c_int, ctypes.c_int64, _SLOTS, ctypes.c_void_p,
+                                                  ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                                  ctypes.c_void_p]),
+    "ds_expert_linear_f8": (ctypes.c_int, [_F8, _F8, _SLOTS, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                           ctypes.c_int64, ctypes.c_void_p]),
+    "ds_expert_weight_grad_f8": (ctypes.c_int, [_F8, _F8, _SLOTS, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                                ctypes.c_int64, ctypes.c_void_p]),
+    "ds_adamw": (ctypes.c_int, [ctypes.POINTER(ds_adamw_tensor), ctypes.c_int, ctypes.POINTER(ds_adamw_options),
+                                ctypes.c_void_p]),
     "ds_rmsnorm_f8_backward": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
                                               ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
                                               ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
@@ -178,7 +222,7 @@ def lib() -> ctypes.CDLL:
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
-        for which, st in ((0, ds_weights), (1, ds_layer), (2, ds_f8_matrix)):
+        for which, st in enumerate((ds_weights, ds_layer, ds_f8_matrix, ds_expert_slots, ds_adamw_tensor, ds_adamw_options)):
             if L.ds_abi_struct_size(which) != ctypes.sizeof(st):
                 raise ImportError(f"{st.__name__} layout differs between the binding and {LIB_PATH}")
         _lib = L
@@ -438,6 +482,51 @@ def ds_rmsnorm_f8_backward(dy, lddy: int, h, ldh: int, rstd, weight, dh, lddh: i
                                         rows, cols, _ptr(dx), lddx, _ptr(dw), _ptr(ws), ws_bytes, _stream(stream)))
 
 
+def ds_expert_rows(tokens: int, top_k: int, experts: int, align: int) -> int:
+    return int(lib().ds_expert_rows(tokens, top_k, experts, align))
+
+
+def ds_expert_order(ids, id_type: int, slots: ds_expert_slots, stream=None) -> None:
+    _check(lib().ds_expert_order(_ptr(ids), id_type, ctypes.byref(slots), _stream(stream)))
+
+
+def ds_expert_gather(x, type_: int, ldx: int, cols: int, slots: ds_expert_slots, out, ldo: int, stream=None) -> None:
+    _check(lib().ds_expert_gather(_ptr(x), type_, ldx, cols, ctypes.byref(slots), _ptr(out), ldo, _stream(stream)))
+
+
+def ds_expert_gather_f8(x: ds_f8_matrix, slots: ds_expert_slots, out: ds_f8_matrix, stream=None) -> None:
+    _check(lib().ds_expert_gather_f8(ctypes.byref(x), ctypes.byref(slots), ctypes.byref(out), _stream(stream)))
+
+
+def ds_expert_combine(y, type_: int, ldy: int, cols: int, slots: ds_expert_slots, weights, add, ld_add: int, out,
+                      ldo: int, stream=None) -> None:
+    _check(lib().ds_expert_combine(_ptr(y), type_, ldy, cols, ctypes.byref(slots), _ptr(weights), _ptr(add), ld_add,
+                                   _ptr(out), ldo, _stream(stream)))
+
+
+def ds_expert_combine_backward(dout, ldd: int, y, ldy: int, type_: int, cols: int, slots: ds_expert_slots, weights, dy,
+                               lddy: int, dweights, stream=None) -> None:
+    _check(lib().ds_expert_combine_backward(_ptr(dout), ldd, _ptr(y), ldy, type_, cols, ctypes.byref(slots),
+                                            _ptr(weights), _ptr(dy), lddy, _ptr(dweights), _stream(stream)))
+
+
+def ds_expert_linear_f8(x: ds_f8_matrix, w: ds_f8_matrix, slots: ds_expert_slots, bias, y, type_: int, ldy: int,
+                        stream=None) -> None:
+    _check(lib().ds_expert_linear_f8(ctypes.byref(x), ctypes.byref(w), ctypes.byref(slots), _ptr(bias), _ptr(y), type_,
+                                     ldy, _stream(stream)))
+
+
+def ds_expert_weight_grad_f8(dy_t: ds_f8_matrix, x_t: ds_f8_matrix, slots: ds_expert_slots, add, ld_add: int, dw,
+                             lddw: int, stream=None) -> None:
+    _check(lib().ds_expert_weight_grad_f8(ctypes.byref(dy_t), ctypes.byref(x_t), ctypes.byref(slots), _ptr(add), ld_add,
+                                          _ptr(dw), lddw, _stream(stream)))
+
+
+def ds_adamw(tensors, count: int, options: ds_adamw_options, stream=None) -> None:
+    """tensors: a ctypes array of ds_adamw_tensor."""
+    _check(lib().ds_adamw(tensors, count, ctypes.byref(options), _stream(stream)))
+
+
 def ds_gated_f8(gu, type_: int, ld: int, rows: int, features: int, out, ckpt, flags: int = 0, stream=None) -> None:
     _check(lib().ds_gated_f8(_ptr(gu), type_, ld, rows, features, out, ckpt, flags, _stream(stream)))
 
@@ -662,3 +751,6 @@ def conv2d_shift(x, w: PackedShiftWeights, kernel_size, bias=None, stride=(1, 1)
 
 from .float8 import (F8Matrix, expand_shift_weights_f8, gated_f8, gated_f8_backward, linear_f8,  # noqa: E402,F401
                      quantize_f8, rmsnorm_f8, rmsnorm_f8_backward)
+from .experts import (ExpertOrder, expert_combine, expert_combine_backward, expert_gather,  # noqa: E402,F401
+                      expert_linear_f8, expert_order, expert_weight_grad_f8)
+from .optimizer import AdamW  # noqa: E402,F401

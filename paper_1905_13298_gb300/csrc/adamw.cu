@@ -1,0 +1,437 @@
+// One step of Adam with decoupled weight decay over many tensors in one launch
+// (the formulas and the 8-bit states' rounding are in the header).
+//
+// The work is one pass over memory: 28 bytes a value with float32 throughout,
+// 16 with 16-bit gradients, a 16-bit copy and 8-bit states.  A CTA takes 2048
+// consecutive values of one tensor, a thread eight of them, all of whose loads
+// are on their way before the first is used.  The tensors' addresses are in
+// the kernel's parameters: nothing is copied to the device before a step, and
+// a captured step is replayed with them.
+#include <math.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "f8_checks.cuh"
+
+namespace ds {
+namespace {
+
+constexpr int kThreads = 256, kEach = 8, kSpan = kThreads * kEach;
+constexpr int kFew = 40, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
+
+struct Tensor {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void* copy;
+  int64_t n;
+  uint32_t first;   // CTA of its first values
+  float decay;      // 1 - lr * weight_decay, or weight_decay where lr is on the device
+  uint32_t number;  // in the call
+  int8_t p_type, g_type, copy_type;
+  int8_t level;     // the accesses of eight values that all its addresses allow: 2 (32 bytes), 1 (16), 0
+};
+
+struct Factors {
+  float beta1, rest1, beta2, rest2, eps;
+  float rate, root;       // lr / (1 - beta1^t), (1 - beta2^t)^(-1/2)
+  float lr;
+  double log1, log2;      // of the betas, where t is on the device
+  const int64_t* step_dev;
+  const float *lr_dev, *grad_scale;
+  uint32_t step, seed;
+};
+
+template <int N>
+struct Params {
+  Factors f;
+  int count;
+  Tensor t[N];
+};
+static_assert(sizeof(Params<kFew>) <= 4096 && sizeof(Params<kMany>) <= 32764, "kernel parameters");
+
+// Eight consecutive values as they lie in memory, of a type known at run time: the same branch for a whole CTA.  They
+// are taken apart only after all arrays' loads have been issued.
+struct Raw {
+  uint32_t r[8];
+};
+__device__ __forceinline__ void load_raw(Raw& o, const void* base, int type, int64_t i, int n, int level) {
+  if (type == DS_TYPE_F32) {
+    const float* p = static_cast<const float*>(base) + i;
+    if (level == 2 && n == 8) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(o.r[0]), "=r"(o.r[1]), "=r"(o.r[2]), "=r"(o.r[3]), "=r"(o.r[4]), "=r"(o.r[5]), "=r"(o.r[6]),
+                     "=r"(o.r[7])
+                   : "l"(p));
+    } else if (level >= 1 && n == 8) {
+      const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+      o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w, o.r[4] = b.x, o.r[5] = b.y, o.r[6] = b.z, o.r[7] = b.w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o.r[k] = k < n ? __float_as_uint(p[k]) : 0u;
+    }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + i;
+    if (level >= 1 && n == 8) {
+      const uint4 a = *reinterpret_cast<const uint4*>(p);
+      o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        o.r[k] = (2 * k < n ? p[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)p[2 * k + 1] << 16 : 0u);
+    }
+  }
+}
+__device__ __forceinline__ void get_raw(const Raw& o, int type, float v[8]) {
+  if (type == DS_TYPE_F32) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(o.r[k]);
+  } else if (type == DS_TYPE_BF16) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) unpack2(o.r[k], v[2 * k], v[2 * k + 1], (const __nv_bfloat16*)nullptr);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) unpack2(o.r[k], v[2 * k], v[2 * k + 1], (const __half*)nullptr);
+  }
+}
+__device__ __forceinline__ void store_values(void* base, int type, int64_t i, int n, int level, const float v[8]) {
+  if (type == DS_TYPE_F32) {
+    float* p = static_cast<float*>(base) + i;
+    if (level == 2 && n == 8) {
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                   "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                   : "memory");
+    } else {
+      store8<false>(p, n, level >= 1, v);
+    }
+  } else if (type == DS_TYPE_BF16) {
+    store8<false>(static_cast<__nv_bfloat16*>(base) + i, n, level >= 1, v);
+  } else {
+    store8<false>(static_cast<__half*>(base) + i, n, level >= 1, v);
+  }
+}
+
+// Eight 8-bit values (level >= 1: 8-byte aligned), the missing ones zero.
+__device__ __forceinline__ uint2 load_bytes(const void* base, int64_t i, int n, int level) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
+  if (level >= 1 && n == 8) return *reinterpret_cast<const uint2*>(p);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < n) w[k >> 2] |= (uint32_t)p[k] << (8 * (k & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_bytes(void* base, int64_t i, int n, int level, uint2 q) {
+  uint8_t* p = static_cast<uint8_t*>(base) + i;
+  if (level >= 1 && n == 8) {
+    *reinterpret_cast<uint2*>(p) = q;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) p[k] = (uint8_t)((k < 4 ? q.x >> (8 * k) : q.y >> (8 * (k - 4))) & 0xFFu);
+  }
+}
+
+__device__ __forceinline__ uint32_t hash(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x243F6A89u;
+  x = (x ^ (x >> 15)) * 0xB7E15163u;
+  return x ^ (x >> 16);
+}
+
+// u >= 0 (in units of the scale) to one of its e4m3 neighbours; `bits` = 16 * (16 random bits) + 8 fills what three bits
+// of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the neighbours are 2^-9 apart, as they
+// are from 2^-6 to 2^-5, where u is moved for it.
+__device__ __forceinline__ float to_neighbour(float u, uint32_t bits) {
+  const float off = u < 0x1p-6f ? 0x1p-6f : 0.f;
+  return __uint_as_float((__float_as_uint(__fadd_rn(u, off)) + bits) & 0xFFF00000u) - off;
+}
+
+// A block of 128 values that 16 lanes hold, to 8 bits: random[k] is the hash of value k, of which the low half counts,
+// or (ROOT) the high half.  All 32 lanes of a warp call it.
+template <bool ROOT>
+__device__ __forceinline__ uint2 block_to_f8(const float v[8], const uint32_t random[8], float* scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int d = 8; d >= 1; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+  // NaN and infinities are above all finite values
+  const bool odd = __any_sync(0xFFFFFFFFu, top >= 0x7F800000u);
+  if (odd) top = __float_as_uint(max16(amax8_finite(v)));
+  const F8Scale s = f8_scale<false>(__uint_as_float(top), false);
+  float w[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t bits = ROOT ? (random[k] >> 12) & 0xFFFF0u : (random[k] << 4) & 0xFFFF0u;
+    const float u = __fmul_rn(fabsf(v[k]), s.inv);
+    float o = to_neighbour(u, bits + 8u);
+    if (ROOT && v[k] > 0.f) o = fmaxf(o, 0x1p-9f);
+    if (odd && !(fabsf(v[k]) < kInf)) o = __uint_as_float(0x7FC00000u);
+    w[k] = copysignf(o, v[k]);
+  }
+  *scale = s.s;
+  return make_uint2(f8x2<false>(w[0], w[1]) | f8x2<false>(w[2], w[3]) << 16,
+                    f8x2<false>(w[4], w[5]) | f8x2<false>(w[6], w[7]) << 16);
+}
+
+// 1 - beta^t from the logarithm of beta, for a t that only the device knows.
+__device__ __forceinline__ float rest_of_power(double log_beta, int64_t t) {
+  return -expm1f((float)((double)t * log_beta));
+}
+
+template <bool F8, int N>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Params<N> P) {
+  int lo = 0, hi = P.count - 1;  // the last tensor that starts at or before this CTA
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (P.t[mid].first <= blockIdx.x)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  const Tensor& T = P.t[lo];
+  const int64_t i = (int64_t)(blockIdx.x - T.first) * kSpan + threadIdx.x * kEach;
+  const int64_t left = T.n - i;
+  const int n = left >= 8 ? 8 : (left < 0 ? 0 : (int)left);
+
+  Raw rp, rg, rm, rv;
+  uint2 qm = make_uint2(0u, 0u), qv = qm;
+  float sm = 0.f, sv = 0.f;
+  load_raw(rg, T.g, T.g_type, i, n, T.level);
+  if constexpr (F8) {
+    qm = load_bytes(T.m, i, n, T.level);
+    qv = load_bytes(T.v, i, n, T.level);
+    if (n > 0) {
+      sm = T.m_scale[i / kF8Block];
+      sv = T.v_scale[i / kF8Block];
+    }
+  } else {
+    load_raw(rm, T.m, DS_TYPE_F32, i, n, T.level);
+    load_raw(rv, T.v, DS_TYPE_F32, i, n, T.level);
+  }
+  load_raw(rp, T.p, T.p_type, i, n, T.level);
+
+  const Factors& f = P.f;
+  float rate = f.rate, root_factor = f.root, decay = T.decay;
+  uint32_t step = f.step;
+  if (f.lr_dev || f.step_dev) {
+    const float lr = f.lr_dev ? *f.lr_dev : f.lr;
+    float rest1 = f.rate, rest2 = f.root;  // where t is known: 1 - beta1^t, and the root's factor
+    if (f.step_dev) {
+      const int64_t t = *f.step_dev;
+      step = (uint32_t)t;
+      rest1 = rest_of_power(f.log1, t);
+      rest2 = __frcp_rn(__fsqrt_rn(rest_of_power(f.log2, t)));
+    }
+    rate = __fdiv_rn(lr, rest1);
+    root_factor = rest2;
+    decay = 1.f - lr * T.decay;
+  }
+
+  float p[8], g[8], m[8], v[8], root[8];
+  get_raw(rg, T.g_type, g);
+  if (f.grad_scale) {
+    const float s = *f.grad_scale;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) g[k] = __fmul_rn(g[k], s);
+  }
+  if constexpr (F8) {
+    f8x8_value<false>(qm, m);
+    f8x8_value<false>(qv, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      m[k] = __fmul_rn(m[k], sm);
+      const float r = __fmul_rn(v[k], sv);
+      v[k] = __fmul_rn(r, r);
+    }
+  } else {
+    get_raw(rm, DS_TYPE_F32, m);
+    get_raw(rv, DS_TYPE_F32, v);
+  }
+  get_raw(rp, T.p_type, p);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    m[k] = __fadd_rn(__fmul_rn(m[k], f.beta1), __fmul_rn(g[k], f.rest1));
+    v[k] = __fadd_rn(__fmul_rn(v[k], f.beta2), __fmul_rn(__fmul_rn(g[k], g[k]), f.rest2));
+    root[k] = __fsqrt_rn(v[k]);
+    const float under = __fadd_rn(__fmul_rn(root[k], root_factor), f.eps);
+    p[k] = __fsub_rn(__fmul_rn(p[k], decay), __fdiv_rn(__fmul_rn(m[k], rate), under));
+  }
+  store_values(T.p, T.p_type, i, n, T.level, p);
+  if (T.copy) store_values(T.copy, T.copy_type, i, n, T.level, p);
+  if constexpr (F8) {
+    const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
+    uint32_t random[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) random[k] = hash(((uint32_t)i + k) * 0x9E3779B1u + key);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k >= n) m[k] = root[k] = 0.f;  // (values that do not exist: 0 / 0 with eps = 0)
+    qm = block_to_f8<false>(m, random, &sm);
+    qv = block_to_f8<true>(root, random, &sv);
+    store_bytes(T.m, i, n, T.level, qm);
+    store_bytes(T.v, i, n, T.level, qv);
+    if ((threadIdx.x & 15) == 0 && n > 0) {
+      T.m_scale[i / kF8Block] = sm;
+      T.v_scale[i / kF8Block] = sv;
+    }
+  } else {
+    store_values(T.m, DS_TYPE_F32, i, n, T.level, m);
+    store_values(T.v, DS_TYPE_F32, i, n, T.level, v);
+  }
+}
+
+template <int N>
+cudaError_t launch(const std::vector<Tensor>& all, size_t from, int count, uint32_t ctas, const Factors& f, bool f8,
+                   cudaStream_t st) {
+  Params<N> p;
+  p.f = f;
+  p.count = count;
+  for (int k = 0; k < count; ++k) p.t[k] = all[from + k];
+  if (f8)
+    adamw_kernel<true, N><<<ctas, kThreads, 0, st>>>(p);
+  else
+    adamw_kernel<false, N><<<ctas, kThreads, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_all(std::vector<Tensor>& all, const Factors& f, bool f8, cudaStream_t st) {
+  size_t from = 0;
+  while (from < all.size()) {
+    uint64_t ctas = 0;
+    size_t to = from;
+    for (; to < all.size() && to - from < (size_t)kMany; ++to) {
+      const uint64_t mine = (uint64_t)((all[to].n + kSpan - 1) / kSpan);
+      if (to > from && ctas + mine > ((uint64_t)1 << 31) - 1) break;
+      all[to].first = (uint32_t)ctas;
+      ctas += mine;
+    }
+    const int count = (int)(to - from);
+    const cudaError_t e = count <= kFew ? launch<kFew>(all, from, count, (uint32_t)ctas, f, f8, st)
+                                        : launch<kMany>(all, from, count, (uint32_t)ctas, f, f8, st);
+    if (e != cudaSuccess) return e;
+    from = to;
+  }
+  return cudaSuccess;
+}
+
+// A tensor's memories: [at, end), and whether the call writes them.
+struct Piece {
+  uintptr_t at, end;
+  int tensor;
+  bool written;
+};
+
+// Written memory is apart from everything else; sorted by address, a piece can only overlap the ones that reach past its
+// start, of which the one that reaches furthest (and the written one that does) are kept.
+ds_status check_pieces(std::vector<Piece>& pieces) {
+  bool sorted = true;
+  for (size_t k = 1; k < pieces.size() && sorted; ++k) sorted = pieces[k - 1].at <= pieces[k].at;
+  if (!sorted)
+    std::sort(pieces.begin(), pieces.end(), [](const Piece& a, const Piece& b) { return a.at < b.at; });
+  uintptr_t any = 0, written = 0;
+  for (const Piece& q : pieces) {
+    if (q.at < written || (q.written && q.at < any))
+      return fail(DS_ERR_INVALID_ARG, "memory of tensor %d overlaps that of another tensor or of itself", q.tensor);
+    if (q.end > any) any = q.end;
+    if (q.written && q.end > written) written = q.end;
+  }
+  return DS_OK;
+}
+
+ds_status adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_options* o, cudaStream_t st) {
+  if (count < 0) return fail(DS_ERR_SHAPE, "count must not be negative");
+  if (!o || (!tensors && count > 0)) return fail(DS_ERR_INVALID_ARG, "NULL pointer argument");
+  if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1))
+    return fail(DS_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+  if (!(o->eps >= 0)) return fail(DS_ERR_INVALID_ARG, "eps must not be negative");
+  if (!o->step_dev && o->step < 1) return fail(DS_ERR_INVALID_ARG, "the step must be at least 1");
+  if (!o->lr_dev && !(o->lr >= 0)) return fail(DS_ERR_INVALID_ARG, "lr must not be negative");
+  if (!aligned(o->step_dev, 8) || !aligned(o->lr_dev, 4) || !aligned(o->grad_scale, 4))
+    return fail(DS_ERR_ALIGNMENT, "step_dev must be 8-byte aligned, lr_dev and grad_scale 4-byte aligned");
+  std::vector<Tensor> all;
+  std::vector<Piece> pieces;
+  all.reserve(count);
+  pieces.reserve((size_t)count * 7);
+  bool f8 = false, known = false;
+  for (int k = 0; k < count; ++k) {
+    const ds_adamw_tensor& t = tensors[k];
+    ds_status r;
+    if (t.n < 0) return fail(DS_ERR_SHAPE, "tensor %d: n must not be negative", k);
+    if (t.n > (int64_t)1 << 40) return fail(DS_ERR_UNSUPPORTED, "tensor %d: too large", k);
+    if ((r = check_type(t.p_type)) != DS_OK || (r = check_type(t.g_type)) != DS_OK) return r;
+    if (t.copy && (r = check_type(t.copy_type)) != DS_OK) return r;
+    if (!(t.weight_decay >= 0)) return fail(DS_ERR_INVALID_ARG, "tensor %d: weight_decay must not be negative", k);
+    if (t.n == 0) continue;
+    if (!t.p || !t.g || !t.m || !t.v) return fail(DS_ERR_INVALID_ARG, "tensor %d: NULL pointer", k);
+    if (!t.m_scale != !t.v_scale) return fail(DS_ERR_INVALID_ARG, "tensor %d: one scale of two is given", k);
+    if (known && f8 != (t.m_scale != nullptr))
+      return fail(DS_ERR_INVALID_ARG, "tensor %d: states of another kind than the others'", k);
+    known = true;
+    f8 = t.m_scale != nullptr;
+    const int64_t ps = type_size(t.p_type), gs = type_size(t.g_type), cs = type_size(t.copy_type), ss = f8 ? 1 : 4;
+    if (!aligned(t.p, ps) || !aligned(t.g, gs) || !aligned(t.m, ss) || !aligned(t.v, ss) || !aligned(t.copy, cs) ||
+        !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))
+      return fail(DS_ERR_ALIGNMENT, "tensor %d: memory is not aligned to its type", k);
+    auto level = [](const void* p, int64_t size) {
+      return size == 4 ? (aligned(p, 32) ? 2 : (aligned(p, 16) ? 1 : 0)) : (aligned(p, 8 * size) ? 2 : 0);
+    };
+    int lv = level(t.p, ps);
+    for (int x : {level(t.g, gs), level(t.m, ss), level(t.v, ss), t.copy ? level(t.copy, cs) : 2}) lv = x < lv ? x : lv;
+    Tensor d = {};
+    d.p = t.p, d.g = t.g, d.m = t.m, d.v = t.v, d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.copy = t.copy, d.n = t.n;
+    d.decay = o->lr_dev || o->step_dev ? t.weight_decay : (float)(1.0 - o->lr * (double)t.weight_decay);
+    d.number = (uint32_t)k;
+    d.p_type = (int8_t)t.p_type, d.g_type = (int8_t)t.g_type, d.copy_type = (int8_t)t.copy_type, d.level = (int8_t)lv;
+    all.push_back(d);
+    auto piece = [&](const void* p, int64_t bytes, bool written) {
+      if (!p) return;
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+      pieces.push_back(Piece{at, at + (uintptr_t)bytes, k, written});
+    };
+    piece(t.p, t.n * ps, true);
+    piece(t.g, t.n * gs, false);
+    piece(t.m, t.n * ss, true);
+    piece(t.v, t.n * ss, true);
+    piece(t.m_scale, blocks_of(t.n) * 4, true);
+    piece(t.v_scale, blocks_of(t.n) * 4, true);
+    piece(t.copy, t.n * cs, true);
+  }
+  if (all.empty()) return DS_OK;
+  for (const void* p : {(const void*)o->step_dev, (const void*)o->lr_dev, (const void*)o->grad_scale})
+    if (p) pieces.push_back(Piece{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (p == o->step_dev ? 8 : 4), -1, false});
+  const ds_status r = check_pieces(pieces);
+  if (r != DS_OK) return r;
+
+  Factors f = {};
+  f.beta1 = (float)o->beta1, f.rest1 = (float)(1.0 - o->beta1);
+  f.beta2 = (float)o->beta2, f.rest2 = (float)(1.0 - o->beta2);
+  f.eps = (float)o->eps;
+  f.lr = (float)o->lr;
+  f.step_dev = o->step_dev, f.lr_dev = o->lr_dev, f.grad_scale = o->grad_scale;
+  f.seed = o->seed;
+  f.step = (uint32_t)o->step;
+  f.log1 = log(o->beta1), f.log2 = log(o->beta2);
+  if (!o->step_dev) {
+    const double rest1 = 1.0 - pow(o->beta1, (double)o->step), rest2 = 1.0 - pow(o->beta2, (double)o->step);
+    f.rate = o->lr_dev ? (float)rest1 : (float)(o->lr / rest1);
+    f.root = (float)(1.0 / sqrt(rest2));
+  }
+  return cuda_check(launch_all(all, f, f8, st), "adamw launch");
+}
+
+}  // namespace
+}  // namespace ds
+
+extern "C" ds_status ds_adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_options* options, void* stream) {
+  ds::NvtxRange nvtx_range("ds_adamw");
+  ds::clear_error();
+  try {
+    return ds::adamw(tensors, count, options, static_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return ds::fail(DS_ERR_UNSUPPORTED, "no host memory for the list of %d tensors", count);
+  }
+}

@@ -245,6 +245,9 @@ size_t ds_abi_struct_size(int which) {
   return which == 0   ? sizeof(ds_weights)
          : which == 1 ? sizeof(ds_layer)
          : which == 2 ? sizeof(ds_f8_matrix)
+         : which == 3 ? sizeof(ds_expert_slots)
+         : which == 4 ? sizeof(ds_adamw_tensor)
+         : which == 5 ? sizeof(ds_adamw_options)
                       : 0;
 }
 

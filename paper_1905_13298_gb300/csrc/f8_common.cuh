@@ -500,6 +500,7 @@ cudaError_t launch_linear_f8(const LinearF8Params& p, cudaStream_t st);
 int linear_f8_tile(const LinearF8Params& p);  // rows of the tile that the launch would take
 int read_f8_fault_flag();
 int read_gated_f8_fault_flag();
+int read_expert_f8_fault_flag();
 void set_f8_wait_cycles(long long cycles);
 long long f8_wait_cycles();  // limit of a bounded wait of the next launches
 

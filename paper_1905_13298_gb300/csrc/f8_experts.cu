@@ -1,0 +1,240 @@
+// Products of the experts' parts with 8-bit operands: the persistent kernel of
+// large products (f8_linear.cuh) over the tiles of all experts.  Which rows an
+// expert has is known on the device only, so every CTA makes the list of the
+// tiles from the segments' offsets when it starts; nothing waits for the host.
+#include "experts.cuh"
+#include "f8_linear.cuh"
+
+namespace ds {
+namespace {
+
+// One expert's part of the output, for the stores.
+struct OutputPart {
+  const float *bias, *add;
+  void* y;
+  int64_t M, N, ld_add, ldy;
+  int type, vec, pairs;
+};
+
+// y = x w_e^T.  Tiles of expert after expert, and behind them those of the rows that no expert has (no blocks: zeros).
+template <int COLS_OF_TILE>
+struct SegmentTiles {
+  static constexpr int N = COLS_OF_TILE;
+  static constexpr bool EMPTY = true;
+  static constexpr uint32_t GROUP = 16;  // row tiles that share columns, as TileOrder::G
+  const int32_t* offsets;
+  int experts;
+  uint32_t rows, cols, tiles_n;
+  uint32_t* start;  // shared memory: [experts + 2], first rows of the segments; the last two: rows in use, all rows
+  uint32_t* first;  // [experts + 2], first tiles
+  static size_t bytes(int experts) { return (size_t)(experts + 2) * 8; }
+
+  __device__ __forceinline__ SegmentTiles ready(const Params&, void* at) const {
+    SegmentTiles s = *this;
+    s.start = static_cast<uint32_t*>(at);
+    s.first = s.start + experts + 2;
+    for (int e = threadIdx.x; e < experts + 2; e += blockDim.x) {
+      const uint32_t o = e <= experts ? (uint32_t)offsets[e] : rows;
+      s.start[e] = o < rows ? o : rows;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {  // a lane counts the tiles of some experts in a row
+      const int per = (experts + 1 + 31) / 32, from = threadIdx.x * per;
+      uint32_t sum = 0;
+      for (int e = from; e < from + per && e <= experts; ++e) sum += s.tiles_m(e) * tiles_n;
+      uint32_t upto = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (threadIdx.x >= d) upto += up;
+      }
+      uint32_t at_tile = upto - sum;
+      for (int e = from; e < from + per && e <= experts; ++e) {
+        s.first[e] = at_tile;
+        at_tile += s.tiles_m(e) * tiles_n;
+      }
+      if (threadIdx.x == 31) s.first[experts + 1] = upto;
+    }
+    return s;  // a barrier follows before it is used
+  }
+  __device__ __forceinline__ uint32_t tiles_m(int e) const {
+    return start[e + 1] > start[e] ? (start[e + 1] - start[e] + ROWS - 1) / ROWS : 0u;
+  }
+  __device__ __forceinline__ int expert(uint32_t t) const {  // the last one whose first tile is not behind t
+    int lo = 0, hi = experts;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= t)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  }
+  __device__ __forceinline__ uint32_t count() const { return first[experts + 1]; }
+  __device__ __forceinline__ Tile at(const Params& P, uint32_t t) const {
+    const int e = expert(t);
+    int tm, tn;
+    grouped(t - first[e], tiles_m(e), tiles_n, GROUP, tm, tn);
+    return Tile{(int)start[e] + tm * ROWS, (int)((uint32_t)e * cols) + tn * N, 0, e < experts ? P.nk : 0};
+  }
+  __device__ __forceinline__ int64_t blocks(const Params& P) const {
+    const uint32_t n = first[experts], mine = blockIdx.x < n ? (n - blockIdx.x - 1) / gridDim.x + 1 : 0;
+    return (int64_t)mine * P.nk;
+  }
+  __device__ __forceinline__ int aligned(const Params& P, const Tile&) const { return P.aligned; }
+  template <typename F>
+  __device__ __forceinline__ void place(const Params& P, const Tile& tile, uint32_t t, const F& store) const {
+    const int e = expert(t);
+    const OutputPart o{e < experts && P.bias ? P.bias + (int64_t)e * cols : nullptr,
+                       nullptr, P.y, (int64_t)start[e + 1], (int64_t)cols, 0, P.ldy, P.type, P.vec, P.pairs};
+    store(o, (int64_t)tile.m0, (int64_t)(tile.n0 - (int)((uint32_t)e * cols)));
+  }
+};
+
+// dw_e = dy_t x_t^T over the blocks of each segment: P.x is dy_t, P.w is x_t.  An expert without rows has tiles without
+// blocks.
+template <int COLS_OF_TILE>
+struct GradientTiles {
+  static constexpr int N = COLS_OF_TILE;
+  static constexpr bool EMPTY = true;
+  const int32_t* offsets;
+  int experts;
+  uint32_t rows, tiles_m, tiles_n, G;
+  uint32_t* start;  // shared memory: [experts + 1], first blocks of the segments
+  static size_t bytes(int experts) { return (size_t)(experts + 1) * 4; }
+
+  __device__ __forceinline__ GradientTiles ready(const Params&, void* at) const {
+    GradientTiles s = *this;
+    s.start = static_cast<uint32_t*>(at);
+    for (int e = threadIdx.x; e <= experts; e += blockDim.x) {
+      const uint32_t o = (uint32_t)offsets[e];
+      s.start[e] = ((o < rows ? o : rows) + BK - 1) / BK;
+    }
+    return s;
+  }
+  __device__ __forceinline__ uint32_t count() const { return (uint32_t)experts * tiles_m * tiles_n; }
+  __device__ __forceinline__ uint32_t expert(uint32_t t) const { return t / (tiles_m * tiles_n); }
+  __device__ __forceinline__ int blocks_of_expert(uint32_t e) const {
+    return start[e + 1] > start[e] ? (int)(start[e + 1] - start[e]) : 0;
+  }
+  __device__ __forceinline__ Tile at(const Params&, uint32_t t) const {
+    const uint32_t e = expert(t);
+    int tm, tn;
+    grouped(t - e * (tiles_m * tiles_n), tiles_m, tiles_n, G, tm, tn);
+    return Tile{tm * ROWS, tn * N, (int)start[e], blocks_of_expert(e)};
+  }
+  __device__ __forceinline__ int64_t blocks(const Params&) const {
+    int64_t n = 0;
+    for (uint32_t t = blockIdx.x; t < count(); t += gridDim.x) n += blocks_of_expert(expert(t));
+    return n;
+  }
+  __device__ __forceinline__ int aligned(const Params& P, const Tile& t) const {
+    return P.aligned == 8 && t.kb0 % 8 == 0 ? 8 : (P.aligned >= 4 && t.kb0 % 4 == 0 ? 4 : 1);
+  }
+  template <typename F>
+  __device__ __forceinline__ void place(const Params& P, const Tile& tile, uint32_t t, const F& store) const {
+    const int64_t row = (int64_t)expert(t) * P.M;
+    const OutputPart o{nullptr, P.add ? P.add + row * P.ld_add : nullptr, static_cast<float*>(P.y) + row * P.ldy,
+                       P.M, P.N, P.ld_add, P.ldy, P.type, P.vec, P.pairs};
+    store(o, (int64_t)tile.m0, (int64_t)tile.n0);
+  }
+};
+
+template <bool COLS, bool WIDE, typename Order>
+cudaError_t launch(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, const Order& order, int64_t most,
+                   cudaStream_t st) {
+  using Cfg = BigCfg<COLS, Order::N>;
+  static const cudaError_t attr =
+      cudaFuncSetAttribute(linear_f8_big_kernel<COLS, WIDE, Order>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)(Cfg::SMEM + Order::bytes(DS_EXPERTS_MAX)));
+  if (attr != cudaSuccess) return attr;
+  static_assert(Cfg::SMEM + (DS_EXPERTS_MAX + 2) * 8 <= 232448, "shared memory of a CTA");
+  const int64_t sms = sm_count() > 0 ? sm_count() : 1;
+  linear_f8_big_kernel<COLS, WIDE, Order><<<(unsigned)(most < sms ? most : sms), Cfg::THREADS,
+                                            Cfg::SMEM + Order::bytes(order.experts), st>>>(mx, mw, p, order);
+  return cudaGetLastError();
+}
+
+template <typename Order>
+cudaError_t start(const CUtensorMap& mx, const CUtensorMap& mw, const Params& p, const Order& order, int64_t most, bool wide,
+                  cudaStream_t st) {
+  if (p.w.shift)
+    return wide ? launch<false, true>(mx, mw, p, order, most, st) : launch<false, false>(mx, mw, p, order, most, st);
+  return wide ? launch<true, true>(mx, mw, p, order, most, st) : launch<true, false>(mx, mw, p, order, most, st);
+}
+
+// What both products' parameters have in common; wide: rows are aligned for stores of eight values.
+Params params_of(const ExpertProduct& e, const ds_f8_matrix* x, const ds_f8_matrix* w, bool* wide) {
+  Params p = {};
+  p.x = scales_at(x);
+  p.w = scales_at(w);
+  p.bias = e.bias;
+  p.add = e.add;
+  p.y = e.y;
+  p.M = x->rows;
+  p.N = w->rows;
+  p.ld_add = e.ld_add;
+  p.ldy = e.ldy;
+  p.nk = (int)((x->cols + BK - 1) / BK);
+  p.idesc = idesc_of(x, w);
+  p.type = e.type;
+  const size_t size = e.type == DS_TYPE_F32 ? 4 : 2;
+  auto rows = [&](int n) {
+    return aligned(e.y, n * size) && e.ldy % n == 0;
+  };
+  p.vec = rows(4) && (e.add == nullptr || (aligned(e.add, 16) && e.ld_add % 4 == 0));
+  p.pairs = rows(2) && (e.add == nullptr || (aligned(e.add, 8) && e.ld_add % 2 == 0));
+  *wide = p.vec && rows(8);
+  auto scales = [&](int n) {
+    return aligned(p.x.s, 4 * n) && p.x.ld % n == 0 && aligned(p.w.s, 4 * n) && p.w.ld % n == 0;
+  };
+  p.aligned = scales(8) ? 8 : (scales(4) ? 4 : 1);
+  p.wait_cycles = f8_wait_cycles();
+  return p;
+}
+
+int64_t over(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
+template <int N>
+cudaError_t linear(const ExpertProduct& e, cudaStream_t st) {
+  bool wide;
+  const Params p = params_of(e, e.x, e.w, &wide);
+  const int64_t cols = e.w->rows / e.s->experts;
+  CUtensorMap mx = {}, mw = {};
+  if (p.nk > 0 && (!make_map(&mx, e.x, ROWS) || !make_map(&mw, e.w, N))) return cudaErrorInvalidValue;
+  SegmentTiles<N> t = {};
+  t.offsets = e.s->offsets;
+  t.experts = e.s->experts;
+  t.rows = (uint32_t)e.s->rows;
+  t.cols = (uint32_t)cols;
+  t.tiles_n = (uint32_t)over(cols, N);
+  const int64_t most = (over(e.s->rows, ROWS) + e.s->experts) * t.tiles_n;
+  return start(mx, mw, p, t, most, wide, st);
+}
+
+template <int N>
+cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
+  bool wide;
+  const Params p = params_of(e, e.w, e.x, &wide);
+  CUtensorMap mx = {}, mw = {};
+  if (p.nk > 0 && (!make_map(&mx, e.w, ROWS) || !make_map(&mw, e.x, N))) return cudaErrorInvalidValue;
+  GradientTiles<N> t = {};
+  t.offsets = e.s->offsets;
+  t.experts = e.s->experts;
+  t.rows = (uint32_t)e.s->rows;
+  t.tiles_m = (uint32_t)over(p.M, ROWS);
+  t.tiles_n = (uint32_t)over(p.N, N);
+  t.G = t.tiles_m < 12 ? t.tiles_m : 12;  // about one wave of tiles is a square
+  return start(mx, mw, p, t, (int64_t)t.experts * t.tiles_m * t.tiles_n, wide, st);
+}
+
+}  // namespace
+
+cudaError_t launch_expert_linear_f8(const ExpertProduct& e, cudaStream_t st) { return linear<256>(e, st); }
+
+cudaError_t launch_expert_weight_grad_f8(const ExpertProduct& e, cudaStream_t st) { return weight_grad<256>(e, st); }
+
+int read_expert_f8_fault_flag() { return read_and_clear_fault(); }
+
+}  // namespace ds
