@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "f8_checks.cuh"
@@ -18,7 +19,10 @@
 namespace ds {
 namespace {
 
-constexpr int kThreads = 256, kEach = 8, kSpan = kThreads * kEach;
+constexpr int kThreads = 256, kEach = 8;
+// Groups of eight values of a thread: with 8-bit states, two share the work that does not depend on values.
+constexpr int groups_of(bool f8) { return f8 ? 2 : 1; }
+constexpr int64_t span_of(bool f8) { return (int64_t)kThreads * kEach * groups_of(f8); }
 constexpr int kFew = 40, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
 
 struct Tensor {
@@ -135,46 +139,99 @@ __device__ __forceinline__ void store_bytes(void* base, int64_t i, int n, int le
   }
 }
 
-__device__ __forceinline__ uint32_t hash(uint32_t x) {
-  x = (x ^ (x >> 16)) * 0x243F6A89u;
-  x = (x ^ (x >> 15)) * 0xB7E15163u;
-  return x ^ (x >> 16);
+__device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
+__device__ __forceinline__ float lo_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
+// Sums one by one: packed ones are contracted with the products before them, which the definition rounds.
+__device__ __forceinline__ uint64_t add_each(uint64_t a, uint64_t b) {
+  return pair(__fadd_rn(lo_of(a), lo_of(b)), __fadd_rn(hi_of(a), hi_of(b)));
+}
+__device__ __forceinline__ uint64_t sub_each(uint64_t a, uint64_t b) {
+  return pair(__fsub_rn(lo_of(a), lo_of(b)), __fsub_rn(hi_of(a), hi_of(b)));
+}
+// The largest magnitude of three; NaN where one is.
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
-// u >= 0 (in units of the scale) to one of its e4m3 neighbours; `bits` = 16 * (16 random bits) + 8 fills what three bits
-// of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the neighbours are 2^-9 apart, as they
-// are from 2^-6 to 2^-5, where u is moved for it.
+// Square roots of two values, correctly rounded, for 0 and from 2^-149 to 2^67; NaN above that.  An approximate
+// reciprocal root y of the values in units of 2^-60 gives the root g and half its reciprocal h; one step by their
+// residual 1/2 - g h, then one by the root's own residual v - g^2, which is exact (P. Markstein, IBM J. Res. Dev. 34 (1),
+// 1990).  The same as __fsqrt_rn for all mantissas of two neighbouring exponents, and so for all of these numbers.
+__device__ __forceinline__ uint64_t root2(uint64_t v) {
+  const uint64_t u = mul2(v, both(0x1p60f));
+  float y0, y1;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo_of(u)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi_of(u)));
+  const uint64_t y = pair(fminf(y0, 0x1p64f), fminf(y1, 0x1p64f));  // of 0 as well
+  const uint64_t g = mul2(u, y), h = mul2(y, both(0.5f));
+  const uint64_t t = fma2(mul2(g, both(-1.f)), h, both(0.5f));
+  const uint64_t g1 = fma2(g, t, g), h1 = fma2(h, t, h);
+  const uint64_t d = fma2(mul2(g1, both(-1.f)), g1, u);
+  return mul2(fma2(d, h1, g1), both(0x1p-30f));
+}
+// Quotients a / b, correctly rounded, for b from 2^-60 to 2^60 and a up to 2^60, where they are 0 or normal and a is not
+// below 2^-102 (there the last place may be off): a quotient of one step by the correctly rounded reciprocal and its
+// exact remainder, by the same paper.
+__device__ __forceinline__ uint64_t quotient2(uint64_t a, uint64_t b) {
+  float y0, y1;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo_of(b)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi_of(b)));
+  const uint64_t y = pair(y0, y1), minus = mul2(b, both(-1.f));
+  const uint64_t r = fma2(fma2(minus, y, both(1.f)), y, y);
+  const uint64_t q = mul2(a, r);
+  return fma2(fma2(minus, q, a), r, q);
+}
+
+// A magnitude in units of the scale, and `bits` = 16 * (16 random bits): to one of its e4m3 neighbours.  bits + 8 fills
+// what three bits of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the neighbours are 2^-9
+// apart, as they are from 2^-6 to 2^-5, where u is moved for it.
 __device__ __forceinline__ float to_neighbour(float u, uint32_t bits) {
   const float off = u < 0x1p-6f ? 0x1p-6f : 0.f;
-  return __uint_as_float((__float_as_uint(__fadd_rn(u, off)) + bits) & 0xFFF00000u) - off;
+  return __uint_as_float((__float_as_uint(__fadd_rn(u, off)) + bits + 8u) & 0xFFF00000u) - off;
 }
 
-// A block of 128 values that 16 lanes hold, to 8 bits: random[k] is the hash of value k, of which the low half counts,
-// or (ROOT) the high half.  All 32 lanes of a warp call it.
-template <bool ROOT>
-__device__ __forceinline__ uint2 block_to_f8(const float v[8], const uint32_t random[8], float* scale) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
-#pragma unroll
-  for (int d = 8; d >= 1; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-  // NaN and infinities are above all finite values
-  const bool odd = __any_sync(0xFFFFFFFFu, top >= 0x7F800000u);
-  if (odd) top = __float_as_uint(max16(amax8_finite(v)));
-  const F8Scale s = f8_scale<false>(__uint_as_float(top), false);
+// A block of 128 values that 16 lanes hold, to 8 bits.  ODD: some of the values are not finite.
+template <bool ROOT, bool ODD>
+__device__ __forceinline__ uint2 block_to_f8(const uint64_t v[4], const uint32_t bits[8], F8Scale s) {
   float w[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t bits = ROOT ? (random[k] >> 12) & 0xFFFF0u : (random[k] << 4) & 0xFFFF0u;
-    const float u = __fmul_rn(fabsf(v[k]), s.inv);
-    float o = to_neighbour(u, bits + 8u);
-    if (ROOT && v[k] > 0.f) o = fmaxf(o, 0x1p-9f);
-    if (odd && !(fabsf(v[k]) < kInf)) o = __uint_as_float(0x7FC00000u);
-    w[k] = copysignf(o, v[k]);
+  for (int k = 0; k < 4; ++k) {
+    const uint64_t u2 = mul2(v[k], both(s.inv));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float u = h ? hi_of(u2) : lo_of(u2);
+      float o = to_neighbour(fabsf(u), bits[2 * k + h]);
+      if (ROOT)
+        o = fmaxf(o, fminf(u * 0x1p127f, 0x1p-9f));  // u > 0 is above 2^-136
+      else
+        o = copysignf(o, u);
+      if (ODD && !(fabsf(h ? hi_of(v[k]) : lo_of(v[k])) < kInf)) o = __uint_as_float(0x7FC00000u);
+      w[2 * k + h] = o;
+    }
   }
-  *scale = s.s;
   return make_uint2(f8x2<false>(w[0], w[1]) | f8x2<false>(w[2], w[3]) << 16,
                     f8x2<false>(w[4], w[5]) | f8x2<false>(w[6], w[7]) << 16);
+}
+
+// The largest of the bit patterns of 16 lanes' magnitudes: NaN is above infinity, and that above all numbers.
+__device__ __forceinline__ float top16(float v) {
+  const uint32_t lanes = threadIdx.x & 16 ? 0xFFFF0000u : 0x0000FFFFu;
+  return __uint_as_float(__reduce_max_sync(lanes, __float_as_uint(v) & 0x7FFFFFFFu));
+}
+__device__ __forceinline__ float top8(const uint64_t v[4]) {
+  float t = max3_abs(lo_of(v[0]), hi_of(v[0]), lo_of(v[1]));
+  t = max3_abs(t, hi_of(v[1]), lo_of(v[2]));
+  t = max3_abs(t, hi_of(v[2]), lo_of(v[3]));
+  return max3_abs(t, hi_of(v[3]), 0.f);
+}
+__device__ __forceinline__ float finite_top8(const uint64_t v[4]) {
+  float t = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) t = fmaxf(t, fmaxf(finite_abs(lo_of(v[k])), finite_abs(hi_of(v[k]))));
+  return t;
 }
 
 // 1 - beta^t from the logarithm of beta, for a t that only the device knows.
@@ -193,26 +250,30 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
       hi = mid - 1;
   }
   const Tensor& T = P.t[lo];
-  const int64_t i = (int64_t)(blockIdx.x - T.first) * kSpan + threadIdx.x * kEach;
-  const int64_t left = T.n - i;
-  const int n = left >= 8 ? 8 : (left < 0 ? 0 : (int)left);
-
-  Raw rp, rg, rm, rv;
-  uint2 qm = make_uint2(0u, 0u), qv = qm;
-  float sm = 0.f, sv = 0.f;
-  load_raw(rg, T.g, T.g_type, i, n, T.level);
-  if constexpr (F8) {
-    qm = load_bytes(T.m, i, n, T.level);
-    qv = load_bytes(T.v, i, n, T.level);
-    if (n > 0) {
-      sm = T.m_scale[i / kF8Block];
-      sv = T.v_scale[i / kF8Block];
+  struct Loaded {
+    Raw p, g, m, v;
+    uint2 qm, qv;
+    float sm, sv;
+  };
+  auto load = [&](int64_t i, int n) {
+    Loaded o;
+    load_raw(o.g, T.g, T.g_type, i, n, T.level);
+    if constexpr (F8) {
+      o.qm = load_bytes(T.m, i, n, T.level);
+      o.qv = load_bytes(T.v, i, n, T.level);
+      o.sm = n > 0 ? T.m_scale[i / kF8Block] : 0.f;
+      o.sv = n > 0 ? T.v_scale[i / kF8Block] : 0.f;
+    } else {
+      load_raw(o.m, T.m, DS_TYPE_F32, i, n, T.level);
+      load_raw(o.v, T.v, DS_TYPE_F32, i, n, T.level);
     }
-  } else {
-    load_raw(rm, T.m, DS_TYPE_F32, i, n, T.level);
-    load_raw(rv, T.v, DS_TYPE_F32, i, n, T.level);
-  }
-  load_raw(rp, T.p, T.p_type, i, n, T.level);
+    load_raw(o.p, T.p, T.p_type, i, n, T.level);
+    return o;
+  };
+  const int64_t n_all = T.n;
+  auto values_at = [&](int64_t i) { return left8(n_all, i); };
+  int64_t i = (int64_t)(blockIdx.x - T.first) * span_of(F8) + threadIdx.x * kEach;
+  Loaded in = load(i, values_at(i));
 
   const Factors& f = P.f;
   float rate = f.rate, root_factor = f.root, decay = T.decay;
@@ -231,56 +292,125 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     decay = 1.f - lr * T.decay;
   }
 
-  float p[8], g[8], m[8], v[8], root[8];
-  get_raw(rg, T.g_type, g);
-  if (f.grad_scale) {
-    const float s = *f.grad_scale;
+#pragma unroll 1
+  for (int group = 0; group < groups_of(F8); ++group, i += kThreads * kEach) {
+    const int n = values_at(i);
+    // Pairs of values: two operations per instruction.  Every product and sum is rounded by itself, as defined.
+    uint64_t p[4], g[4], m[4], v[4], root[4];
+    auto pairs = [](const float (&x)[8], uint64_t (&o)[4]) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) g[k] = __fmul_rn(g[k], s);
-  }
-  if constexpr (F8) {
-    f8x8_value<false>(qm, m);
-    f8x8_value<false>(qv, v);
+      for (int k = 0; k < 4; ++k) o[k] = pair(x[2 * k], x[2 * k + 1]);
+    };
+    auto values = [](const uint64_t (&x)[4], float (&o)[8]) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      m[k] = __fmul_rn(m[k], sm);
-      const float r = __fmul_rn(v[k], sv);
-      v[k] = __fmul_rn(r, r);
+      for (int k = 0; k < 4; ++k) unpair(x[k], o[2 * k], o[2 * k + 1]);
+    };
+    float each[8];
+    get_raw(in.g, T.g_type, each);
+    pairs(each, g);
+    if (f.grad_scale) {
+      const uint64_t s = both(*f.grad_scale);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[k] = mul2(g[k], s);
     }
-  } else {
-    get_raw(rm, DS_TYPE_F32, m);
-    get_raw(rv, DS_TYPE_F32, v);
-  }
-  get_raw(rp, T.p_type, p);
+    if constexpr (F8) {
+      f8x8_value<false>(in.qm, each);
+      pairs(each, m);
+      f8x8_value<false>(in.qv, each);
+      pairs(each, v);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    m[k] = __fadd_rn(__fmul_rn(m[k], f.beta1), __fmul_rn(g[k], f.rest1));
-    v[k] = __fadd_rn(__fmul_rn(v[k], f.beta2), __fmul_rn(__fmul_rn(g[k], g[k]), f.rest2));
-    root[k] = __fsqrt_rn(v[k]);
-    const float under = __fadd_rn(__fmul_rn(root[k], root_factor), f.eps);
-    p[k] = __fsub_rn(__fmul_rn(p[k], decay), __fdiv_rn(__fmul_rn(m[k], rate), under));
-  }
-  store_values(T.p, T.p_type, i, n, T.level, p);
-  if (T.copy) store_values(T.copy, T.copy_type, i, n, T.level, p);
-  if constexpr (F8) {
-    const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
-    uint32_t random[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) random[k] = hash(((uint32_t)i + k) * 0x9E3779B1u + key);
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k >= n) m[k] = root[k] = 0.f;  // (values that do not exist: 0 / 0 with eps = 0)
-    qm = block_to_f8<false>(m, random, &sm);
-    qv = block_to_f8<true>(root, random, &sv);
-    store_bytes(T.m, i, n, T.level, qm);
-    store_bytes(T.v, i, n, T.level, qv);
-    if ((threadIdx.x & 15) == 0 && n > 0) {
-      T.m_scale[i / kF8Block] = sm;
-      T.v_scale[i / kF8Block] = sv;
+      for (int k = 0; k < 4; ++k) {
+        m[k] = mul2(m[k], both(in.sm));
+        const uint64_t r = mul2(v[k], both(in.sv));
+        v[k] = mul2(r, r);
+      }
+    } else {
+      get_raw(in.m, DS_TYPE_F32, each);
+      pairs(each, m);
+      get_raw(in.v, DS_TYPE_F32, each);
+      pairs(each, v);
     }
-  } else {
-    store_values(T.m, DS_TYPE_F32, i, n, T.level, m);
-    store_values(T.v, DS_TYPE_F32, i, n, T.level, v);
+    get_raw(in.p, T.p_type, each);
+    pairs(each, p);
+    const int64_t next = i + kThreads * kEach;
+    if (group + 1 < groups_of(F8)) in = load(next, values_at(next));  // on its way while this group is worked on
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = add_each(mul2(m[k], both(f.beta1)), mul2(g[k], both(f.rest1)));
+      v[k] = add_each(mul2(v[k], both(f.beta2)), mul2(mul2(g[k], g[k]), both(f.rest2)));
+    }
+    auto root_any = [&] {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) root[k] = pair(__fsqrt_rn(lo_of(v[k])), __fsqrt_rn(hi_of(v[k])));
+    };
+    // FAST: by quotient2, within its range
+    auto update = [&](auto fast) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint64_t up = mul2(m[k], both(rate)), under = add_each(mul2(root[k], both(root_factor)), both(f.eps));
+        uint64_t q;
+        if constexpr (decltype(fast)::value)
+          q = quotient2(up, under);
+        else
+          q = pair(__fdiv_rn(lo_of(up), lo_of(under)), __fdiv_rn(hi_of(up), hi_of(under)));
+        p[k] = sub_each(mul2(p[k], both(decay)), q);
+      }
+      values(p, each);
+      store_values(T.p, T.p_type, i, n, T.level, each);
+      if (T.copy) store_values(T.copy, T.copy_type, i, n, T.level, each);
+    };
+    if constexpr (F8) {
+      const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) root[k] = root2(v[k]);
+      if (n < 8) {  // values that do not exist add nothing to a block
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k >= n) {
+            const uint64_t keep = k & 1 ? 0xFFFFFFFFull : 0xFFFFFFFFull << 32;
+            m[k / 2] &= keep, v[k / 2] &= keep, root[k / 2] &= keep;
+          }
+      }
+      float top_m = top16(top8(m)), top_v = top16(top8(root));
+      const bool fast = top_m * rate <= 0x1p60f && top_v < kInf && top_v * root_factor <= 0x1p59f && f.eps >= 0x1p-60f &&
+                        f.eps <= 0x1p59f;
+      auto states = [&](auto odd) {
+        const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
+        uint32_t low[8], high[8];
+        uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key;
+#pragma unroll
+        for (int k = 0; k < 8; ++k, x0 += 0x9E3779B1u) {
+          // the hash but for its last step, which changes the low half only
+          uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
+          x = (x ^ (x >> 15)) * 0xB7E15163u;
+          low[k] = ((x << 4) ^ (x >> 12)) & 0xFFFF0u;
+          high[k] = (x >> 12) & 0xFFFF0u;
+        }
+        store_bytes(T.m, i, n, T.level, block_to_f8<false, decltype(odd)::value>(m, low, s_m));
+        store_bytes(T.v, i, n, T.level, block_to_f8<true, decltype(odd)::value>(root, high, s_v));
+        if ((threadIdx.x & 15) == 0 && n > 0) {
+          T.m_scale[i / kF8Block] = s_m.s;
+          T.v_scale[i / kF8Block] = s_v.s;
+        }
+      };
+      if (__all_sync(0xFFFFFFFFu, fast)) {
+        update(std::true_type());
+        states(std::false_type());
+      } else {  // values that are not finite, or far from what training meets
+        root_any();
+        update(std::false_type());
+        top_m = top16(finite_top8(m));
+        top_v = top16(finite_top8(root));
+        states(std::true_type());
+      }
+    } else {
+      root_any();
+      update(std::false_type());
+      values(m, each);
+      store_values(T.m, DS_TYPE_F32, i, n, T.level, each);
+      values(v, each);
+      store_values(T.v, DS_TYPE_F32, i, n, T.level, each);
+    }
   }
 }
 
@@ -299,12 +429,13 @@ cudaError_t launch(const std::vector<Tensor>& all, size_t from, int count, uint3
 }
 
 cudaError_t launch_all(std::vector<Tensor>& all, const Factors& f, bool f8, cudaStream_t st) {
+  const int64_t span = span_of(f8);
   size_t from = 0;
   while (from < all.size()) {
     uint64_t ctas = 0;
     size_t to = from;
     for (; to < all.size() && to - from < (size_t)kMany; ++to) {
-      const uint64_t mine = (uint64_t)((all[to].n + kSpan - 1) / kSpan);
+      const uint64_t mine = (uint64_t)((all[to].n + span - 1) / span);
       if (to > from && ctas + mine > ((uint64_t)1 << 31) - 1) break;
       all[to].first = (uint32_t)ctas;
       ctas += mine;
