@@ -19,10 +19,7 @@
 namespace ds {
 namespace {
 
-constexpr int kThreads = 256, kEach = 8;
-// Groups of eight values of a thread: with 8-bit states, two share the work that does not depend on values.
-constexpr int groups_of(bool f8) { return f8 ? 2 : 1; }
-constexpr int64_t span_of(bool f8) { return (int64_t)kThreads * kEach * groups_of(f8); }
+constexpr int kThreads = 256, kEach = 8, kSpan = kThreads * kEach;
 constexpr int kFew = 40, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
 
 struct Tensor {
@@ -142,13 +139,11 @@ __device__ __forceinline__ void store_bytes(void* base, int64_t i, int n, int le
 __device__ __forceinline__ uint64_t both(float v) { return pair(v, v); }
 __device__ __forceinline__ float lo_of(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float hi_of(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
-// Sums one by one: packed ones are contracted with the products before them, which the definition rounds.
-__device__ __forceinline__ uint64_t add_each(uint64_t a, uint64_t b) {
-  return pair(__fadd_rn(lo_of(a), lo_of(b)), __fadd_rn(hi_of(a), hi_of(b)));
-}
-__device__ __forceinline__ uint64_t sub_each(uint64_t a, uint64_t b) {
-  return pair(__fsub_rn(lo_of(a), lo_of(b)), __fsub_rn(hi_of(a), hi_of(b)));
-}
+// A product that a sum follows.  The definition rounds it, and a packed sum would be contracted with a packed product;
+// as a fused one with zero it is not (the sign of a product of zero apart, it is the same).
+__device__ __forceinline__ uint64_t product(uint64_t a, uint64_t b) { return fma2(a, b, 0); }
+__device__ __forceinline__ uint64_t sum(uint64_t a, uint64_t b) { return fma2(a, both(1.f), b); }
+__device__ __forceinline__ uint64_t difference(uint64_t a, uint64_t b) { return fma2(b, both(-1.f), a); }
 // The largest magnitude of three; NaN where one is.
 __device__ __forceinline__ float max3_abs(float a, float b, float c) {
   float r;
@@ -161,16 +156,17 @@ __device__ __forceinline__ float max3_abs(float a, float b, float c) {
 // residual 1/2 - g h, then one by the root's own residual v - g^2, which is exact (P. Markstein, IBM J. Res. Dev. 34 (1),
 // 1990).  The same as __fsqrt_rn for all mantissas of two neighbouring exponents, and so for all of these numbers.
 __device__ __forceinline__ uint64_t root2(uint64_t v) {
-  const uint64_t u = mul2(v, both(0x1p60f));
+  const uint64_t from = fma2(v, both(0x1p60f), both(0x1p-126f));  // changes 0 only
   float y0, y1;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo_of(u)));
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi_of(u)));
-  const uint64_t y = pair(fminf(y0, 0x1p64f), fminf(y1, 0x1p64f));  // of 0 as well
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo_of(from)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi_of(from)));
+  // the negatives of u and g are what the residuals need
+  const uint64_t y = pair(y0, y1), u = mul2(v, both(-0x1p60f));
   const uint64_t g = mul2(u, y), h = mul2(y, both(0.5f));
-  const uint64_t t = fma2(mul2(g, both(-1.f)), h, both(0.5f));
+  const uint64_t t = fma2(g, h, both(0.5f));
   const uint64_t g1 = fma2(g, t, g), h1 = fma2(h, t, h);
-  const uint64_t d = fma2(mul2(g1, both(-1.f)), g1, u);
-  return mul2(fma2(d, h1, g1), both(0x1p-30f));
+  const uint64_t d = fma2(g1, g1, u);
+  return mul2(fma2(d, h1, g1), both(-0x1p-30f));
 }
 // Quotients a / b, correctly rounded, for b from 2^-60 to 2^60 and a up to 2^60, where they are 0 or normal and a is not
 // below 2^-102 (there the last place may be off): a quotient of one step by the correctly rounded reciprocal and its
@@ -185,35 +181,41 @@ __device__ __forceinline__ uint64_t quotient2(uint64_t a, uint64_t b) {
   return fma2(fma2(minus, q, a), r, q);
 }
 
-// A magnitude in units of the scale, and `bits` = 16 * (16 random bits): to one of its e4m3 neighbours.  bits + 8 fills
-// what three bits of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the neighbours are 2^-9
-// apart, as they are from 2^-6 to 2^-5, where u is moved for it.
-__device__ __forceinline__ float to_neighbour(float u, uint32_t bits) {
-  const float off = u < 0x1p-6f ? 0x1p-6f : 0.f;
-  return __uint_as_float((__float_as_uint(__fadd_rn(u, off)) + bits + 8u) & 0xFFF00000u) - off;
+// Two values in units of the scale, and for each `bits` = 16 * (16 random bits): to one of their e4m3 neighbours.
+// bits + 8 fills what three bits of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the
+// neighbours are 2^-9 apart, as they are from 2^-6 to 2^-5, where u is moved for it.
+template <bool SIGNED>
+__device__ __forceinline__ uint64_t to_neighbours(uint64_t u, uint32_t bits0, uint32_t bits1) {
+  auto offset = [](float v) {
+    const float off = SIGNED ? copysignf(0x1p-6f, v) : 0x1p-6f;
+    return fabsf(v) < 0x1p-6f ? off : 0.f;
+  };
+  auto round = [](float v, uint32_t bits) { return (__float_as_uint(v) + bits + 8u) & 0xFFF00000u; };
+  const uint64_t off = pair(offset(lo_of(u)), offset(hi_of(u))), w = sum(u, off);
+  return difference(pair(round(lo_of(w), bits0), round(hi_of(w), bits1)), off);
 }
 
 // A block of 128 values that 16 lanes hold, to 8 bits.  ODD: some of the values are not finite.
 template <bool ROOT, bool ODD>
 __device__ __forceinline__ uint2 block_to_f8(const uint64_t v[4], const uint32_t bits[8], F8Scale s) {
-  float w[8];
+  uint32_t q[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const uint64_t u2 = mul2(v[k], both(s.inv));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float u = h ? hi_of(u2) : lo_of(u2);
-      float o = to_neighbour(fabsf(u), bits[2 * k + h]);
-      if (ROOT)
-        o = fmaxf(o, fminf(u * 0x1p127f, 0x1p-9f));  // u > 0 is above 2^-136
-      else
-        o = copysignf(o, u);
-      if (ODD && !(fabsf(h ? hi_of(v[k]) : lo_of(v[k])) < kInf)) o = __uint_as_float(0x7FC00000u);
-      w[2 * k + h] = o;
+    const uint64_t u = mul2(v[k], both(s.inv));
+    float lo, hi;
+    unpair(to_neighbours<!ROOT>(u, bits[2 * k], bits[2 * k + 1]), lo, hi);
+    if (ROOT) {  // u > 0 is above 2^-136
+      const uint64_t large = mul2(u, both(0x1p127f));
+      lo = fmaxf(lo, fminf(lo_of(large), 0x1p-9f));
+      hi = fmaxf(hi, fminf(hi_of(large), 0x1p-9f));
     }
+    if (ODD) {
+      if (!(fabsf(lo_of(v[k])) < kInf)) lo = __uint_as_float(0x7FC00000u);
+      if (!(fabsf(hi_of(v[k])) < kInf)) hi = __uint_as_float(0x7FC00000u);
+    }
+    q[k] = f8x2<false>(lo, hi);
   }
-  return make_uint2(f8x2<false>(w[0], w[1]) | f8x2<false>(w[2], w[3]) << 16,
-                    f8x2<false>(w[4], w[5]) | f8x2<false>(w[6], w[7]) << 16);
+  return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }
 
 // The largest of the bit patterns of 16 lanes' magnitudes: NaN is above infinity, and that above all numbers.
@@ -250,30 +252,32 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
       hi = mid - 1;
   }
   const Tensor& T = P.t[lo];
-  struct Loaded {
+  const int64_t i = (int64_t)(blockIdx.x - T.first) * kSpan + threadIdx.x * kEach;
+  const int n = left8(T.n, i);
+  // the same for a whole CTA: one branch around all the loads and one around all the stores
+  const bool full = T.level == 2 && T.n - (int64_t)(blockIdx.x - T.first) * kSpan >= kSpan;
+  struct {
     Raw p, g, m, v;
     uint2 qm, qv;
     float sm, sv;
-  };
-  auto load = [&](int64_t i, int n) {
-    Loaded o;
-    load_raw(o.g, T.g, T.g_type, i, n, T.level);
+  } in;
+  auto load = [&](int n, int level) {
+    load_raw(in.g, T.g, T.g_type, i, n, level);
     if constexpr (F8) {
-      o.qm = load_bytes(T.m, i, n, T.level);
-      o.qv = load_bytes(T.v, i, n, T.level);
-      o.sm = n > 0 ? T.m_scale[i / kF8Block] : 0.f;
-      o.sv = n > 0 ? T.v_scale[i / kF8Block] : 0.f;
+      in.qm = load_bytes(T.m, i, n, level);
+      in.qv = load_bytes(T.v, i, n, level);
+      in.sm = n > 0 ? T.m_scale[i / kF8Block] : 0.f;
+      in.sv = n > 0 ? T.v_scale[i / kF8Block] : 0.f;
     } else {
-      load_raw(o.m, T.m, DS_TYPE_F32, i, n, T.level);
-      load_raw(o.v, T.v, DS_TYPE_F32, i, n, T.level);
+      load_raw(in.m, T.m, DS_TYPE_F32, i, n, level);
+      load_raw(in.v, T.v, DS_TYPE_F32, i, n, level);
     }
-    load_raw(o.p, T.p, T.p_type, i, n, T.level);
-    return o;
+    load_raw(in.p, T.p, T.p_type, i, n, level);
   };
-  const int64_t n_all = T.n;
-  auto values_at = [&](int64_t i) { return left8(n_all, i); };
-  int64_t i = (int64_t)(blockIdx.x - T.first) * span_of(F8) + threadIdx.x * kEach;
-  Loaded in = load(i, values_at(i));
+  if (full)
+    load(8, 2);
+  else
+    load(n, T.level);
 
   const Factors& f = P.f;
   float rate = f.rate, root_factor = f.root, decay = T.decay;
@@ -292,126 +296,136 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     decay = 1.f - lr * T.decay;
   }
 
-#pragma unroll 1
-  for (int group = 0; group < groups_of(F8); ++group, i += kThreads * kEach) {
-    const int n = values_at(i);
-    // Pairs of values: two operations per instruction.  Every product and sum is rounded by itself, as defined.
-    uint64_t p[4], g[4], m[4], v[4], root[4];
-    auto pairs = [](const float (&x)[8], uint64_t (&o)[4]) {
+  // Pairs of values: two operations per instruction.  Every product and sum is rounded by itself, as defined.
+  uint64_t p[4], g[4], m[4], v[4], root[4];
+  auto pairs = [](const float (&x)[8], uint64_t (&o)[4]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = pair(x[2 * k], x[2 * k + 1]);
-    };
-    auto values = [](const uint64_t (&x)[4], float (&o)[8]) {
+    for (int k = 0; k < 4; ++k) o[k] = pair(x[2 * k], x[2 * k + 1]);
+  };
+  auto values = [](const uint64_t (&x)[4], float (&o)[8]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) unpair(x[k], o[2 * k], o[2 * k + 1]);
-    };
-    float each[8];
-    get_raw(in.g, T.g_type, each);
-    pairs(each, g);
-    if (f.grad_scale) {
-      const uint64_t s = both(*f.grad_scale);
+    for (int k = 0; k < 4; ++k) unpair(x[k], o[2 * k], o[2 * k + 1]);
+  };
+  float each[8];
+  get_raw(in.g, T.g_type, each);
+  pairs(each, g);
+  if (f.grad_scale) {
+    const uint64_t s = both(*f.grad_scale);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) g[k] = mul2(g[k], s);
-    }
-    if constexpr (F8) {
-      f8x8_value<false>(in.qm, each);
-      pairs(each, m);
-      f8x8_value<false>(in.qv, each);
-      pairs(each, v);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        m[k] = mul2(m[k], both(in.sm));
-        const uint64_t r = mul2(v[k], both(in.sv));
-        v[k] = mul2(r, r);
-      }
-    } else {
-      get_raw(in.m, DS_TYPE_F32, each);
-      pairs(each, m);
-      get_raw(in.v, DS_TYPE_F32, each);
-      pairs(each, v);
-    }
-    get_raw(in.p, T.p_type, each);
-    pairs(each, p);
-    const int64_t next = i + kThreads * kEach;
-    if (group + 1 < groups_of(F8)) in = load(next, values_at(next));  // on its way while this group is worked on
+    for (int k = 0; k < 4; ++k) g[k] = mul2(g[k], s);
+  }
+  if constexpr (F8) {
+    f8x8_value<false>(in.qm, each);
+    pairs(each, m);
+    f8x8_value<false>(in.qv, each);
+    pairs(each, v);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      m[k] = add_each(mul2(m[k], both(f.beta1)), mul2(g[k], both(f.rest1)));
-      v[k] = add_each(mul2(v[k], both(f.beta2)), mul2(mul2(g[k], g[k]), both(f.rest2)));
+      m[k] = mul2(m[k], both(in.sm));
+      const uint64_t r = mul2(v[k], both(in.sv));
+      v[k] = mul2(r, r);
     }
-    auto root_any = [&] {
+  } else {
+    get_raw(in.m, DS_TYPE_F32, each);
+    pairs(each, m);
+    get_raw(in.v, DS_TYPE_F32, each);
+    pairs(each, v);
+  }
+  get_raw(in.p, T.p_type, each);
+  pairs(each, p);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) root[k] = pair(__fsqrt_rn(lo_of(v[k])), __fsqrt_rn(hi_of(v[k])));
-    };
-    // FAST: by quotient2, within its range
-    auto update = [&](auto fast) {
+  for (int k = 0; k < 4; ++k) {
+    m[k] = sum(product(m[k], both(f.beta1)), product(g[k], both(f.rest1)));
+    v[k] = sum(product(v[k], both(f.beta2)), product(mul2(g[k], g[k]), both(f.rest2)));
+  }
+  auto root_any = [&] {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint64_t up = mul2(m[k], both(rate)), under = add_each(mul2(root[k], both(root_factor)), both(f.eps));
-        uint64_t q;
-        if constexpr (decltype(fast)::value)
-          q = quotient2(up, under);
-        else
-          q = pair(__fdiv_rn(lo_of(up), lo_of(under)), __fdiv_rn(hi_of(up), hi_of(under)));
-        p[k] = sub_each(mul2(p[k], both(decay)), q);
-      }
-      values(p, each);
-      store_values(T.p, T.p_type, i, n, T.level, each);
-      if (T.copy) store_values(T.copy, T.copy_type, i, n, T.level, each);
-    };
-    if constexpr (F8) {
-      const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
+    for (int k = 0; k < 4; ++k) root[k] = pair(__fsqrt_rn(lo_of(v[k])), __fsqrt_rn(hi_of(v[k])));
+  };
+  // FAST: by quotient2, within its range
+  auto update = [&](auto fast) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) root[k] = root2(v[k]);
-      if (n < 8) {  // values that do not exist add nothing to a block
+    for (int k = 0; k < 4; ++k) {
+      const uint64_t up = mul2(m[k], both(rate)), under = sum(product(root[k], both(root_factor)), both(f.eps));
+      uint64_t q;
+      if constexpr (decltype(fast)::value)
+        q = quotient2(up, under);
+      else
+        q = pair(__fdiv_rn(lo_of(up), lo_of(under)), __fdiv_rn(hi_of(up), hi_of(under)));
+      p[k] = difference(product(p[k], both(decay)), q);
+    }
+  };
+  uint2 qm, qv;
+  float sm, sv;
+  if constexpr (F8) {
+    const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k >= n) {
-            const uint64_t keep = k & 1 ? 0xFFFFFFFFull : 0xFFFFFFFFull << 32;
-            m[k / 2] &= keep, v[k / 2] &= keep, root[k / 2] &= keep;
-          }
-      }
-      float top_m = top16(top8(m)), top_v = top16(top8(root));
-      const bool fast = top_m * rate <= 0x1p60f && top_v < kInf && top_v * root_factor <= 0x1p59f && f.eps >= 0x1p-60f &&
-                        f.eps <= 0x1p59f;
-      auto states = [&](auto odd) {
-        const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
-        uint32_t low[8], high[8];
-        uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key;
+    for (int k = 0; k < 4; ++k) root[k] = root2(v[k]);
+    if (n < 8) {  // values that do not exist add nothing to a block
 #pragma unroll
-        for (int k = 0; k < 8; ++k, x0 += 0x9E3779B1u) {
-          // the hash but for its last step, which changes the low half only
-          uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
-          x = (x ^ (x >> 15)) * 0xB7E15163u;
-          low[k] = ((x << 4) ^ (x >> 12)) & 0xFFFF0u;
-          high[k] = (x >> 12) & 0xFFFF0u;
+      for (int k = 0; k < 8; ++k)
+        if (k >= n) {
+          const uint64_t keep = k & 1 ? 0xFFFFFFFFull : 0xFFFFFFFFull << 32;
+          m[k / 2] &= keep, v[k / 2] &= keep, root[k / 2] &= keep;
         }
-        store_bytes(T.m, i, n, T.level, block_to_f8<false, decltype(odd)::value>(m, low, s_m));
-        store_bytes(T.v, i, n, T.level, block_to_f8<true, decltype(odd)::value>(root, high, s_v));
-        if ((threadIdx.x & 15) == 0 && n > 0) {
-          T.m_scale[i / kF8Block] = s_m.s;
-          T.v_scale[i / kF8Block] = s_v.s;
-        }
-      };
-      if (__all_sync(0xFFFFFFFFu, fast)) {
-        update(std::true_type());
-        states(std::false_type());
-      } else {  // values that are not finite, or far from what training meets
-        root_any();
-        update(std::false_type());
-        top_m = top16(finite_top8(m));
-        top_v = top16(finite_top8(root));
-        states(std::true_type());
+    }
+    float top_m = top16(top8(m)), top_v = top16(top8(root));
+    const bool fast = top_m * rate <= 0x1p60f && top_v < kInf && top_v * root_factor <= 0x1p59f && f.eps >= 0x1p-60f &&
+                      f.eps <= 0x1p59f;
+    auto states = [&](auto odd) {
+      const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
+      uint32_t low[8], high[8];
+      uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key;
+#pragma unroll
+      for (int k = 0; k < 8; ++k, x0 += 0x9E3779B1u) {
+        // the hash but for its last step, which changes the low half only
+        uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
+        x = (x ^ (x >> 15)) * 0xB7E15163u;
+        low[k] = ((x << 4) ^ (x >> 12)) & 0xFFFF0u;
+        high[k] = (x >> 12) & 0xFFFF0u;
       }
-    } else {
+      qm = block_to_f8<false, decltype(odd)::value>(m, low, s_m);
+      qv = block_to_f8<true, decltype(odd)::value>(root, high, s_v);
+      sm = s_m.s;
+      sv = s_v.s;
+    };
+    if (__all_sync(0xFFFFFFFFu, fast)) {
+      update(std::true_type());
+      states(std::false_type());
+    } else {  // values that are not finite, or far from what training meets
       root_any();
       update(std::false_type());
-      values(m, each);
-      store_values(T.m, DS_TYPE_F32, i, n, T.level, each);
-      values(v, each);
-      store_values(T.v, DS_TYPE_F32, i, n, T.level, each);
+      top_m = top16(finite_top8(m));
+      top_v = top16(finite_top8(root));
+      states(std::true_type());
     }
+  } else {
+    root_any();
+    update(std::false_type());
   }
+  auto store = [&](int n, int level) {
+    float each[8];
+    values(p, each);
+    store_values(T.p, T.p_type, i, n, level, each);
+    if (T.copy) store_values(T.copy, T.copy_type, i, n, level, each);
+    if constexpr (F8) {
+      store_bytes(T.m, i, n, level, qm);
+      store_bytes(T.v, i, n, level, qv);
+      if ((threadIdx.x & 15) == 0 && n > 0) {
+        T.m_scale[i / kF8Block] = sm;
+        T.v_scale[i / kF8Block] = sv;
+      }
+    } else {
+      values(m, each);
+      store_values(T.m, DS_TYPE_F32, i, n, level, each);
+      values(v, each);
+      store_values(T.v, DS_TYPE_F32, i, n, level, each);
+    }
+  };
+  if (full)
+    store(8, 2);
+  else
+    store(n, T.level);
 }
 
 template <int N>
@@ -429,13 +443,13 @@ cudaError_t launch(const std::vector<Tensor>& all, size_t from, int count, uint3
 }
 
 cudaError_t launch_all(std::vector<Tensor>& all, const Factors& f, bool f8, cudaStream_t st) {
-  const int64_t span = span_of(f8);
+
   size_t from = 0;
   while (from < all.size()) {
     uint64_t ctas = 0;
     size_t to = from;
     for (; to < all.size() && to - from < (size_t)kMany; ++to) {
-      const uint64_t mine = (uint64_t)((all[to].n + span - 1) / span);
+      const uint64_t mine = (uint64_t)((all[to].n + kSpan - 1) / kSpan);
       if (to > from && ctas + mine > ((uint64_t)1 << 31) - 1) break;
       all[to].first = (uint32_t)ctas;
       ctas += mine;
