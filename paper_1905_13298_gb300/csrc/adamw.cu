@@ -1,8 +1,9 @@
 // One step of Adam with decoupled weight decay over many tensors in one launch
 // (the formulas and the 8-bit states' rounding are in the header).
 //
-// The work is one pass over memory: 28 bytes a value with float32 throughout,
-// 16 with 16-bit gradients, a 16-bit copy and 8-bit states.  A CTA takes 2048
+// The work is one pass over memory: 28 bytes a value with float32 throughout
+// and 16-bit gradients and copies, 16 with 8-bit states.  With float32 states
+// it runs at the rate of a copy (50 M values 203 us).  A CTA takes 1024
 // consecutive values of one tensor, a thread eight of them, all of whose loads
 // are on their way before the first is used.  The tensors' addresses are in
 // the kernel's parameters: nothing is copied to the device before a step, and
@@ -19,7 +20,7 @@
 namespace ds {
 namespace {
 
-constexpr int kThreads = 256, kEach = 8, kSpan = kThreads * kEach;
+constexpr int kThreads = 128, kEach = 8, kSpan = kThreads * kEach;
 constexpr int kFew = 40, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
 
 struct Tensor {
@@ -195,27 +196,24 @@ __device__ __forceinline__ uint64_t to_neighbours(uint64_t u, uint32_t bits0, ui
   return difference(pair(round(lo_of(w), bits0), round(hi_of(w), bits1)), off);
 }
 
-// A block of 128 values that 16 lanes hold, to 8 bits.  ODD: some of the values are not finite.
+// Two values of a block to 8 bits; `random`: the hash of each but for its last step, which changes the low half only.
+// ODD: some of the block's values are not finite.
 template <bool ROOT, bool ODD>
-__device__ __forceinline__ uint2 block_to_f8(const uint64_t v[4], const uint32_t bits[8], F8Scale s) {
-  uint32_t q[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint64_t u = mul2(v[k], both(s.inv));
-    float lo, hi;
-    unpair(to_neighbours<!ROOT>(u, bits[2 * k], bits[2 * k + 1]), lo, hi);
-    if (ROOT) {  // u > 0 is above 2^-136
-      const uint64_t large = mul2(u, both(0x1p127f));
-      lo = fmaxf(lo, fminf(lo_of(large), 0x1p-9f));
-      hi = fmaxf(hi, fminf(hi_of(large), 0x1p-9f));
-    }
-    if (ODD) {
-      if (!(fabsf(lo_of(v[k])) < kInf)) lo = __uint_as_float(0x7FC00000u);
-      if (!(fabsf(hi_of(v[k])) < kInf)) hi = __uint_as_float(0x7FC00000u);
-    }
-    q[k] = f8x2<false>(lo, hi);
+__device__ __forceinline__ uint32_t two_to_f8(uint64_t v, uint32_t random0, uint32_t random1, float inv) {
+  auto bits = [](uint32_t x) { return (ROOT ? x >> 12 : (x << 4) ^ (x >> 12)) & 0xFFFF0u; };
+  const uint64_t u = mul2(v, both(inv));
+  float lo, hi;
+  unpair(to_neighbours<!ROOT>(u, bits(random0), bits(random1)), lo, hi);
+  if (ROOT) {  // u > 0 is above 2^-136
+    const uint64_t large = mul2(u, both(0x1p127f));
+    lo = fmaxf(lo, fminf(lo_of(large), 0x1p-9f));
+    hi = fmaxf(hi, fminf(hi_of(large), 0x1p-9f));
   }
-  return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+  if (ODD) {
+    if (!(fabsf(lo_of(v)) < kInf)) lo = __uint_as_float(0x7FC00000u);
+    if (!(fabsf(hi_of(v)) < kInf)) hi = __uint_as_float(0x7FC00000u);
+  }
+  return f8x2<false>(lo, hi);
 }
 
 // The largest of the bit patterns of 16 lanes' magnitudes: NaN is above infinity, and that above all numbers.
@@ -241,8 +239,12 @@ __device__ __forceinline__ float rest_of_power(double log_beta, int64_t t) {
   return -expm1f((float)((double)t * log_beta));
 }
 
+// With 8-bit states arithmetic takes as long as memory, 690 instructions for eight values of 32 threads: 48 warps of an SM
+// hide its latency best, although 40 registers are a few too little (9 tensors of 50 M values, 16-bit gradients and
+// copies: 144 us or 5.6 TB/s; 158 with 40 warps and 48 registers, 164 with 32 warps and 64).  Copies of the next values
+// through shared memory meanwhile, and factors kept as pairs in the parameters, gained nothing.
 template <bool F8, int N>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Params<N> P) {
+__global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __grid_constant__ Params<N> P) {
   int lo = 0, hi = P.count - 1;  // the last tensor that starts at or before this CTA
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -354,6 +356,16 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         q = pair(__fdiv_rn(lo_of(up), lo_of(under)), __fdiv_rn(hi_of(up), hi_of(under)));
       p[k] = difference(product(p[k], both(decay)), q);
     }
+    auto store = [&](int n, int level) {
+      float each[8];
+      values(p, each);
+      store_values(T.p, T.p_type, i, n, level, each);
+      if (T.copy) store_values(T.copy, T.copy_type, i, n, level, each);
+    };
+    if (full)
+      store(8, 2);
+    else
+      store(n, T.level);
   };
   uint2 qm, qv;
   float sm, sv;
@@ -374,18 +386,21 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
                       f.eps <= 0x1p59f;
     auto states = [&](auto odd) {
       const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
-      uint32_t low[8], high[8];
-      uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key;
-#pragma unroll
-      for (int k = 0; k < 8; ++k, x0 += 0x9E3779B1u) {
-        // the hash but for its last step, which changes the low half only
+      uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key, a[4], b[4];
+      auto random = [&] {
         uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
         x = (x ^ (x >> 15)) * 0xB7E15163u;
-        low[k] = ((x << 4) ^ (x >> 12)) & 0xFFFF0u;
-        high[k] = (x >> 12) & 0xFFFF0u;
+        x0 += 0x9E3779B1u;
+        return x;
+      };
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x = random(), y = random();
+        a[k] = two_to_f8<false, decltype(odd)::value>(m[k], x, y, s_m.inv);
+        b[k] = two_to_f8<true, decltype(odd)::value>(root[k], x, y, s_v.inv);
       }
-      qm = block_to_f8<false, decltype(odd)::value>(m, low, s_m);
-      qv = block_to_f8<true, decltype(odd)::value>(root, high, s_v);
+      qm = make_uint2(a[0] | a[1] << 16, a[2] | a[3] << 16);
+      qv = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
       sm = s_m.s;
       sv = s_v.s;
     };
@@ -404,10 +419,6 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     update(std::false_type());
   }
   auto store = [&](int n, int level) {
-    float each[8];
-    values(p, each);
-    store_values(T.p, T.p_type, i, n, level, each);
-    if (T.copy) store_values(T.copy, T.copy_type, i, n, level, each);
     if constexpr (F8) {
       store_bytes(T.m, i, n, level, qm);
       store_bytes(T.v, i, n, level, qv);
@@ -416,6 +427,7 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         T.v_scale[i / kF8Block] = sv;
       }
     } else {
+      float each[8];
       values(m, each);
       store_values(T.m, DS_TYPE_F32, i, n, level, each);
       values(v, each);
