@@ -61,46 +61,59 @@ __device__ __forceinline__ int expert_of(const OrderParams& P, int64_t s, int64_
   return id >= 0 && id < P.experts ? id : -1;
 }
 
+constexpr int kHeld = 4;  // ids that a lane keeps from the first pass to the second
+
+// CLUSTER: more than one CTA.
+template <bool CLUSTER>
 __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams P) {
   extern __shared__ int order_smem[];
-  const int E = P.experts;
-  int* const hist = order_smem;                   // [warps][E]: counts, then rows of this warp's next slots
-  int* const total = hist + kOrderWarps * E;      // [E] of this CTA
-  int* const end_of = total + E;                  // [E] rows in use of each expert end here
+  const int E = P.experts, warps = blockDim.x >> 5;
+  int* const hist = order_smem;          // [warps][E]: counts, then rows of this warp's next slots
+  int* const total = hist + warps * E;   // [E] of this CTA
+  int* const end_of = total + E;         // [E] rows in use of each expert end here
   __shared__ int warp_sum[kOrderWarps];
   __shared__ int rows_used;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const uint32_t rank = CLUSTER ? cluster_rank() : 0, ranks = CLUSTER ? cluster_size() : 1;
   int* const mine = hist + warp * E;
+  const int64_t from = ((int64_t)rank * warps + warp) * P.per_warp;
+  const int64_t to = from + P.per_warp < P.slots ? from + P.per_warp : P.slots;
+  int held[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) held[k] = expert_of(P, from + 32 * k + lane, to);
   for (int e = lane; e < E; e += 32) mine[e] = 0;
   __syncwarp();
-  const int64_t from = ((int64_t)rank * kOrderWarps + warp) * P.per_warp;
-  const int64_t to = from + P.per_warp < P.slots ? from + P.per_warp : P.slots;
-  for (int64_t s = from; s < to; s += 32) {
-    const int e = expert_of(P, s + lane, to);
+  auto count_32 = [&](int e) {
     const uint32_t same = __match_any_sync(0xFFFFFFFFu, e);
     if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
     __syncwarp();
-  }
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (from + 32 * k < to) count_32(held[k]);
+  for (int64_t s = from + 32 * kHeld; s < to; s += 32) count_32(expert_of(P, s + lane, to));
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kOrderThreads) {
-    int sum = 0;
-    for (int w = 0; w < kOrderWarps; ++w) {
-      const int c = hist[w * E + e];
-      hist[w * E + e] = sum;
-      sum += c;
-    }
-    total[e] = sum;
-  }
-  cluster_barrier();
-  // a thread per expert (there are at most as many): counts of the CTAs before this one, and of all
-  int before = 0, count = 0;
+  // a thread per expert (there are at most as many)
   const int e = threadIdx.x;
+  int here = 0;
   if (e < E) {
-    for (uint32_t r = 0; r < ranks; ++r) {
-      const int c = load_of_rank(&total[e], r);
-      if (r < rank) before += c;
-      count += c;
+#pragma unroll 8
+    for (int w = 0; w < warps; ++w) here += hist[w * E + e];
+  }
+  int before = 0, count = here;  // slots of the CTAs before this one, and of all
+  if constexpr (CLUSTER) {
+    if (e < E) total[e] = here;
+    cluster_barrier();
+    if (e < E) {
+      int c[8];
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r) c[r] = r < ranks ? load_of_rank(&total[e], r) : 0;
+      count = 0;
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r) {
+        if (r < rank) before += c[r];
+        count += c[r];
+      }
     }
   }
   const int room = (count + P.align - 1) / P.align * P.align;
@@ -115,7 +128,13 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   int start = sum - room;
   for (int w = 0; w < warp; ++w) start += warp_sum[w];
   if (e < E) {
-    for (int w = 0; w < kOrderWarps; ++w) hist[w * E + e] += start + before;
+    int at = start + before;
+#pragma unroll 8
+    for (int w = 0; w < warps; ++w) {
+      const int c = hist[w * E + e];
+      hist[w * E + e] = at;
+      at += c;
+    }
     end_of[e] = start + count;
     if (rank == 0) {
       P.counts[e] = count;
@@ -125,8 +144,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     if (e == E - 1) rows_used = start + room;
   }
   __syncthreads();
-  for (int64_t s = from; s < to; s += 32) {
-    const int id = expert_of(P, s + lane, to);
+  auto place_32 = [&](int64_t s, int id) {
     const uint32_t same = __match_any_sync(0xFFFFFFFFu, id);
     int row = -1;
     if (id >= 0) row = mine[id] + __popc(same & ((1u << lane) - 1u));
@@ -135,15 +153,19 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     __syncwarp();
     if (s + lane < to) P.position[s + lane] = row;
     if (row >= 0 && row < P.rows) P.slot[row] = (int32_t)(s + lane);
-  }
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (from + 32 * k < to) place_32(from + 32 * k, held[k]);
+  for (int64_t s = from + 32 * kHeld; s < to; s += 32) place_32(s, expert_of(P, s + lane, to));
   // rows without a slot: behind each expert's, up to the next one's, and behind the last
-  for (int x = (int)rank * kOrderWarps + warp; x < E; x += (int)ranks * kOrderWarps) {
+  for (int x = (int)rank * warps + warp; x < E; x += (int)ranks * warps) {
     const int stop = (end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
     for (int64_t r = end_of[x] + lane; r < stop && r < P.rows; r += 32) P.slot[r] = -1;
   }
-  for (int64_t r = rows_used + (int64_t)rank * kOrderThreads + threadIdx.x; r < P.rows; r += ranks * kOrderThreads)
+  for (int64_t r = rows_used + (int64_t)rank * blockDim.x + threadIdx.x; r < P.rows; r += ranks * blockDim.x)
     P.slot[r] = -1;
-  cluster_barrier();  // the other CTAs read this one's counts until here
+  if constexpr (CLUSTER) cluster_barrier();  // the other CTAs read this one's counts until here
 }
 
 // ---------------------------------------------------------------------------
@@ -151,15 +173,12 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
-template <int UNIT>
+// An access of BYTES bytes and the values in it.
+template <int BYTES>
 struct UnitOf;
 template <>
 struct UnitOf<16> {
   using T = uint4;
-};
-template <>
-struct UnitOf<8> {
-  using T = uint2;
 };
 template <>
 struct UnitOf<4> {
@@ -169,209 +188,255 @@ template <>
 struct UnitOf<2> {
   using T = uint16_t;
 };
+template <typename T, int BYTES>
+struct Unit {
+  static constexpr int COUNT = BYTES / (int)sizeof(T);
+  typename UnitOf<BYTES>::T u;
+  __device__ __forceinline__ void get(float (&v)[COUNT]) const {
+    const T* p = reinterpret_cast<const T*>(&u);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = to_float(p[i]);
+  }
+  __device__ __forceinline__ void set(const float (&v)[COUNT]) {
+    T* p = reinterpret_cast<T*>(&u);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) from_float(v[i], p[i]);
+  }
+};
+// Unit i of row r.
+template <typename U>
+__device__ __forceinline__ U* unit_at(void* base, int64_t r, int64_t ld_bytes, int64_t i) {
+  return reinterpret_cast<U*>(static_cast<char*>(base) + r * ld_bytes) + i;
+}
+template <typename U>
+__device__ __forceinline__ const U* unit_at(const void* base, int64_t r, int64_t ld_bytes, int64_t i) {
+  return reinterpret_cast<const U*>(static_cast<const char*>(base) + r * ld_bytes) + i;
+}
+
+constexpr int kZeroRows = 8;  // rows of a warp that looks for rows without a slot
+
+// The first rows of which `rows` from r0 on hold no slot, as bits.
+__device__ __forceinline__ uint32_t rows_without(const int32_t* slot, int64_t r0, int64_t rows) {
+  const int lane = threadIdx.x & 31;
+  const int64_t r = r0 + lane;
+  return __ballot_sync(0xFFFFFFFFu, lane < kZeroRows && r < rows && slot[r < rows ? r : 0] < 0);
+}
 
 struct GatherParams {
   RowCopy a, b;
   const int32_t *position, *slot;
   int64_t tokens, rows;
   int top_k;
-  int64_t units;  // of a row of a (whole ones)
-  int rest;       // bytes of a row behind them
-  int64_t parts;  // a warp copies a part of a row
-  int64_t copies; // warps that copy; the others write zeros
+  int64_t units;   // of a row of a (whole ones)
+  int rest;        // bytes of a row behind them
+  int64_t parts;   // a warp copies a part of a row
+  int64_t copies;  // warps that copy; the others write zeros
 };
 
-constexpr int kPart = 4;        // units of a lane
-constexpr int kZeroRows = 8;    // rows of a warp that looks for rows without a slot
+constexpr int kPart = 4;  // units of a lane
 
-template <int UNIT>
+template <int BYTES>
 __device__ __forceinline__ void zero_row(const GatherParams& P, int64_t r, int lane) {
-  using T = typename UnitOf<UNIT>::T;
-  T* to = reinterpret_cast<T*>(static_cast<char*>(P.a.dst) + r * P.a.ld_dst);
-  for (int64_t u = lane; u < P.units; u += 32) to[u] = T{};
-  if (lane < P.rest) static_cast<uint8_t*>(P.a.dst)[r * P.a.ld_dst + P.units * UNIT + lane] = 0;
-  if (P.b.src) {
-    float* s = reinterpret_cast<float*>(static_cast<char*>(P.b.dst) + r * P.b.ld_dst);
-    for (int64_t u = lane; u < P.b.bytes / 4; u += 32) s[u] = 0.f;
-  }
+  using T = typename UnitOf<BYTES>::T;
+  for (int64_t u = lane; u < P.units; u += 32) *unit_at<T>(P.a.dst, r, P.a.ld_dst, u) = T{};
+  if (lane < P.rest) unit_at<uint8_t>(P.a.dst, r, P.a.ld_dst, P.units * BYTES)[lane] = 0;
+  if (P.b.src)
+    for (int64_t u = lane; u < P.b.bytes / 4; u += 32) *unit_at<float>(P.b.dst, r, P.b.ld_dst, u) = 0.f;
 }
 
 // A warp reads a part of a token's row and writes it to the rows of the token's slots.
-template <int UNIT>
+template <int BYTES>
 __global__ void __launch_bounds__(kThreads) gather_kernel(const GatherParams P) {
-  using T = typename UnitOf<UNIT>::T;
+  using T = typename UnitOf<BYTES>::T;
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (id >= P.copies) {
-    const int64_t r0 = (id - P.copies) * kZeroRows, r = r0 + lane;
-    uint32_t todo = __ballot_sync(0xFFFFFFFFu, lane < kZeroRows && r < P.rows && P.slot[r < P.rows ? r : 0] < 0);
-    while (todo) {
-      zero_row<UNIT>(P, r0 + __ffs(todo) - 1, lane);
-      todo &= todo - 1;
-    }
+    const int64_t r0 = (id - P.copies) * kZeroRows;
+    for (uint32_t todo = rows_without(P.slot, r0, P.rows); todo; todo &= todo - 1)
+      zero_row<BYTES>(P, r0 + __ffs(todo) - 1, lane);
     return;
   }
   const int64_t t = id / P.parts, u0 = (id - t * P.parts) * (32 * kPart) + lane;
-  const char* from = static_cast<const char*>(P.a.src) + t * P.a.ld_src;
   T v[kPart];
 #pragma unroll
   for (int i = 0; i < kPart; ++i)
-    if (u0 + 32 * i < P.units) v[i] = reinterpret_cast<const T*>(from)[u0 + 32 * i];
+    if (u0 + 32 * i < P.units) v[i] = *unit_at<T>(P.a.src, t, P.a.ld_src, u0 + 32 * i);
   // the row's last bytes, and the second matrix, go with its first part
   const bool first = u0 == lane;
   uint8_t last = 0;
-  if (first && lane < P.rest) last = reinterpret_cast<const uint8_t*>(from)[P.units * UNIT + lane];
+  if (first && lane < P.rest) last = unit_at<uint8_t>(P.a.src, t, P.a.ld_src, P.units * BYTES)[lane];
   for (int j0 = 0; j0 < P.top_k; j0 += 32) {
     const int32_t mine = j0 + lane < P.top_k ? P.position[t * P.top_k + j0 + lane] : -1;
     const int n = P.top_k - j0 < 32 ? P.top_k - j0 : 32;
     for (int j = 0; j < n; ++j) {
       const int64_t row = __shfl_sync(0xFFFFFFFFu, mine, j);
       if (row < 0 || row >= P.rows) continue;
-      char* to = static_cast<char*>(P.a.dst) + row * P.a.ld_dst;
 #pragma unroll
       for (int i = 0; i < kPart; ++i)
-        if (u0 + 32 * i < P.units) reinterpret_cast<T*>(to)[u0 + 32 * i] = v[i];
-      if (first && lane < P.rest) reinterpret_cast<uint8_t*>(to)[P.units * UNIT + lane] = last;
-      if (first && P.b.src) {
-        const float* s = reinterpret_cast<const float*>(static_cast<const char*>(P.b.src) + t * P.b.ld_src);
-        float* d = reinterpret_cast<float*>(static_cast<char*>(P.b.dst) + row * P.b.ld_dst);
-        for (int64_t u = lane; u < P.b.bytes / 4; u += 32) d[u] = s[u];
-      }
+        if (u0 + 32 * i < P.units) *unit_at<T>(P.a.dst, row, P.a.ld_dst, u0 + 32 * i) = v[i];
+      if (first && lane < P.rest) unit_at<uint8_t>(P.a.dst, row, P.a.ld_dst, P.units * BYTES)[lane] = last;
+      if (first && P.b.src)
+        for (int64_t u = lane; u < P.b.bytes / 4; u += 32)
+          *unit_at<float>(P.b.dst, row, P.b.ld_dst, u) = *unit_at<float>(P.b.src, t, P.b.ld_src, u);
     }
   }
 }
 
 struct CombineParams {
   const void *y, *add;
-  int64_t ldy, ld_add, ldo, cols, tokens, rows, parts;
-  const int32_t *position, *slot;
+  int64_t ldy, ld_add, ldo;  // in bytes
+  int64_t units, tokens, rows, parts;
+  const int32_t* position;
   const float* weights;
   void* out;
-  int top_k, vec;
+  int top_k;
 };
 
-constexpr int kRowsAtOnce = 8;  // rows of a token on their way at once
+// Units of a lane: with AT_ONCE rows of each, up to 128 bytes are on their way.
+constexpr int units_of(int bytes, int at_once) { return bytes == 16 ? (at_once == 8 ? 1 : 2) : 4; }
 
-// A warp makes 256 values of a token's sum.
-template <typename T>
+// A warp makes a part of a token's sum, from AT_ONCE rows at a time.
+template <typename T, int BYTES, int AT_ONCE>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams P) {
+  using U = Unit<T, BYTES>;
+  constexpr int N = units_of(BYTES, AT_ONCE);
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int64_t t = id / P.parts, c = (id - t * P.parts) * 256 + lane * 8;
+  const int64_t t = id / P.parts, u0 = (id - t * P.parts) * (32 * N) + lane;
   if (t >= P.tokens) return;
-  const int n = left8(P.cols, c);
-  const bool vec = P.vec;
-  Raw8<T> more;
-  if (P.add) more.template load<true>(static_cast<const T*>(P.add) + t * P.ld_add + c, n, vec);
-  float acc[8] = {};
-  for (int j0 = 0; j0 < P.top_k; j0 += kRowsAtOnce) {
+  float acc[N][U::COUNT] = {};
+  U more[N];
+  if (P.add) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (u0 + 32 * i < P.units) more[i] = *unit_at<U>(P.add, t, P.ld_add, u0 + 32 * i);
+  }
+  for (int j0 = 0; j0 < P.top_k; j0 += AT_ONCE) {
     int32_t at = -1;
     float w = 1.f;
-    if (lane < kRowsAtOnce && j0 + lane < P.top_k) {
+    if (lane < AT_ONCE && j0 + lane < P.top_k) {
       at = P.position[t * P.top_k + j0 + lane];
+      if (at >= P.rows) at = -1;
       if (P.weights) w = P.weights[t * P.top_k + j0 + lane];
     }
-    Raw8<T> v[kRowsAtOnce];
-    int32_t row[kRowsAtOnce];
+    U v[AT_ONCE][N];
+    int32_t row[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < kRowsAtOnce; ++j) {
+    for (int j = 0; j < AT_ONCE; ++j) {
       row[j] = __shfl_sync(0xFFFFFFFFu, at, j);
-      if (row[j] >= 0 && row[j] < P.rows)
-        v[j].template load<true>(static_cast<const T*>(P.y) + row[j] * P.ldy + c, n, vec);
+      if (row[j] < 0) continue;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (u0 + 32 * i < P.units) v[j][i] = *unit_at<U>(P.y, row[j], P.ldy, u0 + 32 * i);
     }
 #pragma unroll
-    for (int j = 0; j < kRowsAtOnce; ++j) {
+    for (int j = 0; j < AT_ONCE; ++j) {
       const float wj = __shfl_sync(0xFFFFFFFFu, w, j);
-      if (row[j] < 0 || row[j] >= P.rows) continue;
-      float f[8];
-      v[j].get(f);
+      if (row[j] < 0) continue;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = fmaf(wj, f[i], acc[i]);
+      for (int i = 0; i < N; ++i) {
+        float f[U::COUNT];
+        v[j][i].get(f);
+#pragma unroll
+        for (int k = 0; k < U::COUNT; ++k) acc[i][k] = fmaf(wj, f[k], acc[i][k]);
+      }
     }
   }
-  if (P.add) {
-    float f[8];
-    more.get(f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += f[i];
+  for (int i = 0; i < N; ++i) {
+    if (u0 + 32 * i >= P.units) continue;
+    if (P.add) {
+      float f[U::COUNT];
+      more[i].get(f);
+#pragma unroll
+      for (int k = 0; k < U::COUNT; ++k) acc[i][k] += f[k];
+    }
+    U o;
+    o.set(acc[i]);
+    *unit_at<U>(P.out, t, P.ldo, u0 + 32 * i) = o;
   }
-  store8<true>(static_cast<T*>(P.out) + t * P.ldo + c, n, vec, acc);
 }
 
 struct CombineBackwardParams {
   const void *d, *y;
-  int64_t ldd, ldy, lddy, cols, tokens, rows;
+  int64_t ldd, ldy, lddy;  // in bytes
+  int64_t units, tokens, rows;
   const int32_t *position, *slot;
   const float* weights;
   void* dy;
   float* dweights;
-  int top_k, vec;
+  int top_k;
 };
 
-// A warp goes through a token's row; with slots in groups, the row of dout is read once for each group.
-template <typename T>
+// A warp goes through a token's row; with slots in groups of AT_ONCE, the row of dout is read once for each group.
+template <typename T, int BYTES, int AT_ONCE>
 __global__ void __launch_bounds__(kThreads) combine_backward_kernel(const CombineBackwardParams P) {
+  using U = Unit<T, BYTES>;
+  constexpr int N = units_of(BYTES, AT_ONCE);
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const bool vec = P.vec;
   if (id >= P.tokens) {
-    const int64_t r0 = (id - P.tokens) * kZeroRows, r = r0 + lane;
-    uint32_t todo = __ballot_sync(0xFFFFFFFFu, lane < kZeroRows && r < P.rows && P.slot[r < P.rows ? r : 0] < 0);
-    const float zero[8] = {};
-    while (todo) {
-      T* to = static_cast<T*>(P.dy) + (r0 + __ffs(todo) - 1) * P.lddy;
-      for (int64_t c = lane * 8; c < P.cols; c += 256) store8<true>(to + c, left8(P.cols, c), vec, zero);
-      todo &= todo - 1;
-    }
+    const int64_t r0 = (id - P.tokens) * kZeroRows;
+    for (uint32_t todo = rows_without(P.slot, r0, P.rows); todo; todo &= todo - 1)
+      for (int64_t u = lane; u < P.units; u += 32) *unit_at<U>(P.dy, r0 + __ffs(todo) - 1, P.lddy, u) = U{};
     return;
   }
   const int64_t t = id;
-  const T* const d = static_cast<const T*>(P.d) + t * P.ldd;
-  for (int j0 = 0; j0 < P.top_k; j0 += kRowsAtOnce) {
+  for (int j0 = 0; j0 < P.top_k; j0 += AT_ONCE) {
     int32_t at = -1;
     float w = 1.f;
-    if (lane < kRowsAtOnce && j0 + lane < P.top_k) {
+    if (lane < AT_ONCE && j0 + lane < P.top_k) {
       at = P.position[t * P.top_k + j0 + lane];
+      if (at >= P.rows) at = -1;
       if (P.weights) w = P.weights[t * P.top_k + j0 + lane];
     }
-    int32_t row[kRowsAtOnce];
-    float wj[kRowsAtOnce], dot[kRowsAtOnce];
+    int32_t row[AT_ONCE];
+    float wj[AT_ONCE], dot[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < kRowsAtOnce; ++j) {
+    for (int j = 0; j < AT_ONCE; ++j) {
       row[j] = __shfl_sync(0xFFFFFFFFu, at, j);
-      if (row[j] >= P.rows) row[j] = -1;
       wj[j] = __shfl_sync(0xFFFFFFFFu, w, j);
       dot[j] = 0.f;
     }
-    for (int64_t c = lane * 8; c < P.cols; c += 256) {
-      const int n = left8(P.cols, c);
-      Raw8<T> rd, ry[kRowsAtOnce];
-      rd.template load<true>(d + c, n, vec);
+    // N units of all rows are loaded before the first is stored, which may be where y lies
+    for (int64_t u0 = lane; u0 < P.units; u0 += 32 * N) {
+      U rd[N], ry[AT_ONCE][N];
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (u0 + 32 * i < P.units) rd[i] = *unit_at<U>(P.d, t, P.ldd, u0 + 32 * i);
       if (P.dweights) {
 #pragma unroll
-        for (int j = 0; j < kRowsAtOnce; ++j)
-          if (row[j] >= 0) ry[j].template load<true>(static_cast<const T*>(P.y) + row[j] * P.ldy + c, n, vec);
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (row[j] >= 0 && u0 + 32 * i < P.units) ry[j][i] = *unit_at<U>(P.y, row[j], P.ldy, u0 + 32 * i);
       }
-      float f[8];
-      rd.get(f);
 #pragma unroll
-      for (int j = 0; j < kRowsAtOnce; ++j) {
-        if (row[j] < 0) continue;
-        if (P.dweights) {
-          float g[8];
-          ry[j].get(g);
+      for (int i = 0; i < N; ++i) {
+        if (u0 + 32 * i >= P.units) break;
+        float f[U::COUNT];
+        rd[i].get(f);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dot[j] = fmaf(f[i], g[i], dot[j]);
+        for (int j = 0; j < AT_ONCE; ++j) {
+          if (row[j] < 0) continue;
+          if (P.dweights) {
+            float g[U::COUNT];
+            ry[j][i].get(g);
+#pragma unroll
+            for (int k = 0; k < U::COUNT; ++k) dot[j] = fmaf(f[k], g[k], dot[j]);
+          }
+          float o[U::COUNT];
+#pragma unroll
+          for (int k = 0; k < U::COUNT; ++k) o[k] = wj[j] * f[k];
+          U s;
+          s.set(o);
+          *unit_at<U>(P.dy, row[j], P.lddy, u0 + 32 * i) = s;
         }
-        float o[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = wj[j] * f[i];
-        store8<true>(static_cast<T*>(P.dy) + row[j] * P.lddy + c, n, vec, o);
       }
     }
     if (P.dweights) {
 #pragma unroll
-      for (int j = 0; j < kRowsAtOnce; ++j) {
+      for (int j = 0; j < AT_ONCE; ++j) {
 #pragma unroll
         for (int x = 16; x >= 1; x >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], x);
         if (lane == j && j0 + j < P.top_k) P.dweights[t * P.top_k + j0 + j] = dot[j];
@@ -382,55 +447,101 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(const Combin
 
 int64_t over(int64_t n, int64_t d) { return (n + d - 1) / d; }
 
-bool rows_aligned(const void* p, int64_t ld, int type) {
-  return p == nullptr || (aligned(p, 16) && ld * type_size(type) % 16 == 0);
-}
-
-template <int UNIT>
+template <int BYTES>
 cudaError_t launch_gather(GatherParams& p, cudaStream_t st) {
-  p.units = p.a.bytes / UNIT;
-  p.rest = (int)(p.a.bytes % UNIT);
+  p.units = p.a.bytes / BYTES;
+  p.rest = (int)(p.a.bytes % BYTES);
   p.parts = over(p.units > 0 ? p.units : 1, 32 * kPart);
   p.copies = p.tokens * p.parts;
   const int64_t ctas = over(p.copies + over(p.rows, kZeroRows), kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
-  if (ctas > 0) gather_kernel<UNIT><<<(unsigned)ctas, kThreads, 0, st>>>(p);
+  if (ctas > 0) gather_kernel<BYTES><<<(unsigned)ctas, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t launch_combine(const CombineParams& p, cudaStream_t st) {
+template <typename T, int BYTES, int AT_ONCE>
+cudaError_t launch_combine(CombineParams& p, cudaStream_t st) {
+  p.parts = over(p.units, 32 * units_of(BYTES, AT_ONCE));
   const int64_t ctas = over(p.tokens * p.parts, kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
-  combine_kernel<T><<<(unsigned)ctas, kThreads, 0, st>>>(p);
+  combine_kernel<T, BYTES, AT_ONCE><<<(unsigned)ctas, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
-template <typename T>
-cudaError_t launch_combine_backward(const CombineBackwardParams& p, cudaStream_t st) {
+template <typename T, int BYTES, int AT_ONCE>
+cudaError_t launch_combine(CombineBackwardParams& p, cudaStream_t st) {
   const int64_t ctas = over(p.tokens + over(p.rows, kZeroRows), kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
-  combine_backward_kernel<T><<<(unsigned)ctas, kThreads, 0, st>>>(p);
+  combine_backward_kernel<T, BYTES, AT_ONCE><<<(unsigned)ctas, kThreads, 0, st>>>(p);
   return cudaGetLastError();
+}
+// As many rows at once as a token has, of 2, 4 or 8: registers and instructions for more cost a third of the time.
+template <typename T, int BYTES, typename Params>
+cudaError_t choose_rows(Params& p, int64_t bytes, cudaStream_t st) {
+  p.units = bytes / BYTES;
+  if (p.top_k <= 2) return launch_combine<T, BYTES, 2>(p, st);
+  if (p.top_k <= 4) return launch_combine<T, BYTES, 4>(p, st);
+  return launch_combine<T, BYTES, 8>(p, st);
+}
+// `unit`: the bytes of an access that all rows allow.
+template <typename T, typename Params>
+cudaError_t choose_unit(Params& p, int64_t bytes, int unit, cudaStream_t st) {
+  if (unit == 16) return choose_rows<T, 16>(p, bytes, st);
+  if constexpr (sizeof(T) == 2) {
+    if (unit == 2) return choose_rows<T, 2>(p, bytes, st);
+  }
+  return choose_rows<T, 4>(p, bytes, st);
+}
+template <typename Params>
+cudaError_t choose_type(Params& p, int type, int64_t cols, int unit, cudaStream_t st) {
+  if (type == DS_TYPE_F32) return choose_unit<float>(p, cols * 4, unit, st);
+  if (type == DS_TYPE_BF16) return choose_unit<__nv_bfloat16>(p, cols * 2, unit, st);
+  return choose_unit<__half>(p, cols * 2, unit, st);
+}
+
+// 16 where the row's bytes and these rows' addresses are multiples of it, else 4, else 2.
+struct Rows {
+  const void* p;
+  int64_t ld;
+};
+template <size_t N>
+int unit_of(int64_t bytes, const Rows (&rows)[N]) {
+  for (int u = 16; u > 2; u /= 4) {
+    bool all = bytes % u == 0;
+    for (const Rows& r : rows) all = all && (r.p == nullptr || (aligned(r.p, u) && r.ld % u == 0));
+    if (all) return u;
+  }
+  return 2;
 }
 
 }  // namespace
 
 cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_slots& s, cudaStream_t st) {
-  const size_t smem = sizeof(int) * (size_t)s.experts * (kOrderWarps + 2);
-  static const cudaError_t attr = cudaFuncSetAttribute(
-      order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(int) * DS_EXPERTS_MAX * (kOrderWarps + 2)));
+  static const cudaError_t attr = [] {
+    const int most = (int)sizeof(int) * DS_EXPERTS_MAX * (kOrderWarps + 2);
+    const cudaError_t e = cudaFuncSetAttribute(order_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e != cudaSuccess ? e
+                            : cudaFuncSetAttribute(order_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  }();
   if (attr != cudaSuccess) return attr;
   OrderParams p;
   p.ids = ids;
   p.offsets = s.offsets, p.counts = s.counts, p.position = s.position, p.slot = s.slot;
   p.slots = s.tokens * s.top_k, p.rows = s.rows;
   p.experts = s.experts, p.align = s.align, p.wide = id_type == DS_INDEX_I64;
+  // warps for 32 slots each, and a thread for each expert
+  int64_t threads = over(p.slots > p.experts ? p.slots : p.experts, 32) * 32;
+  if (threads > kOrderThreads) threads = kOrderThreads;
   int ctas = 1;
-  while (ctas < 8 && p.slots > (int64_t)ctas * kOrderThreads) ctas *= 2;
-  p.per_warp = over(over(p.slots, (int64_t)ctas * kOrderWarps), 32) * 32;
+  while (ctas < 8 && p.slots > (int64_t)ctas * threads) ctas *= 2;
+  p.per_warp = over(over(p.slots, ctas * threads / 32), 32) * 32;
+  const size_t smem = sizeof(int) * (size_t)p.experts * (size_t)(threads / 32 + 2);
+  if (ctas == 1) {
+    order_kernel<false><<<1, (unsigned)threads, smem, st>>>(p);
+    return cudaGetLastError();
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(kOrderThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -440,7 +551,7 @@ cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_sl
   at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, order_kernel, p);
+  return cudaLaunchKernelEx(&cfg, order_kernel<true>, p);
 }
 
 cudaError_t launch_expert_gather(const RowCopy& a, const RowCopy& b, const ds_expert_slots& s, cudaStream_t st) {
@@ -448,41 +559,34 @@ cudaError_t launch_expert_gather(const RowCopy& a, const RowCopy& b, const ds_ex
   p.a = a, p.b = b;
   p.position = s.position, p.slot = s.slot;
   p.tokens = s.tokens, p.rows = s.rows, p.top_k = s.top_k;
-  switch (a.unit) {
-    case 16: return launch_gather<16>(p, st);
-    case 8: return launch_gather<8>(p, st);
-    case 4: return launch_gather<4>(p, st);
-    default: return launch_gather<2>(p, st);
-  }
+  // rows of 8-bit values start at multiples of 16 bytes, and may end anywhere
+  const int unit = b.src ? 16 : unit_of(a.bytes, {Rows{a.src, a.ld_src}, Rows{a.dst, a.ld_dst}});
+  if (unit == 16) return launch_gather<16>(p, st);
+  return unit == 4 ? launch_gather<4>(p, st) : launch_gather<2>(p, st);
 }
 
 cudaError_t launch_expert_combine(const void* y, int type, int64_t ldy, int64_t cols, const ds_expert_slots& s,
                                   const float* weights, const void* add, int64_t ld_add, void* out, int64_t ldo,
                                   cudaStream_t st) {
+  const int64_t size = type_size(type);
   CombineParams p = {};
   p.y = y, p.add = add, p.out = out, p.weights = weights;
-  p.ldy = ldy, p.ld_add = ld_add, p.ldo = ldo, p.cols = cols;
+  p.ldy = ldy * size, p.ld_add = ld_add * size, p.ldo = ldo * size;
   p.tokens = s.tokens, p.rows = s.rows, p.top_k = s.top_k;
-  p.position = s.position, p.slot = s.slot;
-  p.parts = over(cols, 256);
-  p.vec = rows_aligned(y, ldy, type) && rows_aligned(add, ld_add, type) && rows_aligned(out, ldo, type);
-  if (type == DS_TYPE_F32) return launch_combine<float>(p, st);
-  if (type == DS_TYPE_BF16) return launch_combine<__nv_bfloat16>(p, st);
-  return launch_combine<__half>(p, st);
+  p.position = s.position;
+  return choose_type(p, type, cols, unit_of(cols * size, {Rows{y, p.ldy}, Rows{add, p.ld_add}, Rows{out, p.ldo}}), st);
 }
 
 cudaError_t launch_expert_combine_backward(const void* dout, int64_t ldd, const void* y, int64_t ldy, int type,
                                            int64_t cols, const ds_expert_slots& s, const float* weights, void* dy,
                                            int64_t lddy, float* dweights, cudaStream_t st) {
+  const int64_t size = type_size(type);
   CombineBackwardParams p = {};
   p.d = dout, p.y = y, p.dy = dy, p.weights = weights, p.dweights = dweights;
-  p.ldd = ldd, p.ldy = ldy, p.lddy = lddy, p.cols = cols;
+  p.ldd = ldd * size, p.ldy = ldy * size, p.lddy = lddy * size;
   p.tokens = s.tokens, p.rows = s.rows, p.top_k = s.top_k;
   p.position = s.position, p.slot = s.slot;
-  p.vec = rows_aligned(dout, ldd, type) && rows_aligned(dweights ? y : nullptr, ldy, type) && rows_aligned(dy, lddy, type);
-  if (type == DS_TYPE_F32) return launch_combine_backward<float>(p, st);
-  if (type == DS_TYPE_BF16) return launch_combine_backward<__nv_bfloat16>(p, st);
-  return launch_combine_backward<__half>(p, st);
+  return choose_type(p, type, cols, unit_of(cols * size, {Rows{dout, p.ldd}, Rows{y, p.ldy}, Rows{dy, p.lddy}}), st);
 }
 
 }  // namespace ds

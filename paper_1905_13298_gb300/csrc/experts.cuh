@@ -22,7 +22,6 @@ struct RowCopy {
   const void* src;
   void* dst;
   int64_t ld_src, ld_dst, bytes;  // in bytes
-  int unit;                       // bytes of an access that both matrices are aligned for
 };
 cudaError_t launch_expert_gather(const RowCopy& a, const RowCopy& b, const ds_expert_slots& s, cudaStream_t st);
 cudaError_t launch_expert_combine(const void* y, int type, int64_t ldy, int64_t cols, const ds_expert_slots& s,

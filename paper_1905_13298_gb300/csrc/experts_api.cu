@@ -42,16 +42,9 @@ ds_status check_f8_rows(const char* name, const ds_f8_matrix* m, int64_t rows, i
   return check_f8_out(name, m, rows, cols, true);
 }
 
-// Bytes of an access to rows of these addresses and strides: at most 16.
-int unit_of(const void* a, int64_t lda, const void* b, int64_t ldb) {
-  int u = 16;
-  while (u > 1 && !(aligned(a, u) && aligned(b, u) && lda % u == 0 && ldb % u == 0)) u /= 2;
-  return u;
-}
-
 // Warps of a launch stay inside a grid's 2^31 - 1 CTAs.
 ds_status check_size(const ds_expert_slots* s, int64_t cols) {
-  if ((s->tokens + s->rows) > ((int64_t)1 << 38) / (cols / 64 + 1)) return fail(DS_ERR_UNSUPPORTED, "rows x cols too large");
+  if ((s->tokens + s->rows) > ((int64_t)1 << 34) / (cols / 64 + 1)) return fail(DS_ERR_UNSUPPORTED, "rows x cols too large");
   return DS_OK;
 }
 
@@ -98,7 +91,7 @@ ds_status ds_expert_gather(const void* x, int type, int64_t ldx, int64_t cols, c
   const Span ins[] = {span("x", x, strided(s->tokens, cols, ldx, size)), position_of(s), slot_of(s)};
   if ((r = check_apart(outs, ins)) != DS_OK) return r;
   if (cols == 0 || s->rows == 0) return DS_OK;
-  const RowCopy a{x, out, ldx * size, ldo * size, cols * size, unit_of(x, ldx * size, out, ldo * size)};
+  const RowCopy a{x, out, ldx * size, ldo * size, cols * size};
   return cuda_check(launch_expert_gather(a, RowCopy{}, *s, static_cast<cudaStream_t>(stream)), "expert_gather launch");
 }
 
@@ -116,8 +109,8 @@ ds_status ds_expert_gather_f8(const ds_f8_matrix* x, const ds_expert_slots* s, c
   const Span ins[] = {values_of("x", x), scales_of("x's scales", x), position_of(s), slot_of(s)};
   if ((r = check_apart(outs, ins)) != DS_OK) return r;
   if (x->cols == 0 || s->rows == 0) return DS_OK;
-  const RowCopy a{x->q, out->q, x->ld, out->ld, x->cols, 16};
-  const RowCopy b{x->scale, out->scale, 4 * x->ld_scale, 4 * out->ld_scale, 4 * blocks_of(x->cols), 4};
+  const RowCopy a{x->q, out->q, x->ld, out->ld, x->cols};
+  const RowCopy b{x->scale, out->scale, 4 * x->ld_scale, 4 * out->ld_scale, 4 * blocks_of(x->cols)};
   return cuda_check(launch_expert_gather(a, b, *s, static_cast<cudaStream_t>(stream)), "expert_gather_f8 launch");
 }
 
