@@ -37,10 +37,8 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ int load_of_rank(const int* p, uint32_t rank) {
   const uint32_t own = (uint32_t)__cvta_generic_to_shared(p);
   uint32_t at;
@@ -103,7 +101,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   int before = 0, count = here;  // slots of the CTAs before this one, and of all
   if constexpr (CLUSTER) {
     if (e < E) total[e] = here;
-    cluster_barrier();
+    cluster_arrive();
+    cluster_wait();
     if (e < E) {
       int c[8];
 #pragma unroll
@@ -115,6 +114,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
         count += c[r];
       }
     }
+    __syncwarp();
+    cluster_arrive();  // the other CTAs' counts have been read
   }
   const int room = (count + P.align - 1) / P.align * P.align;
   int sum = room;
@@ -165,13 +166,16 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   }
   for (int64_t r = rows_used + (int64_t)rank * blockDim.x + threadIdx.x; r < P.rows; r += ranks * blockDim.x)
     P.slot[r] = -1;
-  if constexpr (CLUSTER) cluster_barrier();  // the other CTAs read this one's counts until here
+  __syncwarp();
+  if constexpr (CLUSTER) cluster_wait();  // this CTA's counts have been read by the others
 }
 
 // ---------------------------------------------------------------------------
 // Rows
 // ---------------------------------------------------------------------------
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+// CTAs of four warps, and one wide access of each row for a lane: loads that start later while others end (8192 x 4 slots,
+// 2048 bf16: combine 33 us, 42 with 256 threads and two accesses; its gradient 49 and 53; gather 28.5 and 34).
+constexpr int kThreads = 128, kWarps = kThreads / 32;
 
 // An access of BYTES bytes and the values in it.
 template <int BYTES>
@@ -213,7 +217,7 @@ __device__ __forceinline__ const U* unit_at(const void* base, int64_t r, int64_t
   return reinterpret_cast<const U*>(static_cast<const char*>(base) + r * ld_bytes) + i;
 }
 
-constexpr int kZeroRows = 8;  // rows of a warp that looks for rows without a slot
+constexpr int kZeroRows = 2;  // rows of a warp that looks for rows without a slot
 
 // The first rows of which `rows` from r0 on hold no slot, as bits.
 __device__ __forceinline__ uint32_t rows_without(const int32_t* slot, int64_t r0, int64_t rows) {
@@ -292,14 +296,14 @@ struct CombineParams {
   int top_k;
 };
 
-// Units of a lane: with AT_ONCE rows of each, up to 128 bytes are on their way.
-constexpr int units_of(int bytes, int at_once) { return bytes == 16 ? (at_once == 8 ? 1 : 2) : 4; }
+// Units of a lane.
+constexpr int units_of(int bytes) { return bytes == 16 ? 1 : 8; }
 
 // A warp makes a part of a token's sum, from AT_ONCE rows at a time.
 template <typename T, int BYTES, int AT_ONCE>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams P) {
   using U = Unit<T, BYTES>;
-  constexpr int N = units_of(BYTES, AT_ONCE);
+  constexpr int N = units_of(BYTES);
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int64_t t = id / P.parts, u0 = (id - t * P.parts) * (32 * N) + lane;
@@ -372,7 +376,7 @@ struct CombineBackwardParams {
 template <typename T, int BYTES, int AT_ONCE>
 __global__ void __launch_bounds__(kThreads) combine_backward_kernel(const CombineBackwardParams P) {
   using U = Unit<T, BYTES>;
-  constexpr int N = units_of(BYTES, AT_ONCE);
+  constexpr int N = units_of(BYTES);
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (id >= P.tokens) {
@@ -461,7 +465,7 @@ cudaError_t launch_gather(GatherParams& p, cudaStream_t st) {
 
 template <typename T, int BYTES, int AT_ONCE>
 cudaError_t launch_combine(CombineParams& p, cudaStream_t st) {
-  p.parts = over(p.units, 32 * units_of(BYTES, AT_ONCE));
+  p.parts = over(p.units, 32 * units_of(BYTES));
   const int64_t ctas = over(p.tokens * p.parts, kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
   combine_kernel<T, BYTES, AT_ONCE><<<(unsigned)ctas, kThreads, 0, st>>>(p);

@@ -8,12 +8,14 @@
 namespace ds {
 namespace {
 
-// One expert's part of the output, for the stores.
+// One expert's part of the output, for the stores, and a tile's place in it.
 struct OutputPart {
   const float *bias, *add;
   void* y;
   int64_t M, N, ld_add, ldy;
   int type, vec, pairs;
+  int m0, n0;
+  __device__ __forceinline__ const OutputPart& to(const Params&) const { return *this; }
 };
 
 // y = x w_e^T.  Tiles of expert after expert, and behind them those of the rows that no expert has (no blocks: zeros).
@@ -83,12 +85,12 @@ struct SegmentTiles {
     return (int64_t)mine * P.nk;
   }
   __device__ __forceinline__ int aligned(const Params& P, const Tile&) const { return P.aligned; }
-  template <typename F>
-  __device__ __forceinline__ void place(const Params& P, const Tile& tile, uint32_t t, const F& store) const {
+  __device__ __forceinline__ OutputPart output(const Params& P, uint32_t t) const {
     const int e = expert(t);
-    const OutputPart o{e < experts && P.bias ? P.bias + (int64_t)e * cols : nullptr,
-                       nullptr, P.y, (int64_t)start[e + 1], (int64_t)cols, 0, P.ldy, P.type, P.vec, P.pairs};
-    store(o, (int64_t)tile.m0, (int64_t)(tile.n0 - (int)((uint32_t)e * cols)));
+    const Tile tile = at(P, t);
+    return OutputPart{e < experts && P.bias ? P.bias + (int64_t)e * cols : nullptr,
+                      nullptr, P.y, (int64_t)start[e + 1], (int64_t)cols, 0, P.ldy, P.type, P.vec, P.pairs,
+                      tile.m0, tile.n0 - (int)((uint32_t)e * cols)};
   }
 };
 
@@ -132,12 +134,11 @@ struct GradientTiles {
   __device__ __forceinline__ int aligned(const Params& P, const Tile& t) const {
     return P.aligned == 8 && t.kb0 % 8 == 0 ? 8 : (P.aligned >= 4 && t.kb0 % 4 == 0 ? 4 : 1);
   }
-  template <typename F>
-  __device__ __forceinline__ void place(const Params& P, const Tile& tile, uint32_t t, const F& store) const {
+  __device__ __forceinline__ OutputPart output(const Params& P, uint32_t t) const {
     const int64_t row = (int64_t)expert(t) * P.M;
-    const OutputPart o{nullptr, P.add ? P.add + row * P.ld_add : nullptr, static_cast<float*>(P.y) + row * P.ldy,
-                       P.M, P.N, P.ld_add, P.ldy, P.type, P.vec, P.pairs};
-    store(o, (int64_t)tile.m0, (int64_t)tile.n0);
+    const Tile tile = at(P, t);
+    return OutputPart{nullptr, P.add ? P.add + row * P.ld_add : nullptr, static_cast<float*>(P.y) + row * P.ldy,
+                      P.M, P.N, P.ld_add, P.ldy, DS_TYPE_F32, P.vec, P.pairs, tile.m0, tile.n0};
   }
 };
 

@@ -483,9 +483,13 @@ struct TileOrder {
     return (int64_t)mine * P.nk;
   }
   __device__ __forceinline__ int aligned(const Params& P, const Tile&) const { return P.aligned; }
-  template <typename F>
-  __device__ __forceinline__ void place(const Params& P, const Tile& t, uint32_t, const F& store) const {
-    store(P, (int64_t)t.m0, (int64_t)t.n0);
+  struct Output {
+    int m0, n0;
+    __device__ __forceinline__ const Params& to(const Params& P) const { return P; }
+  };
+  __device__ __forceinline__ Output output(const Params& P, uint32_t t) const {
+    const Tile tile = at(P, t);
+    return Output{tile.m0, tile.n0};
   }
 };
 
@@ -584,10 +588,12 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
       constexpr int PER = (USED + SPAN - 1) / SPAN;
       const int j = threadIdx.x - 64;
       ScaleFeed<PER, GROUP> feed;
-      int nk = 0, vec = 1;
+      int tile_blocks = 0, tile_vec = 1;  // of tiles that differ; of a single product's they are the same
+      auto nk = [&] { return Order::EMPTY ? tile_blocks : P.nk; };
+      auto vec = [&] { return Order::EMPTY ? tile_vec : P.aligned; };
       auto point = [&](const Tile& tile) {  // at the scales of a tile's rows
-        nk = tile.nk;
-        vec = tiles.aligned(P, tile);
+        tile_blocks = tile.nk;
+        tile_vec = tiles.aligned(P, tile);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
           const int r = j + SPAN * i;
@@ -612,26 +618,26 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
       if constexpr (!COLS) {
         if (!Order::EMPTY || t < ntiles) {
           point(tiles.at(P, t));
-          feed.load(0, nk, vec);
+          feed.load(0, nk(), vec());
         }
       }
       while (t < ntiles && ok) {
         if constexpr (COLS) point(tiles.at(P, t));
-        const int blocks = nk;
+        const int blocks = nk();
         t = pass(t + gridDim.x);
         for (int i0 = 0; i0 < blocks && ok; i0 += GROUP) {
           float v[PER][GROUP];
-          if constexpr (COLS) feed.load(i0, nk, vec);
+          if constexpr (COLS) feed.load(i0, nk(), vec());
 #pragma unroll
           for (int i = 0; i < PER; ++i)
 #pragma unroll
             for (int b = 0; b < GROUP; ++b) v[i][b] = feed.next[i][b];
           if constexpr (!COLS) {
             if (i0 + GROUP < blocks) {
-              feed.load(i0 + GROUP, nk, vec);
+              feed.load(i0 + GROUP, nk(), vec());
             } else if (t < ntiles) {
               point(tiles.at(P, t));
-              feed.load(0, nk, vec);
+              feed.load(0, nk(), vec());
             }
           }
 #pragma unroll
@@ -737,12 +743,11 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
             add_block(std::true_type());
         }
       }
-      tiles.place(P, tiles.at(P, t), t, [&](const auto& to, int64_t m, int64_t n) {
-        if constexpr (WIDE)
-          store_wide<!COLS>(to, m + 32 * q, n + col0, acc);
-        else
-          store_narrow<!COLS>(to, m + 32 * q, n + col0, acc, sh->patch[e]);
-      });
+      const auto part = tiles.output(P, t);
+      if constexpr (WIDE)
+        store_wide<!COLS>(part.to(P), part.m0 + 32 * q, part.n0 + col0, acc);
+      else
+        store_narrow<!COLS>(part.to(P), part.m0 + 32 * q, part.n0 + col0, acc, sh->patch[e]);
     }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
