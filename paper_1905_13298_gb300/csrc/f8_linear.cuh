@@ -464,33 +464,39 @@ __device__ __forceinline__ void grouped(uint32_t r, uint32_t tiles_m, uint32_t t
   tn = (int)(q / size);
 }
 
-// The tiles of one product.  What the kernel asks of an order of tiles: how many there are and where each lies, all
-// blocks of the reduction that a CTA's tiles have, and where a tile's sums go.
+// The tiles of one product.  What the kernel asks of an order of tiles: all blocks of the reduction that a CTA's tiles
+// have, walks over these tiles (each of a CTA's parts goes its own), and where a tile's sums go.
 template <int COLS_OF_TILE>
 struct TileOrder {
   static constexpr int N = COLS_OF_TILE;
   static constexpr bool EMPTY = false;  // whether tiles may have no blocks
   uint32_t tiles_m, tiles_n, G;
-  __device__ __forceinline__ TileOrder ready(const Params&, void*) const { return *this; }
-  __device__ __forceinline__ uint32_t count() const { return tiles_m * tiles_n; }
-  __device__ __forceinline__ Tile at(const Params& P, uint32_t t) const {
-    int tm, tn;
-    grouped(t, tiles_m, tiles_n, G, tm, tn);
-    return Tile{tm * ROWS, tn * N, 0, P.nk};
-  }
-  __device__ __forceinline__ int64_t blocks(const Params& P) const {
-    const uint32_t mine = blockIdx.x < count() ? (count() - blockIdx.x - 1) / gridDim.x + 1 : 0;
-    return (int64_t)mine * P.nk;
-  }
-  __device__ __forceinline__ int aligned(const Params& P, const Tile&) const { return P.aligned; }
   struct Output {
     int m0, n0;
     __device__ __forceinline__ const Params& to(const Params& P) const { return P; }
   };
-  __device__ __forceinline__ Output output(const Params& P, uint32_t t) const {
-    const Tile tile = at(P, t);
-    return Output{tile.m0, tile.n0};
+  struct Walk {
+    uint32_t t;
+    __device__ __forceinline__ bool ended(const TileOrder& o) const { return t >= o.tiles_m * o.tiles_n; }
+    __device__ __forceinline__ void next(const TileOrder&) { t += gridDim.x; }
+    __device__ __forceinline__ int blocks(const Params& P, const TileOrder&) const { return P.nk; }
+    __device__ __forceinline__ Tile tile(const Params& P, const TileOrder& o) const {
+      int tm, tn;
+      grouped(t, o.tiles_m, o.tiles_n, o.G, tm, tn);
+      return Tile{tm * ROWS, tn * N, 0, P.nk};
+    }
+    __device__ __forceinline__ Output output(const Params& P, const TileOrder& o) const {
+      const Tile at = tile(P, o);
+      return Output{at.m0, at.n0};
+    }
+  };
+  __device__ __forceinline__ TileOrder ready(const Params&, void*) const { return *this; }
+  __device__ __forceinline__ Walk walk() const { return Walk{blockIdx.x}; }
+  __device__ __forceinline__ int64_t blocks(const Params& P) const {
+    const uint32_t n = tiles_m * tiles_n, mine = blockIdx.x < n ? (n - blockIdx.x - 1) / gridDim.x + 1 : 0;
+    return (int64_t)mine * P.nk;
   }
+  __device__ __forceinline__ int aligned(const Params& P, const Tile&) const { return P.aligned; }
 };
 
 // COLS: w has a scale per row, so the columns of a tile differ; otherwise a warp's 128 columns share one.
@@ -530,7 +536,6 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = sh->tmem_base;
-  const uint32_t ntiles = tiles.count();
 
   if (warp < Cfg::OTHERS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Cfg::REGS_OTHERS));
@@ -539,8 +544,8 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
       Ring<BIG_STAGES> st;
       uint32_t issued = 0;
       bool ok = true;
-      for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
-        const Tile tile = tiles.at(P, t);
+      for (auto walk = tiles.walk(); !walk.ended(tiles) && ok; walk.next(tiles)) {
+        const Tile tile = walk.tile(P, tiles);
         for (int i = 0; i < tile.nk; ++i, ++issued, st.next()) {
           ok = mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault);
           if (!ok) break;
@@ -609,22 +614,23 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
       Ring<BIG_STAGES> st;
       uint32_t it = 0;
       bool ok = true;
-      auto pass = [&](uint32_t t) {  // the first tile from t on that has blocks
+      auto walk = tiles.walk();
+      auto pass = [&] {  // to the first tile that has blocks
         if constexpr (Order::EMPTY)
-          while (t < ntiles && tiles.at(P, t).nk == 0) t += gridDim.x;
-        return t;
+          while (!walk.ended(tiles) && walk.blocks(P, tiles) == 0) walk.next(tiles);
       };
-      uint32_t t = pass(blockIdx.x);
+      pass();
       if constexpr (!COLS) {
-        if (!Order::EMPTY || t < ntiles) {
-          point(tiles.at(P, t));
+        if (!Order::EMPTY || !walk.ended(tiles)) {
+          point(walk.tile(P, tiles));
           feed.load(0, nk(), vec());
         }
       }
-      while (t < ntiles && ok) {
-        if constexpr (COLS) point(tiles.at(P, t));
+      while (!walk.ended(tiles) && ok) {
+        if constexpr (COLS) point(walk.tile(P, tiles));
         const int blocks = nk();
-        t = pass(t + gridDim.x);
+        walk.next(tiles);
+        pass();
         for (int i0 = 0; i0 < blocks && ok; i0 += GROUP) {
           float v[PER][GROUP];
           if constexpr (COLS) feed.load(i0, nk(), vec());
@@ -635,8 +641,8 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
           if constexpr (!COLS) {
             if (i0 + GROUP < blocks) {
               feed.load(i0 + GROUP, nk(), vec());
-            } else if (t < ntiles) {
-              point(tiles.at(P, t));
+            } else if (!walk.ended(tiles)) {
+              point(walk.tile(P, tiles));
               feed.load(0, nk(), vec());
             }
           }
@@ -678,11 +684,11 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
       if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
       ac.next();
     };
-    for (uint32_t t = blockIdx.x; t < ntiles && ok; t += gridDim.x) {
+    for (auto walk = tiles.walk(); !walk.ended(tiles) && ok; walk.next(tiles)) {
       float acc[kBigCols];
 #pragma unroll
       for (int j = 0; j < kBigCols; ++j) acc[j] = 0.f;
-      const int nk = tiles.at(P, t).nk;
+      const int nk = walk.blocks(P, tiles);
       for (int i = 0; i < nk; ++i, ++it) {
         if (!wait_block()) break;
         const uint32_t taddr = tmem + ac.slot * N;
@@ -743,7 +749,7 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
             add_block(std::true_type());
         }
       }
-      const auto part = tiles.output(P, t);
+      const auto part = walk.output(P, tiles);
       if constexpr (WIDE)
         store_wide<!COLS>(part.to(P), part.m0 + 32 * q, part.n0 + col0, acc);
       else
