@@ -21,7 +21,7 @@ namespace ds {
 namespace {
 
 constexpr int kThreads = 128, kEach = 8, kSpan = kThreads * kEach;
-constexpr int kFew = 40, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
+constexpr int kFew = 50, kMany = 400;  // tensors of a launch: parameters of up to 4 KB, or up to 32 KB
 
 struct Tensor {
   void* p;
@@ -481,22 +481,28 @@ struct Piece {
   int tensor;
   bool written;
 };
+constexpr int kKinds = 8;  // p, g, m, v, their scales, copy, and what the options point to
 
-// Written memory is apart from everything else; sorted by address, a piece can only overlap the ones that reach past its
-// start, of which the one that reaches furthest (and the written one that does) are kept.
-ds_status check_pieces(std::vector<Piece>& pieces) {
-  bool sorted = true;
-  for (size_t k = 1; k < pieces.size() && sorted; ++k) sorted = pieces[k - 1].at <= pieces[k].at;
-  if (!sorted)
-    std::sort(pieces.begin(), pieces.end(), [](const Piece& a, const Piece& b) { return a.at < b.at; });
+// Written memory is apart from everything else.  The pieces are gone through by address (those of one kind often lie in
+// order already): one can only overlap those before it that reach past its start, of which the one that reaches furthest
+// and the written one that does are kept.
+ds_status check_pieces(std::vector<Piece> (&kinds)[kKinds]) {
+  size_t next[kKinds] = {};
+  auto before = [](const Piece& a, const Piece& b) { return a.at < b.at; };
+  for (auto& pieces : kinds)
+    if (!std::is_sorted(pieces.begin(), pieces.end(), before)) std::sort(pieces.begin(), pieces.end(), before);
   uintptr_t any = 0, written = 0;
-  for (const Piece& q : pieces) {
+  for (;;) {
+    int first = -1;
+    for (int k = 0; k < kKinds; ++k)
+      if (next[k] < kinds[k].size() && (first < 0 || kinds[k][next[k]].at < kinds[first][next[first]].at)) first = k;
+    if (first < 0) return DS_OK;
+    const Piece& q = kinds[first][next[first]++];
     if (q.at < written || (q.written && q.at < any))
       return fail(DS_ERR_INVALID_ARG, "memory of tensor %d overlaps that of another tensor or of itself", q.tensor);
     if (q.end > any) any = q.end;
     if (q.written && q.end > written) written = q.end;
   }
-  return DS_OK;
 }
 
 ds_status adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_options* o, cudaStream_t st) {
@@ -510,9 +516,9 @@ ds_status adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_option
   if (!aligned(o->step_dev, 8) || !aligned(o->lr_dev, 4) || !aligned(o->grad_scale, 4))
     return fail(DS_ERR_ALIGNMENT, "step_dev must be 8-byte aligned, lr_dev and grad_scale 4-byte aligned");
   std::vector<Tensor> all;
-  std::vector<Piece> pieces;
+  std::vector<Piece> pieces[kKinds];
   all.reserve(count);
-  pieces.reserve((size_t)count * 7);
+  for (auto& k : pieces) k.reserve(count + 3);
   bool f8 = false, known = false;
   for (int k = 0; k < count; ++k) {
     const ds_adamw_tensor& t = tensors[k];
@@ -544,22 +550,22 @@ ds_status adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_option
     d.number = (uint32_t)k;
     d.p_type = (int8_t)t.p_type, d.g_type = (int8_t)t.g_type, d.copy_type = (int8_t)t.copy_type, d.level = (int8_t)lv;
     all.push_back(d);
-    auto piece = [&](const void* p, int64_t bytes, bool written) {
+    auto piece = [&](int kind, const void* p, int64_t bytes, bool written) {
       if (!p) return;
       const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-      pieces.push_back(Piece{at, at + (uintptr_t)bytes, k, written});
+      pieces[kind].push_back(Piece{at, at + (uintptr_t)bytes, k, written});
     };
-    piece(t.p, t.n * ps, true);
-    piece(t.g, t.n * gs, false);
-    piece(t.m, t.n * ss, true);
-    piece(t.v, t.n * ss, true);
-    piece(t.m_scale, blocks_of(t.n) * 4, true);
-    piece(t.v_scale, blocks_of(t.n) * 4, true);
-    piece(t.copy, t.n * cs, true);
+    piece(0, t.p, t.n * ps, true);
+    piece(1, t.g, t.n * gs, false);
+    piece(2, t.m, t.n * ss, true);
+    piece(3, t.v, t.n * ss, true);
+    piece(4, t.m_scale, blocks_of(t.n) * 4, true);
+    piece(5, t.v_scale, blocks_of(t.n) * 4, true);
+    piece(6, t.copy, t.n * cs, true);
   }
   if (all.empty()) return DS_OK;
   for (const void* p : {(const void*)o->step_dev, (const void*)o->lr_dev, (const void*)o->grad_scale})
-    if (p) pieces.push_back(Piece{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (p == o->step_dev ? 8 : 4), -1, false});
+    if (p) pieces[7].push_back(Piece{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (p == o->step_dev ? 8 : 4), -1, false});
   const ds_status r = check_pieces(pieces);
   if (r != DS_OK) return r;
 

@@ -48,7 +48,7 @@ class ExpertOrder:
     a slot or -1, and ``slot`` [rows], the slot (token * top_k + choice) of a row or -1.  Segments start at multiples
     of ``align``."""
 
-    __slots__ = ("offsets", "counts", "position", "slot", "desc")
+    __slots__ = ("offsets", "counts", "position", "slot", "device", "desc")
 
     def __init__(self, offsets, counts, position, slot, align: int = 1):
         if offsets.dim() != 1 or offsets.shape[0] < 2:
@@ -59,7 +59,7 @@ class ExpertOrder:
         if device < 0:
             raise ValueError("offsets must be a CUDA tensor")
         experts, (tokens, top_k), rows = offsets.shape[0] - 1, position.shape, slot.shape[0]
-        self.offsets, self.counts, self.position, self.slot = offsets, counts, position, slot
+        self.offsets, self.counts, self.position, self.slot, self.device = offsets, counts, position, slot, device
         self.desc = ds_expert_slots(_ints(offsets, "offsets", (experts + 1,), device),
                                     _ints(counts, "counts", (experts,), device),
                                     _ints(position, "position", (tokens, top_k), device),
@@ -90,8 +90,8 @@ def _order(order, device: int):
     """The order's descriptor; its tensors are on the input's device."""
     if not isinstance(order, ExpertOrder):
         raise ValueError("order must be an ExpertOrder")
-    if order.offsets.get_device() != device:
-        raise ValueError(f"order is on {order.offsets.device}, the input on cuda:{device}")
+    if order.device != device:
+        raise ValueError(f"order is on cuda:{order.device}, the input on cuda:{device}")
     return order.desc
 
 
@@ -125,14 +125,15 @@ def expert_order(ids, experts: int, align: int = 1, stream=None) -> ExpertOrder:
     rows = lib().ds_expert_rows(tokens, top_k, experts, align)
     if rows < 0:
         raise DsError(DS_ERR_UNSUPPORTED, "too many experts, tokens or rows, or align too large")
-    # one memory for all four: a decoding step is short
-    parts = (experts + 1, experts, tokens * top_k, rows)
-    offsets, counts, position, slot = torch.empty(sum(parts), dtype=torch.int32, device=ids.device).split(parts)
-    order = ExpertOrder.__new__(ExpertOrder)
-    order.offsets, order.counts, order.position, order.slot = offsets, counts, position.view(tokens, top_k), slot
-    at = offsets.data_ptr()
-    order.desc = ds_expert_slots(at, at + 4 * (experts + 1), at + 4 * (2 * experts + 1),
-                                 at + 4 * (2 * experts + 1 + tokens * top_k), tokens, rows, top_k, experts, align, 0)
+    order, kind, where = ExpertOrder.__new__(ExpertOrder), torch.int32, ids.device
+    # four allocations cost the host less than four views of one
+    offsets = order.offsets = torch.empty(experts + 1, dtype=kind, device=where)
+    counts = order.counts = torch.empty(experts, dtype=kind, device=where)
+    position = order.position = torch.empty((tokens, top_k), dtype=kind, device=where)
+    slot = order.slot = torch.empty(rows, dtype=kind, device=where)
+    order.device = device
+    order.desc = ds_expert_slots(offsets.data_ptr(), counts.data_ptr(), position.data_ptr(), slot.data_ptr(), tokens,
+                                 rows, top_k, experts, align, 0)
     _check(lib().ds_expert_order(ids.data_ptr(), _INDEX[ids.dtype], order.desc, _on_stream(device)))
     return order
 

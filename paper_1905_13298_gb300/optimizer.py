@@ -85,7 +85,7 @@ class AdamW:
                 c = self.copies[k]
                 d.copy, d.copy_type = _flat(c, f"copies[{k}]", n, _TYPES, device), _TYPES[c.dtype]
         self._take(self.grads)
-        self._held = self._addresses()
+        self._hold()
         self.lr, self.betas, self.eps, self.grad_scale, self.steps, self.seed = lr, betas, eps, grad_scale, steps, seed
 
     def _take(self, grads) -> None:
@@ -94,8 +94,10 @@ class AdamW:
         for d, (at, kind) in zip(self._tensors, got):
             d.g, d.g_type = at, kind
 
-    def _addresses(self) -> list:
-        return [t.data_ptr() for t in self.params + self.grads]
+    def _hold(self) -> None:
+        """Notes where parameters and gradients lie: a step refuses ones that were given other memory since."""
+        self._at = [t.data_ptr for t in self.params + self.grads]
+        self._held = [at() for at in self._at]
 
     def step(self, grads=None, stream=None) -> None:
         """One step; ``grads`` replace those of the steps before."""
@@ -109,8 +111,8 @@ class AdamW:
                 raise ValueError(f"grads has {len(grads)} entries, expected {len(self.params)}")
             self._take(grads)
             self.grads = grads
-            self._held = self._addresses()
-        elif self._addresses() != self._held:
+            self._hold()
+        elif [at() for at in self._at] != self._held:
             raise ValueError("a parameter or gradient has other memory than when it was given")
         o = ds_adamw_options(0.0, self.betas[0], self.betas[1], self.eps, 0, None, None, None, self.seed & 0xFFFFFFFF, 0)
         if isinstance(self.lr, torch.Tensor):
