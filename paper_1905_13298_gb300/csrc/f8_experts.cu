@@ -18,11 +18,71 @@ struct OutputPart {
   __device__ __forceinline__ const OutputPart& to(const Params&) const { return *this; }
 };
 
+// y = x w_e^T by the kernel of small products: a CTA's tile among those of all experts.  Every warp finds it for itself,
+// by the number of row tiles before each expert, so that no barrier is needed.
+template <int BN>
+struct SegmentPlace {
+  const int32_t* offsets;
+  int experts;
+  uint32_t rows, cols, tiles_n;
+  int m0, n0, e, end;  // of the tile: rows of x and w, the expert (`experts`: rows that none has), the segment's end
+
+  __device__ __forceinline__ uint32_t first_row(int i) const {
+    const uint32_t o = i <= experts ? (uint32_t)offsets[i] : rows;
+    return o < rows ? o : rows;
+  }
+  __device__ __forceinline__ bool find(const Params&, uint32_t tile) {
+    const uint32_t rt = tile / tiles_n, lane = threadIdx.x & 31;
+    const int per = (experts + 1 + 31) / 32, from = (int)lane * per;
+    const int to = from + per < experts + 1 ? from + per : experts + 1;
+    auto row_tiles = [&](uint32_t a, uint32_t b) { return b > a ? (b - a + BN - 1) / BN : 0u; };
+    uint32_t sum = 0, row = from < to ? first_row(from) : 0;
+    for (int i = from; i < to; ++i) {
+      const uint32_t next = first_row(i + 1);
+      sum += row_tiles(row, next);
+      row = next;
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+      if (lane >= d) upto += up;
+    }
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, rt < upto);
+    if (here == 0) return false;
+    const int src = __ffs(here) - 1;
+    uint32_t left = rt - (upto - sum);
+    if ((int)lane == src) {
+      row = first_row(from);
+      for (int i = from; i < to; ++i) {
+        const uint32_t next = first_row(i + 1), n = row_tiles(row, next);
+        if (left < n) {
+          e = i, m0 = (int)(row + left * BN), end = (int)next;
+          break;
+        }
+        left -= n;
+        row = next;
+      }
+    }
+    e = __shfl_sync(0xFFFFFFFFu, e, src);
+    m0 = __shfl_sync(0xFFFFFFFFu, m0, src);
+    end = __shfl_sync(0xFFFFFFFFu, end, src);
+    n0 = (int)((uint32_t)e * cols + (tile - rt * tiles_n) * ROWS);
+    return true;
+  }
+  __device__ __forceinline__ int blocks(const Params& P) const { return e < experts ? P.nk : 0; }
+  __device__ __forceinline__ OutputPart output(const Params& P) const {
+    return OutputPart{e < experts && P.bias ? P.bias + (int64_t)e * cols : nullptr,
+                      nullptr, P.y, (int64_t)end, (int64_t)cols, 0, P.ldy, P.type, P.vec, P.pairs, m0, column(P)};
+  }
+  __device__ __forceinline__ int column(const Params&) const { return n0 - (int)((uint32_t)e * cols); }
+};
+
 // y = x w_e^T.  Tiles of expert after expert, and behind them those of the rows that no expert has (no blocks: zeros).
 template <int COLS_OF_TILE>
 struct SegmentTiles {
   static constexpr int N = COLS_OF_TILE;
-  static constexpr bool EMPTY = true;
+  static constexpr bool EMPTY = true, ADDS = false;
   static constexpr uint32_t GROUP = 16;  // row tiles that share columns, as TileOrder::G
   const int32_t* offsets;
   int experts;
@@ -104,7 +164,7 @@ struct SegmentTiles {
 template <int COLS_OF_TILE>
 struct GradientTiles {
   static constexpr int N = COLS_OF_TILE;
-  static constexpr bool EMPTY = true;
+  static constexpr bool EMPTY = true, ADDS = true;
   const int32_t* offsets;
   int experts;
   uint32_t rows, tiles_m, tiles_n, G;
@@ -237,6 +297,44 @@ cudaError_t linear(const ExpertProduct& e, cudaStream_t st) {
   return start(mx, mw, p, t, most, wide, st);
 }
 
+// `met`: experts that may have rows.
+template <int BN>
+cudaError_t linear_small(const ExpertProduct& e, int64_t met, cudaStream_t st) {
+  using Place = SegmentPlace<BN>;
+  constexpr size_t smem = smem_bytes<BN>();
+  static const cudaError_t attr =
+      cudaFuncSetAttribute(linear_f8_kernel<BN, Place>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (attr != cudaSuccess) return attr;
+  bool wide;
+  Params p = params_of(e, e.x, e.w, &wide);
+  p.idesc = idesc_of(e.w, e.x);  // w along the lanes
+  CUtensorMap mx = {}, mw = {};
+  if (p.nk > 0 && (!make_map(&mx, e.x, BN) || !make_map(&mw, e.w, ROWS))) return cudaErrorInvalidValue;
+  Place place = {};
+  place.offsets = e.s->offsets;
+  place.experts = e.s->experts;
+  place.rows = (uint32_t)e.s->rows;
+  place.cols = (uint32_t)(e.w->rows / e.s->experts);
+  place.tiles_n = (uint32_t)over(place.cols, ROWS);
+  // enough for any choice of experts; the reduction is split while the experts that are likely met leave SMs without work
+  const int64_t most = over(e.s->rows, BN) + met + 1, likely = met * place.tiles_n;
+  int split = 1;
+  while (split < 8 && 2 * split <= p.nk && 2 * split * likely <= 2 * (int64_t)(sm_count() > 0 ? sm_count() : 1)) split *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(most * place.tiles_n * split));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)split;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, linear_f8_kernel<BN, Place>, mw, mx, p, split, place);
+}
+
 template <int N>
 cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
   bool wide;
@@ -255,7 +353,18 @@ cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_expert_linear_f8(const ExpertProduct& e, cudaStream_t st) { return linear<256>(e, st); }
+// The kernel of small products while an expert has few rows, its tile's rows of x above their mean (experts differ); us of
+// 32 experts of 2048 x 4096, 4 of them for each of so many tokens, with 16, 32, 64 rows and by the large kernel:
+//   1 token 9.3, 9.8, 12.3, 19.4;  16: 35, 36, 39, 45;  64: 48, 47, 52, 58;  128: 61, 52, 55, 59;  256: 88, 67, 61, 63;
+//   512: 147, 97, 82, 63
+cudaError_t launch_expert_linear_f8(const ExpertProduct& e, cudaStream_t st) {
+  const int64_t slots = e.s->tokens * e.s->top_k, met = slots < e.s->experts ? slots : e.s->experts;
+  const int64_t each = met > 0 ? over(slots, met) : 0;
+  if (each <= 10) return linear_small<16>(e, met, st);
+  if (each <= 21) return linear_small<32>(e, met, st);
+  if (each <= 42) return linear_small<64>(e, met, st);
+  return linear<256>(e, st);
+}
 
 cudaError_t launch_expert_weight_grad_f8(const ExpertProduct& e, cudaStream_t st) { return weight_grad<256>(e, st); }
 

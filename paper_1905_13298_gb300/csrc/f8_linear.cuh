@@ -1,5 +1,5 @@
 // The 8-bit product's device code that the dense products and the experts' share:
-// scales, stores, and the persistent kernel of large products.
+// scales, stores, and the kernels of small and of large products.
 #pragma once
 
 #include <type_traits>
@@ -395,6 +395,260 @@ struct ScaleFeed {
 // microseconds, and this many cycles (8 ms) are waited for them.
 constexpr long long kLandedCycles = 1 << 24;
 
+constexpr int kThreads = 256;
+constexpr int kEpiWarps = 4;
+
+// STAGES of the data ring, ACC accumulators in tensor memory, CTAs that share an SM.
+template <int BN>
+struct Cfg;
+template <>
+struct Cfg<16> {
+  static constexpr int STAGES = 5, ACC = 4, CTAS = 2;
+};
+template <>
+struct Cfg<32> {
+  static constexpr int STAGES = 5, ACC = 4, CTAS = 2;
+};
+template <>
+struct Cfg<64> {
+  static constexpr int STAGES = 4, ACC = 4, CTAS = 2;
+};
+
+template <int BN>
+struct __align__(16) Shared {
+  static constexpr int SLOTS = Cfg<BN>::STAGES + Cfg<BN>::ACC + 1;  // of scales: see kScaleSlots
+  float scale[SLOTS][ROWS + BN];                                    // rows of w, then rows of x
+  uint64_t full[Cfg<BN>::STAGES];   // a stage's copies and scales have come
+  uint64_t mult[Cfg<BN>::STAGES];   // its products are done
+  uint64_t tempty[Cfg<BN>::ACC];    // an accumulator has been read
+  uint64_t done;
+  uint32_t tmem_base;
+  int abort;
+};
+
+template <int BN>
+constexpr size_t smem_bytes() {
+  return (size_t)Cfg<BN>::STAGES * (ROWS + BN) * BK + sizeof(Shared<BN>) + 1024;
+}
+
+// Where a CTA's tile of a single product lies: rows m0 .. of x and n0 .. of w; how many blocks its reduction has, and
+// what its sums go to.
+template <int BN>
+struct OnePlace {
+  int m0, n0;
+  __device__ __forceinline__ bool find(const Params& P, uint32_t tile) {
+    const uint32_t tiles_n = (uint32_t)((P.N + ROWS - 1) / ROWS), tm = tile / tiles_n;
+    n0 = (int)(tile - tm * tiles_n) * ROWS, m0 = (int)tm * BN;
+    return true;
+  }
+  __device__ __forceinline__ int blocks(const Params& P) const { return P.nk; }
+  __device__ __forceinline__ const Params& output(const Params& P) const { return P; }
+  __device__ __forceinline__ int column(const Params&) const { return n0; }
+};
+
+// One tile: 128 rows of w (n0 ..), BN rows of x (m0 ..).  blockIdx.x = tile * split + rank in the cluster; the rank
+// takes the blocks [rank nk / split, (rank + 1) nk / split) of the reduction.  Warp 0 loads, warp 1 multiplies, warps 2
+// and 3 bring scales (as in the large kernel below), warps 4-7 add.
+template <int BN, typename Place>
+__global__ void __launch_bounds__(kThreads, Cfg<BN>::CTAS) linear_f8_kernel(const __grid_constant__ CUtensorMap tmap_w,
+                                                             const __grid_constant__ CUtensorMap tmap_x,
+                                                             const Params P, const int split, Place place) {
+  constexpr int STAGES = Cfg<BN>::STAGES, ACC = Cfg<BN>::ACC;
+  constexpr int A_BYTES = ROWS * BK, STAGE_BYTES = A_BYTES + BN * BK;
+  constexpr int TMEM_COLS = ACC * BN;
+  static_assert(TMEM_COLS >= 32 && TMEM_COLS <= 512, "tensor memory");
+  static_assert(STAGES * STAGE_BYTES >= BN * ROWS * 4, "the ring holds the exchanged sums");
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  Shared<BN>* sh = reinterpret_cast<Shared<BN>*>(ring + STAGES * STAGE_BYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t tile = blockIdx.x / split;
+  const int rank = (int)(blockIdx.x - tile * split);
+  if (!place.find(P, tile)) return;  // the same for a whole cluster
+  const int n0 = place.n0, m0 = place.m0, blocks = place.blocks(P);
+  const int kb0 = (int)((int64_t)blocks * rank / split);
+  const int nk = (int)((int64_t)blocks * (rank + 1) / split) - kb0;
+  volatile int* abort = &sh->abort;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&sh->full[s], 3);  // the copies, and two warps with scales
+      mbar_init(&sh->mult[s], 1);
+    }
+    for (int b = 0; b < ACC; ++b) mbar_init(&sh->tempty[b], kEpiWarps);
+    mbar_init(&sh->done, 1);
+    sh->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                 "r"(TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = sh->tmem_base;
+
+  uint64_t acc[BN / 2];
+#pragma unroll
+  for (int j = 0; j < BN / 2; ++j) acc[j] = 0;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      Ring<STAGES> st;
+      int i = 0;
+      for (; i < nk; ++i, st.next()) {
+        if (!mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault)) break;
+        unsigned char* a = ring + st.slot * STAGE_BYTES;
+        mbar_expect_tx(&sh->full[st.slot], STAGE_BYTES);
+        tma_load_2d(a, &tmap_w, &sh->full[st.slot], (kb0 + i) * BK, n0);
+        tma_load_2d(a + A_BYTES, &tmap_x, &sh->full[st.slot], (kb0 + i) * BK, m0);
+      }
+      // the last copies issued land before the CTA leaves
+      for (int j = i > STAGES ? i - STAGES : 0; j < i; ++j)
+        mbar_drain(&sh->full[j % STAGES], (uint32_t)(j / STAGES) & 1u, *abort ? kLandedCycles : kTimeoutCycles);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = P.idesc | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
+      const uint64_t adesc = sw128_desc(smem_u32(ring)), bdesc = sw128_desc(smem_u32(ring) + A_BYTES);
+      Ring<STAGES> st;
+      Ring<ACC> ac;
+      for (int i = 0; i < nk; ++i, st.next(), ac.next()) {
+        if (!mbar_wait(&sh->full[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault) ||
+            !mbar_wait(&sh->tempty[ac.slot], ac.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault))
+          break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t at = (uint64_t)(st.slot * (STAGE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < BK / 32; ++k)
+          umma_f8(tmem_base + ac.slot * BN, adesc + at + 2 * k, bdesc + at + 2 * k, idesc, k > 0);
+        umma_commit(&sh->mult[st.slot]);
+      }
+      // every MMA issued by this CTA has completed before its memory is used again
+      umma_commit(&sh->done);
+      mbar_drain(&sh->done, 0u);
+    }
+  } else if (warp < 4) {
+    constexpr int XROWS = (BN + 63) / 64, PER = 2 + XROWS, GROUP = 4;
+    const int j = threadIdx.x - 64;
+    ScaleFeed<PER, GROUP> feed;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int64_t n = n0 + j + 64 * i, m = m0 + j + 64 * (i - 2);
+      feed.src[i] = nullptr;
+      if (i < 2) {
+        if (n < P.N) feed.src[i] = P.w.s + (n >> P.w.shift) * P.w.ld + kb0;
+      } else if (j + 64 * (i - 2) < BN && m < P.M) {
+        feed.src[i] = P.x.s + (m >> P.x.shift) * P.x.ld + kb0;
+      }
+    }
+    const int vec = kb0 % 4 == 0 ? P.aligned : 1;
+    feed.load(0, nk, vec);
+    Ring<STAGES> st;
+    Ring<Shared<BN>::SLOTS> sc;
+    bool ok = true;
+    for (int i0 = 0; i0 < nk && ok; i0 += GROUP) {
+      float v[PER][GROUP];
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int b = 0; b < GROUP; ++b) v[i][b] = feed.next[i][b];
+      if (i0 + GROUP < nk) feed.load(i0 + GROUP, nk, vec);
+#pragma unroll
+      for (int b = 0; b < GROUP; ++b) {
+        if (i0 + b >= nk) break;
+        ok = __all_sync(0xFFFFFFFFu,
+                        mbar_wait(&sh->mult[st.slot], st.parity ^ 1u, abort, P.wait_cycles, &g_f8_fault));
+        if (!ok) break;
+        float* to = sh->scale[sc.slot] + j;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (i < 2 || j + 64 * (i - 2) < BN) to[64 * i] = v[i][b];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->full[st.slot]);
+        st.next();
+        sc.next();
+      }
+    }
+  } else {
+    const int q = warp & 3;
+    Ring<STAGES> st;
+    Ring<ACC> ac;
+    Ring<Shared<BN>::SLOTS> sc;
+    for (int i = 0; i < nk; ++i, st.next(), ac.next(), sc.next()) {
+      const bool ok = mbar_wait(&sh->mult[st.slot], st.parity, abort, P.wait_cycles, &g_f8_fault);
+      if (!__all_sync(0xFFFFFFFFu, ok)) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t t = tmem_base + ((uint32_t)(32 * q) << 16) + ac.slot * BN;
+      const float* scale = sh->scale[sc.slot];
+      const float rs = scale[32 * q + lane];
+      const uint64_t row2 = pair(rs, rs);
+#pragma unroll
+      for (int c = 0; c < BN; c += 16) {
+        uint32_t r[16];
+        tmem_ld16(t + c, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const ulonglong2 s2 = *reinterpret_cast<const ulonglong2*>(&scale[ROWS + c + j]);
+          acc[(c + j) / 2] = fma2(mul2(pair(r[j], r[j + 1]), row2), s2.x, acc[(c + j) / 2]);
+          acc[(c + j) / 2 + 1] = fma2(mul2(pair(r[j + 2], r[j + 3]), row2), s2.y, acc[(c + j) / 2 + 1]);
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->tempty[ac.slot]);
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS)
+                 : "memory");
+  }
+  // the ring is free: the CTA's sums, [x row][w row]
+  float* part = reinterpret_cast<float*>(ring);
+  if (warp >= 4) {
+    const int at = 32 * (warp & 3) + lane;
+#pragma unroll
+    for (int j = 0; j < BN / 2; ++j) {
+      part[(2 * j) * ROWS + at] = __uint_as_float((uint32_t)acc[j]);
+      part[(2 * j + 1) * ROWS + at] = __uint_as_float((uint32_t)(acc[j] >> 32));
+    }
+  }
+  __syncwarp();
+  if (split > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  // rank r adds up and writes the r-th share of the tile
+  const uint32_t part_addr = smem_u32(part);
+  const auto& to = place.output(P);
+  const int col0 = place.column(P);
+  for (int i = rank * kThreads + threadIdx.x; i < BN * (ROWS / 4); i += split * kThreads) {
+    const int c = i / (ROWS / 4), r4 = (i % (ROWS / 4)) * 4;
+    if (m0 + c >= to.M || col0 + r4 >= to.N) continue;
+    const uint32_t at = part_addr + (uint32_t)(c * ROWS + r4) * 4;
+    float4 u[8];  // all on their way before the first is added
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (s < split)
+        u[s] = split > 1 ? ld_cluster4(map_rank(at, s)) : *reinterpret_cast<const float4*>(&part[c * ROWS + r4]);
+    float4 v = u[0];
+#pragma unroll
+    for (int s = 1; s < 8; ++s)
+      if (s < split) v.x += u[s].x, v.y += u[s].y, v.z += u[s].z, v.w += u[s].w;
+    finish4(to, m0 + c, col0 + r4, v);
+  }
+  __syncwarp();
+  if (split > 1) cluster_sync();  // a CTA's sums are read by the others until here
+}
+
 // ---------------------------------------------------------------------------
 // Large products: one persistent CTA per SM walks tiles of 128 rows of x (the
 // lanes) by N = 256 or 128 rows of w (the columns).  Warp 0 loads, warp 1
@@ -470,6 +724,7 @@ template <int COLS_OF_TILE>
 struct TileOrder {
   static constexpr int N = COLS_OF_TILE;
   static constexpr bool EMPTY = false;  // whether tiles may have no blocks
+  static constexpr bool ADDS = false;   // whether sums are added to others' that are asked for ahead
   uint32_t tiles_m, tiles_n, G;
   struct Output {
     int m0, n0;
@@ -750,6 +1005,17 @@ __global__ void __launch_bounds__(BigCfg<COLS, Order::N>::THREADS, 1)
         }
       }
       const auto part = walk.output(P, tiles);
+      if constexpr (Order::ADDS) {
+        // All that the sums are added to is asked for at once, a row per thread: the loads that follow, of which registers
+        // hold a quarter at a time, then wait for memory once and not four times (32 x 2048 x 2048 from 8192 x 4 slots 281
+        // us, 321 without; asked for while the sums are made it slows the operands' copies, 293 us)
+        if (part.add && part.m0 + 32 * q + lane < part.M) {
+          const float* row = part.add + (part.m0 + 32 * q + lane) * part.ld_add;
+#pragma unroll
+          for (int c = part.n0 + col0; c < part.n0 + col0 + kBigCols; c += 32)
+            if (c < part.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + c));
+        }
+      }
       if constexpr (WIDE)
         store_wide<!COLS>(part.to(P), part.m0 + 32 * q, part.n0 + col0, acc);
       else
