@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     __syncwarp();
     cluster_arrive();  // the other CTAs' counts have been read
   }
-  const int room = (count + P.align - 1) / P.align * P.align;
+  const int room = (int)(((uint32_t)count + P.align - 1) / P.align * P.align);
   int sum = room;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   for (int64_t s = from + 32 * kHeld; s < to; s += 32) place_32(s, expert_of(P, s + lane, to));
   // rows without a slot: behind each expert's, up to the next one's, and behind the last
   for (int x = (int)rank * warps + warp; x < E; x += (int)ranks * warps) {
-    const int stop = (end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
+    const int64_t stop = ((int64_t)end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
     for (int64_t r = end_of[x] + lane; r < stop && r < P.rows; r += 32) P.slot[r] = -1;
   }
   for (int64_t r = rows_used + (int64_t)rank * blockDim.x + threadIdx.x; r < P.rows; r += ranks * blockDim.x)

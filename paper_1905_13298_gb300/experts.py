@@ -149,12 +149,12 @@ def expert_gather(x, order: ExpertOrder, out=None, stream=None):
         desc, dx = _order(order, device), x.desc
         if x.tiles or (out is not None and _f8(out, "out").blocks != dx.blocks):
             raise ValueError("x and out must have blocks by rows: rows of tiles cannot be moved")
+        if dx.rows != desc.tokens:
+            raise ValueError(f"x has {dx.rows} rows, the order {desc.tokens} tokens")
         if out is None:
             out = F8Matrix.empty(desc.rows, dx.cols, x.q.device, x.q.dtype)
         else:
             _on_gpu(out.q, "out", device)
-        if dx.rows != desc.tokens:
-            raise ValueError(f"x has {dx.rows} rows, the order {desc.tokens} tokens")
         _check(lib().ds_expert_gather_f8(dx, desc, out.desc, _on_stream(device)))
         return out
     ldx = _matrix(x, "x")
@@ -162,6 +162,8 @@ def expert_gather(x, order: ExpertOrder, out=None, stream=None):
     desc = _order(order, device)
     if x.shape[0] != desc.tokens:
         raise ValueError(f"x has {x.shape[0]} rows, the order {desc.tokens} tokens")
+    if isinstance(out, F8Matrix):
+        raise ValueError("out is an F8Matrix, x is not")
     if out is None:
         out = torch.empty((desc.rows, cols), dtype=x.dtype, device=x.device)
         po, ldo = out.data_ptr(), cols

@@ -96,8 +96,8 @@ class AdamW:
 
     def _hold(self) -> None:
         """Notes where parameters and gradients lie: a step refuses ones that were given other memory since."""
-        self._at = [t.data_ptr for t in self.params + self.grads]
-        self._held = [at() for at in self._at]
+        self._all = self.params + self.grads
+        self._held = list(map(torch.Tensor.data_ptr, self._all))
 
     def step(self, grads=None, stream=None) -> None:
         """One step; ``grads`` replace those of the steps before."""
@@ -112,7 +112,7 @@ class AdamW:
             self._take(grads)
             self.grads = grads
             self._hold()
-        elif [at() for at in self._at] != self._held:
+        elif list(map(torch.Tensor.data_ptr, self._all)) != self._held:
             raise ValueError("a parameter or gradient has other memory than when it was given")
         o = ds_adamw_options(0.0, self.betas[0], self.betas[1], self.eps, 0, None, None, None, self.seed & 0xFFFFFFFF, 0)
         if isinstance(self.lr, torch.Tensor):
