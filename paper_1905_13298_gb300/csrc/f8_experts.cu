@@ -2,6 +2,14 @@
 // large products (f8_linear.cuh) over the tiles of all experts.  Which rows an
 // expert has is known on the device only, so every CTA makes the list of the
 // tiles from the segments' offsets when it starts; nothing waits for the host.
+//
+// What bounds them: as the dense product, 48 KB of operands a block of a tile
+// through L2 and the read-back of the block's sums.  8192 x 4 rows of 32
+// experts, 2048 -> 4096: 345 us, 1.59 PFLOP/s (the dense product of as many
+// rows 323); weight gradients of 32 x 2048 x 2048 added to others 280 us, of
+// which the products take 144 and the sums' way out and in the rest.  With few
+// rows an expert, its weights from memory: 16 x 4 rows of the same experts 35
+// us, 5.3 TB/s of the weights met.
 #include "experts.cuh"
 #include "f8_linear.cuh"
 
@@ -280,6 +288,20 @@ Params params_of(const ExpertProduct& e, const ds_f8_matrix* x, const ds_f8_matr
 
 int64_t over(int64_t n, int64_t d) { return (n + d - 1) / d; }
 
+// Whether tiles of 128 columns take less time than those of 256, by the estimate of the dense product's tiles (1.3 us and
+// 0.6 a block, 0.7 and 0.4 for half the width, 0.013 a column where rows are not aligned) for experts of as many rows
+// each: 512 x 4 slots, 32 experts of 2048 -> 512 18.7 us, 20.9 with 256; 600 tokens to 4 of 1024 -> 2048 10.2, 12.6;
+// 4096 x 2, 8 of 1024 -> 512 14.5, 13.0; 3000 x 6, 60 of 700 -> 333 32.5, 40.6.
+bool narrow_tiles(const ExpertProduct& e, int64_t slots, int64_t met) {
+  bool wide;
+  const Params p = params_of(e, e.x, e.w, &wide);
+  const int64_t cols = e.w->rows / e.s->experts, rows = slots / ROWS + (met + 1) / 2, sms = sm_count() > 0 ? sm_count() : 1;
+  auto time = [&](int n, double tile, double block) {
+    return (double)over(rows * over(cols, n), sms) * (tile + block * p.nk + (wide ? 0.0 : 0.013 * n));
+  };
+  return time(128, 0.7, 0.4) < time(256, 1.3, 0.6);
+}
+
 template <int N>
 cudaError_t linear(const ExpertProduct& e, cudaStream_t st) {
   bool wide;
@@ -335,7 +357,7 @@ cudaError_t linear_small(const ExpertProduct& e, int64_t met, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, linear_f8_kernel<BN, Place>, mw, mx, p, split, place);
 }
 
-template <int N>
+template <int N, bool WIDE>
 cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
   bool wide;
   const Params p = params_of(e, e.w, e.x, &wide);
@@ -348,7 +370,8 @@ cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
   t.tiles_m = (uint32_t)over(p.M, ROWS);
   t.tiles_n = (uint32_t)over(p.N, N);
   t.G = t.tiles_m < 12 ? t.tiles_m : 12;  // about one wave of tiles is a square
-  return start(mx, mw, p, t, (int64_t)t.experts * t.tiles_m * t.tiles_n, wide, st);
+  const int64_t tiles = (int64_t)t.experts * t.tiles_m * t.tiles_n;
+  return p.w.shift ? launch<false, WIDE>(mx, mw, p, t, tiles, st) : launch<true, WIDE>(mx, mw, p, t, tiles, st);
 }
 
 }  // namespace
@@ -359,14 +382,20 @@ cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
 //   512: 147, 97, 82, 63
 cudaError_t launch_expert_linear_f8(const ExpertProduct& e, cudaStream_t st) {
   const int64_t slots = e.s->tokens * e.s->top_k, met = slots < e.s->experts ? slots : e.s->experts;
-  const int64_t each = met > 0 ? over(slots, met) : 0;
+  const int64_t each = met > 0 ? over(over(slots, met), e.s->align) * e.s->align : 0;  // gaps are multiplied too
   if (each <= 10) return linear_small<16>(e, met, st);
   if (each <= 21) return linear_small<32>(e, met, st);
   if (each <= 42) return linear_small<64>(e, met, st);
-  return linear<256>(e, st);
+  return narrow_tiles(e, slots, met) ? linear<128>(e, st) : linear<256>(e, st);
 }
 
-cudaError_t launch_expert_weight_grad_f8(const ExpertProduct& e, cudaStream_t st) { return weight_grad<256>(e, st); }
+// Tiles of half the width where rows of dw are not aligned: 60 x 333 x 700 from 3000 x 6 slots 37 us, 46 with 256 columns;
+// elsewhere they take 1 to 5% more or less.
+cudaError_t launch_expert_weight_grad_f8(const ExpertProduct& e, cudaStream_t st) {
+  bool wide;
+  params_of(e, e.w, e.x, &wide);
+  return wide ? weight_grad<256, true>(e, st) : weight_grad<128, false>(e, st);
+}
 
 int read_expert_f8_fault_flag() { return read_and_clear_fault(); }
 

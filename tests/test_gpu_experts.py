@@ -284,3 +284,46 @@ def test_one_expert_is_the_dense_product(dslib, n, k, tiles):
     b = _np(dslib.linear_f8(x, w, dtype=torch.float32))
     terms = np.abs(x.dequantize().cpu().numpy()).astype(np.float64) @ np.abs(w.dequantize().cpu().numpy()).T
     _near(a, b, TOL * terms)
+
+
+@pytest.mark.parametrize("k,tiles", [(130, False), (256, True), (512, False)])
+@pytest.mark.parametrize("kind,align", [("even", 1), ("dropped", 128)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_linear_of_many_rows(dslib, k, tiles, kind, align, out):
+    """More rows than the device has SMs for tiles of half the width: by tiles of the whole width, aligned and not."""
+    tokens, top_k, experts, n = 5000, 2, 6, 256
+    r = _rng("many", k, kind, out)
+    order, want = _order(dslib, _ids(r, tokens, top_k, experts, kind), experts, align)
+    rows = r.standard_normal((order.rows, k))
+    rows[want[3] < 0] = 0
+    x, vx = _f8(dslib, rows)
+    w, vw = _f8(dslib, r.standard_normal((experts * n, k)) * k**-0.5, tiles)
+    y, size = X.linear(vx, vw.reshape(experts, n, k), want[0])
+    got = dslib.expert_linear_f8(x, w, order, dtype=TYPES[out])
+    _near(_np(got), y, HALF[out] * np.abs(y) + TOL * size + TINY[out])
+    for extra in (1, 2):
+        held = _strided(torch.full_like(got, 3.0), extra)
+        dslib.expert_linear_f8(x, w, order, out=held)
+        # tiles of another width sum in the same order: the same bits
+        assert torch.equal(held, got)
+    assert dslib.lib().ds_f8_fault_flag() == 0
+
+
+def test_weight_grad_of_many_tiles(dslib):
+    """More tiles than SMs, experts without rows among them, reductions of none to many blocks."""
+    tokens, experts, n, k = 1500, 40, 256, 512
+    r = _rng("tiles")
+    ids = np.minimum(r.geometric(0.12, (tokens, 2)) - 1, experts + 3).astype(np.int64)
+    order, want = _order(dslib, ids, experts, 128)
+    assert int((order.counts == 0).sum()) > 0
+    d = X.gather(r.standard_normal((tokens, n)) * 1e-3, want[3], 2)
+    x = X.gather(r.standard_normal((tokens, k)), want[3], 2)
+    for tiles in (True, False):
+        dt, vd = _f8(dslib, np.ascontiguousarray(d.T))
+        xt, vx = _f8(dslib, np.ascontiguousarray(x.T), tiles)
+        dw, size = X.weight_grad(vd, vx, want[0])
+        got = dslib.expert_weight_grad_f8(dt, xt, order)
+        _near(_np(got), dw, HALF["f32"] * np.abs(dw) + TOL * size + 1e-38)
+        add = torch.randn(got.shape, device="cuda")
+        both = dslib.expert_weight_grad_f8(dt, xt, order, add=add)
+        assert torch.equal(both, got + add)  # one rounding more, as the sum of the two
