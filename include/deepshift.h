@@ -753,7 +753,7 @@ ds_status ds_expert_combine_backward(const void* dout, int64_t ldd, const void* 
 /*
  * The products of the experts' parts, over 8-bit matrices as ds_linear_f8 takes them:
  *   y[r] = bias[e] + x[r] w_e^T     for the rows r of each segment e (gaps too: x holds zeros there)
- *   x     [rows][K], DS_F8_ROWS or DS_F8_TILES
+ *   x     [rows][K], DS_F8_ROWS (or DS_F8_TILES where align is a multiple of 128)
  *   w     [experts * N][K], w_e its rows [e N, (e + 1) N); in tiles only where N is a multiple of 128
  *   bias  device float32 [experts][N], contiguous, or NULL
  *   y     device [rows][N] of `type`; zeros from row offsets[experts] on

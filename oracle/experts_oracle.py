@@ -1,8 +1,6 @@
 """Numpy oracle of the experts' operators and of the optimizer step, from their definitions."""
 import numpy as np
 
-from .float8_oracle import dequantize  # noqa: F401
-
 
 def rows_needed(tokens, top_k, experts, align):
     """The largest number of rows that any choice of experts takes."""

@@ -1,12 +1,13 @@
 // Tokens in order of their expert, and back.
 //
 // ds_expert_order is a counting sort that keeps the order of equal keys, in
-// one launch: a cluster of up to eight CTAs, whose warps take consecutive
+// one launch: a cluster of up to 16 CTAs, whose warps take consecutive
 // ranges of the slots.  A warp counts its slots by expert in shared memory (32
 // at a time, those of one expert found by a match over the warp), the counts
 // are added up over warps, CTAs and experts, and a second pass over the ids
-// gives each slot its row.  It is bound by latency: 64 slots take 4.2 to 5.2 us,
-// 32768 of 32 experts 9.6, of which launch and cluster barriers are 5.7.
+// gives each slot its row.  It is bound by latency: 64 slots take 4.3 us, 32768
+// of 32 experts 7.3 (9.4 with eight CTAs), of which launch and cluster barriers
+// are 5.7.
 //
 // The other operators move rows and are bound by memory: a token's row is read
 // once and written to the rows of its slots; a token's sum reads its slots'
@@ -60,7 +61,8 @@ __device__ __forceinline__ int expert_of(const OrderParams& P, int64_t s, int64_
   return id >= 0 && id < P.experts ? id : -1;
 }
 
-constexpr int kHeld = 4;  // ids that a lane keeps from the first pass to the second
+constexpr int kHeld = 4;            // ids that a lane keeps from the first pass to the second
+constexpr uint32_t kMostCtas = 16;  // of a cluster
 
 // CLUSTER: more than one CTA.
 template <bool CLUSTER>
@@ -105,12 +107,12 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     cluster_arrive();
     cluster_wait();
     if (e < E) {
-      int c[8];
+      int c[kMostCtas];
 #pragma unroll
-      for (uint32_t r = 0; r < 8; ++r) c[r] = r < ranks ? load_of_rank(&total[e], r) : 0;
+      for (uint32_t r = 0; r < kMostCtas; ++r) c[r] = r < ranks ? load_of_rank(&total[e], r) : 0;
       count = 0;
 #pragma unroll
-      for (uint32_t r = 0; r < 8; ++r) {
+      for (uint32_t r = 0; r < kMostCtas; ++r) {
         if (r < rank) before += c[r];
         count += c[r];
       }
@@ -162,7 +164,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   for (int64_t s = from + 32 * kHeld; s < to; s += 32) place_32(s, expert_of(P, s + lane, to));
   // rows without a slot: behind each expert's, up to the next one's, and behind the last
   for (int x = (int)rank * warps + warp; x < E; x += (int)ranks * warps) {
-    const int64_t stop = ((int64_t)end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
+    const int64_t stop = ((uint32_t)end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
     for (int64_t r = end_of[x] + lane; r < stop && r < P.rows; r += 32) P.slot[r] = -1;
   }
   for (int64_t r = rows_used + (int64_t)rank * blockDim.x + threadIdx.x; r < P.rows; r += ranks * blockDim.x)
@@ -518,6 +520,21 @@ int unit_of(int64_t bytes, const Rows (&rows)[N]) {
   return 2;
 }
 
+// A cluster of so many CTAs; `at` has to live as long as the configuration.
+cudaLaunchConfig_t order_config(unsigned ctas, unsigned threads, size_t smem, cudaLaunchAttribute* at) {
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = ctas;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
 }  // namespace
 
 cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_slots& s, cudaStream_t st) {
@@ -528,6 +545,17 @@ cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_sl
                             : cudaFuncSetAttribute(order_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
   }();
   if (attr != cudaSuccess) return attr;
+  // CTAs of a cluster: 16 where the device takes so many of the largest size at once, else the portable 8
+  static const int most_ctas = [] {
+    cudaLaunchAttribute at[1];
+    cudaLaunchConfig_t cfg = order_config(kMostCtas, kOrderThreads, sizeof(int) * DS_EXPERTS_MAX * (kOrderWarps + 2), at);
+    int n = 0;
+    const bool takes =
+        cudaFuncSetAttribute(order_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&n, order_kernel<true>, &cfg) == cudaSuccess && n > 0;
+    if (!takes) cudaGetLastError();
+    return takes ? (int)kMostCtas : 8;
+  }();
   OrderParams p;
   p.ids = ids;
   p.offsets = s.offsets, p.counts = s.counts, p.position = s.position, p.slot = s.slot;
@@ -537,25 +565,16 @@ cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_sl
   int64_t threads = over(p.slots > p.experts ? p.slots : p.experts, 32) * 32;
   if (threads > kOrderThreads) threads = kOrderThreads;
   int ctas = 1;
-  while (ctas < 8 && p.slots > (int64_t)ctas * threads) ctas *= 2;
+  while (ctas < most_ctas && p.slots > (int64_t)ctas * threads) ctas *= 2;
   p.per_warp = over(over(p.slots, ctas * threads / 32), 32) * 32;
   const size_t smem = sizeof(int) * (size_t)p.experts * (size_t)(threads / 32 + 2);
   if (ctas == 1) {
     order_kernel<false><<<1, (unsigned)threads, smem, st>>>(p);
     return cudaGetLastError();
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
   cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)ctas;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cudaLaunchConfig_t cfg = order_config((unsigned)ctas, (unsigned)threads, smem, at);
+  cfg.stream = st;
   return cudaLaunchKernelEx(&cfg, order_kernel<true>, p);
 }
 
