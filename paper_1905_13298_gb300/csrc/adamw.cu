@@ -182,36 +182,41 @@ __device__ __forceinline__ uint64_t quotient2(uint64_t a, uint64_t b) {
   return fma2(fma2(minus, q, a), r, q);
 }
 
-// Two values in units of the scale, and for each `bits` = 16 * (16 random bits): to one of their e4m3 neighbours.
-// bits + 8 fills what three bits of a mantissa leave of 23, and carries into the upper neighbour.  Below 2^-6 the
-// neighbours are 2^-9 apart, as they are from 2^-6 to 2^-5, where u is moved for it.
+// Values in units of the scale to one of their e4m3 neighbours, with 16 random bits in `bits` (from bit 4 on): bits + 8
+// fills what three bits of a mantissa leave of 23, and carries into the upper neighbour.  For magnitudes from 2^-6 on.
+__device__ __forceinline__ uint32_t to_neighbour(float u, uint32_t bits) {
+  return (__float_as_uint(u) + bits + 8u) & 0xFFF00000u;
+}
+// The same for all magnitudes: below 2^-6 the neighbours are 2^-9 apart, as they are from 2^-6 to 2^-5, where u is moved
+// for it.
 template <bool SIGNED>
 __device__ __forceinline__ uint64_t to_neighbours(uint64_t u, uint32_t bits0, uint32_t bits1) {
   auto offset = [](float v) {
     const float off = SIGNED ? copysignf(0x1p-6f, v) : 0x1p-6f;
     return fabsf(v) < 0x1p-6f ? off : 0.f;
   };
-  auto round = [](float v, uint32_t bits) { return (__float_as_uint(v) + bits + 8u) & 0xFFF00000u; };
   const uint64_t off = pair(offset(lo_of(u)), offset(hi_of(u))), w = sum(u, off);
-  return difference(pair(round(lo_of(w), bits0), round(hi_of(w), bits1)), off);
+  return difference(pair(to_neighbour(lo_of(w), bits0), to_neighbour(hi_of(w), bits1)), off);
 }
 
-// Two values of a block to 8 bits; `random`: the hash of each but for its last step, which changes the low half only.
-// ODD: some of the block's values are not finite.
-template <bool ROOT, bool ODD>
-__device__ __forceinline__ uint32_t two_to_f8(uint64_t v, uint32_t random0, uint32_t random1, float inv) {
+// Two values of a block (in units of its scale) to 8 bits; `random`: the hash of each but for its last step, which
+// changes the low half only.  LARGE: none of the warp's magnitudes is below 2^-6, or not finite.
+template <bool ROOT, bool LARGE>
+__device__ __forceinline__ uint32_t two_to_f8(uint64_t u, uint32_t random0, uint32_t random1) {
   auto bits = [](uint32_t x) { return (ROOT ? x >> 12 : (x << 4) ^ (x >> 12)) & 0xFFFF0u; };
-  const uint64_t u = mul2(v, both(inv));
   float lo, hi;
-  unpair(to_neighbours<!ROOT>(u, bits(random0), bits(random1)), lo, hi);
-  if (ROOT) {  // u > 0 is above 2^-136
-    const uint64_t large = mul2(u, both(0x1p127f));
-    lo = fmaxf(lo, fminf(lo_of(large), 0x1p-9f));
-    hi = fmaxf(hi, fminf(hi_of(large), 0x1p-9f));
-  }
-  if (ODD) {
-    if (!(fabsf(lo_of(v)) < kInf)) lo = __uint_as_float(0x7FC00000u);
-    if (!(fabsf(hi_of(v)) < kInf)) hi = __uint_as_float(0x7FC00000u);
+  if (LARGE) {
+    lo = __uint_as_float(to_neighbour(lo_of(u), bits(random0)));
+    hi = __uint_as_float(to_neighbour(hi_of(u), bits(random1)));
+  } else {
+    unpair(to_neighbours<!ROOT>(u, bits(random0), bits(random1)), lo, hi);
+    if (ROOT) {  // u > 0 is above 2^-136
+      const uint64_t large = mul2(u, both(0x1p127f));
+      lo = fmaxf(lo, fminf(lo_of(large), 0x1p-9f));
+      hi = fmaxf(hi, fminf(hi_of(large), 0x1p-9f));
+    }
+    if (!(fabsf(lo_of(u)) < kInf)) lo = __uint_as_float(0x7FC00000u);
+    if (!(fabsf(hi_of(u)) < kInf)) hi = __uint_as_float(0x7FC00000u);
   }
   return f8x2<false>(lo, hi);
 }
@@ -226,6 +231,13 @@ __device__ __forceinline__ float top8(const uint64_t v[4]) {
   t = max3_abs(t, hi_of(v[1]), lo_of(v[2]));
   t = max3_abs(t, hi_of(v[2]), lo_of(v[3]));
   return max3_abs(t, hi_of(v[3]), 0.f);
+}
+// The least magnitude of eight; NaN where one is.
+__device__ __forceinline__ float least8(const uint64_t v[4]) {
+  float t = __uint_as_float(0x7F800000u);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) asm("min.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(t) : "f"(t), "f"(lo_of(v[k])), "f"(hi_of(v[k])));
+  return t;
 }
 __device__ __forceinline__ float finite_top8(const uint64_t v[4]) {
   float t = 0.f;
@@ -384,36 +396,47 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
     float top_m = top16(top8(m)), top_v = top16(top8(root));
     const bool fast = top_m * rate <= 0x1p60f && top_v < kInf && top_v * root_factor <= 0x1p59f && f.eps >= 0x1p-60f &&
                       f.eps <= 0x1p59f;
-    auto states = [&](auto odd) {
+    auto states = [&] {
       const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
-      uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key, a[4], b[4];
-      auto random = [&] {
-        uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
-        x = (x ^ (x >> 15)) * 0xB7E15163u;
-        x0 += 0x9E3779B1u;
-        return x;
-      };
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t x = random(), y = random();
-        a[k] = two_to_f8<false, decltype(odd)::value>(m[k], x, y, s_m.inv);
-        b[k] = two_to_f8<true, decltype(odd)::value>(root[k], x, y, s_v.inv);
+        m[k] = mul2(m[k], both(s_m.inv));
+        root[k] = mul2(root[k], both(s_v.inv));
       }
-      qm = make_uint2(a[0] | a[1] << 16, a[2] | a[3] << 16);
-      qv = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+      auto round = [&](auto large) {
+        uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key, a[4], b[4];
+        auto random = [&] {
+          uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
+          x = (x ^ (x >> 15)) * 0xB7E15163u;
+          x0 += 0x9E3779B1u;
+          return x;
+        };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t x = random(), y = random();
+          a[k] = two_to_f8<false, decltype(large)::value>(m[k], x, y);
+          b[k] = two_to_f8<true, decltype(large)::value>(root[k], x, y);
+        }
+        qm = make_uint2(a[0] | a[1] << 16, a[2] | a[3] << 16);
+        qv = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+      };
+      // most warps hold no value below the format's smallest normal one
+      if (__all_sync(0xFFFFFFFFu, fast && fminf(least8(m), least8(root)) >= 0x1p-6f))
+        round(std::true_type());
+      else
+        round(std::false_type());
       sm = s_m.s;
       sv = s_v.s;
     };
     if (__all_sync(0xFFFFFFFFu, fast)) {
       update(std::true_type());
-      states(std::false_type());
     } else {  // values that are not finite, or far from what training meets
       root_any();
       update(std::false_type());
       top_m = top16(finite_top8(m));
       top_v = top16(finite_top8(root));
-      states(std::true_type());
     }
+    states();
   } else {
     root_any();
     update(std::false_type());
