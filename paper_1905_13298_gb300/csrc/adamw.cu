@@ -152,22 +152,17 @@ __device__ __forceinline__ float max3_abs(float a, float b, float c) {
   return r;
 }
 
-// Square roots of two values, correctly rounded, for 0 and from 2^-149 to 2^67; NaN above that.  An approximate
-// reciprocal root y of the values in units of 2^-60 gives the root g and half its reciprocal h; one step by their
-// residual 1/2 - g h, then one by the root's own residual v - g^2, which is exact (P. Markstein, IBM J. Res. Dev. 34 (1),
-// 1990).  The same as __fsqrt_rn for all mantissas of two neighbouring exponents, and so for all of these numbers.
+// Square roots of two values, correctly rounded, for 0 and from 2^-149 to 2^67; NaN above that.  With an approximate
+// reciprocal root y of the values u in units of 2^-60, g = u y and one correction by the root's residual u - g^2, which is
+// exact (P. Markstein, IBM J. Res. Dev. 34 (1), 1990).  Equal to __fsqrt_rn: compared for all of these numbers.
 __device__ __forceinline__ uint64_t root2(uint64_t v) {
   const uint64_t from = fma2(v, both(0x1p60f), both(0x1p-126f));  // changes 0 only
   float y0, y1;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo_of(from)));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi_of(from)));
-  // the negatives of u and g are what the residuals need
-  const uint64_t y = pair(y0, y1), u = mul2(v, both(-0x1p60f));
-  const uint64_t g = mul2(u, y), h = mul2(y, both(0.5f));
-  const uint64_t t = fma2(g, h, both(0.5f));
-  const uint64_t g1 = fma2(g, t, g), h1 = fma2(h, t, h);
-  const uint64_t d = fma2(g1, g1, u);
-  return mul2(fma2(d, h1, g1), both(-0x1p-30f));
+  // the negatives of u and g, which the residual needs
+  const uint64_t y = pair(y0, y1), u = mul2(v, both(-0x1p60f)), g = mul2(u, y);
+  return mul2(fma2(fma2(g, g, u), mul2(y, both(0.5f)), g), both(-0x1p-30f));
 }
 // Quotients a / b, correctly rounded, for b from 2^-60 to 2^60 and a up to 2^60, where they are 0 or normal and a is not
 // below 2^-102 (there the last place may be off): a quotient of one step by the correctly rounded reciprocal and its
@@ -251,9 +246,9 @@ __device__ __forceinline__ float rest_of_power(double log_beta, int64_t t) {
   return -expm1f((float)((double)t * log_beta));
 }
 
-// With 8-bit states arithmetic takes as long as memory, 690 instructions for eight values of 32 threads: 48 warps of an SM
+// With 8-bit states arithmetic takes as long as memory, 650 instructions for eight values of 32 threads: 48 warps of an SM
 // hide its latency best, although 40 registers are a few too little (9 tensors of 50 M values, 16-bit gradients and
-// copies: 144 us or 5.6 TB/s; 158 with 40 warps and 48 registers, 164 with 32 warps and 64).  Copies of the next values
+// copies: 133 us or 6.1 TB/s; 143 with 40 warps and 48 registers, 149 with 32 warps and 64).  Copies of the next values
 // through shared memory meanwhile, and factors kept as pairs in the parameters, gained nothing.
 template <bool F8, int N>
 __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __grid_constant__ Params<N> P) {
