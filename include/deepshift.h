@@ -821,8 +821,8 @@ typedef struct ds_adamw_options {
 /*
  * Updates `count` tensors (a host array, read during the call): p, m, v, their
  * scales and copy in place.  The tensors' memories are contiguous, aligned to
- * their type (16 bytes take the vector path), and apart from each other; all
- * states are of one kind.  n = 0 is accepted.  One launch for up to 400
+ * their type (eight values take the vector path), and apart from each other;
+ * all states are of one kind.  n = 0 is accepted.  One launch for up to 400
  * tensors.  Errors: DS_ERR_INVALID_ARG (NULL, a type, betas outside [0, 1),
  * step below 1, overlap), DS_ERR_SHAPE, DS_ERR_ALIGNMENT, DS_ERR_UNSUPPORTED
  * (n above 2^40).

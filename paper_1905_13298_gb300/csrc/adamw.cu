@@ -3,8 +3,9 @@
 //
 // The work is one pass over memory: 28 bytes a value with float32 throughout
 // and 16-bit gradients and copies, 16 with 8-bit states.  With float32 states
-// it runs at the rate of a copy (50 M values 203 us).  A CTA takes 1024
-// consecutive values of one tensor, a thread eight of them, all of whose loads
+// it runs at the rate of a copy (50 M values 203 us; 216 where tensors are not
+// aligned, 133 and 192 with 8-bit states).  A CTA takes 1024 consecutive values
+// of one tensor, a thread eight of them, all of whose loads
 // are on their way before the first is used.  The tensors' addresses are in
 // the kernel's parameters: nothing is copied to the device before a step, and
 // a captured step is replayed with them.
@@ -34,7 +35,7 @@ struct Tensor {
   float decay;      // 1 - lr * weight_decay, or weight_decay where lr is on the device
   uint32_t number;  // in the call
   int8_t p_type, g_type, copy_type;
-  int8_t level;     // the accesses of eight values that all its addresses allow: 2 (32 bytes), 1 (16), 0
+  int8_t aligned;   // all its addresses are multiples of eight values
 };
 
 struct Factors {
@@ -55,35 +56,42 @@ struct Params {
 };
 static_assert(sizeof(Params<kFew>) <= 4096 && sizeof(Params<kMany>) <= 32764, "kernel parameters");
 
-// Eight consecutive values as they lie in memory, of a type known at run time: the same branch for a whole CTA.  They
-// are taken apart only after all arrays' loads have been issued.
+// A thread's eight values as they lie in memory, of a type known at run time: the same branch for a whole CTA.  They are
+// taken apart only after all arrays' loads have been issued.
 struct Raw {
   uint32_t r[8];
 };
-__device__ __forceinline__ void load_raw(Raw& o, const void* base, int type, int64_t i, int n, int level) {
+// Where they lie: eight in a row from `first` (STEP = 1), all of them there and their addresses multiples of the access,
+// or every 16th (STEP = 16) while they exist: 16 threads then read one value each of 16 in a row, at any address.  Either
+// way these threads hold 128 in a row, a block of the 8-bit states.
+template <int STEP>
+struct Place {
+  int64_t first, end;
+  __device__ __forceinline__ bool has(int k) const { return STEP == 1 || first + STEP * k < end; }
+};
+template <int STEP>
+__device__ __forceinline__ void load_raw(Raw& o, const void* base, int type, const Place<STEP>& at) {
   if (type == DS_TYPE_F32) {
-    const float* p = static_cast<const float*>(base) + i;
-    if (level == 2 && n == 8) {
+    const float* p = static_cast<const float*>(base) + at.first;
+    if constexpr (STEP == 1) {
       asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(o.r[0]), "=r"(o.r[1]), "=r"(o.r[2]), "=r"(o.r[3]), "=r"(o.r[4]), "=r"(o.r[5]), "=r"(o.r[6]),
                      "=r"(o.r[7])
                    : "l"(p));
-    } else if (level >= 1 && n == 8) {
-      const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
-      o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w, o.r[4] = b.x, o.r[5] = b.y, o.r[6] = b.z, o.r[7] = b.w;
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o.r[k] = k < n ? __float_as_uint(p[k]) : 0u;
+      for (int k = 0; k < 8; ++k) o.r[k] = at.has(k) ? __float_as_uint(p[STEP * k]) : 0u;
     }
   } else {
-    const uint16_t* p = static_cast<const uint16_t*>(base) + i;
-    if (level >= 1 && n == 8) {
+    const uint16_t* p = static_cast<const uint16_t*>(base) + at.first;
+    if constexpr (STEP == 1) {
       const uint4 a = *reinterpret_cast<const uint4*>(p);
       o.r[0] = a.x, o.r[1] = a.y, o.r[2] = a.z, o.r[3] = a.w;
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        o.r[k] = (2 * k < n ? p[2 * k] : 0u) | (2 * k + 1 < n ? (uint32_t)p[2 * k + 1] << 16 : 0u);
+        o.r[k] = (at.has(2 * k) ? p[STEP * 2 * k] : 0u) |
+                 (at.has(2 * k + 1) ? (uint32_t)p[STEP * (2 * k + 1)] << 16 : 0u);
     }
   }
 }
@@ -99,41 +107,51 @@ __device__ __forceinline__ void get_raw(const Raw& o, int type, float v[8]) {
     for (int k = 0; k < 4; ++k) unpack2(o.r[k], v[2 * k], v[2 * k + 1], (const __half*)nullptr);
   }
 }
-__device__ __forceinline__ void store_values(void* base, int type, int64_t i, int n, int level, const float v[8]) {
-  if (type == DS_TYPE_F32) {
-    float* p = static_cast<float*>(base) + i;
-    if (level == 2 && n == 8) {
-      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
-                   "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
-                   : "memory");
-    } else {
-      store8<false>(p, n, level >= 1, v);
-    }
-  } else if (type == DS_TYPE_BF16) {
-    store8<false>(static_cast<__nv_bfloat16*>(base) + i, n, level >= 1, v);
+template <int STEP, typename T>
+__device__ __forceinline__ void store_values_as(T* p, const Place<STEP>& at, const float v[8]) {
+  p += at.first;
+  if constexpr (STEP != 1) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (at.has(k)) from_float(v[k], p[STEP * k]);
+  } else if constexpr (sizeof(T) == 4) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+                 "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
   } else {
-    store8<false>(static_cast<__half*>(base) + i, n, level >= 1, v);
+    store8<false>(p, 8, true, v);
   }
 }
+template <int STEP>
+__device__ __forceinline__ void store_values(void* base, int type, const Place<STEP>& at, const float v[8]) {
+  if (type == DS_TYPE_F32)
+    store_values_as(static_cast<float*>(base), at, v);
+  else if (type == DS_TYPE_BF16)
+    store_values_as(static_cast<__nv_bfloat16*>(base), at, v);
+  else
+    store_values_as(static_cast<__half*>(base), at, v);
+}
 
-// Eight 8-bit values (level >= 1: 8-byte aligned), the missing ones zero.
-__device__ __forceinline__ uint2 load_bytes(const void* base, int64_t i, int n, int level) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
-  if (level >= 1 && n == 8) return *reinterpret_cast<const uint2*>(p);
+// Eight 8-bit values, the missing ones zero.
+template <int STEP>
+__device__ __forceinline__ uint2 load_bytes(const void* base, const Place<STEP>& at) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + at.first;
+  if constexpr (STEP == 1) return *reinterpret_cast<const uint2*>(p);
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    if (k < n) w[k >> 2] |= (uint32_t)p[k] << (8 * (k & 3));
+    if (at.has(k)) w[k >> 2] |= (uint32_t)p[STEP * k] << (8 * (k & 3));
   return make_uint2(w[0], w[1]);
 }
-__device__ __forceinline__ void store_bytes(void* base, int64_t i, int n, int level, uint2 q) {
-  uint8_t* p = static_cast<uint8_t*>(base) + i;
-  if (level >= 1 && n == 8) {
+template <int STEP>
+__device__ __forceinline__ void store_bytes(void* base, const Place<STEP>& at, uint2 q) {
+  uint8_t* p = static_cast<uint8_t*>(base) + at.first;
+  if constexpr (STEP == 1) {
     *reinterpret_cast<uint2*>(p) = q;
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = (uint8_t)((k < 4 ? q.x >> (8 * k) : q.y >> (8 * (k - 4))) & 0xFFu);
+      if (at.has(k)) p[STEP * k] = (uint8_t)((k < 4 ? q.x >> (8 * k) : q.y >> (8 * (k - 4))) & 0xFFu);
   }
 }
 
@@ -261,32 +279,35 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
       hi = mid - 1;
   }
   const Tensor& T = P.t[lo];
-  const int64_t i = (int64_t)(blockIdx.x - T.first) * kSpan + threadIdx.x * kEach;
-  const int n = left8(T.n, i);
+  const int64_t base = (int64_t)(blockIdx.x - T.first) * kSpan;
   // the same for a whole CTA: one branch around all the loads and one around all the stores
-  const bool full = T.level == 2 && T.n - (int64_t)(blockIdx.x - T.first) * kSpan >= kSpan;
+  const bool full = T.aligned && T.n - base >= kSpan;
+  const Place<1> row{base + threadIdx.x * kEach, T.n};
+  const Place<16> spread{base + (threadIdx.x & ~15) * kEach + (threadIdx.x & 15), T.n};
+  const int64_t block = base / kF8Block + (threadIdx.x >> 4);
+  const bool some = block * kF8Block < T.n;
   struct {
     Raw p, g, m, v;
     uint2 qm, qv;
     float sm, sv;
   } in;
-  auto load = [&](int n, int level) {
-    load_raw(in.g, T.g, T.g_type, i, n, level);
+  auto load = [&](const auto& at) {
+    load_raw(in.g, T.g, T.g_type, at);
     if constexpr (F8) {
-      in.qm = load_bytes(T.m, i, n, level);
-      in.qv = load_bytes(T.v, i, n, level);
-      in.sm = n > 0 ? T.m_scale[i / kF8Block] : 0.f;
-      in.sv = n > 0 ? T.v_scale[i / kF8Block] : 0.f;
+      in.qm = load_bytes(T.m, at);
+      in.qv = load_bytes(T.v, at);
+      in.sm = some ? T.m_scale[block] : 0.f;
+      in.sv = some ? T.v_scale[block] : 0.f;
     } else {
-      load_raw(in.m, T.m, DS_TYPE_F32, i, n, level);
-      load_raw(in.v, T.v, DS_TYPE_F32, i, n, level);
+      load_raw(in.m, T.m, DS_TYPE_F32, at);
+      load_raw(in.v, T.v, DS_TYPE_F32, at);
     }
-    load_raw(in.p, T.p, T.p_type, i, n, level);
+    load_raw(in.p, T.p, T.p_type, at);
   };
   if (full)
-    load(8, 2);
+    load(row);
   else
-    load(n, T.level);
+    load(spread);
 
   const Factors& f = P.f;
   float rate = f.rate, root_factor = f.root, decay = T.decay;
@@ -363,27 +384,27 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
         q = pair(__fdiv_rn(lo_of(up), lo_of(under)), __fdiv_rn(hi_of(up), hi_of(under)));
       p[k] = difference(product(p[k], both(decay)), q);
     }
-    auto store = [&](int n, int level) {
+    auto store = [&](const auto& at) {
       float each[8];
       values(p, each);
-      store_values(T.p, T.p_type, i, n, level, each);
-      if (T.copy) store_values(T.copy, T.copy_type, i, n, level, each);
+      store_values(T.p, T.p_type, at, each);
+      if (T.copy) store_values(T.copy, T.copy_type, at, each);
     };
     if (full)
-      store(8, 2);
+      store(row);
     else
-      store(n, T.level);
+      store(spread);
   };
   uint2 qm, qv;
-  float sm, sv;
+  float sm = 0.f, sv = 0.f;
   if constexpr (F8) {
     const uint32_t key = step * 0xBB67AE85u + T.number * 0x6A09E667u + f.seed;
 #pragma unroll
     for (int k = 0; k < 4; ++k) root[k] = root2(v[k]);
-    if (n < 8) {  // values that do not exist add nothing to a block
+    if (!full) {  // values that do not exist add nothing to a block
 #pragma unroll
       for (int k = 0; k < 8; ++k)
-        if (k >= n) {
+        if (!spread.has(k)) {
           const uint64_t keep = k & 1 ? 0xFFFFFFFFull : 0xFFFFFFFFull << 32;
           m[k / 2] &= keep, v[k / 2] &= keep, root[k / 2] &= keep;
         }
@@ -399,11 +420,12 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
         root[k] = mul2(root[k], both(s_v.inv));
       }
       auto round = [&](auto large) {
-        uint32_t x0 = (uint32_t)i * 0x9E3779B1u + key, a[4], b[4];
+        const uint32_t step = full ? 0x9E3779B1u : 16u * 0x9E3779B1u;
+        uint32_t x0 = (uint32_t)(full ? row.first : spread.first) * 0x9E3779B1u + key, a[4], b[4];
         auto random = [&] {
           uint32_t x = (x0 ^ (x0 >> 16)) * 0x243F6A89u;
           x = (x ^ (x >> 15)) * 0xB7E15163u;
-          x0 += 0x9E3779B1u;
+          x0 += step;
           return x;
         };
 #pragma unroll
@@ -436,26 +458,26 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
     root_any();
     update(std::false_type());
   }
-  auto store = [&](int n, int level) {
+  auto store = [&](const auto& at) {
     if constexpr (F8) {
-      store_bytes(T.m, i, n, level, qm);
-      store_bytes(T.v, i, n, level, qv);
-      if ((threadIdx.x & 15) == 0 && n > 0) {
-        T.m_scale[i / kF8Block] = sm;
-        T.v_scale[i / kF8Block] = sv;
-      }
+      store_bytes(T.m, at, qm);
+      store_bytes(T.v, at, qv);
     } else {
       float each[8];
       values(m, each);
-      store_values(T.m, DS_TYPE_F32, i, n, level, each);
+      store_values(T.m, DS_TYPE_F32, at, each);
       values(v, each);
-      store_values(T.v, DS_TYPE_F32, i, n, level, each);
+      store_values(T.v, DS_TYPE_F32, at, each);
     }
   };
   if (full)
-    store(8, 2);
+    store(row);
   else
-    store(n, T.level);
+    store(spread);
+  if (F8 && (threadIdx.x & 15) == 0 && some) {
+    T.m_scale[block] = sm;
+    T.v_scale[block] = sv;
+  }
 }
 
 template <int N>
@@ -557,16 +579,13 @@ ds_status adamw(const ds_adamw_tensor* tensors, int count, const ds_adamw_option
     if (!aligned(t.p, ps) || !aligned(t.g, gs) || !aligned(t.m, ss) || !aligned(t.v, ss) || !aligned(t.copy, cs) ||
         !aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))
       return fail(DS_ERR_ALIGNMENT, "tensor %d: memory is not aligned to its type", k);
-    auto level = [](const void* p, int64_t size) {
-      return size == 4 ? (aligned(p, 32) ? 2 : (aligned(p, 16) ? 1 : 0)) : (aligned(p, 8 * size) ? 2 : 0);
-    };
-    int lv = level(t.p, ps);
-    for (int x : {level(t.g, gs), level(t.m, ss), level(t.v, ss), t.copy ? level(t.copy, cs) : 2}) lv = x < lv ? x : lv;
     Tensor d = {};
     d.p = t.p, d.g = t.g, d.m = t.m, d.v = t.v, d.m_scale = t.m_scale, d.v_scale = t.v_scale, d.copy = t.copy, d.n = t.n;
     d.decay = o->lr_dev || o->step_dev ? t.weight_decay : (float)(1.0 - o->lr * (double)t.weight_decay);
     d.number = (uint32_t)k;
-    d.p_type = (int8_t)t.p_type, d.g_type = (int8_t)t.g_type, d.copy_type = (int8_t)t.copy_type, d.level = (int8_t)lv;
+    d.p_type = (int8_t)t.p_type, d.g_type = (int8_t)t.g_type, d.copy_type = (int8_t)t.copy_type;
+    d.aligned = aligned(t.p, 8 * ps) && aligned(t.g, 8 * gs) && aligned(t.m, 8 * ss) && aligned(t.v, 8 * ss) &&
+                aligned(t.copy, 8 * cs);
     all.push_back(d);
     auto piece = [&](int kind, const void* p, int64_t bytes, bool written) {
       if (!p) return;
