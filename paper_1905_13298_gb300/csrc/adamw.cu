@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(kThreads, F8 ? 12 : 8) adamw_kernel(const __gr
       const F8Scale s_m = f8_scale<false>(top_m, false), s_v = f8_scale<false>(top_v, false);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        m[k] = mul2(m[k], both(s_m.inv));
-        root[k] = mul2(root[k], both(s_v.inv));
+        m[k] = product(m[k], both(s_m.inv));  // a sum may follow, in to_neighbours
+        root[k] = product(root[k], both(s_v.inv));
       }
       auto round = [&](auto large) {
         const uint32_t step = full ? 0x9E3779B1u : 16u * 0x9E3779B1u;

@@ -222,7 +222,7 @@ __device__ __forceinline__ const U* unit_at(const void* base, int64_t r, int64_t
 
 constexpr int kZeroRows = 2;  // rows of a warp that looks for rows without a slot
 
-// The first rows of which `rows` from r0 on hold no slot, as bits.
+// Which of the kZeroRows rows from r0 on hold no slot, as bits; there are `rows` in all.
 __device__ __forceinline__ uint32_t rows_without(const int32_t* slot, int64_t r0, int64_t rows) {
   const int lane = threadIdx.x & 31;
   const int64_t r = r0 + lane;

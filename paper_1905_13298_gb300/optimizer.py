@@ -6,6 +6,8 @@
 """
 from __future__ import annotations
 
+from numbers import Real
+
 import torch
 
 from . import DsError, _check, ds_adamw_options, ds_adamw_tensor, lib
@@ -63,7 +65,7 @@ class AdamW:
         self.m = [zeros(p.numel()) for p in self.params] if m is None else list(m)
         self.v = [zeros(p.numel()) for p in self.params] if v is None else list(v)
         self.copies = None if copies is None else list(copies)
-        decay = [weight_decay] * count if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        decay = [weight_decay] * count if isinstance(weight_decay, Real) else list(weight_decay)
         for name, x in (("grads", self.grads), ("m", self.m), ("v", self.v), ("weight_decay", decay),
                         ("copies", self.copies)):
             if x is not None and len(x) != count:
@@ -84,6 +86,7 @@ class AdamW:
             if self.copies is not None and self.copies[k] is not None:
                 c = self.copies[k]
                 d.copy, d.copy_type = _flat(c, f"copies[{k}]", n, _TYPES, device), _TYPES[c.dtype]
+        self._states = [*self.m, *self.v, *(self.copies or [])]  # their memory stays, whatever becomes of the lists
         self._take(self.grads)
         self._hold()
         self.lr, self.betas, self.eps, self.grad_scale, self.steps, self.seed = lr, betas, eps, grad_scale, steps, seed

@@ -287,3 +287,14 @@ def test_refusals_on_a_gpu(dslib):
         opt.step()
     shared = dslib.AdamW([torch.ones(100, device="cuda"), torch.ones(100, device="cuda")], [g, g])  # reading twice is fine
     shared.step()
+
+
+def test_memory_of_replaced_states_stays(dslib):
+    """A step writes the states that the optimizer was made with, also where its lists were given others since."""
+    p, g = torch.ones(70_000, device="cuda"), torch.full((70_000,), 1e-3, device="cuda")
+    opt = dslib.AdamW([p], [g])
+    held = opt.m[0]
+    opt.m[0], opt.v[0] = None, None
+    over = [torch.full((70_000,), 7.0, device="cuda") for _ in range(4)]
+    opt.step()
+    assert all(bool((t == 7).all()) for t in over) and bool((held != 0).all())
