@@ -12,7 +12,7 @@
 #include <math.h>
 
 #include <algorithm>
-#include <new>
+#include <exception>
 #include <type_traits>
 #include <vector>
 
@@ -631,7 +631,7 @@ extern "C" ds_status ds_adamw(const ds_adamw_tensor* tensors, int count, const d
   ds::clear_error();
   try {
     return ds::adamw(tensors, count, options, static_cast<cudaStream_t>(stream));
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {
     return ds::fail(DS_ERR_UNSUPPORTED, "no host memory for the list of %d tensors", count);
   }
 }

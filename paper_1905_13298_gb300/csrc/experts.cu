@@ -61,7 +61,7 @@ __device__ __forceinline__ int expert_of(const OrderParams& P, int64_t s, int64_
   return id >= 0 && id < P.experts ? id : -1;
 }
 
-constexpr int kHeld = 4;            // ids that a lane keeps from the first pass to the second
+constexpr int kHeld = 8;            // ids of a lane on their way at once; the first ones are kept for the second pass
 constexpr uint32_t kMostCtas = 16;  // of a cluster
 
 // CLUSTER: more than one CTA.
@@ -80,8 +80,11 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   const int64_t from = ((int64_t)rank * warps + warp) * P.per_warp;
   const int64_t to = from + P.per_warp < P.slots ? from + P.per_warp : P.slots;
   int held[kHeld];
+  auto load = [&](int64_t s, int (&ids)[kHeld]) {
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) held[k] = expert_of(P, from + 32 * k + lane, to);
+    for (int k = 0; k < kHeld; ++k) ids[k] = expert_of(P, s + 32 * k + lane, to);
+  };
+  load(from, held);
   for (int e = lane; e < E; e += 32) mine[e] = 0;
   __syncwarp();
   auto count_32 = [&](int e) {
@@ -89,10 +92,17 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
     __syncwarp();
   };
+  auto count = [&](int64_t s, const int (&ids)[kHeld]) {
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (from + 32 * k < to) count_32(held[k]);
-  for (int64_t s = from + 32 * kHeld; s < to; s += 32) count_32(expert_of(P, s + lane, to));
+    for (int k = 0; k < kHeld; ++k)
+      if (s + 32 * k < to) count_32(ids[k]);
+  };
+  count(from, held);
+  for (int64_t s = from + 32 * kHeld; s < to; s += 32 * kHeld) {
+    int ids[kHeld];
+    load(s, ids);
+    count(s, ids);
+  }
   __syncthreads();
   // a thread per expert (there are at most as many)
   const int e = threadIdx.x;
@@ -101,7 +111,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
 #pragma unroll 8
     for (int w = 0; w < warps; ++w) here += hist[w * E + e];
   }
-  int before = 0, count = here;  // slots of the CTAs before this one, and of all
+  int before = 0, all = here;  // slots of the CTAs before this one, and of all
   if constexpr (CLUSTER) {
     if (e < E) total[e] = here;
     cluster_arrive();
@@ -110,17 +120,17 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
       int c[kMostCtas];
 #pragma unroll
       for (uint32_t r = 0; r < kMostCtas; ++r) c[r] = r < ranks ? load_of_rank(&total[e], r) : 0;
-      count = 0;
+      all = 0;
 #pragma unroll
       for (uint32_t r = 0; r < kMostCtas; ++r) {
         if (r < rank) before += c[r];
-        count += c[r];
+        all += c[r];
       }
     }
     __syncwarp();
     cluster_arrive();  // the other CTAs' counts have been read
   }
-  const int room = (int)(((uint32_t)count + P.align - 1) / P.align * P.align);
+  const int room = (int)(((uint32_t)all + P.align - 1) / P.align * P.align);
   int sum = room;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -139,9 +149,9 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
       hist[w * E + e] = at;
       at += c;
     }
-    end_of[e] = start + count;
+    end_of[e] = start + all;
     if (rank == 0) {
-      P.counts[e] = count;
+      P.counts[e] = all;
       P.offsets[e + 1] = start + room;
       if (e == 0) P.offsets[0] = 0;
     }
@@ -158,10 +168,17 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
     if (s + lane < to) P.position[s + lane] = row;
     if (row >= 0 && row < P.rows) P.slot[row] = (int32_t)(s + lane);
   };
+  auto place = [&](int64_t s, const int (&ids)[kHeld]) {
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (from + 32 * k < to) place_32(from + 32 * k, held[k]);
-  for (int64_t s = from + 32 * kHeld; s < to; s += 32) place_32(s, expert_of(P, s + lane, to));
+    for (int k = 0; k < kHeld; ++k)
+      if (s + 32 * k < to) place_32(s + 32 * k, ids[k]);
+  };
+  place(from, held);
+  for (int64_t s = from + 32 * kHeld; s < to; s += 32 * kHeld) {
+    int ids[kHeld];
+    load(s, ids);
+    place(s, ids);
+  }
   // rows without a slot: behind each expert's, up to the next one's, and behind the last
   for (int x = (int)rank * warps + warp; x < E; x += (int)ranks * warps) {
     const int64_t stop = ((uint32_t)end_of[x] + P.align - 1) / P.align * P.align;  // segments start at multiples
@@ -375,20 +392,24 @@ struct CombineBackwardParams {
   int top_k;
 };
 
-// A warp goes through a token's row; with slots in groups of AT_ONCE, the row of dout is read once for each group.
-template <typename T, int BYTES, int AT_ONCE>
-__global__ void __launch_bounds__(kThreads) combine_backward_kernel(const CombineBackwardParams P) {
+constexpr int kMostShare = 16;  // warps of a token
+
+// A warp goes through a token's row, or (SHARED) all of a CTA's warps through parts of it in turn, where tokens are few;
+// with slots in groups of AT_ONCE, the row of dout is read once for each group.
+template <typename T, int BYTES, int AT_ONCE, bool SHARED>
+__global__ void __launch_bounds__(SHARED ? 32 * kMostShare : kThreads)
+    combine_backward_kernel(const CombineBackwardParams P) {
   using U = Unit<T, BYTES>;
   constexpr int N = units_of(BYTES);
-  const int lane = threadIdx.x & 31;
-  const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (id >= P.tokens) {
-    const int64_t r0 = (id - P.tokens) * kZeroRows;
+  __shared__ float part[SHARED ? kMostShare : 1][AT_ONCE];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = SHARED ? (int)(blockDim.x >> 5) : 1;
+  const int64_t t = SHARED ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWarps + warp;
+  if (t >= P.tokens) {
+    const int64_t r0 = (SHARED ? (t - P.tokens) * share + warp : t - P.tokens) * kZeroRows;
     for (uint32_t todo = rows_without(P.slot, r0, P.rows); todo; todo &= todo - 1)
       for (int64_t u = lane; u < P.units; u += 32) *unit_at<U>(P.dy, r0 + __ffs(todo) - 1, P.lddy, u) = U{};
     return;
   }
-  const int64_t t = id;
   for (int j0 = 0; j0 < P.top_k; j0 += AT_ONCE) {
     int32_t at = -1;
     float w = 1.f;
@@ -406,7 +427,7 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(const Combin
       dot[j] = 0.f;
     }
     // N units of all rows are loaded before the first is stored, which may be where y lies
-    for (int64_t u0 = lane; u0 < P.units; u0 += 32 * N) {
+    for (int64_t u0 = (SHARED ? warp * (32 * N) : 0) + lane; u0 < P.units; u0 += share * (32 * N)) {
       U rd[N], ry[AT_ONCE][N];
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -446,7 +467,20 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(const Combin
       for (int j = 0; j < AT_ONCE; ++j) {
 #pragma unroll
         for (int x = 16; x >= 1; x >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], x);
-        if (lane == j && j0 + j < P.top_k) P.dweights[t * P.top_k + j0 + j] = dot[j];
+        if constexpr (SHARED) {
+          if (lane == j) part[warp][j] = dot[j];
+        } else {
+          if (lane == j && j0 + j < P.top_k) P.dweights[t * P.top_k + j0 + j] = dot[j];
+        }
+      }
+      if constexpr (SHARED) {  // the warps' parts in their order
+        __syncthreads();
+        if (threadIdx.x < AT_ONCE && j0 + (int)threadIdx.x < P.top_k) {
+          float sum = 0.f;
+          for (int w = 0; w < share; ++w) sum += part[w][threadIdx.x];
+          P.dweights[t * P.top_k + j0 + threadIdx.x] = sum;
+        }
+        __syncthreads();
       }
     }
   }
@@ -476,9 +510,18 @@ cudaError_t launch_combine(CombineParams& p, cudaStream_t st) {
 }
 template <typename T, int BYTES, int AT_ONCE>
 cudaError_t launch_combine(CombineBackwardParams& p, cudaStream_t st) {
-  const int64_t ctas = over(p.tokens + over(p.rows, kZeroRows), kWarps);
+  // Warps of a token while the device is not full of tokens' warps, at least two rounds through the row for each (16 x 8
+  // slots of 16384 bf16 8.8 us, 46 with one warp; 512 x 8 51, 130)
+  const int64_t room = 32 * (int64_t)(sm_count() > 0 ? sm_count() : 1), rounds = over(p.units, 32 * units_of(BYTES));
+  int share = 1;
+  while (share < kMostShare && 2 * share * p.tokens <= room && 4 * share <= rounds) share *= 2;
+  const int64_t zeros = over(p.rows, kZeroRows);
+  const int64_t ctas = share > 1 ? p.tokens + over(zeros, share) : over(p.tokens + zeros, kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
-  combine_backward_kernel<T, BYTES, AT_ONCE><<<(unsigned)ctas, kThreads, 0, st>>>(p);
+  if (share > 1)
+    combine_backward_kernel<T, BYTES, AT_ONCE, true><<<(unsigned)ctas, 32 * share, 0, st>>>(p);
+  else
+    combine_backward_kernel<T, BYTES, AT_ONCE, false><<<(unsigned)ctas, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 // As many rows at once as a token has, of 2, 4 or 8: registers and instructions for more cost a third of the time.

@@ -9,6 +9,8 @@
 // float32 and differ per row (a sum times either scale has to stay within the
 // normal numbers), and no sum is held in fewer than 32 bits.
 //
+// The kernels are in f8_linear.cuh, which the experts' products share.
+//
 // linear_f8_kernel lays 128 rows of w along the lanes of tensor memory and BN
 // rows of x along its columns: with one token in flight the weights, which
 // are all the traffic, still fill the tensor core's 128 lanes.  A
