@@ -237,13 +237,21 @@ __device__ __forceinline__ const U* unit_at(const void* base, int64_t r, int64_t
   return reinterpret_cast<const U*>(static_cast<const char*>(base) + r * ld_bytes) + i;
 }
 
-constexpr int kZeroRows = 2;  // rows of a warp that looks for rows without a slot
+// n / d for d of at most 2^31, without a division of 64 bits where n has 32: that costs more than a short row.
+__device__ __forceinline__ int64_t quotient(int64_t n, int64_t d) {
+  return n >> 32 == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
+}
 
-// Which of the kZeroRows rows from r0 on hold no slot, as bits; there are `rows` in all.
-__device__ __forceinline__ uint32_t rows_without(const int32_t* slot, int64_t r0, int64_t rows) {
+// Which of the n rows from r0 on hold no slot, as bits; there are `rows` in all.
+__device__ __forceinline__ uint32_t rows_without(const int32_t* slot, int64_t r0, int n, int64_t rows) {
   const int lane = threadIdx.x & 31;
   const int64_t r = r0 + lane;
-  return __ballot_sync(0xFFFFFFFFu, lane < kZeroRows && r < rows && slot[r < rows ? r : 0] < 0);
+  return __ballot_sync(0xFFFFFFFFu, lane < n && r < rows && slot[r < rows ? r : 0] < 0);
+}
+// Rows that a warp looks through for those without a slot: up to 8 KB, which it then may have to write.
+int rows_to_zero(int64_t row_bytes) {
+  const int64_t n = 8192 / (row_bytes > 0 ? row_bytes : 1);
+  return n < 1 ? 1 : (n < 32 ? (int)n : 32);
 }
 
 struct GatherParams {
@@ -255,9 +263,10 @@ struct GatherParams {
   int rest;        // bytes of a row behind them
   int64_t parts;   // a warp copies a part of a row
   int64_t copies;  // warps that copy; the others write zeros
+  int zero_rows;   // that such a warp looks through
 };
 
-constexpr int kPart = 4;  // units of a lane
+constexpr int kPart = 2;  // units of a lane
 
 template <int BYTES>
 __device__ __forceinline__ void zero_row(const GatherParams& P, int64_t r, int lane) {
@@ -275,12 +284,12 @@ __global__ void __launch_bounds__(kThreads) gather_kernel(const GatherParams P) 
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (id >= P.copies) {
-    const int64_t r0 = (id - P.copies) * kZeroRows;
-    for (uint32_t todo = rows_without(P.slot, r0, P.rows); todo; todo &= todo - 1)
+    const int64_t r0 = (id - P.copies) * P.zero_rows;
+    for (uint32_t todo = rows_without(P.slot, r0, P.zero_rows, P.rows); todo; todo &= todo - 1)
       zero_row<BYTES>(P, r0 + __ffs(todo) - 1, lane);
     return;
   }
-  const int64_t t = id / P.parts, u0 = (id - t * P.parts) * (32 * kPart) + lane;
+  const int64_t t = quotient(id, P.parts), u0 = (id - t * P.parts) * (32 * kPart) + lane;
   T v[kPart];
 #pragma unroll
   for (int i = 0; i < kPart; ++i)
@@ -326,7 +335,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams P
   constexpr int N = units_of(BYTES);
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int64_t t = id / P.parts, u0 = (id - t * P.parts) * (32 * N) + lane;
+  const int64_t t = quotient(id, P.parts), u0 = (id - t * P.parts) * (32 * N) + lane;
   if (t >= P.tokens) return;
   float acc[N][U::COUNT] = {};
   U more[N];
@@ -389,7 +398,7 @@ struct CombineBackwardParams {
   const float* weights;
   void* dy;
   float* dweights;
-  int top_k;
+  int top_k, zero_rows;
 };
 
 constexpr int kMostShare = 16;  // warps of a token
@@ -405,8 +414,8 @@ __global__ void __launch_bounds__(SHARED ? 32 * kMostShare : kThreads)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = SHARED ? (int)(blockDim.x >> 5) : 1;
   const int64_t t = SHARED ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWarps + warp;
   if (t >= P.tokens) {
-    const int64_t r0 = (SHARED ? (t - P.tokens) * share + warp : t - P.tokens) * kZeroRows;
-    for (uint32_t todo = rows_without(P.slot, r0, P.rows); todo; todo &= todo - 1)
+    const int64_t r0 = (SHARED ? (t - P.tokens) * share + warp : t - P.tokens) * P.zero_rows;
+    for (uint32_t todo = rows_without(P.slot, r0, P.zero_rows, P.rows); todo; todo &= todo - 1)
       for (int64_t u = lane; u < P.units; u += 32) *unit_at<U>(P.dy, r0 + __ffs(todo) - 1, P.lddy, u) = U{};
     return;
   }
@@ -494,7 +503,8 @@ cudaError_t launch_gather(GatherParams& p, cudaStream_t st) {
   p.rest = (int)(p.a.bytes % BYTES);
   p.parts = over(p.units > 0 ? p.units : 1, 32 * kPart);
   p.copies = p.tokens * p.parts;
-  const int64_t ctas = over(p.copies + over(p.rows, kZeroRows), kWarps);
+  p.zero_rows = rows_to_zero(p.a.bytes);
+  const int64_t ctas = over(p.copies + over(p.rows, p.zero_rows), kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
   if (ctas > 0) gather_kernel<BYTES><<<(unsigned)ctas, kThreads, 0, st>>>(p);
   return cudaGetLastError();
@@ -515,7 +525,8 @@ cudaError_t launch_combine(CombineBackwardParams& p, cudaStream_t st) {
   const int64_t room = 32 * (int64_t)(sm_count() > 0 ? sm_count() : 1), rounds = over(p.units, 32 * units_of(BYTES));
   int share = 1;
   while (share < kMostShare && 2 * share * p.tokens <= room && 4 * share <= rounds) share *= 2;
-  const int64_t zeros = over(p.rows, kZeroRows);
+  p.zero_rows = rows_to_zero(p.units * BYTES);
+  const int64_t zeros = over(p.rows, p.zero_rows);
   const int64_t ctas = share > 1 ? p.tokens + over(zeros, share) : over(p.tokens + zeros, kWarps);
   if (ctas > ((int64_t)1 << 31) - 1) return cudaErrorInvalidValue;
   if (share > 1)
