@@ -5,8 +5,8 @@
 // ranges of the slots.  A warp counts its slots by expert in shared memory (32
 // at a time, those of one expert found by a match over the warp), the counts
 // are added up over warps, CTAs and experts, and a second pass over the ids
-// gives each slot its row.  It is bound by latency: 64 slots take 4.3 us, 32768
-// of 32 experts 7.3 (9.4 with eight CTAs), of which launch and cluster barriers
+// gives each slot its row.  It is bound by latency: 64 slots take 4.7 us, 32768
+// of 32 experts 7.6 (9.4 with eight CTAs), of which launch and cluster barriers
 // are 5.7.
 //
 // The other operators move rows and are bound by memory: a token's row is read

@@ -231,8 +231,7 @@ def _f8(ds, x, tiles=False, fmt="e4m3"):
                                               (300, 512, False, False), (128, 256, True, True)])
 @pytest.mark.parametrize("out,bias", [("bf16", False), ("f32", True), ("f16", False)])
 def test_linear(dslib, tokens, top_k, experts, align, kind, n, k, tiles, xtiles, out, bias):
-    if xtiles and align % 128:
-        pytest.skip("rows of tiles belong together")
+    xtiles = xtiles and align % 128 == 0  # the rows of a tile belong to one expert
     r = _rng("linear", tokens, experts, n, k, out)
     order, want = _order(dslib, _ids(r, tokens, top_k, experts, kind), experts, align)
     rows = X.gather(r.standard_normal((tokens, k)), want[3], top_k)
