@@ -273,7 +273,7 @@ __device__ __forceinline__ void zero_row(const GatherParams& P, int64_t r, int l
   using T = typename UnitOf<BYTES>::T;
   for (int64_t u = lane; u < P.units; u += 32) *unit_at<T>(P.a.dst, r, P.a.ld_dst, u) = T{};
   if (lane < P.rest) unit_at<uint8_t>(P.a.dst, r, P.a.ld_dst, P.units * BYTES)[lane] = 0;
-  if (P.b.src)
+  if (P.b.dst)
     for (int64_t u = lane; u < P.b.bytes / 4; u += 32) *unit_at<float>(P.b.dst, r, P.b.ld_dst, u) = 0.f;
 }
 
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kThreads) gather_kernel(const GatherParams P) 
       for (int i = 0; i < kPart; ++i)
         if (u0 + 32 * i < P.units) *unit_at<T>(P.a.dst, row, P.a.ld_dst, u0 + 32 * i) = v[i];
       if (first && lane < P.rest) unit_at<uint8_t>(P.a.dst, row, P.a.ld_dst, P.units * BYTES)[lane] = last;
-      if (first && P.b.src)
+      if (first && P.b.dst)
         for (int64_t u = lane; u < P.b.bytes / 4; u += 32)
           *unit_at<float>(P.b.dst, row, P.b.ld_dst, u) = *unit_at<float>(P.b.src, t, P.b.ld_src, u);
     }
@@ -638,7 +638,7 @@ cudaError_t launch_expert_gather(const RowCopy& a, const RowCopy& b, const ds_ex
   p.position = s.position, p.slot = s.slot;
   p.tokens = s.tokens, p.rows = s.rows, p.top_k = s.top_k;
   // rows of 8-bit values start at multiples of 16 bytes, and may end anywhere
-  const int unit = b.src ? 16 : unit_of(a.bytes, {Rows{a.src, a.ld_src}, Rows{a.dst, a.ld_dst}});
+  const int unit = b.dst ? 16 : unit_of(a.bytes, {Rows{a.src, a.ld_src}, Rows{a.dst, a.ld_dst}});
   if (unit == 16) return launch_gather<16>(p, st);
   return unit == 4 ? launch_gather<4>(p, st) : launch_gather<2>(p, st);
 }

@@ -17,7 +17,8 @@ struct ExpertProduct {  // y = x w_e^T for the rows of each segment, or (grad) d
 };
 
 cudaError_t launch_expert_order(const void* ids, int id_type, const ds_expert_slots& s, cudaStream_t st);
-// Rows of `bytes` each, copied to the rows of their token's slots; with a second matrix of the same rows.
+// Rows of `bytes` each, copied to the rows of their token's slots; with a second matrix of the same rows where its dst is
+// given (a source without tokens has no memory).
 struct RowCopy {
   const void* src;
   void* dst;

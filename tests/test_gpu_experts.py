@@ -141,6 +141,27 @@ def test_gather_f8(dslib, cols, fmt):
     assert np.array_equal(m.scale.cpu().numpy(), X.gather(s, want[3], 3))
 
 
+@pytest.mark.parametrize("tokens", [0, 3])
+def test_gather_f8_zeroes_rows_behind(dslib, tokens):
+    """Rows above what the tokens need hold no slot: their values and scales are zeros, also without any token, where x has
+    no memory."""
+    t = lambda *s: torch.full(s, 99, dtype=torch.int32, device="cuda")  # noqa: E731
+    order = dslib.ExpertOrder(t(4), t(3), t(tokens, 2), t(128 + tokens))
+    ids = torch.arange(2 * tokens, device="cuda").view(tokens, 2) % 3
+    dslib.ds_expert_order(ids, dslib.DS_INDEX_I64, order.desc)
+    x = dslib.F8Matrix.empty(tokens, 400, torch.device("cuda"))
+    x.q.view(torch.uint8).fill_(0x38)  # ones
+    x.scale.fill_(2.0)
+    out = dslib.F8Matrix.empty(order.rows, 400, torch.device("cuda"))
+    out.q.view(torch.uint8).fill_(0x7F)  # NaN
+    out.scale.fill_(float("nan"))
+    assert dslib.expert_gather(x, order, out=out) is out
+    held = order.slot >= 0
+    assert int(held.sum()) == 2 * tokens
+    assert torch.equal(out.scale, (2.0 * held[:, None]).expand(-1, 4))
+    assert torch.equal(out.dequantize(), (2.0 * held[:, None]).expand(-1, 400))
+
+
 @pytest.mark.parametrize("cols", COLS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("tokens,top_k,experts,align,kind", [(5, 3, 4, 1, "dropped"), (33, 17, 6, 16, "even"), (64, 2, 5, 128, "dropped"), (4, 2, 3, 1, "none")])
