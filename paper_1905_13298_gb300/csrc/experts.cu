@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_kernel(const OrderParams 
   int before = 0, all = here;  // slots of the CTAs before this one, and of all
   if constexpr (CLUSTER) {
     if (e < E) total[e] = here;
+    __syncwarp();  // a warp arrives together: the barrier is an aligned one
     cluster_arrive();
     cluster_wait();
     if (e < E) {
