@@ -186,6 +186,7 @@ struct GradientTiles {
       const uint32_t o = (uint32_t)offsets[e];
       s.start[e] = ((o < rows ? o : rows) + BK - 1) / BK;
     }
+    __syncwarp();  // one warp allocates tensor memory next, all its lanes together
     return s;
   }
   __device__ __forceinline__ int blocks_of_expert(int e) const {
