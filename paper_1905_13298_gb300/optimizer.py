@@ -33,6 +33,11 @@ def _scalar(t, name: str, dtype, device: int) -> int:
     return _flat(t, name, 1, (dtype,), device)
 
 
+def _memory(tensors) -> list:
+    """The storages of tensors: while one is held, its memory goes to nobody else, whatever the tensor is given instead."""
+    return [t.untyped_storage() for t in tensors if isinstance(t, torch.Tensor)]
+
+
 class AdamW:
     """Adam with decoupled weight decay on ``params`` (float32, bfloat16 or float16), updated in place from ``grads``
     (tensors of the same sizes, any of these dtypes), which the optimizer keeps and reads at each step.
@@ -43,7 +48,11 @@ class AdamW:
     the rounded parameters to.  ``weight_decay`` is one number or one per tensor.  ``steps`` is how many steps were
     done: a number, or a CUDA int64 tensor, which ``step`` then counts up on the device; with that, ``lr`` may be a
     CUDA float32 tensor too, and a step can be captured in a CUDA graph.  ``grad_scale``, a CUDA float32 tensor of one
-    value, multiplies all gradients.  ``seed`` begins the random bits that 8-bit states are rounded by."""
+    value, multiplies all gradients.  ``seed`` begins the random bits that 8-bit states are rounded by.
+
+    A step works on the memory that parameters, states and copies had when the optimizer was made, and holds it.  Where a
+    parameter, gradient or copy has been given other memory since, it is refused.  States are loaded by copying into them
+    (``opt.m[k].copy_(...)``): entries of ``m`` and ``v`` that are replaced or given other memory are passed over."""
 
     def __init__(self, params, grads, m=None, v=None, copies=None, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay=0.01, grad_scale=None, steps=0, seed: int = 0, state_dtype=torch.float32):
@@ -86,21 +95,21 @@ class AdamW:
             if self.copies is not None and self.copies[k] is not None:
                 c = self.copies[k]
                 d.copy, d.copy_type = _flat(c, f"copies[{k}]", n, _TYPES, device), _TYPES[c.dtype]
-        self._states = [*self.m, *self.v, *(self.copies or [])]  # their memory stays, whatever becomes of the lists
+        self._kept = self.params + [c for c in self.copies or [] if c is not None]
+        self._kept_at = list(map(torch.Tensor.data_ptr, self._kept))
+        states = [t for state in (*self.m, *self.v) for t in (state if isinstance(state, (tuple, list)) else (state,))]
+        self._kept_memory = _memory(self._kept + states)
         self._take(self.grads)
-        self._hold()
         self.lr, self.betas, self.eps, self.grad_scale, self.steps, self.seed = lr, betas, eps, grad_scale, steps, seed
 
     def _take(self, grads) -> None:
+        """Notes gradients, and where all lies that a step looks at: it refuses what was given other memory since."""
         got = [(_flat(g, f"grads[{k}]", self._tensors[k].n, _TYPES, self._device), _TYPES[g.dtype])
                for k, g in enumerate(grads)]
         for d, (at, kind) in zip(self._tensors, got):
             d.g, d.g_type = at, kind
-
-    def _hold(self) -> None:
-        """Notes where parameters and gradients lie: a step refuses ones that were given other memory since."""
-        self._all = self.params + self.grads
-        self._held = list(map(torch.Tensor.data_ptr, self._all))
+        self._all, self._held = self._kept + grads, self._kept_at + [at for at, _ in got]
+        self._grad_memory = _memory(grads)
 
     def step(self, grads=None, stream=None) -> None:
         """One step; ``grads`` replace those of the steps before."""
@@ -112,11 +121,12 @@ class AdamW:
             grads = list(grads)
             if len(grads) != len(self.params):
                 raise ValueError(f"grads has {len(grads)} entries, expected {len(self.params)}")
+        look, held = (self._all, self._held) if grads is None else (self._kept, self._kept_at)
+        if list(map(torch.Tensor.data_ptr, look)) != held:
+            raise ValueError("a parameter, gradient or copy has other memory than when it was given")
+        if grads is not None:
             self._take(grads)
             self.grads = grads
-            self._hold()
-        elif list(map(torch.Tensor.data_ptr, self._all)) != self._held:
-            raise ValueError("a parameter or gradient has other memory than when it was given")
         o = ds_adamw_options(0.0, self.betas[0], self.betas[1], self.eps, 0, None, None, None, self.seed & 0xFFFFFFFF, 0)
         if isinstance(self.lr, torch.Tensor):
             o.lr_dev = _scalar(self.lr, "lr", torch.float32, device)

@@ -406,3 +406,30 @@ def test_optimizer_refuses_before_any_launch(ds, first_gpu, monkeypatch):
         with pytest.raises(ValueError):
             ok.step(**bad)
     assert ok.grads == [g] and ok.steps == 0
+
+
+def test_optimizer_refuses_memory_that_was_replaced(ds, first_gpu, monkeypatch):
+    """A parameter, gradient or copy that lies elsewhere than it did, with the step's own gradients or with new ones."""
+    monkeypatch.setattr(torch.Tensor, "data_ptr", lambda t: t.data_ptr())
+    monkeypatch.setattr(ds.optimizer, "lib", None)  # nothing is launched
+
+    class At(Gpu):
+        at = 0
+
+        def data_ptr(self):
+            return self.at
+
+    def moved(which, grads):
+        tensors = []
+        for k in range(6):
+            tensors.append(At(300, dtype=torch.bfloat16 if k == 4 else torch.float32))
+            tensors[k].at = (k + 1) << 40
+        p, g, m, v, c, new = tensors
+        opt = ds.AdamW([p], [g], m=[m], v=[v], copies=[c])
+        tensors[which].at += 1 << 30
+        with pytest.raises(ValueError, match="other memory"):
+            opt.step([new] if grads else None)
+        assert opt.steps == 0 and opt.grads == [g]
+
+    for which, grads in ((0, False), (0, True), (1, False), (4, False), (4, True)):
+        moved(which, grads)

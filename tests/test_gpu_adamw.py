@@ -298,3 +298,39 @@ def test_memory_of_replaced_states_stays(dslib):
     over = [torch.full((70_000,), 7.0, device="cuda") for _ in range(4)]
     opt.step()
     assert all(bool((t == 7).all()) for t in over) and bool((held != 0).all())
+
+
+@pytest.mark.parametrize("state", [torch.float32, F8])
+def test_memory_of_states_with_another_storage_stays(dslib, state):
+    """Where a state was given other memory, the step goes on with what it was made with, which nothing else got."""
+    n = 70_000
+    p, g = torch.ones(n, device="cuda"), torch.full((n,), 1e-3, device="cuda")
+    q = p.clone()
+    a, b = dslib.AdamW([p], [g], state_dtype=state), dslib.AdamW([q], [g], state_dtype=state)
+    a.step()
+    b.step()
+    for t in (a.m[0], a.v[0]):
+        for x in (t if isinstance(t, tuple) else (t,)):
+            x.data = x.clone()
+    over = [torch.full((n,), 7, device="cuda", dtype=torch.uint8 if state == F8 else torch.float32) for _ in range(8)]
+    scales = [torch.full((-(-n // 128),), 7.0, device="cuda") for _ in range(8)]
+    a.step()
+    b.step()
+    assert torch.equal(p, q) and all(bool((t == 7).all()) for t in over + scales)
+
+
+def test_copies_and_parameters_with_another_storage_are_refused(dslib):
+    """Also where the step is given its gradients; nothing is written, and nothing else got the memory."""
+    n = 70_000
+    g = torch.full((n,), 1e-3, device="cuda")
+    for which in (0, 1):
+        for new in (None, [g.clone()]):
+            p, c = torch.ones(n, device="cuda"), torch.ones(n, device="cuda", dtype=torch.bfloat16)
+            opt = dslib.AdamW([p], [g], copies=[c])
+            (p, c)[which].data = torch.zeros_like((p, c)[which])
+            over = [torch.full_like((p, c)[which], 7.0) for _ in range(4)]
+            for _ in range(2):
+                with pytest.raises(ValueError, match="other memory"):
+                    opt.step(new)
+            assert opt.steps == 0 and all(bool((t == 7).all()) for t in over)
+            assert bool((opt.m[0] == 0).all()) and bool(((p, c)[which] == 0).all()) and bool(((p, c)[1 - which] == 1).all())
