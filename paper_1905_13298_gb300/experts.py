@@ -23,6 +23,8 @@ A training step of such a block reads::
 """
 from __future__ import annotations
 
+from operator import attrgetter
+
 import torch
 
 from . import DS_INDEX_I32, DS_INDEX_I64, DsError, DS_ERR_UNSUPPORTED, _check, ds_expert_slots, lib
@@ -46,9 +48,10 @@ class ExpertOrder:
     """Which rows the slots (token, choice) of a block with experts have, as ``expert_order`` makes it: int32 tensors
     ``offsets`` [experts + 1] of the experts' segments, ``counts`` [experts], ``position`` [tokens, top_k], the row of
     a slot or -1, and ``slot`` [rows], the slot (token * top_k + choice) of a row or -1.  Segments start at multiples
-    of ``align``."""
+    of ``align``.  The tensors stay those that it was made with: calls read their memory."""
 
-    __slots__ = ("offsets", "counts", "position", "slot", "device", "desc")
+    __slots__ = ("_offsets", "_counts", "_position", "_slot", "device", "desc")
+    offsets, counts, position, slot = (property(attrgetter(name)) for name in __slots__[:4])
 
     def __init__(self, offsets, counts, position, slot, align: int = 1):
         if offsets.dim() != 1 or offsets.shape[0] < 2:
@@ -59,7 +62,7 @@ class ExpertOrder:
         if device < 0:
             raise ValueError("offsets must be a CUDA tensor")
         experts, (tokens, top_k), rows = offsets.shape[0] - 1, position.shape, slot.shape[0]
-        self.offsets, self.counts, self.position, self.slot, self.device = offsets, counts, position, slot, device
+        self._offsets, self._counts, self._position, self._slot, self.device = offsets, counts, position, slot, device
         self.desc = ds_expert_slots(_ints(offsets, "offsets", (experts + 1,), device),
                                     _ints(counts, "counts", (experts,), device),
                                     _ints(position, "position", (tokens, top_k), device),
@@ -127,10 +130,10 @@ def expert_order(ids, experts: int, align: int = 1, stream=None) -> ExpertOrder:
         raise DsError(DS_ERR_UNSUPPORTED, "too many experts, tokens or rows, or align too large")
     order, kind, where = ExpertOrder.__new__(ExpertOrder), torch.int32, ids.device
     # four allocations cost the host less than four views of one
-    offsets = order.offsets = torch.empty(experts + 1, dtype=kind, device=where)
-    counts = order.counts = torch.empty(experts, dtype=kind, device=where)
-    position = order.position = torch.empty((tokens, top_k), dtype=kind, device=where)
-    slot = order.slot = torch.empty(rows, dtype=kind, device=where)
+    offsets = order._offsets = torch.empty(experts + 1, dtype=kind, device=where)
+    counts = order._counts = torch.empty(experts, dtype=kind, device=where)
+    position = order._position = torch.empty((tokens, top_k), dtype=kind, device=where)
+    slot = order._slot = torch.empty(rows, dtype=kind, device=where)
     order.device = device
     order.desc = ds_expert_slots(offsets.data_ptr(), counts.data_ptr(), position.data_ptr(), slot.data_ptr(), tokens,
                                  rows, top_k, experts, align, 0)

@@ -389,6 +389,16 @@ def test_helpers_refuse_what_the_abi_cannot_see(ds, first_gpu):
         ds.expert_order(i(6, 2), 1025)
 
 
+def test_tensors_of_an_order_cannot_be_replaced(ds, first_gpu):
+    """Its descriptor holds their addresses: another tensor would be passed over, and the memory of the first one lost."""
+    order = _expert_order(ds)
+    for name in ("offsets", "counts", "position", "slot"):
+        held = getattr(order, name)
+        with pytest.raises(AttributeError):
+            setattr(order, name, Gpu(*held.shape, dtype=torch.int32))
+        assert getattr(order, name) is held
+
+
 def test_optimizer_refuses_before_any_launch(ds, first_gpu, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "data_ptr", lambda t: t.data_ptr())
     f = lambda *s, dtype=torch.float32, device=0: Gpu(*s, dtype=dtype, device=device)  # noqa: E731
