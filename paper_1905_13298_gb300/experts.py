@@ -148,16 +148,16 @@ def expert_gather(x, order: ExpertOrder, out=None, stream=None):
         with _given(stream):
             return expert_gather(x, order, out)
     if isinstance(x, F8Matrix):
-        device = _on_gpu(x.q, "x")
+        device = _on_gpu(x._q, "x")
         desc, dx = _order(order, device), x.desc
         if x.tiles or (out is not None and _f8(out, "out").blocks != dx.blocks):
             raise ValueError("x and out must have blocks by rows: rows of tiles cannot be moved")
         if dx.rows != desc.tokens:
             raise ValueError(f"x has {dx.rows} rows, the order {desc.tokens} tokens")
         if out is None:
-            out = F8Matrix.empty(desc.rows, dx.cols, x.q.device, x.q.dtype)
+            out = F8Matrix.empty(desc.rows, dx.cols, x._q.device, x._q.dtype)
         else:
-            _on_gpu(out.q, "out", device)
+            _on_gpu(out._q, "out", device)
         _check(lib().ds_expert_gather_f8(dx, desc, out.desc, _on_stream(device)))
         return out
     ldx = _matrix(x, "x")
@@ -240,15 +240,15 @@ def expert_linear_f8(x: F8Matrix, w: F8Matrix, order: ExpertOrder, bias=None, ou
         with _given(stream):
             return expert_linear_f8(x, w, order, bias, out, dtype)
     dx, dw = _f8(x, "x"), _f8(w, "w")
-    device = _on_gpu(x.q, "x")
-    _on_gpu(w.q, "w", device)
+    device = _on_gpu(x._q, "x")
+    _on_gpu(w._q, "w", device)
     desc = _order(order, device)
     n = dw.rows // desc.experts
     y = out
     if y is None:
         if dtype not in _TYPES:
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        y = torch.empty((desc.rows, n), dtype=dtype, device=x.q.device)
+        y = torch.empty((desc.rows, n), dtype=dtype, device=x._q.device)
         py, ldy = y.data_ptr(), n
     else:
         if y.dtype not in _TYPES:
@@ -272,8 +272,8 @@ def expert_weight_grad_f8(dy_t: F8Matrix, x_t: F8Matrix, order: ExpertOrder, add
         with _given(stream):
             return expert_weight_grad_f8(dy_t, x_t, order, add, out)
     dd, dx = _f8(dy_t, "dy_t"), _f8(x_t, "x_t")
-    device = _on_gpu(dy_t.q, "dy_t")
-    _on_gpu(x_t.q, "x_t", device)
+    device = _on_gpu(dy_t._q, "dy_t")
+    _on_gpu(x_t._q, "x_t", device)
     desc = _order(order, device)
     shape = (desc.experts, dd.rows, dx.rows)
 
@@ -286,6 +286,6 @@ def expert_weight_grad_f8(dy_t: F8Matrix, x_t: F8Matrix, order: ExpertOrder, add
         return t.data_ptr()
 
     pa = held(add, "add")
-    dw = torch.empty(shape, dtype=torch.float32, device=dy_t.q.device) if out is None else out
+    dw = torch.empty(shape, dtype=torch.float32, device=dy_t._q.device) if out is None else out
     _check(lib().ds_expert_weight_grad_f8(dd, dx, desc, pa, dx.rows, held(dw, "out"), dx.rows, _on_stream(device)))
     return dw

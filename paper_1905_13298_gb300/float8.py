@@ -23,6 +23,8 @@ A training step of a gated feed-forward block reads::
 """
 from __future__ import annotations
 
+from operator import attrgetter
+
 import torch
 
 from . import (DS_F8_E4M3, DS_F8_E5M2, DS_F8_POW2, DS_F8_ROWS, DS_F8_TILES, DS_TYPE_BF16, DS_TYPE_F16, DS_TYPE_F32,
@@ -36,9 +38,11 @@ BLOCK = 128
 
 class F8Matrix:
     """8-bit values ``q`` [rows, cols] (``torch.float8_e4m3fn`` or ``float8_e5m2``, rows a multiple of 16 bytes apart)
-    and float32 scales: ``scale`` [rows, ceil(cols / 128)], or with ``tiles`` [ceil(rows / 128), ceil(cols / 128)]."""
+    and float32 scales: ``scale`` [rows, ceil(cols / 128)], or with ``tiles`` [ceil(rows / 128), ceil(cols / 128)].  Both stay
+    the tensors that it was made with: calls read and write their memory."""
 
-    __slots__ = ("q", "scale", "desc")
+    __slots__ = ("_q", "_scale", "desc")
+    q, scale = property(attrgetter("_q")), property(attrgetter("_scale"))
 
     def __init__(self, q, scale, tiles: bool = False):
         fmt = _FORMATS.get(q.dtype)
@@ -57,7 +61,7 @@ class F8Matrix:
             raise ValueError(f"scale has shape {tuple(scale.shape)}, expected {want}")
         if q.get_device() < 0 or q.get_device() != scale.get_device():
             raise ValueError("q and scale must be CUDA tensors of one device")
-        self.q, self.scale = q, scale
+        self._q, self._scale = q, scale
         self.desc = ds_f8_matrix(q.data_ptr(), scale.data_ptr(), rows, cols, ld, ld_scale, fmt,
                                  DS_F8_TILES if tiles else DS_F8_ROWS)
 
@@ -70,11 +74,11 @@ class F8Matrix:
         m = cls.__new__(cls)
         ld, nb = (cols + 15) // 16 * 16, (cols + BLOCK - 1) // BLOCK
         if ld == cols:
-            m.q = torch.empty((rows, cols), dtype=dtype, device=device)
+            m._q = torch.empty((rows, cols), dtype=dtype, device=device)
         else:
-            m.q = torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device)
-        m.scale = torch.empty(((rows + BLOCK - 1) // BLOCK if tiles else rows, nb), dtype=torch.float32, device=device)
-        m.desc = ds_f8_matrix(m.q.data_ptr(), m.scale.data_ptr(), rows, cols, ld, nb, fmt,
+            m._q = torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device)
+        m._scale = torch.empty(((rows + BLOCK - 1) // BLOCK if tiles else rows, nb), dtype=torch.float32, device=device)
+        m.desc = ds_f8_matrix(m._q.data_ptr(), m._scale.data_ptr(), rows, cols, ld, nb, fmt,
                               DS_F8_TILES if tiles else DS_F8_ROWS)
         return m
 
@@ -206,8 +210,8 @@ def quantize_f8(x, blocks: str | None = "rows", transposed: str | None = None, p
         raise ValueError("neither the matrix nor its transpose is asked for")
     is_f8 = isinstance(x, F8Matrix)
     if is_f8:
-        rows, cols, device = x.desc.rows, x.desc.cols, x.q.device
-        _on_gpu(x.q, "x")
+        rows, cols, device = x.desc.rows, x.desc.cols, x._q.device
+        _on_gpu(x._q, "x")
     else:
         ld = _matrix(x, "x")
         rows, cols = x.shape
@@ -245,13 +249,13 @@ def linear_f8(x: F8Matrix, w: F8Matrix, bias=None, add=None, out=None, dtype=tor
             return linear_f8(x, w, bias, add, out, dtype)
     dx, dw = _f8(x, "x"), _f8(w, "w")
     M, N = dx.rows, dw.rows
-    device = _on_gpu(x.q, "x")
-    _on_gpu(w.q, "w", device)
+    device = _on_gpu(x._q, "x")
+    _on_gpu(w._q, "w", device)
     y = out
     if y is None:
         if dtype not in _TYPES:
             raise ValueError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        y = torch.empty((M, N), dtype=dtype, device=x.q.device)
+        y = torch.empty((M, N), dtype=dtype, device=x._q.device)
         py, ldy = y.data_ptr(), N
     else:
         if y.dtype not in _TYPES:
@@ -354,7 +358,7 @@ def gated_f8_backward(kept: F8Matrix, da, pow2: bool = False, dtype=torch.float8
     rows, features = da.shape
     if features == 0 or dk.rows != rows or dk.cols != _gate_width(features):
         raise ValueError(f"kept is {dk.rows} x {dk.cols}, expected {rows} x {_gate_width(features)}")
-    device = _on_gpu(da, "da", _on_gpu(kept.q, "kept"))
+    device = _on_gpu(da, "da", _on_gpu(kept._q, "kept"))
     dgu = F8Matrix.empty(rows, dk.cols, da.device, dtype)
     dgu_t = F8Matrix.empty(dk.cols, rows, da.device, dtype) if transposed else None
     a_t = F8Matrix.empty(features, rows, da.device, dtype) if transposed else None

@@ -61,3 +61,14 @@ def test_tensors_of_the_current_gpu_are_not(ds, monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     with pytest.raises((AssertionError, RuntimeError)):
         ds.linear_f8(_matrix(ds, 4, 256), _matrix(ds, 4, 256))
+
+
+def test_tensors_of_a_matrix_cannot_be_replaced(ds):
+    """Its descriptor holds their addresses: others would be passed over, and the memory of the first ones lost."""
+    m = _matrix(ds, 4, 256)
+    q, scale = m.q, m.scale
+    with pytest.raises(AttributeError):
+        m.q = OnSecondGpu(4, 256, dtype=torch.float8_e4m3fn)
+    with pytest.raises(AttributeError):
+        m.scale = OnSecondGpu(4, 2, dtype=torch.float32)
+    assert m.q is q and m.scale is scale
