@@ -15,6 +15,7 @@ Run it (one GPU) to train a block on a synthetic target and to time a step and a
 from __future__ import annotations
 
 import argparse
+from numbers import Real
 
 import torch
 
@@ -100,7 +101,7 @@ class GatedFeedForward:
     def adamw(self, grads, **options) -> AdamW:
         """An optimizer of the masters, for ``step_by``; no decay of the norm's weight unless options say otherwise."""
         names, decay = list(self.masters()), options.pop("weight_decay", 0.01)
-        each = [0.0 if k == "norm" else decay for k in names] if isinstance(decay, (int, float)) else list(decay)
+        each = [0.0 if k == "norm" else decay for k in names] if isinstance(decay, Real) else list(decay)
         return AdamW(list(self.masters().values()), [grads[k] for k in names], weight_decay=each, **options)
 
     def step_by(self, optimizer: AdamW, grads) -> None:

@@ -443,3 +443,16 @@ def test_optimizer_refuses_memory_that_was_replaced(ds, first_gpu, monkeypatch):
 
     for which, grads in ((0, False), (0, True), (1, False), (4, False), (4, True)):
         moved(which, grads)
+
+
+def test_weight_decay_of_a_block_is_any_number(ds, monkeypatch):
+    """One number of any type for all weights but the norm's, or one for each."""
+    from paper_1905_13298_gb300 import feed_forward
+    monkeypatch.setattr(feed_forward, "AdamW", lambda params, grads, weight_decay, **options: weight_decay)
+    block = feed_forward.GatedFeedForward.__new__(feed_forward.GatedFeedForward)
+    block.norm, block.gate_up, block.down = "norm", "gate_up", "down"
+    grads = dict.fromkeys(block.masters())
+    for number in (0.5, 1, np.float32(0.5), np.int64(1)):
+        assert block.adamw(grads, weight_decay=number) == [0.0, number, number]
+    assert block.adamw(grads) == [0.0, 0.01, 0.01]
+    assert block.adamw(grads, weight_decay=[0.1, 0.2, 0.3]) == [0.1, 0.2, 0.3]
