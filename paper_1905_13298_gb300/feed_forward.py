@@ -141,7 +141,14 @@ class ExpertsFeedForward(GatedFeedForward):
         self.w_down, self.w_down_t = both(self.down)
 
     def use_shift_weights(self) -> None:
-        raise NotImplementedError("shift weights are packed for one matrix")
+        """As for the block without experts: the experts' weights, and their transposes, are exact; the router keeps its own."""
+        def both(w):
+            m = expand_shift_weights_f8(pack_shift_weights(*quantize_shift_weights(w.flatten(0, 1))))
+            turned = m.dequantize().view(w.shape).transpose(1, 2).reshape(-1, w.shape[1])
+            return m, quantize_f8(turned, "tiles", pow2=True)[0]
+
+        self.w_gate_up, self.w_gate_up_t = both(self.gate_up)
+        self.w_down, self.w_down_t = both(self.down)
 
     def route(self, n, padding=None):
         """(ids, weights) [tokens, top_k] of the norm's 8-bit rows; tokens of ``padding`` (truth values) go nowhere."""

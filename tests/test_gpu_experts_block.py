@@ -63,6 +63,28 @@ def test_training_step_against_float64(dslib, padded):
     assert dslib.lib().ds_f8_fault_flag() == 0
 
 
+def test_shift_weights_have_their_gradients(dslib):
+    """The experts' weights are s * 2^p exactly, transposes too; y and gradients are theirs, within the roundings counted
+    above without those of the weights (there are none)."""
+    b, (x, s, dy, dh) = _block(), _inputs(7)
+    b.use_shift_weights()
+    for w, m, m_t in ((b.gate_up, b.w_gate_up, b.w_gate_up_t), (b.down, b.w_down, b.w_down_t)):
+        sign, power = dslib.quantize_shift_weights(w)
+        assert torch.equal(m.dequantize().view(w.shape), sign.float() * torch.exp2(power.float()))
+        assert torch.equal(m_t.dequantize().view(w.shape[0], w.shape[2], w.shape[1]), m.dequantize().view(w.shape).transpose(1, 2))
+    y, h, saved = b.forward(x, s)
+    dx, grads = b.backward(dy, dh, saved)
+    want_y, want_dx, want = _exact(b, x, s, dy, dh, saved[3], None)
+    assert _off(y, want_y) < 0.0636 and _off(dx, want_dx) < 0.12
+    for k, g in grads.items():
+        assert _off(g, want[k]) < 0.12, (k, _off(g, want[k]))
+    t, _ = b.token(x[:7], s[:7])
+    assert _off(t, y[:7].double()) < 0.02
+    b.refresh()  # back to the rounded float weights
+    assert not torch.equal(b.w_down.dequantize(), dslib.expand_shift_weights_f8(
+        dslib.pack_shift_weights(*dslib.quantize_shift_weights(b.down.flatten(0, 1)))).dequantize())
+
+
 def test_token_is_the_forward_pass(dslib):
     """Without gaps between segments and without a checkpoint: y within a bf16 step and the products' order of sums."""
     b, (x, s, _, _) = _block(), _inputs(6)
