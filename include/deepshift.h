@@ -74,7 +74,8 @@ const char* ds_last_error(void);
 int ds_version(void);
 
 /* sizeof of the ABI structs as compiled into the library (0: ds_weights, 1: ds_layer, 2: ds_f8_matrix,
- * 3: ds_expert_slots, 4: ds_adamw_tensor, 5: ds_adamw_options), so that bindings can check their layout; 0 for any other argument (a library utility: no counterpart in the paper). */
+ * 3: ds_expert_slots, 4: ds_adamw_tensor, 5: ds_adamw_options), so that bindings can check their layout; 0 for any
+ * other argument (a library utility: no counterpart in the paper). */
 size_t ds_abi_struct_size(int which);
 
 /* ---------------------------------------------------------------------------
@@ -771,24 +772,34 @@ ds_status ds_expert_weight_grad_f8(const ds_f8_matrix* dy_t, const ds_f8_matrix*
 /* ---------------------------------------------------------------------------
  * Optimizer: one step of Adam with decoupled weight decay over many tensors.
  * For each value, with t the step's number (from 1) and each operation rounded
- * to float32 (the factors are computed in float64 and rounded once):
+ * to float32 (the factors are computed in float64 and rounded once; those of a
+ * t or lr on the device in float32, within 2^-21 of it):
  *   g' = g * grad_scale
  *   m  = beta1 * m + (1 - beta1) * g'
  *   v  = beta2 * v + (1 - beta2) * (g' * g')
  *   p  = p * (1 - lr * weight_decay)
  *        - m * (lr / (1 - beta1^t)) / (sqrt(v) * (1 - beta2^t)^(-1/2) + eps)
- * p is rounded once to its type; `copy` is p rounded to another.
+ * p is rounded once to its type, to the nearest; `copy` is p, as it was before
+ * that, rounded to another.  A 16-bit p keeps no update below half its step:
+ * for these, p is float32 and `copy` the 16-bit values.
  *
  * The states m and v are float32, or 8 bits: e4m3 values of m and of sqrt(v),
  * with a float32 scale for each 128 consecutive values of a tensor,
  *   scale = max(amax / 448, 2^-126),  u = value * min(448 / amax, 2^126),
  * amax the block's largest finite magnitude.  u becomes one of its two e4m3
  * neighbours, the one of larger magnitude with the probability of u's distance
- * from the other one: the expected value of a state is then what the recurrence
- * says.  (To the nearest it would stand still: a step changes v by 1 - beta2
- * of itself, a rounding to 3 bits loses up to 12%.)  A positive sqrt(v) is held
- * as at least the smallest value, 2^-9, so that no later step divides by eps
- * alone what it should divide by a root; infinities and NaN become NaN.  The
+ * from the other one, so that its expected value is u.  (To the nearest a state
+ * would stand still: a step changes v by 1 - beta2 of itself, a rounding to 3
+ * bits loses up to 12%.)  For m that makes the expected value what the
+ * recurrence says; v is the square of the root that is held, and each
+ * rounding's variance is added to it: its mean is above the recurrence's, by at
+ * most 2/15 while a block's scale stays and its roots are at least 2^-6 of it
+ * (with beta2 = 0.999 5.5% for normal gradients, 7% where one in 20 is not
+ * zero; the mean of 1 / sqrt(v) is then 1.2 and 2% above).  A positive sqrt(v)
+ * is held as at least the smallest value, 2^-9, and its square is not 0 where
+ * the block's largest root is at least 2^-57 and beta2 above 1/2, so that a
+ * later step divides by a root and not by eps alone.  Infinities and NaN become
+ * NaN.  The
  * step itself takes m and v before they are rounded.  With i the index of a
  * value in its tensor and n the tensor's number in the call, the random bits
  * of m and sqrt(v) are the low and the high half of a hash of

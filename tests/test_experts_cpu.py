@@ -130,6 +130,40 @@ def test_states_round_to_neighbours_and_keep_the_mean():
     assert np.all(q[root > 0] >= 2.0**-9) and np.all(q[root == 0] == 0)
 
 
+def test_8bit_second_moment_is_above_the_recurrence_by_at_most_2_15():
+    """The held root r of a value moves from r to a neighbour of sqrt(b r^2 + (1 - b) g^2), and is itself one (the block's
+    scale stays).  Between neighbours d apart a rounding has the variance (u - r) (r + d - u) <= d |u - r|, with d <= u / 8
+    and |u - r| = (1 - b) |g^2 - r^2| / (u + r): at most (1 - b) (g^2 + r^2) / 16 (u / (u + r) is 1/2 for b near 1).  So
+    E r^2 = b E r^2 + (1 - b) E g^2 + that: E r^2 is at least E g^2, and at most 17/15 of it.  A value's square has a
+    standard deviation below a half of it (a step adds 4 r^2 times the variance, which decays as b^2): 5 of the mean's."""
+    r, n, b = np.random.default_rng(8), 128 * 32, np.float32(0.999)
+    root, v = np.zeros(n, np.float32), np.zeros(n)
+    root[::128] = 4  # with a gradient of 4: the blocks' scales stay
+    v[::128] = 16
+    for t in range(1, 2001):
+        g = r.standard_normal(n).astype(np.float32)
+        g[::128] = 4
+        v = 0.999 * v + 0.001 * g.astype(np.float64) ** 2
+        new = np.sqrt(root * root * b + g * g * (np.float32(1) - b))
+        q, s = X.state_to_f8(new, X.random_bits(n, t, 0, 3)[1], True)
+        root = q * np.repeat(s, 128)
+    small = np.arange(n) % 128 != 0
+    assert np.allclose(s, 4 / 448, rtol=1e-3)
+    off = (root[small].astype(np.float64) ** 2).mean() / v[small].mean() - 1
+    assert -5 * 0.5 / np.sqrt(small.sum()) <= off <= 2 / 15 + 5 * 0.5 / np.sqrt(small.sum()), off
+
+
+@pytest.mark.parametrize("beta2", [0.501, 0.9, 0.999])
+@pytest.mark.parametrize("top", [2.0**-57, 1e-16, 1.0])
+def test_smallest_8bit_root_has_a_square(beta2, top):
+    """Where the block's largest root is at least 2^-57, 2^-9 / 448 of it squared is above 2^-150: float32 holds 2^-149."""
+    root = np.full(128, 1e-44, np.float32)
+    root[0] = top
+    q, s = X.state_to_f8(root, np.zeros(128, np.uint32), True)
+    held = q * np.repeat(s, 128)
+    assert np.all(held[1:] == np.float32(2.0**-9) * s[0]) and np.all(held * held * np.float32(beta2) > 0)
+
+
 # ---------------------------------------------------------------------------------------------- refusals of the ABI
 
 

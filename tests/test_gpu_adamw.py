@@ -169,6 +169,44 @@ def test_8bit_states_move(dslib):
     assert abs(float(got) / v - 1) < 0.2, (float(got), v)
 
 
+def test_8bit_second_moment_is_above_the_recurrence_by_at_most_2_15(dslib):
+    """As the oracle's (test_experts_cpu.py, where the bounds are derived), with 2^17 values: blocks whose scale stays."""
+    n = 1 << 17
+    r = torch.Generator(device="cuda").manual_seed(8)
+    q, s = torch.zeros(n, device="cuda"), torch.full((n // 128,), 4 / 448, device="cuda")
+    q[::128] = 448
+    g, v = torch.empty(n, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+    state = (torch.zeros(n, device="cuda").to(F8), torch.zeros(n // 128, device="cuda"))
+    opt = dslib.AdamW([torch.zeros(n, device="cuda")], [g], m=[state], v=[(q.to(F8), s)], lr=0.0, betas=(0.9, 0.999))
+    for _ in range(2000):
+        g.normal_(generator=r)
+        g[::128] = 4
+        v = 0.999 * v + 0.001 * g.double().square()
+        opt.step()
+    small = torch.arange(n, device="cuda") % 128 != 0
+    held = (opt.v[0][0].float().view(-1, 128) * opt.v[0][1][:, None]).view(-1)
+    off = float(held[small].double().square().mean() / v[small].mean()) - 1
+    few = 5 * 0.5 / float(small.sum()) ** 0.5
+    assert -few <= off <= 2 / 15 + few, off
+
+
+@pytest.mark.parametrize("beta2", [0.501, 0.999])
+@pytest.mark.parametrize("top,lost", [(1.0, False), (2.0**-57, False), (1e-18, True)])
+def test_smallest_8bit_root_has_a_square(dslib, beta2, top, lost):
+    """Without a gradient and with eps 0 a step divides 0 by the root: NaN shows a root whose square was 0 in float32."""
+    n = 256
+    q = torch.full((n,), 2.0**-9, device="cuda")
+    q[::128] = 448
+    zero = (torch.zeros(n, device="cuda").to(F8), torch.zeros(2, device="cuda"))
+    p = torch.ones(n, device="cuda")
+    state = (q.to(F8), torch.full((2,), top / 448, device="cuda"))
+    dslib.AdamW([p], [torch.zeros(n, device="cuda")], m=[zero], v=[state], betas=(0.9, beta2), eps=0.0, weight_decay=0.0).step()
+    if lost:
+        assert bool(torch.isnan(p[1:128]).all()) and bool((p[::128] == 1).all())
+    else:
+        assert bool((p == 1).all())
+
+
 @pytest.mark.parametrize("state", [torch.float32, F8])
 def test_values_that_are_not_finite(dslib, state):
     """An infinite or NaN gradient spoils its own value and no other; its 8-bit states become NaN."""
