@@ -23,7 +23,6 @@ struct OutputPart {
   int64_t M, N, ld_add, ldy;
   int type, vec, pairs;
   int m0, n0;
-  __device__ __forceinline__ const OutputPart& to(const Params&) const { return *this; }
 };
 
 // y = x w_e^T by the kernel of small products: a CTA's tile among those of all experts.  Every warp finds it for itself,
@@ -90,7 +89,8 @@ struct SegmentPlace {
 template <int COLS_OF_TILE>
 struct SegmentTiles {
   static constexpr int N = COLS_OF_TILE;
-  static constexpr bool EMPTY = true, ADDS = false;
+  static constexpr bool WALKS = true;
+  static constexpr bool ADDS = false;  // whether sums are added to others' that are asked for ahead
   static constexpr uint32_t GROUP = 16;  // row tiles that share columns, as TileOrder::G
   const int32_t* offsets;
   int experts;
@@ -172,7 +172,7 @@ struct SegmentTiles {
 template <int COLS_OF_TILE>
 struct GradientTiles {
   static constexpr int N = COLS_OF_TILE;
-  static constexpr bool EMPTY = true, ADDS = true;
+  static constexpr bool WALKS = true, ADDS = true;
   const int32_t* offsets;
   int experts;
   uint32_t rows, tiles_m, tiles_n, G;
