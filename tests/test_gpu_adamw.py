@@ -372,3 +372,26 @@ def test_copies_and_parameters_with_another_storage_are_refused(dslib):
                     opt.step(new)
             assert opt.steps == 0 and all(bool((t == 7).all()) for t in over)
             assert bool((opt.m[0] == 0).all()) and bool(((p, c)[which] == 0).all()) and bool(((p, c)[1 - which] == 1).all())
+
+
+@pytest.mark.parametrize("beta1,beta2", [(0.9, 0.999), (0.5, 0.75)])
+def test_roots_and_quotients_are_correctly_rounded(dslib, beta1, beta2):
+    """The roots and quotients of steps with 8-bit states, by one correction each, are those of correctly rounded operations:
+    2^22 of them over all exponents that this path takes (v up to 2^67, m from 2^-74 to 2^60, roots from below eps = 2^-60
+    on).  Without a gradient, decay and parameter a step is -(m / (sqrt(v) + eps)), m and v beta times what the states hold."""
+    n, r = 1 << 22, _rng("exact", beta1, beta2)
+    scale = lambda low, high: (np.exp2(r.integers(low, high, n // 128)) * r.uniform(1, 2, n // 128)).astype(np.float32)  # noqa: E731
+    q = lambda codes: torch.from_numpy(r.choice(np.array(codes, np.uint8), n)).view(F8).cuda()  # noqa: E731
+    positive = list(range(127))
+    ms, vs = (q(positive + [c + 128 for c in positive]), scale(-65, 50)), (q(positive), scale(-68, 24))
+    value = lambda s: _np(s[0]) * np.repeat(s[1], 128)  # noqa: E731
+    m, root = value(ms), value(vs)
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    on_gpu = lambda s: (s[0], torch.from_numpy(s[1]).cuda())  # noqa: E731
+    t = 1_000_000  # beta^t is 0: the factors of m and of the root are 1
+    opt = dslib.AdamW([p], [g], m=[on_gpu(ms)], v=[on_gpu(vs)], lr=1.0, betas=(beta1, beta2), eps=2.0**-60, weight_decay=0.0, steps=t - 1)
+    opt.step()
+    with np.errstate(under="ignore"):
+        want = X.adamw32(np.zeros(n, np.float32), np.zeros(n, np.float32), m, root * root, t, 1.0, (beta1, beta2), 2.0**-60, 0.0)[0]
+    assert np.isfinite(want).all() and (want != 0).mean() > 0.9
+    assert np.array_equal(_np(p), want)
