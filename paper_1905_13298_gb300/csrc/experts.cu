@@ -5,13 +5,14 @@
 // ranges of the slots.  A warp counts its slots by expert in shared memory (32
 // at a time, those of one expert found by a match over the warp), the counts
 // are added up over warps, CTAs and experts, and a second pass over the ids
-// gives each slot its row.  It is bound by latency: 64 slots take 4.7 us, 32768
-// of 32 experts 7.6 (9.4 with eight CTAs), of which launch and cluster barriers
+// gives each slot its row.  It is bound by latency: 64 slots take 4.4 us, 32768
+// of 32 experts 7.4 (9.4 with eight CTAs), of which launch and cluster barriers
 // are 5.7.
 //
 // The other operators move rows and are bound by memory: a token's row is read
 // once and written to the rows of its slots; a token's sum reads its slots'
-// rows, all on their way at once.
+// rows, all on their way at once.  8192 x 4 slots of 2048: 8-bit rows gathered
+// in 15.7 us, 16-bit ones in 28.7 (0.89 and 0.93 of HBM).
 #include "experts.cuh"
 
 namespace ds {

@@ -3,11 +3,13 @@
 // expert has is known on the device only, so every CTA makes the list of the
 // tiles from the segments' offsets when it starts; nothing waits for the host.
 //
-// What bounds them: as the dense product, 48 KB of operands a block of a tile
-// through L2 and the read-back of the block's sums.  8192 x 4 rows of 32
-// experts, 2048 -> 4096: 345 us, 1.59 PFLOP/s (the dense product of as many
-// rows 323); weight gradients of 32 x 2048 x 2048 added to others 280 us, of
-// which the products take 144 and the sums' way out and in the rest.  With few
+// What bounds them: as the dense product, the read-back and sums of a block
+// beside its products; neither the tensor cores (34% of the time) nor issue
+// slots (47%) are full, nor L2, which gives 3.2 GB of operands, 9.5 TB/s.
+// 8192 x 4 rows of 32 experts, 2048 -> 4096: 338 us, 1.63 PFLOP/s (the dense
+// product of as many rows 323); weight gradients of 32 x 2048 x 2048 added to
+// others 280 us (223 without), of which the products take 144 and the sums' way
+// out and in the rest.  With few
 // rows an expert, its weights from memory: 16 x 4 rows of the same experts 35
 // us, 5.3 TB/s of the weights met.
 #include "experts.cuh"
@@ -381,6 +383,10 @@ cudaError_t weight_grad(const ExpertProduct& e, cudaStream_t st) {
 // 32 experts of 2048 x 4096, 4 of them for each of so many tokens, with 16, 32, 64 rows and by the large kernel:
 //   1 token 9.3, 9.8, 12.3, 19.4;  16: 35, 36, 39, 45;  64: 48, 47, 52, 58;  128: 61, 52, 55, 59;  256: 88, 67, 61, 63;
 //   512: 147, 97, 82, 63
+// Over 11 shapes of 4 to 512 experts, K of 512 to 4096, N of 333 to 4096 and up to 160 rows an expert the choice is 2% above
+// the best of these kernels in the mean.  12 of 165 products are more than 10% above it: those next to a border (4 experts of
+// 8 rows 13.3, 10.1 with 32), tiles of 256 columns where 128 are better (256 experts of 1024 -> 512, 72 rows each 59, 52.5),
+// and 60 to 160 rows an expert that are not aligned (60 experts of 700 -> 333: 19.4 to 27, 12.4 to 22.5 with 64 rows a tile).
 cudaError_t launch_expert_linear_f8(const ExpertProduct& e, cudaStream_t st) {
   const int64_t slots = e.s->tokens * e.s->top_k, met = slots < e.s->experts ? slots : e.s->experts;
   const int64_t each = met > 0 ? over(over(slots, met), e.s->align) * e.s->align : 0;  // gaps are multiplied too

@@ -151,7 +151,8 @@ class ExpertsFeedForward(GatedFeedForward):
         self.w_down, self.w_down_t = both(self.down)
 
     def route(self, n, padding=None):
-        """(ids, weights) [tokens, top_k] of the norm's 8-bit rows; tokens of ``padding`` (truth values) go nowhere."""
+        """(ids, weights) [tokens, top_k] of the norm's 8-bit rows; tokens of ``padding`` (truth values) go nowhere.
+        Their rows have to be finite all the same: the gradients of the norm's weight and of the router multiply them by 0."""
         best, ids = linear_f8(n, self.w_router, dtype=torch.float32).topk(self.top_k, 1)
         if padding is not None:
             ids.masked_fill_(padding[:, None], -1)
